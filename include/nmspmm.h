@@ -425,6 +425,98 @@ nm_status nm_gemm_i8_dense_out_expand(const int8_t *X, int m, const int8_t *W, i
  * NM_ERR_HIP. */
 nm_status nm_quantize_f16(const uint16_t *x, int64_t count, float inv_scale, int8_t *xq, void *stream);
 
+/* ---------------------------------------------------------------- around the linears
+ * The operators that a transformer block needs next to its linears: int8 codes
+ * of activation rows with a scale for each token, the norms before and after a
+ * block fused with its gate and residual scale, their backward pass.  Bound in
+ * nmblock.py.
+ *
+ * Activations are of one type (NM_TYPE_*), in rows whose values are
+ * consecutive; inputs may have any row stride (ld, in values), outputs are
+ * [m x d] without gaps.  Pointers need the alignment of their type only; rows
+ * that are whole 16-byte pieces at 16-byte boundaries take the fast path.
+ * Parameters (weights, biases, gates) and their gradients are float32. */
+#define NM_TYPE_F16 1    /* IEEE binary16 */
+#define NM_TYPE_BF16 2   /* bfloat16 */
+#define NM_TYPE_F32 3    /* IEEE binary32 */
+
+/* Codes of rows: top = max_t |x[i][t]|, scale[i] = top / 127,
+ * xq[i][t] = rint(x[i][t] * (127 / top)), both quotients and the product in
+ * binary32, ties to even.  A row with top < 2^-100 has scale 0 and zero codes;
+ * a row that holds an infinity or NaN has the scale NaN and zero codes.
+ * x device [m x k] of `type`, row stride ldx >= k; xq device int8 [m x kp]
+ * with kp = k rounded up to a multiple of 16, the padding zero, 16-byte
+ * aligned; scale device float32 [m].  m == 0 is a no-op.  Asynchronous on
+ * `stream`.  Errors: NM_ERR_SHAPE (m < 0 or >= 2^30, k < 1 or >= 2^30, ldx < k),
+ * NM_ERR_ARG (NULL or misaligned pointer, unknown type), NM_ERR_HIP. */
+nm_status nm_quantize_rows(const void *x, int64_t ldx, int type, int m, int k, int8_t *xq, float *scale,
+                           void *stream);
+
+/* A norm over the channels of a token: hat(v) * weight + bias with
+ * hat(v) = v / sqrt(mean(v^2) + eps) (RMS) or
+ * hat(v) = (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) (layer norm);
+ * NONE is v itself (weight and bias then are not read).  Statistics are in
+ * binary32.  weight, bias: device float32 [d]; NULL means 1 and 0.  eps > 0. */
+#define NM_NORM_NONE 0
+#define NM_NORM_RMS 1
+#define NM_NORM_LAYER 2
+typedef struct nm_norm {
+    int32_t kind;
+    float eps;
+    const float *weight;
+    const float *bias;
+} nm_norm;
+
+/* A block's end and the next one's beginning, for m tokens of d channels:
+ *   u = post(y);  res = alpha * r + gate * u;  z = pre(res)
+ * y the block's output and r the residual stream (either may be NULL: then its
+ * term is absent); gate device float32 [groups x d], row i / (m / groups) for
+ * token i (groups divides m), or NULL (1, groups = 1).  Outputs, each of
+ * which may be NULL: res and z of `type`, and the codes zq (int8 [m x dp], dp =
+ * d rounded up to 16) with scales zs (float32 [m]) of z as nm_quantize_rows
+ * defines them.  z is computed from res before its rounding to `type`.
+ * res may be r or y itself (same row stride d), no other overlap.  d <= 16384. */
+typedef struct nm_norm_args {
+    const void *y, *r;
+    int64_t ldy, ldr;
+    int32_t type, m, d, groups;
+    const float *gate;
+    float alpha;
+    nm_norm post, pre;
+    void *res, *z;
+    int8_t *zq;
+    float *zs;
+} nm_norm_args;
+/* m == 0 is a no-op.  Errors: NM_ERR_ARG (NULL args, neither y nor r, no
+ * output, zq without zs, unknown type or norm, eps <= 0, a misaligned
+ * pointer), NM_ERR_SHAPE (m < 0 or >= 2^30, d < 1 or > 16384, groups < 1 or not
+ * dividing m, a row stride below d), NM_ERR_HIP. */
+nm_status nm_norm_residual(const nm_norm_args *args, void *stream);
+
+/* Its backward pass at the given y and res (res as nm_norm_residual stored
+ * it): from dz and dres, the gradients of z and of res (either may be NULL),
+ *   dt = dres + (gradient of pre at res, of dz)
+ *   dr = alpha * dt;  dy = gradient of post at y, of gate * dt
+ *   dgate[g] = sum over group g of dt * u;  the norms' weights and biases
+ * Sums run over all tokens in a fixed order (the same bits every time).  Every
+ * output may be NULL; y may be NULL where dy, dgate and post's gradients are;
+ * res may be NULL where pre is NONE.  ws: nm_norm_residual_backward_workspace
+ * bytes of device memory, any content, 16-byte aligned. */
+typedef struct nm_norm_grad_args {
+    const void *y, *res, *dz, *dres;
+    int64_t ldy, ldres, lddz, lddres;
+    int32_t type, m, d, groups;
+    const float *gate;
+    float alpha;
+    nm_norm post, pre;
+    void *dy, *dr;
+    float *dgate, *dpre_weight, *dpre_bias, *dpost_weight, *dpost_bias;
+} nm_norm_grad_args;
+nm_status nm_norm_residual_backward_workspace(int m, int d, int groups, size_t *bytes);
+/* With m == 0 the parameter gradients are set to zero.  Errors: as
+ * nm_norm_residual, and NM_ERR_WORKSPACE. */
+nm_status nm_norm_residual_backward(const nm_norm_grad_args *args, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -6,9 +6,11 @@
   csrc/probe/*.hip, linked against libnmspmm.so for the GEMM kernels its
   store-only probe launches.
 """
+import concurrent.futures
 import glob
 import os
 import subprocess
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -17,7 +19,7 @@ PROBE_LIB = os.path.join(HERE, "libnmprobe.so")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 ARCH = "gfx950"
 FLAGS = [
-    f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-shared", "-Wall",
+    f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall",
     # packed fp32 instructions are kept out of every kernel
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
@@ -47,10 +49,20 @@ def _hipcc(cmd, out, verbose):
     return out
 
 
+def _library(srcs, out, link, verbose):
+    """Compiles the sources beside each other (each to an object of its own) and links them."""
+    with tempfile.TemporaryDirectory() as tmp:
+        def one(src):
+            obj = os.path.join(tmp, os.path.basename(src) + ".o")
+            return _hipcc(["hipcc", *FLAGS, f"-I{INCLUDE}", "-c", src], obj, verbose)
+        with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
+            objs = list(pool.map(one, srcs))
+        _hipcc(["hipcc", f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, *link], out, verbose)
+
+
 def build(verbose: bool = False) -> str:
-    _hipcc(["hipcc", *FLAGS, f"-I{INCLUDE}", *sources()], LIB, verbose)
-    _hipcc(["hipcc", *FLAGS, f"-I{INCLUDE}", *probe_sources(), f"-L{HERE}", "-lnmspmm",
-            "-Wl,-rpath,$ORIGIN"], PROBE_LIB, verbose)
+    _library(sources(), LIB, [], verbose)
+    _library(probe_sources(), PROBE_LIB, [f"-L{HERE}", "-lnmspmm", "-Wl,-rpath,$ORIGIN"], verbose)
     return LIB
 
 

@@ -1,0 +1,576 @@
+// The norms around a block with its gate and residual scale, their backward
+// pass, and int8 codes of rows with a scale for each.
+//
+//   u = post(y);  res = alpha r + gate u;  z = pre(res)
+//
+// All of it is bound by memory: a row (token) is read once, stays in the
+// registers of its team of waves, and is written once.  A team is as few waves
+// as hold the row in 16 (backward: 8) values a lane, so the statistics of up to
+// 1024 channels need no LDS and no barrier.  Teams walk over rows with the next
+// row's loads in flight, and keep the channel parameters in registers.
+// Statistics are in binary32, the variance from the centred row (not from the
+// difference of two sums, which cancels where the mean is large).
+#include <hip/hip_runtime.h>
+
+#include "nmspmm_block.h"
+#include "nmspmm_values.h"
+
+namespace nmspmm {
+namespace {
+
+typedef unsigned int v2u __attribute__((ext_vector_type(2)));
+
+// A lane's part of a row: CH chunks of VEC consecutive channels, chunk c of
+// lane l of the team at channel (c * lanes + l) * VEC.  VEC = 8 needs d % 8 == 0
+// and 16-byte aligned rows; any other row goes one channel at a time.
+template <class T, int VEC, int CH>
+struct Part {
+    T v[CH][VEC];
+};
+
+template <class T, int VEC, int CH>
+__device__ __forceinline__ void load_part(Part<T, VEC, CH> &p, const T *row, int d, int at, int step) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int ch = at + c * step;
+        if constexpr (VEC == 8) {
+            Raw8<T> t = {};
+            if (ch < d) t = load8(row + ch);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p.v[c][e] = t.v[e];
+        } else {
+            p.v[c][0] = ch < d ? row[ch] : (T)0.f;
+        }
+    }
+}
+template <int VEC, int CH>
+__device__ __forceinline__ void load_param(float (&p)[CH][VEC], const float *row, float absent, int d, int at,
+                                           int step) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const bool in = row && at + c * step < d;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) p[c][e] = absent;
+        if (in) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) p[c][e] = row[at + c * step + e];
+        }
+    }
+}
+template <class T, int VEC, int CH>
+__device__ __forceinline__ void store_part(T *row, const float (&f)[CH][VEC], int d, int at, int step) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int ch = at + c * step;
+        if (ch >= d) continue;
+        if constexpr (VEC == 8)
+            store8(row + ch, f[c]);
+        else
+            row[ch] = (T)f[c][0];
+    }
+}
+
+template <int VEC, int CH>
+__device__ __forceinline__ float total(const float (&f)[CH][VEC]) {
+    float s = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) s += f[c][e];
+    return s;
+}
+// Subtracts the mean where the lane holds channels of the row (the others stay
+// zero) and returns the sum of squares.
+template <int VEC, int CH>
+__device__ __forceinline__ float centre(float (&f)[CH][VEC], float mean, int d, int at, int step) {
+    float s = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const float mu = at + c * step < d ? mean : 0.f;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            f[c][e] -= mu;
+            s = __builtin_fmaf(f[c][e], f[c][e], s);
+        }
+    }
+    return s;
+}
+
+constexpr int team_threads(int wpr) { return wpr > 4 ? 64 * wpr : 256; }
+
+// --------------------------------------------------------------- forward
+template <class T, int VEC, int CH, int WPR>
+__global__ __launch_bounds__(team_threads(WPR)) void k_norm_residual(NormArgs a) {
+    constexpr int TEAMS = team_threads(WPR) / 64 / WPR;
+    __shared__ float box[TEAMS][2][2][WPR];
+    const int team = threadIdx.x / (64 * WPR), lane = threadIdx.x % (64 * WPR);
+    RowReduce<WPR> red{box[team], lane >> 6};
+    const int at = lane * VEC, step = 64 * WPR * VEC;
+    const float per = 1.f / (float)a.d;
+
+    float gate[CH][VEC], wq[CH][VEC], bq[CH][VEC], wp[CH][VEC], bp[CH][VEC];
+    if (a.groups <= 1) load_param(gate, a.gate, 1.f, a.d, at, step);
+    load_param(wp, a.post.weight, 1.f, a.d, at, step);
+    load_param(bp, a.post.bias, 0.f, a.d, at, step);
+    load_param(wq, a.pre.weight, 1.f, a.d, at, step);
+    load_param(bq, a.pre.bias, 0.f, a.d, at, step);
+
+    Part<T, VEC, CH> y = {}, r = {};
+    auto fetch = [&](int row) {
+        if (row >= a.m) return;
+        if (a.y) load_part(y, (const T *)a.y + row * a.ldy, a.d, at, step);
+        if (a.r) load_part(r, (const T *)a.r + row * a.ldr, a.d, at, step);
+    };
+    fetch(blockIdx.x * TEAMS + team);
+    for (int row0 = blockIdx.x * TEAMS; row0 < a.m; row0 += gridDim.x * TEAMS) {
+        const int row = row0 + team;
+        const bool live = row < a.m;
+        if (a.groups > 1)
+            load_param(gate, a.gate + (int64_t)(live ? row / a.per_group : 0) * a.d, 1.f, a.d, at, step);
+        float v[CH][VEC], rf[CH][VEC];
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                v[c][e] = (float)y.v[c][e];
+                rf[c][e] = (float)r.v[c][e];
+            }
+        fetch(row + (int)gridDim.x * TEAMS);
+
+        if (a.post.kind != NM_NORM_NONE) {
+            const float mean = a.post.kind == NM_NORM_LAYER ? red.sum(total(v)) * per : 0.f;
+            const float sq = red.sum(centre(v, mean, a.d, at, step));
+            const float scale = 1.f / __builtin_sqrtf(__builtin_fmaf(sq, per, a.post.eps));
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) v[c][e] = __builtin_fmaf(v[c][e] * scale, wp[c][e], bp[c][e]);
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                v[c][e] = at + c * step < a.d ? __builtin_fmaf(gate[c][e], v[c][e], a.alpha * rf[c][e]) : 0.f;
+        if (a.res && live) store_part((T *)a.res + (int64_t)row * a.d, v, a.d, at, step);
+        if (!a.z && !a.zq) continue;
+
+        // the norm sees the sum before its rounding to T: one rounding for each output
+        if (a.pre.kind != NM_NORM_NONE) {
+            const float mean = a.pre.kind == NM_NORM_LAYER ? red.sum(total(v)) * per : 0.f;
+            const float sq = red.sum(centre(v, mean, a.d, at, step));
+            const float scale = 1.f / __builtin_sqrtf(__builtin_fmaf(sq, per, a.pre.eps));
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) v[c][e] = __builtin_fmaf(v[c][e] * scale, wq[c][e], bq[c][e]);
+        }
+        if (a.z && live) store_part((T *)a.z + (int64_t)row * a.d, v, a.d, at, step);
+        if (a.zq) {
+            float top = 0.f;
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    top = larger(top, at + c * step < a.d ? magnitude(v[c][e]) : 0.f);
+            const RowScale rs = row_scale(red.largest(top));
+            if (live) {
+                if (lane == 0) a.zs[row] = rs.scale;
+#pragma unroll
+                for (int c = 0; c < CH; ++c) {
+                    const int ch = at + c * step;
+                    if (ch >= a.ldq) continue;     // the codes' rows are padded with zeros
+                    int8_t *dst = a.zq + (int64_t)row * a.ldq + ch;
+                    int q[VEC];
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) q[e] = ch < a.d ? row_code(v[c][e], rs.inv) : 0;
+                    if constexpr (VEC == 8)
+                        *(v2u *)dst = v2u{pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7])};
+                    else
+                        *dst = (int8_t)q[0];
+                }
+            }
+        }
+    }
+}
+
+// --------------------------------------------------------------- backward
+// With hat(v) the normalised row and t = dout * weight, a norm's gradient is
+//   dv = (t - [mean(t)] - hat * mean(t * hat)) / deviation     ([]: layer norm)
+// so: dt = dres + that of pre at res;  dr = alpha dt;  dy = that of post at y,
+// of gate * dt.  The statistics are computed again from y and res: the rows are
+// in registers, and saved ones would have to be read.
+//
+// A team takes a run of consecutive rows and sums for its channels what the
+// parameters' gradients need; the teams of a workgroup join their sums in LDS,
+// the workgroups in k_norm_sums: every addition has its place, so results do not
+// change from run to run.  A gate that is shared by fewer tokens than all is
+// finished, or put aside for k_norm_sums, whenever the team reaches the group's end.
+template <class T, int VEC, int CH, int WPR>
+__global__ __launch_bounds__(team_threads(WPR)) void k_norm_residual_backward(NormGradArgs a) {
+    constexpr int TEAMS = team_threads(WPR) / 64 / WPR, LANES = 64 * WPR;
+    __shared__ float box[TEAMS][2][2][WPR];
+    extern __shared__ __attribute__((aligned(16))) float joined[];     // TEAMS > 1: one sum of every team but the first
+    const int team = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+    RowReduce<WPR> red{box[team], lane >> 6};
+    const int at = lane * VEC, step = LANES * VEC;
+    const float per = 1.f / (float)a.d;
+    const int first = (int)(blockIdx.x * TEAMS + team) * a.run;
+    const int end = first + a.run < a.m ? first + a.run : a.m;
+    const bool layer_q = a.pre.kind == NM_NORM_LAYER, layer_p = a.post.kind == NM_NORM_LAYER;
+    const bool has_q = a.pre.kind != NM_NORM_NONE, has_p = a.post.kind != NM_NORM_NONE;
+
+    float gate[CH][VEC], wq[CH][VEC], wp[CH][VEC], bp[CH][VEC];
+    load_param(wp, a.post.weight, 1.f, a.d, at, step);
+    load_param(bp, a.post.bias, 0.f, a.d, at, step);
+    load_param(wq, a.pre.weight, 1.f, a.d, at, step);
+    float s_wq[CH][VEC] = {}, s_bq[CH][VEC] = {}, s_g[CH][VEC] = {}, s_wp[CH][VEC] = {}, s_bp[CH][VEC] = {};
+
+    Part<T, VEC, CH> py = {}, pr = {}, pz = {}, pd = {};
+    auto fetch = [&](int row) {
+        if (row >= end) return;
+        if (a.y) load_part(py, (const T *)a.y + row * a.ldy, a.d, at, step);
+        if (has_q) load_part(pr, (const T *)a.res + row * a.ldr, a.d, at, step);
+        if (a.dz) load_part(pz, (const T *)a.dz + row * a.lddz, a.d, at, step);
+        if (a.dres) load_part(pd, (const T *)a.dres + row * a.lddres, a.d, at, step);
+    };
+    int group = -1;
+    auto group_done = [&]() {
+        // a group within this run is finished; one that other runs share is put
+        // aside, in place 0 if the run began with it (or within it), else in 1
+        const bool whole = group * a.per_group >= first && (group + 1) * a.per_group <= first + a.run;
+        float *dst = whole ? a.dgate + (int64_t)group * a.d
+                           : a.gate_parts + ((int64_t)(first / a.run) * 2 + (group == first / a.per_group ? 0 : 1)) * a.d;
+        store_part(dst, s_g, a.d, at, step);
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) s_g[c][e] = 0.f;
+    };
+    fetch(first);
+    // every team of the workgroup makes a.run turns: the reductions hold barriers
+    for (int i = 0; i < a.run; ++i) {
+        const int row = first + i;
+        const bool live = row < end;
+        if (WPR == 1 && !live) break;
+        if (live && (a.groups <= 1 ? group < 0 : row / a.per_group != group)) {
+            if (a.groups > 1 && group >= 0 && a.dgate) group_done();
+            group = a.groups <= 1 ? 0 : row / a.per_group;
+            load_param(gate, a.gate ? a.gate + (int64_t)group * a.d : nullptr, 1.f, a.d, at, step);
+        }
+        float y[CH][VEC], r[CH][VEC], dz[CH][VEC], dt[CH][VEC];
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                y[c][e] = live ? (float)py.v[c][e] : 0.f;
+                r[c][e] = live ? (float)pr.v[c][e] : 0.f;
+                dz[c][e] = live ? (float)pz.v[c][e] : 0.f;
+                dt[c][e] = live ? (float)pd.v[c][e] : 0.f;
+            }
+        fetch(row + 1);
+
+        float my = has_p ? total(y) : 0.f, mr = total(r);
+        if (layer_p || layer_q) red.sum2(my, mr);
+        float vy = has_p ? centre(y, layer_p ? my * per : 0.f, a.d, at, step) : 0.f;
+        float vr = centre(r, layer_q ? mr * per : 0.f, a.d, at, step);
+        red.sum2(vy, vr);
+        const float inv_y = has_p ? 1.f / __builtin_sqrtf(__builtin_fmaf(vy, per, a.post.eps)) : 1.f;
+        if (has_q) {
+            const float inv_r = 1.f / __builtin_sqrtf(__builtin_fmaf(vr, per, a.pre.eps));
+            float st = 0.f, sth = 0.f;
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float hat = r[c][e] * inv_r, g = dz[c][e];
+                    s_wq[c][e] = __builtin_fmaf(g, hat, s_wq[c][e]);
+                    s_bq[c][e] += g;
+                    r[c][e] = hat;
+                    dz[c][e] = g * wq[c][e];
+                    st += dz[c][e];
+                    sth = __builtin_fmaf(dz[c][e], hat, sth);
+                }
+            red.sum2(st, sth);
+            const float mt = layer_q ? st * per : 0.f, mth = sth * per;
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    dt[c][e] += inv_r * (dz[c][e] - mt - r[c][e] * mth);
+        } else {
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) dt[c][e] += dz[c][e];
+        }
+        if (a.dr && live) {
+            float out[CH][VEC];
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) out[c][e] = a.alpha * dt[c][e];
+            store_part((T *)a.dr + (int64_t)row * a.d, out, a.d, at, step);
+        }
+        if (!a.y) continue;
+
+        float st = 0.f, sth = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const bool in = at + c * step < a.d;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float t = in ? dt[c][e] : 0.f;
+                if (has_p) {
+                    const float hat = y[c][e] * inv_y, g = t * gate[c][e];
+                    s_g[c][e] = __builtin_fmaf(t, __builtin_fmaf(hat, wp[c][e], bp[c][e]), s_g[c][e]);
+                    s_wp[c][e] = __builtin_fmaf(g, hat, s_wp[c][e]);
+                    s_bp[c][e] += g;
+                    y[c][e] = hat;
+                    dt[c][e] = g * wp[c][e];
+                    st += dt[c][e];
+                    sth = __builtin_fmaf(dt[c][e], hat, sth);
+                } else {
+                    s_g[c][e] = __builtin_fmaf(t, y[c][e], s_g[c][e]);
+                    dt[c][e] = t * gate[c][e];
+                }
+            }
+        }
+        if (has_p) {
+            red.sum2(st, sth);
+            const float mt = layer_p ? st * per : 0.f, mth = sth * per;
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) dt[c][e] = inv_y * (dt[c][e] - mt - y[c][e] * mth);
+        }
+        if (a.dy && live) store_part((T *)a.dy + (int64_t)row * a.d, dt, a.d, at, step);
+    }
+    if (a.groups > 1 && group >= 0 && a.dgate) group_done();
+
+    // this workgroup's sums, in the order gate, pre weight, pre bias, post weight, post bias
+    auto join = [&](float (&s)[CH][VEC], float *dst) {
+        if (!dst) return;
+        if constexpr (TEAMS > 1) {
+            __syncthreads();
+            if (team > 0) store_part(joined + (int64_t)(team - 1) * a.d, s, a.d, at, step);
+            __syncthreads();
+            if (team == 0) {
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+                    if (at + c * step < a.d)
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e)
+                            for (int t = 1; t < TEAMS; ++t) s[c][e] += joined[(t - 1) * a.d + at + c * step + e];
+            }
+        }
+        if (team == 0) store_part(dst + (int64_t)blockIdx.x * a.d, s, a.d, at, step);
+    };
+    const int64_t span = (int64_t)gridDim.x * a.d;
+    join(s_g, a.groups <= 1 && a.dgate ? a.parts : nullptr);
+    join(s_wq, a.dpre_weight ? a.parts + span : nullptr);
+    join(s_bq, a.dpre_bias ? a.parts + 2 * span : nullptr);
+    join(s_wp, a.dpost_weight ? a.parts + 3 * span : nullptr);
+    join(s_bp, a.dpost_bias ? a.parts + 4 * span : nullptr);
+}
+
+// Adds what the workgroups and runs left: blocks 0 .. 5 * col_blocks - 1 one kind
+// of sum and 64 channels each, 16 waves taking the workgroups in turn; the
+// others one gate group that several runs share.
+__global__ __launch_bounds__(1024) void k_norm_sums(NormGradArgs a, int workgroups, int col_blocks) {
+    __shared__ float part[16][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int b = blockIdx.x;
+    const int ch = (b % col_blocks) * 64 + lane;
+    const int kind = b / col_blocks;
+    float s = 0.f;
+    float *dst = nullptr;
+    if (kind < 5) {
+        dst = kind == 0 ? (a.groups <= 1 ? a.dgate : nullptr) : kind == 1 ? a.dpre_weight : kind == 2 ? a.dpre_bias
+              : kind == 3 ? a.dpost_weight : a.dpost_bias;
+        if (dst && ch < a.d) {
+            const float *src = a.parts + (int64_t)kind * workgroups * a.d + ch;
+#pragma unroll 8
+            for (int w = wave; w < workgroups; w += 16) s += src[(int64_t)w * a.d];
+        }
+    } else {
+        const int group = kind - 5;
+        const int t0 = group * a.per_group / a.run, t1 = ((group + 1) * a.per_group - 1) / a.run;
+        if (t0 != t1) {
+            dst = a.dgate + (int64_t)group * a.d;
+            if (ch < a.d)
+                for (int t = t0 + wave; t <= t1; t += 16)
+                    s += a.gate_parts[((int64_t)2 * t + (group == t * a.run / a.per_group ? 0 : 1)) * a.d + ch];
+        }
+    }
+    part[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && dst && ch < a.d) {
+        float all = 0.f;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) all += part[w][lane];
+        dst[ch] = all;
+    }
+}
+
+// --------------------------------------------------------------- row codes
+// One team for each row; a row past 16 values a lane is read a second time
+// (from L2) for its codes.
+template <class T, int VEC, int CH, int WPR>
+__global__ __launch_bounds__(team_threads(WPR)) void k_quantize_rows(QuantArgs a) {
+    constexpr int TEAMS = team_threads(WPR) / 64 / WPR;
+    __shared__ float box[TEAMS][2][2][WPR];
+    const int team = threadIdx.x / (64 * WPR), lane = threadIdx.x % (64 * WPR);
+    RowReduce<WPR> red{box[team], lane >> 6};
+    const int step = 64 * WPR * VEC, span = step * CH;
+    for (int64_t row0 = (int64_t)blockIdx.x * TEAMS; row0 < a.m; row0 += (int64_t)gridDim.x * TEAMS) {
+        const int64_t row = row0 + team;
+        const bool live = row < a.m;
+        const T *src = (const T *)a.x + (live ? row : 0) * a.ldx;
+        Part<T, VEC, CH> p;
+        float top = 0.f;
+        int base = 0;
+        for (;; base += span) {
+            load_part(p, src, a.k, base + lane * VEC, step);
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) top = larger(top, magnitude((float)p.v[c][e]));
+            if (base + span >= a.ldq) break;
+        }
+        const RowScale rs = row_scale(red.largest(top));
+        if (live && lane == 0) a.scale[row] = rs.scale;
+        for (;; base -= span) {      // the last part is still in registers
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int ch = base + lane * VEC + c * step;
+                if (!live || ch >= a.ldq) continue;
+                int8_t *dst = a.q + row * a.ldq + ch;
+                int q[VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) q[e] = row_code((float)p.v[c][e], rs.inv);
+                if constexpr (VEC == 8)
+                    *(v2u *)dst = v2u{pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7])};
+                else
+                    *dst = (int8_t)q[0];
+            }
+            if (base == 0) break;
+            load_part(p, src, a.k, base - span + lane * VEC, step);
+        }
+    }
+}
+
+// --------------------------------------------------------------- launches
+// Waves of a team by the row's length, and workgroups that the device holds at once.
+constexpr int kResident = 8;
+
+template <class T, int VEC, int CH, int WPR>
+int norm_one(const NormArgs &a, void *stream) {
+    constexpr int teams = team_threads(WPR) / 64 / WPR;
+    const int64_t want = ((int64_t)a.m + teams - 1) / teams, most = (int64_t)device_cu_count() * kResident;
+    hipLaunchKernelGGL((k_norm_residual<T, VEC, CH, WPR>), dim3((unsigned)(want < most ? want : most)),
+                       dim3(team_threads(WPR)), 0, (hipStream_t)stream, a);
+    return (int)hipGetLastError();
+}
+template <class T, int VEC>
+int norm_by_width(const NormArgs &a, void *stream) {
+    constexpr int full = 16 / VEC;
+    const int w = a.zq ? (int)a.ldq : a.d;
+    if (w <= 512) return norm_one<T, VEC, full / 2, 1>(a, stream);
+    if (w <= 1024) return norm_one<T, VEC, full, 1>(a, stream);
+    if (w <= 2048) return norm_one<T, VEC, full, 2>(a, stream);
+    if (w <= 4096) return norm_one<T, VEC, full, 4>(a, stream);
+    if (w <= 8192) return norm_one<T, VEC, full, 8>(a, stream);
+    return norm_one<T, VEC, full, 16>(a, stream);
+}
+
+template <class T, int VEC, int CH, int WPR>
+int grad_one(const NormGradArgs &a, int workgroups, void *stream) {
+    constexpr int teams = team_threads(WPR) / 64 / WPR;
+    hipLaunchKernelGGL((k_norm_residual_backward<T, VEC, CH, WPR>), dim3(workgroups), dim3(team_threads(WPR)),
+                       (teams - 1) * a.d * 4, (hipStream_t)stream, a);
+    return (int)hipGetLastError();
+}
+template <class T, int VEC>
+int grad_by_width(const NormGradArgs &a, int workgroups, void *stream) {
+    constexpr int half = 8 / VEC;
+    if (a.d <= 512) return grad_one<T, VEC, half, 1>(a, workgroups, stream);
+    if (a.d <= 1024) return grad_one<T, VEC, half, 2>(a, workgroups, stream);
+    if (a.d <= 2048) return grad_one<T, VEC, half, 4>(a, workgroups, stream);
+    if (a.d <= 4096) return grad_one<T, VEC, half, 8>(a, workgroups, stream);
+    if (a.d <= 8192) return grad_one<T, VEC, half, 16>(a, workgroups, stream);
+    return grad_one<T, VEC, 2 * half, 16>(a, workgroups, stream);
+}
+
+template <class T, int VEC, int CH, int WPR>
+int quant_one(const QuantArgs &a, void *stream) {
+    constexpr int teams = team_threads(WPR) / 64 / WPR;
+    const int64_t want = (a.m + teams - 1) / teams, most = (int64_t)device_cu_count() * 2 * kResident;
+    hipLaunchKernelGGL((k_quantize_rows<T, VEC, CH, WPR>), dim3((unsigned)(want < most ? want : most)),
+                       dim3(team_threads(WPR)), 0, (hipStream_t)stream, a);
+    return (int)hipGetLastError();
+}
+template <class T, int VEC>
+int quant_by_width(const QuantArgs &a, void *stream) {
+    constexpr int full = 16 / VEC;
+    if (a.ldq <= 512) return quant_one<T, VEC, full / 2, 1>(a, stream);
+    if (a.ldq <= 1024) return quant_one<T, VEC, full, 1>(a, stream);
+    if (a.ldq <= 2048) return quant_one<T, VEC, full, 2>(a, stream);
+    return quant_one<T, VEC, full, 4>(a, stream);
+}
+
+}  // namespace
+
+// Waves of a backward team, and the workgroups and rows of a team's run for m rows.
+static int grad_teams(int d) { return d <= 512 ? 4 : d <= 1024 ? 2 : 1; }
+
+NormGradShape norm_grad_shape(int m, int d) {
+    const int teams = grad_teams(d);
+    const int most = device_cu_count() * (d <= 2048 ? 4 : 2);
+    const int want = (m + teams - 1) / teams, workgroups = want < most ? want : most;
+    NormGradShape s;
+    s.teams = teams;
+    s.run = (m + workgroups * teams - 1) / (workgroups * teams);
+    s.workgroups = (m + s.run * teams - 1) / (s.run * teams);
+    return s;
+}
+
+int launch_norm_residual(int type, bool vec, const NormArgs &a, void *stream) {
+    switch (type) {
+        case NM_TYPE_F16: return vec ? norm_by_width<half_t, 8>(a, stream) : norm_by_width<half_t, 1>(a, stream);
+        case NM_TYPE_BF16: return vec ? norm_by_width<bf16_t, 8>(a, stream) : norm_by_width<bf16_t, 1>(a, stream);
+        case NM_TYPE_F32: return vec ? norm_by_width<float, 8>(a, stream) : norm_by_width<float, 1>(a, stream);
+    }
+    return (int)hipErrorInvalidValue;
+}
+
+int launch_norm_residual_backward(int type, bool vec, const NormGradArgs &a, int workgroups, void *stream) {
+    int err = (int)hipErrorInvalidValue;
+    switch (type) {
+        case NM_TYPE_F16:
+            err = vec ? grad_by_width<half_t, 8>(a, workgroups, stream) : grad_by_width<half_t, 1>(a, workgroups, stream);
+            break;
+        case NM_TYPE_BF16:
+            err = vec ? grad_by_width<bf16_t, 8>(a, workgroups, stream) : grad_by_width<bf16_t, 1>(a, workgroups, stream);
+            break;
+        case NM_TYPE_F32:
+            err = vec ? grad_by_width<float, 8>(a, workgroups, stream) : grad_by_width<float, 1>(a, workgroups, stream);
+            break;
+    }
+    if (err != 0) return err;
+    const int col_blocks = (a.d + 63) / 64;
+    const int64_t kinds = 5 + (a.groups > 1 && a.dgate ? a.groups : 0);
+    hipLaunchKernelGGL(k_norm_sums, dim3((unsigned)(col_blocks * kinds)), dim3(1024), 0, (hipStream_t)stream, a,
+                       workgroups, col_blocks);
+    return (int)hipGetLastError();
+}
+
+int launch_quantize_rows(int type, bool vec, const QuantArgs &a, void *stream) {
+    switch (type) {
+        case NM_TYPE_F16: return vec ? quant_by_width<half_t, 8>(a, stream) : quant_by_width<half_t, 1>(a, stream);
+        case NM_TYPE_BF16: return vec ? quant_by_width<bf16_t, 8>(a, stream) : quant_by_width<bf16_t, 1>(a, stream);
+        case NM_TYPE_F32: return vec ? quant_by_width<float, 8>(a, stream) : quant_by_width<float, 1>(a, stream);
+    }
+    return (int)hipErrorInvalidValue;
+}
+
+}  // namespace nmspmm

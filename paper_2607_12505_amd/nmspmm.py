@@ -36,6 +36,8 @@ EXPORTED = (
     "nm_spmm", "nm_spmm_ex", "nm_gemm_i8_dense", "nm_gemm_i8_dense_ex", "nm_spmm_out", "nm_gemm_i8_dense_out",
     "nm_quantize_f16", "nm_spmm_noalloc", "nm_expand_size", "nm_expand", "nm_spmm_out_expand",
     "nm_gemm_i8_dense_out_expand",
+    # around the linears (bound in nmblock.py)
+    "nm_quantize_rows", "nm_norm_residual", "nm_norm_residual_backward_workspace", "nm_norm_residual_backward",
 )
 NM_NOALLOC_SCRATCH_BYTES = 16384 + (32 << 20)
 
@@ -124,6 +126,10 @@ def lib() -> ctypes.CDLL:
                                     ctypes.POINTER(NmExpandJob)], i32),
             "nm_gemm_i8_dense_out_expand": ([vp, i32, vp, i32, i32, ctypes.POINTER(NmOutputs), vp, sz, vp, pp,
                                              ctypes.POINTER(NmExpandJob)], i32),
+            "nm_quantize_rows": ([vp, ctypes.c_int64, i32, i32, i32, vp, vp, vp], i32),
+            "nm_norm_residual": ([vp, vp], i32),
+            "nm_norm_residual_backward_workspace": ([i32, i32, i32, ctypes.POINTER(sz)], i32),
+            "nm_norm_residual_backward": ([vp, vp, sz, vp], i32),
         }
         for name, (args, res) in sig.items():
             f = getattr(L, name)

@@ -1,0 +1,303 @@
+"""Norms around a block, their gradients and the row codes, against plain forms in 64 bits (bounds: block_util)."""
+import math
+
+import pytest
+import torch
+
+import block_util as bu
+from paper_2607_12505_amd import nmblock as nb
+
+pytestmark = pytest.mark.gpu
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def rows(g, m, d, T, shift=0.0, pad=0):
+    x = (torch.randn(m, d + pad, generator=g) + shift).to(T).cuda()
+    return x[:, :d]
+
+
+def norm_of(g, d, kind, with_bias=True, with_weight=True, eps=1e-6):
+    if kind is None:
+        return None, None
+    w = (1 + 0.2 * torch.randn(d, generator=g)).cuda() if with_weight else None
+    b = (0.2 * torch.randn(d, generator=g)).cuda() if with_bias else None
+    return nb.Norm(kind, w, b, eps), (kind, w, b, eps)
+
+
+# one lane's channels, whole chunks, odd widths, every number of waves a row
+WIDTHS = [1, 2, 7, 8, 63, 64, 129, 384, 511, 512, 520, 768, 1021, 1024, 1536, 2048, 2049, 4096, 5000, 8192, 16384]
+
+
+@pytest.mark.parametrize("T", bu.TYPES)
+@pytest.mark.parametrize("d", WIDTHS)
+def test_forward(T, d):
+    g = gen(d)
+    m = 5 if d > 4096 else 37
+    pre, p64 = norm_of(g, d, "layer" if d % 2 == 0 else "rms", with_bias=d % 3 != 0)
+    post, q64 = norm_of(g, d, (None, "rms", "layer")[d % 3])
+    y, r = rows(g, m, d, T), rows(g, m, d, T, shift=0.5)
+    gate = torch.randn(d, generator=g).cuda()
+    res, z = nb.norm_residual(y, r, pre=pre, post=post, gate=gate, alpha=0.7)
+    alpha = float(torch.tensor(0.7, dtype=torch.float32))
+    want = bu.norm_residual(y, r, p64, q64, gate, alpha)
+    bu.close(res, want[0], T, want[2])
+    bu.close(z, want[1], T, want[3])
+
+
+@pytest.mark.parametrize("T", bu.TYPES)
+@pytest.mark.parametrize("m,d,groups", [(1, 64, 1), (6, 100, 3), (64, 384, 64), (197 * 4, 192, 4), (12, 1032, 2),
+                                        (3000, 16, 1500)])
+def test_forward_strides_groups_and_absent_parts(T, m, d, groups):
+    g = gen(m + d)
+    pre, p64 = norm_of(g, d, "rms", with_bias=False, with_weight=False)
+    y, r = rows(g, m, d, T, pad=5), rows(g, m, d, T, pad=8)
+    gate = torch.randn(groups, d, generator=g).cuda()
+    res, z = nb.norm_residual(y, r, pre=pre, gate=gate)
+    want = bu.norm_residual(y, r, p64, None, gate, 1.0)
+    bu.close(res, want[0], T, want[2])
+    bu.close(z, want[1], T, want[3])
+    res, z = nb.norm_residual(None, r, pre=pre, alpha=1.0)            # no block before: the stream itself
+    assert torch.equal(res, r.contiguous())
+    want = bu.norm_residual(None, r, p64, None, None, 1.0)
+    bu.close(z, want[1], T, want[3])
+    res, z = nb.norm_residual(y, None, gate=gate)                     # no residual, no norm after
+    want = bu.norm_residual(y, None, None, None, gate, 1.0)
+    assert z is None
+    bu.close(res, want[0], T, want[2])
+    out = r.clone(memory_format=torch.contiguous_format)   # (r of one row is contiguous: contiguous() would be r itself)
+    res, _ = nb.norm_residual(y, out, pre=pre, gate=gate, res=out)    # in place
+    want = bu.norm_residual(y, r, None, None, gate, 1.0)
+    bu.close(out, want[0], T, want[2])
+
+
+@pytest.mark.parametrize("T", [torch.float16, torch.float32])
+def test_layer_norm_of_rows_far_from_zero(T):
+    # the variance of a row whose mean is 1000 times its deviation
+    g = gen(5)
+    y = rows(g, 9, 640, T, shift=1000.0)
+    pre, p64 = norm_of(g, 640, "layer")
+    _, z = nb.norm_residual(y, None, pre=pre)
+    want = bu.norm_residual(y, None, p64, None, None, 1.0)
+    bu.close(z, want[1], T, want[3])
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_constant_zero_and_infinite_rows(kind):
+    d = 200
+    y = torch.zeros(4, d, dtype=torch.float16).cuda()
+    y[1] = 3.0
+    y[2, 7] = float("inf")
+    y[3, 9] = float("nan")
+    pre = nb.Norm(kind, None, None, 1e-6)
+    res, z = nb.norm_residual(y, None, pre=pre)
+    assert torch.equal(z[0], torch.zeros_like(z[0]))
+    want = torch.zeros(d) if kind == "layer" else torch.full((d,), 3 / math.sqrt(9 + 1e-6))
+    assert torch.equal(z[1].cpu(), want.half())
+    assert z[2].isnan().any() and z[3].isnan().all()
+    _, zq, zs = nb.norm_residual_i8(y, None, pre=pre)
+    assert zs[0] == 0 and (zq[0] == 0).all()
+    assert zs[2].isnan() and zs[3].isnan() and (zq[2:] == 0).all()
+
+
+@pytest.mark.parametrize("T", bu.TYPES)
+@pytest.mark.parametrize("m,d", [(1, 1), (3, 16), (5, 24), (33, 1000), (4, 1024), (7, 771), (2, 8200), (2, 16383)])
+def test_codes_of_normalised_rows(T, m, d):
+    # zq zs stands for z within half a code and z's own error; the scale is the row's largest value over 127
+    g = gen(m * d)
+    pre, p64 = norm_of(g, d, "layer")
+    y, r = rows(g, m, d, T), rows(g, m, d, T)
+    res, zq, zs = nb.norm_residual_i8(y, r, pre=pre)
+    assert torch.equal(res, nb.norm_residual(y, r, pre=pre)[0])
+    want = bu.norm_residual(y, r, p64, None, None, 1.0)
+    room = bu.K * bu.E * want[3]
+    top = want[1].abs().amax(1)
+    scale = zs.double().cpu()
+    assert ((scale * 127 - top).abs() <= room.amax(1) + 2 * bu.E * top).all()
+    off = (zq[:, :d].double().cpu() * scale[:, None] - want[1]).abs()
+    assert (off <= 0.5 * scale[:, None] * (1 + 1e-5) + room).all()
+    assert zq.shape[1] == nb.padded(d) and (zq[:, d:] == 0).all()
+
+
+@pytest.mark.parametrize("T", bu.TYPES)
+@pytest.mark.parametrize("m,k,pad", [(1, 1, 0), (1, 1024, 0), (5, 16, 0), (9, 17, 3), (33, 384, 8), (7, 1021, 0),
+                                     (3, 2048, 0), (4, 4097, 1), (2, 4096, 0), (2, 40000, 0), (3, 9001, 7)])
+def test_row_codes_are_the_defined_ones(T, m, k, pad):
+    g = gen(m + k)
+    x = rows(g, m, k, T, pad=pad) * torch.exp(3 * torch.randn(m, 1, generator=g)).cuda().to(T)
+    x = torch.nn.functional.pad(x, (0, pad))[:, :k]
+    q, s = nb.quantize_rows(x)
+    want_q, want_s = bu.codes(x)
+    assert torch.equal(s.cpu(), want_s)
+    assert torch.equal(q[:, :k].cpu(), want_q) and (q[:, k:] == 0).all()
+
+
+def test_row_codes_of_extreme_rows():
+    x = torch.zeros(6, 40)
+    x[1] = 2.0 ** -101
+    x[2] = 2.0 ** -100
+    x[3, 5], x[3, 6] = float("inf"), 1.0
+    x[4, 0] = float("nan")
+    x[5] = torch.linspace(-3.4e38, 3.4e38, 40)
+    q, s = nb.quantize_rows(x.cuda())
+    want_q, want_s = bu.codes(x)
+    assert torch.equal(q[:, :40].cpu(), want_q)
+    assert torch.equal(torch.nan_to_num(s.cpu(), nan=-1.0), torch.nan_to_num(want_s, nan=-1.0))
+
+
+def check_grads(got, want, T, m):
+    for name, (ref, size) in want.items():
+        t = getattr(got, name)
+        wide = name in ("dy", "dr")
+        bu.close(t, ref, T if wide else torch.float32, size, bu.K if wide else bu.K + m // 16)
+
+
+@pytest.mark.parametrize("T", bu.TYPES)
+@pytest.mark.parametrize("d", WIDTHS)
+def test_backward(T, d):
+    g = gen(1000 + d)
+    m = 11 if d > 4096 else 75
+    pre, p64 = norm_of(g, d, "rms" if d % 2 == 0 else "layer")
+    post, q64 = norm_of(g, d, ("layer", None, "rms")[d % 3], with_bias=d % 2 == 0)
+    y, res, dz, dres = (rows(g, m, d, T) for _ in range(4))
+    gate = torch.randn(d, generator=g).cuda()
+    got = nb.norm_residual_backward(dz, dres, y, res, pre=pre, post=post, gate=gate, alpha=1.25)
+    check_grads(got, bu.norm_grads(dz, dres, y, res, p64, q64, gate, 1.25), T, m)
+    assert (got.dpost_weight is None) == (post is None)
+
+
+# groups that end inside a run of rows, runs that end inside a group, one token a group, many runs a group
+@pytest.mark.parametrize("m,d,groups", [(1, 8, 1), (6, 40, 6), (4096, 24, 2), (6000, 40, 1500), (5000, 72, 5000),
+                                        (9000, 136, 90), (2500, 600, 5), (1030, 2056, 103), (7000, 512, 7)])
+@pytest.mark.parametrize("T", [torch.float16, torch.float32])
+def test_backward_of_shared_gates(T, m, d, groups):
+    g = gen(m + groups)
+    pre, p64 = norm_of(g, d, "layer")
+    post, q64 = norm_of(g, d, "rms", with_bias=False)
+    y, res, dz = rows(g, m, d, T), rows(g, m, d, T, pad=16), rows(g, m, d, T, pad=1)
+    gate = torch.randn(groups, d, generator=g).cuda()
+    got = nb.norm_residual_backward(dz, None, y, res, pre=pre, post=post, gate=gate)
+    check_grads(got, bu.norm_grads(dz, None, y, res, p64, q64, gate, 1.0), T, m)
+    again = nb.norm_residual_backward(dz, None, y, res, pre=pre, post=post, gate=gate)
+    assert all(torch.equal(a, b) for a, b in zip(got, again) if a is not None)      # the same bits every time
+
+
+@pytest.mark.parametrize("T", [torch.bfloat16])
+def test_backward_of_parts(T):
+    g = gen(77)
+    m, d = 130, 96
+    pre, p64 = norm_of(g, d, "layer")
+    y, res, dz, dres = (rows(g, m, d, T) for _ in range(4))
+    got = nb.norm_residual_backward(dz, dres, None, res, pre=pre)
+    assert got.dy is None and got.dgate is None
+    check_grads(got, bu.norm_grads(dz, dres, None, res, p64, None, None, 1.0), T, m)
+    gate = torch.randn(d, generator=g).cuda()
+    got = nb.norm_residual_backward(None, dres, y, None, gate=gate)                  # no norm after the sum
+    check_grads(got, bu.norm_grads(None, dres, y, None, None, None, gate, 1.0), T, m)
+    assert torch.equal(got.dr, dres)
+
+
+@pytest.mark.parametrize("kinds", [("rms", "layer"), ("layer", "rms")])
+def test_backward_against_differences(kinds):
+    # the derivative along random directions, by central differences of the 64-bit forward.  With step h
+    # the difference's own error is O(h^2) = 1e-8 relative to third derivatives of order one, the kernel's 64 e a
+    # term: 2e-5 of the sum of the terms' magnitudes covers both.
+    g = gen(3)
+    m, d, h = 12, 48, 1e-4
+    pre, p64 = norm_of(g, d, kinds[0])
+    post, q64 = norm_of(g, d, kinds[1])
+    y, r, dz, dres = (rows(g, m, d, torch.float32) for _ in range(4))
+    gate = torch.randn(3, d, generator=g).cuda()
+    res = bu.norm_residual(y, r, p64, q64, gate, 0.5)[0].float().cuda()
+    got = nb.norm_residual_backward(dz, dres, y, res, pre=pre, post=post, gate=gate, alpha=0.5)
+    base = {"y": y, "r": r, "gate": gate, "pre_w": p64[1], "pre_b": p64[2], "post_w": q64[1], "post_b": q64[2]}
+    grads = {"y": got.dy, "r": got.dr, "gate": got.dgate, "pre_w": got.dpre_weight, "pre_b": got.dpre_bias,
+             "post_w": got.dpost_weight, "post_b": got.dpost_bias}
+
+    def value(v):
+        out, z, _, _ = bu.norm_residual(v["y"], v["r"], (p64[0], v["pre_w"], v["pre_b"], p64[3]),
+                                        (q64[0], v["post_w"], v["post_b"], q64[3]), v["gate"], 0.5)
+        return float((z * dz.double().cpu()).sum() + (out * dres.double().cpu()).sum())
+
+    for name, grad in grads.items():
+        at = base[name].double().cpu()
+        way = torch.randn(at.shape, generator=g, dtype=torch.float64)
+        slope = (value(dict(base, **{name: at + h * way})) - value(dict(base, **{name: at - h * way}))) / (2 * h)
+        terms = way * grad.double().cpu()
+        assert abs(float(terms.sum()) - slope) <= 2e-5 * float(terms.abs().sum()) + 1e-6, name
+
+
+def test_empty_batches():
+    x = torch.empty(0, 32, device="cuda", dtype=torch.float16)
+    pre = nb.Norm("rms", torch.ones(32).cuda())
+    res, z = nb.norm_residual(x, x, pre=pre)
+    assert res.shape == z.shape == (0, 32)
+    assert nb.quantize_rows(x)[0].shape == (0, 32)
+    gate = torch.ones(32).cuda()
+    got = nb.norm_residual_backward(x, x, x, x, pre=pre, gate=gate)
+    assert (got.dgate == 0).all() and (got.dpre_weight == 0).all()
+
+
+def test_other_streams_and_captured_graphs():
+    g = gen(9)
+    d, m = 256, 300
+    pre, _ = norm_of(g, d, "layer")
+    post, _ = norm_of(g, d, "rms")
+    gate = torch.randn(d, generator=g).cuda()
+    y, r, dz = (rows(g, m, d, torch.float16) for _ in range(3))
+    want = nb.norm_residual(y, r, pre=pre, post=post, gate=gate)
+    grads = nb.norm_residual_backward(dz, dz, y, want[0], pre=pre, post=post, gate=gate)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = nb.norm_residual(y, r, pre=pre, post=post, gate=gate, stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = nb.norm_residual(y, r, pre=pre, post=post, gate=gate)
+        back = nb.norm_residual_backward(dz, dz, y, out[0], pre=pre, post=post, gate=gate)
+    for _ in range(3):
+        for t in (*out, *(b for b in back if b is not None)):
+            t.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+        assert all(torch.equal(a, b) for a, b in zip(back, grads) if a is not None)
+
+
+def test_refusals():
+    x = torch.zeros(4, 32, dtype=torch.float16, device="cuda")
+    pre = nb.Norm("rms", torch.ones(32).cuda())
+    bad = [
+        lambda: nb.norm_residual(x.cpu(), x),
+        lambda: nb.norm_residual(x, x.float()),
+        lambda: nb.norm_residual(x.to(torch.float64), None),
+        lambda: nb.norm_residual(x, x[:3]),
+        lambda: nb.norm_residual(x, x[:, :31]),
+        lambda: nb.norm_residual(x.t(), None),
+        lambda: nb.norm_residual(None, None),
+        lambda: nb.norm_residual(x, x, pre=nb.Norm("rms", torch.ones(31).cuda())),
+        lambda: nb.norm_residual(x, x, pre=nb.Norm("rms", torch.ones(32))),
+        lambda: nb.norm_residual(x, x, gate=torch.ones(3, 32).cuda()),
+        lambda: nb.norm_residual(x, x, gate=torch.ones(32).half().cuda()),
+        lambda: nb.norm_residual(x, x, res=torch.empty(4, 31, device="cuda", dtype=torch.float16)),
+        lambda: nb.norm_residual(x, x, z=x),
+        lambda: nb.norm_residual_i8(x, x, pre=None),
+        lambda: nb.norm_residual_backward(None, None, x, x, pre=pre),
+        lambda: nb.norm_residual_backward(x, None, x, x),
+        lambda: nb.norm_residual_backward(x, None, x, None, pre=pre),
+        lambda: nb.norm_residual_backward(x, None, None, x, pre=pre, gate=torch.ones(32).cuda()),
+        lambda: nb.Norm("batch"),
+        lambda: nb.Norm("rms", eps=0.0),
+        lambda: nb.quantize_rows(x.to(torch.int32)),
+        lambda: nb.quantize_rows(x, scale=torch.empty(5, device="cuda")),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail(f"call {i} was accepted")
+    wide = torch.zeros(2, 16400, dtype=torch.float16, device="cuda")
+    with pytest.raises(nb.NmError):
+        nb.norm_residual(wide, wide)

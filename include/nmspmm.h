@@ -440,6 +440,13 @@ nm_status nm_quantize_f16(const uint16_t *x, int64_t count, float inv_scale, int
 #define NM_TYPE_BF16 2   /* bfloat16 */
 #define NM_TYPE_F32 3    /* IEEE binary32 */
 
+/* Activations of the gated feed-forward block. */
+#define NM_ACT_SILU 1       /* g / (1 + exp(-g)) */
+#define NM_ACT_GELU 2       /* g (1 + erf(g / sqrt(2))) / 2 */
+#define NM_ACT_GELU_TANH 3  /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 */
+#define NM_ACT_RELU 4       /* max(g, 0) */
+#define NM_ACT_SIGMOID 5    /* 1 / (1 + exp(-g)) */
+
 /* Codes of rows: top = max_t |x[i][t]|, scale[i] = top / 127,
  * xq[i][t] = rint(x[i][t] * (127 / top)), both quotients and the product in
  * binary32, ties to even.  A row with top < 2^-100 has scale 0 and zero codes;
@@ -516,6 +523,77 @@ nm_status nm_norm_residual_backward_workspace(int m, int d, int groups, size_t *
 /* With m == 0 the parameter gradients are set to zero.  Errors: as
  * nm_norm_residual, and NM_ERR_WORKSPACE. */
 nm_status nm_norm_residual_backward(const nm_norm_grad_args *args, void *ws, size_t ws_bytes, void *stream);
+
+/* A weight with a scale for each channel: a packed weight of nm_compress whose
+ * sizes may be padded with zeros.  n and k are the logical sizes: desc->k is k
+ * rounded up to a multiple of 16, desc->n >= n.  scale, bias (or NULL): device
+ * float32 [desc->n], 16-byte aligned, zero past n. */
+typedef struct nm_scaled_weight {
+    const nm_desc *desc;
+    const int8_t *vals;
+    const uint8_t *meta;
+    const float *scale;
+    const float *bias;
+    int32_t n, k;
+} nm_scaled_weight;
+
+/* The int8 product with scales for each token and channel, for dense and N:M weights:
+ *   y[i][j] = T( sx[i] * scale[j] * sum_t xq[i][t] w[j][t] + bias[j] )
+ * the sum exact, scaled in binary32 (as (sum * sx) * scale + bias) and rounded once to
+ * `type`.  xq device int8 [m x desc->k], sx device float32 [m], as
+ * nm_quantize_rows writes them (what the padding of xq holds does not matter); y
+ * device [m] rows of ldy >= n values.  nm_linear_i8 takes x instead (device [m]
+ * rows of ldx >= k values of xtype) and makes the codes itself.
+ * ws: nm_linear_workspace bytes of device memory, any content, 256-byte
+ * aligned (NULL where that is 0); xtype 0 asks for the size that
+ * nm_gemm_i8_scaled needs.  m == 0 is a no-op.  The sums of a row hold in int32
+ * for k < 2^17.  Errors: NM_ERR_ARG (NULL or misaligned pointer, unknown type, a desc that does not
+ * match n and k), NM_ERR_SHAPE (m < 0 or >= 2^30, k >= 2^17, a row stride
+ * below the row, a weight of 2^32 bytes or more), NM_ERR_WORKSPACE, NM_ERR_HIP. */
+nm_status nm_linear_workspace(const nm_scaled_weight *w, int m, int xtype, size_t *bytes);
+nm_status nm_gemm_i8_scaled(const int8_t *xq, const float *sx, int m, const nm_scaled_weight *w, void *y, int64_t ldy,
+                            int type, void *ws, size_t ws_bytes, void *stream);
+nm_status nm_linear_i8(const void *x, int64_t ldx, int xtype, int m, const nm_scaled_weight *w, void *y, int64_t ldy,
+                       int type, void *ws, size_t ws_bytes, void *stream);
+
+/* The gated feed-forward block's first half in one kernel:
+ *   h[i][j] = T( act(g) * u ),  g, u: the scaled products above with the gate's
+ *   and the up projection's weights, in binary32.
+ * w holds both projections as one weight of desc->n = 2 * n' rows, n' = n rounded
+ * up to a multiple of 32: rows [32 b, 32 b + 16) are gate channels [16 b, 16 b +
+ * 16), the next 16 rows the same up channels; w->n = n is the hidden width and
+ * scale and bias are interleaved the same way.  act: NM_ACT_*.  The other
+ * arguments, workspaces and errors as above. */
+nm_status nm_gated_i8(const int8_t *xq, const float *sx, int m, const nm_scaled_weight *w, int act, void *h,
+                      int64_t ldh, int type, void *ws, size_t ws_bytes, void *stream);
+nm_status nm_gated(const void *x, int64_t ldx, int xtype, int m, const nm_scaled_weight *w, int act, void *h,
+                   int64_t ldh, int type, void *ws, size_t ws_bytes, void *stream);
+
+/* Its backward pass, straight through the rounding to codes: with the operands
+ * as the forward pass used them, x = sx q and W = scale w, from dh
+ *   dg = dh u act'(g),  du = dh act(g)
+ *   dx = dg W_gate + du W_up,  dw_gate = dg^T x,  dw_up = du^T x
+ * and the bias gradients, the sums of dg and du over tokens (binary32).  g and u
+ * are computed again in binary32; dg and du enter the products rounded to `type`
+ * (NM_TYPE_F16 or NM_TYPE_BF16) once, after the fraction of the scale that the
+ * sum's other operand does not hold.  dh [m] rows of lddh >= n, dx
+ * [m x k], dw_* [n x k] without gaps, of `type`; dbias_* float32 [n]; any output may be
+ * NULL.  The weight's layout must be NM_LAYOUT_DENSE (NM_ERR_UNSUPPORTED
+ * otherwise).  With m == 0 the weight and bias gradients are set to zero.  The
+ * same inputs give the same bits.  Other errors as above; NM_ERR_SHAPE too
+ * where 2 n' (or k) times m, each rounded up to 64, reaches 2^31. */
+typedef struct nm_gated_grad_args {
+    const int8_t *xq;
+    const float *sx;
+    const void *dh;
+    int64_t lddh;
+    int32_t m, act, type;
+    void *dx, *dw_gate, *dw_up;
+    float *dbias_gate, *dbias_up;
+} nm_gated_grad_args;
+nm_status nm_gated_backward_workspace(const nm_scaled_weight *w, int m, size_t *bytes);
+nm_status nm_gated_backward(const nm_gated_grad_args *args, const nm_scaled_weight *w, void *ws, size_t ws_bytes,
+                            void *stream);
 
 #ifdef __cplusplus
 }

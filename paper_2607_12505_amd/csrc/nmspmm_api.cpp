@@ -48,8 +48,6 @@ int64_t stored_weight_bytes(int kind, int n, int k, int n_frags, int k_steps) {
                                  : (int64_t)n_frags * k_steps * 64 * (layout_lane_vbytes(kind) + layout_lane_mbytes(kind));
 }
 
-int group_rows_for(int tiles_m, int tile_m) { return tiles_m >= 2 * group_size(tile_m) ? group_size(tile_m) : 0; }
-
 // Whether the byte ranges [a, a + na) and [b, b + nb) intersect (a null or
 // empty range intersects nothing).
 bool overlaps(const void *a, int64_t na, const void *b, int64_t nb) {
@@ -61,6 +59,8 @@ bool overlaps(const void *a, int64_t na, const void *b, int64_t nb) {
 }  // namespace
 
 namespace nmspmm {
+
+int group_rows_for(int tiles_m, int tile_m) { return tiles_m >= 2 * group_size(tile_m) ? group_size(tile_m) : 0; }
 
 // Checks an expansion job before anything is launched.
 static nm_status check_job(const nm_expand_job *job) {

@@ -171,3 +171,339 @@ extern "C" nm_status nm_norm_residual_backward(const nm_norm_grad_args *args, vo
                      pieces(g.dy, g.d, g.d, g.type) && pieces(g.dr, g.d, g.d, g.type) && g.d % 8 == 0;
     return launch_norm_residual_backward(g.type, vec, a, s.workgroups, stream) == 0 ? NM_OK : NM_ERR_HIP;
 }
+
+// ---------------------------------------------------------------- products
+
+namespace {
+
+constexpr int64_t kMaxReduction = 1 << 17;   // 127 * 127 * 2^17 < 2^31
+
+nm_status check_weight(const nm_scaled_weight *w, bool gated) {
+    if (!w) return NM_ERR_ARG;
+    nm_status st = check_desc(w->desc);
+    if (st != NM_OK) return st;
+    const nm_desc &d = *w->desc;
+    if (w->n < 1 || w->k < 1 || w->k > d.k || d.k % 16 != 0 || d.k - w->k >= 16 || d.n % 4 != 0) return NM_ERR_ARG;
+    if (gated ? d.n != 2 * ((w->n + 31) / 32 * 32) : w->n > d.n) return NM_ERR_ARG;
+    if (d.k >= kMaxReduction) return NM_ERR_SHAPE;
+    if (d.vals_bytes + d.meta_bytes >= kWeightLimit) return NM_ERR_SHAPE;
+    if (!w->vals || (d.meta_bytes && !w->meta) || !w->scale || !aligned(w->vals, 16) || !aligned(w->meta, 16) ||
+        !aligned(w->scale, 16) || !aligned(w->bias, 16))
+        return NM_ERR_ARG;
+    return NM_OK;
+}
+
+// Whether a compact weight is expanded once for the call, and the bytes of that.
+int64_t expansion(const nm_desc &d, int m) {
+    nm_plan plan;
+    if (!kind_is_compact(d.kind) || make_plan(d.kind, m, d.n, d.k, NM_OUT_F16, &plan) != NM_OK) return 0;
+    return plan.expand ? plan.expand_bytes : 0;
+}
+
+// The codes of x and their scales at the start of the workspace.
+size_t codes_bytes(int m, int k) { return round256((size_t)m * k) + round256((size_t)m * 4); }
+
+void fill_product(BlockArgs &a, int m, const nm_scaled_weight &w) {
+    const nm_desc &d = *w.desc;
+    a.Y = nullptr;
+    a.Yh = nullptr;
+    a.Yq = nullptr;
+    a.scale = w.scale;
+    a.qscale = w.bias;
+    a.counters = nullptr;
+    a.partials = nullptr;
+    a.m = m;
+    a.n = d.n;
+    a.k = d.k;
+    a.k_steps = d.k_steps;
+    a.n_frags = d.n_frags;
+    a.split_k = 1;
+    a.n_out = w.n;
+}
+
+int place_tiles(BlockArgs &a, int tile) {
+    const int tn = kTiles[tile].tile_n(), tm = kTiles[tile].tile_m();
+    a.tiles_n = (a.n + tn - 1) / tn;
+    a.tiles_m = (a.m + tm - 1) / tm;
+    a.group_rows = group_rows_for(a.tiles_m, tm);
+    a.gemm_grid = a.tiles_n * a.tiles_m * a.split_k;
+    return a.gemm_grid;
+}
+
+// What the estimate of a GEMM's time is given as output: the bytes written for each weight row.
+int out_mode_for(int type, bool gated) {
+    return gated ? (type == NM_TYPE_F32 ? NM_OUT_F16 : NM_OUT_I8) : type == NM_TYPE_F32 ? NM_OUT_I32 : NM_OUT_F16;
+}
+
+struct Product {
+    const int8_t *xq;
+    const float *sx;
+    int m;
+    const nm_scaled_weight *w;
+    void *out;
+    int64_t ldo;
+    int type;
+    bool gated;
+    int act;
+};
+
+// ws: room for the expanded weight where there is one.
+nm_status run_product(const Product &p, char *ws, void *stream) {
+    const nm_desc &d = *p.w->desc;
+    int kind = d.kind;
+    const int8_t *vals = p.w->vals;
+    const uint8_t *meta = p.w->meta;
+    if (expansion(d, p.m)) {
+        int8_t *out = (int8_t *)ws;
+        if (launch_expand(kind, vals, meta, d.n, d.k, out, stream) != 0) return NM_ERR_HIP;
+        kind = expanded_kind(kind);
+        vals = out;
+        meta = kind == NM_KIND_SP42 ? (const uint8_t *)(out + (int64_t)d.n_frags * d.k_steps * kVBlock) : nullptr;
+    }
+    // the kernels address X with 32-bit byte offsets: a longer batch goes in parts
+    const int64_t fits = ((((int64_t)1 << 32) - 1) / d.k) / 1280 * 1280;
+    const int eb = type_bytes(p.type);
+    for (int64_t row = 0; row < p.m; row += fits) {
+        const int m = (int)(p.m - row < fits ? p.m - row : fits);
+        BlockArgs a;
+        fill_product(a, m, *p.w);
+        a.X = p.xq + row * d.k;
+        a.A = vals;
+        a.meta = meta;
+        a.row_scale = p.sx + row;
+        a.out = (char *)p.out + row * p.ldo * eb;
+        a.ldo = p.ldo;
+        a.type = p.type;
+        a.act = p.act;
+        a.stream_out = aligned(p.out, 128) ? stream_out_for(m, (int)(p.ldo < (1 << 30) ? p.ldo : 1), d.k) : 0;
+        const int tile = schedule_among(kind, m, d.n, d.k, out_mode_for(p.type, p.gated), kScaledTiles);
+        const int grid = place_tiles(a, tile);
+        const int err = p.gated ? launch_gated(kind, tile, a, grid, stream) : launch_scaled(kind, tile, a, grid, stream);
+        if (err != 0) return NM_ERR_HIP;
+    }
+    return NM_OK;
+}
+
+nm_status check_product(int m, const nm_scaled_weight *w, bool gated, int act, const void *out, int64_t ldo, int type) {
+    if (m < 0 || m >= kMaxRows) return NM_ERR_SHAPE;
+    nm_status st = check_weight(w, gated);
+    if (st != NM_OK) return st;
+    if (!valid_type(type) || (gated && (act < NM_ACT_SILU || act > NM_ACT_SIGMOID))) return NM_ERR_ARG;
+    if (ldo < w->n) return NM_ERR_SHAPE;
+    if (m > 0 && (!out || !aligned(out, type_bytes(type)))) return NM_ERR_ARG;
+    return NM_OK;
+}
+
+nm_status product_of_codes(const int8_t *xq, const float *sx, int m, const nm_scaled_weight *w, bool gated, int act,
+                           void *out, int64_t ldo, int type, void *ws, size_t ws_bytes, void *stream) {
+    nm_status st = check_product(m, w, gated, act, out, ldo, type);
+    if (st != NM_OK || m == 0) return st;
+    if (!xq || !sx || !aligned(xq, 16) || !aligned(sx, 4)) return NM_ERR_ARG;
+    const size_t need = (size_t)expansion(*w->desc, m);
+    if (need && (!ws || ws_bytes < need || !aligned(ws, 256))) return NM_ERR_WORKSPACE;
+    return run_product({xq, sx, m, w, out, ldo, type, gated, act}, (char *)ws, stream);
+}
+
+nm_status product_of_rows(const void *x, int64_t ldx, int xtype, int m, const nm_scaled_weight *w, bool gated, int act,
+                          void *out, int64_t ldo, int type, void *ws, size_t ws_bytes, void *stream) {
+    nm_status st = check_product(m, w, gated, act, out, ldo, type);
+    if (st != NM_OK) return st;
+    if (!valid_type(xtype)) return NM_ERR_ARG;
+    if (ldx < w->k) return NM_ERR_SHAPE;
+    if (m == 0) return NM_OK;
+    if (!x || !aligned(x, type_bytes(xtype))) return NM_ERR_ARG;
+    const nm_desc &d = *w->desc;
+    const size_t codes = codes_bytes(m, d.k), need = codes + (size_t)expansion(d, m);
+    if (!ws || ws_bytes < need || !aligned(ws, 256)) return NM_ERR_WORKSPACE;
+    int8_t *xq = (int8_t *)ws;
+    float *sx = (float *)((char *)ws + round256((size_t)m * d.k));
+    st = nm_quantize_rows(x, ldx, xtype, m, w->k, xq, sx, stream);
+    if (st != NM_OK) return st;
+    return run_product({xq, sx, m, w, out, ldo, type, gated, act}, (char *)ws + codes, stream);
+}
+
+// ---------------------------------------------------------------- gated backward
+
+// Pieces of the workspace, in their order; sizes in bytes, offsets filled by the constructor.
+struct GradPlan {
+    int64_t rows_w, cols, ldt;     // 2 n', k rounded up to 16, tokens rounded up to 64
+    int grad_tile, dx_tile, dw_tile, dw_split;
+    size_t at_da, at_dat, at_xt, at_wt, at_parts, at_split, bytes;
+    int parts_rows;
+
+    GradPlan(const nm_scaled_weight &w, int m) {
+        const nm_desc &d = *w.desc;
+        rows_w = d.n;
+        cols = d.k;
+        ldt = (int64_t)(m + 63) / 64 * 64;
+        grad_tile = schedule_among(NM_KIND_DENSE, m, d.n, d.k, NM_OUT_I32, kGradTiles);
+        dx_tile = schedule_among(NM_KIND_DENSE, m, d.k, (int)(2 * rows_w), NM_OUT_F16, kCastTiles);
+        const int k_bytes = (int)(2 * ldt);
+        dw_tile = schedule_among(NM_KIND_DENSE, d.n, d.k, k_bytes, NM_OUT_F16, kCastTiles);
+        const TileCfg &g = kTiles[grad_tile];
+        parts_rows = (m + g.tile_m() - 1) / g.tile_m() * g.wm;
+        // the weights' gradient has few tiles and a long reduction: split until
+        // every compute unit has two workgroups, with 16 k-steps or more each
+        const TileCfg &t = kTiles[dw_tile];
+        const int64_t tiles = ((rows_w + t.tile_m() - 1) / t.tile_m()) * ((cols + t.tile_n() - 1) / t.tile_n());
+        dw_split = 1;
+        while (dw_split < 8 && tiles * dw_split < device_cu_count() && k_bytes / kKStep / (2 * dw_split) >= 16 &&
+               tiles <= kMaxSplitTiles && 2 * dw_split * rows_w * cols * 4 < ((int64_t)1 << 31))
+            dw_split *= 2;
+        size_t at = 0;
+        auto take = [&](int64_t n) {
+            const size_t here = at;
+            at += round256((size_t)n);
+            return here;
+        };
+        at_da = take((int64_t)m * rows_w * 2);
+        at_dat = take(rows_w * ldt * 2);
+        at_xt = take(cols * ldt * 2);
+        at_wt = take(cols * rows_w * 2);
+        at_parts = take((int64_t)parts_rows * rows_w * 4);
+        at_split = take(dw_split > 1 ? (int64_t)kCounterBytes + dw_split * rows_w * cols * 4 : 0);
+        bytes = at;
+    }
+};
+
+nm_status check_grad(const nm_scaled_weight *w, int m) {
+    nm_status st = check_weight(w, true);
+    if (st != NM_OK) return st;
+    if (w->desc->layout != NM_LAYOUT_DENSE) return NM_ERR_UNSUPPORTED;
+    if (m < 0 || m >= kMaxRows) return NM_ERR_SHAPE;
+    const int64_t tokens = ((int64_t)m + 63) / 64 * 64, wide = w->desc->n > w->desc->k ? w->desc->n : w->desc->k;
+    if (tokens * ((wide + 63) / 64 * 64) >= ((int64_t)1 << 31)) return NM_ERR_SHAPE;
+    if ((int64_t)w->desc->n * w->desc->k >= ((int64_t)1 << 29)) return NM_ERR_SHAPE;
+    return NM_OK;
+}
+
+}  // namespace
+
+extern "C" nm_status nm_linear_workspace(const nm_scaled_weight *w, int m, int xtype, size_t *bytes) {
+    if (!bytes || !w || (xtype != 0 && !valid_type(xtype))) return NM_ERR_ARG;
+    nm_status st = check_desc(w->desc);
+    if (st != NM_OK) return st;
+    if (m < 0 || m >= kMaxRows) return NM_ERR_SHAPE;
+    *bytes = m == 0 ? 0 : (xtype ? codes_bytes(m, w->desc->k) : 0) + (size_t)expansion(*w->desc, m);
+    return NM_OK;
+}
+
+extern "C" nm_status nm_gemm_i8_scaled(const int8_t *xq, const float *sx, int m, const nm_scaled_weight *w, void *y,
+                                       int64_t ldy, int type, void *ws, size_t ws_bytes, void *stream) {
+    return product_of_codes(xq, sx, m, w, false, 0, y, ldy, type, ws, ws_bytes, stream);
+}
+
+extern "C" nm_status nm_linear_i8(const void *x, int64_t ldx, int xtype, int m, const nm_scaled_weight *w, void *y,
+                                  int64_t ldy, int type, void *ws, size_t ws_bytes, void *stream) {
+    return product_of_rows(x, ldx, xtype, m, w, false, 0, y, ldy, type, ws, ws_bytes, stream);
+}
+
+extern "C" nm_status nm_gated_i8(const int8_t *xq, const float *sx, int m, const nm_scaled_weight *w, int act, void *h,
+                                 int64_t ldh, int type, void *ws, size_t ws_bytes, void *stream) {
+    return product_of_codes(xq, sx, m, w, true, act, h, ldh, type, ws, ws_bytes, stream);
+}
+
+extern "C" nm_status nm_gated(const void *x, int64_t ldx, int xtype, int m, const nm_scaled_weight *w, int act, void *h,
+                              int64_t ldh, int type, void *ws, size_t ws_bytes, void *stream) {
+    return product_of_rows(x, ldx, xtype, m, w, true, act, h, ldh, type, ws, ws_bytes, stream);
+}
+
+extern "C" nm_status nm_gated_backward_workspace(const nm_scaled_weight *w, int m, size_t *bytes) {
+    if (!bytes) return NM_ERR_ARG;
+    nm_status st = check_grad(w, m);
+    if (st != NM_OK) return st;
+    *bytes = m == 0 ? 0 : GradPlan(*w, m).bytes;
+    return NM_OK;
+}
+
+extern "C" nm_status nm_gated_backward(const nm_gated_grad_args *args, const nm_scaled_weight *w, void *ws,
+                                       size_t ws_bytes, void *stream) {
+    if (!args) return NM_ERR_ARG;
+    const nm_gated_grad_args &g = *args;
+    nm_status st = check_grad(w, g.m);
+    if (st != NM_OK) return st;
+    if ((g.type != NM_TYPE_F16 && g.type != NM_TYPE_BF16) || g.act < NM_ACT_SILU || g.act > NM_ACT_SIGMOID)
+        return NM_ERR_ARG;
+    for (const void *p : {(const void *)g.dx, (const void *)g.dw_gate, (const void *)g.dw_up})
+        if (!aligned(p, 2)) return NM_ERR_ARG;
+    if (!aligned(g.dbias_gate, 4) || !aligned(g.dbias_up, 4)) return NM_ERR_ARG;
+    if ((!g.dw_gate) != (!g.dw_up)) return NM_ERR_ARG;
+    const nm_desc &d = *w->desc;
+    if (g.m == 0) {
+        const size_t each = (size_t)w->n * w->k * 2;
+        if ((g.dw_gate && (launch_zero(g.dw_gate, each, stream) != 0 || launch_zero(g.dw_up, each, stream) != 0)) ||
+            (g.dbias_gate && launch_zero(g.dbias_gate, (size_t)w->n * 4, stream) != 0) ||
+            (g.dbias_up && launch_zero(g.dbias_up, (size_t)w->n * 4, stream) != 0))
+            return NM_ERR_HIP;
+        return NM_OK;
+    }
+    if (g.lddh < w->n) return NM_ERR_SHAPE;
+    if (!g.xq || !g.sx || !g.dh || !aligned(g.xq, 16) || !aligned(g.sx, 4) || !aligned(g.dh, 2)) return NM_ERR_ARG;
+    const GradPlan p(*w, g.m);
+    if (!ws || ws_bytes < p.bytes || !aligned(ws, 256)) return NM_ERR_WORKSPACE;
+    char *base = (char *)ws;
+
+    // dg and du
+    BlockArgs a;
+    fill_product(a, g.m, *w);
+    a.X = g.xq;
+    a.A = w->vals;
+    a.meta = nullptr;
+    a.row_scale = g.sx;
+    a.type = g.type;
+    a.act = g.act;
+    a.dh = g.dh;
+    a.lddh = g.lddh;
+    a.da = base + p.at_da;
+    a.dat = base + p.at_dat;
+    a.ldt = p.ldt;
+    a.bias_parts = g.dbias_gate || g.dbias_up ? (float *)(base + p.at_parts) : nullptr;
+    int grid = place_tiles(a, p.grad_tile);
+    if (launch_gated_grad(p.grad_tile, a, grid, stream) != 0) return NM_ERR_HIP;
+    if (a.bias_parts && launch_bias_sums(a.bias_parts, p.parts_rows, d.n, w->n, g.dbias_gate, g.dbias_up, stream) != 0)
+        return NM_ERR_HIP;
+
+    BlockArgs c;
+    fill_product(c, g.m, *w);
+    c.scale = nullptr;
+    c.qscale = nullptr;
+    c.meta = nullptr;
+    c.n = d.k;
+    c.n_out = w->k;
+    c.ldo = w->k;
+    c.n_frags = (d.k + kFragRows - 1) / kFragRows;
+    if (g.dx) {
+        if (launch_transpose_codes(g.type, {w->vals, w->scale, base + p.at_wt, d.k, p.rows_w, d.n, d.k}, stream) != 0)
+            return NM_ERR_HIP;
+        c.X = (const int8_t *)(base + p.at_da);
+        c.A = (const int8_t *)(base + p.at_wt);
+        c.k = (int)(2 * p.rows_w);
+        c.k_steps = c.k / kKStep;
+        c.out = g.dx;
+        c.stream_out = aligned(g.dx, 128) ? stream_out_for(g.m, w->k, c.k) : 0;
+        grid = place_tiles(c, p.dx_tile);
+        if (launch_cast(g.type, p.dx_tile, c, grid, stream) != 0) return NM_ERR_HIP;
+    }
+    if (g.dw_gate) {
+        if (launch_transpose_codes(g.type, {g.xq, g.sx, base + p.at_xt, d.k, p.ldt, g.m, d.k}, stream) != 0)
+            return NM_ERR_HIP;
+        c.X = (const int8_t *)(base + p.at_dat);
+        c.A = (const int8_t *)(base + p.at_xt);
+        c.m = d.n;
+        c.k = (int)(2 * p.ldt);
+        c.k_steps = c.k / kKStep;
+        c.out = g.dw_gate;
+        c.out2 = g.dw_up;
+        c.interleaved = w->n;
+        c.split_k = p.dw_split;
+        if (p.dw_split > 1) {
+            c.counters = (int32_t *)(base + p.at_split);
+            c.partials = (int32_t *)(base + p.at_split + kCounterBytes);
+            if (launch_zero(c.counters, kCounterBytes, stream) != 0) return NM_ERR_HIP;
+        }
+        c.stream_out = 0;
+        grid = place_tiles(c, p.dw_tile);
+        if (launch_cast(g.type, p.dw_tile, c, grid, stream) != 0) return NM_ERR_HIP;
+    }
+    return NM_OK;
+}

@@ -56,4 +56,49 @@ int launch_norm_residual(int type, bool vec, const NormArgs &a, void *stream);
 int launch_norm_residual_backward(int type, bool vec, const NormGradArgs &a, int workgroups, void *stream);
 int launch_quantize_rows(int type, bool vec, const QuantArgs &a, void *stream);
 
+// ---------------------------------------------------------------- products
+
+// GemmArgs plus what the epilogues of the block's products need.  `scale` and
+// `qscale` hold the channels' scales and biases (qscale null: none).
+struct BlockArgs : GemmArgs {
+    const float *row_scale = nullptr;   // [m]
+    void *out = nullptr;                // rows of ldo values, n_out of them wanted
+    int64_t ldo = 0;
+    int n_out = 0;
+    int type = 0;                       // NM_TYPE_* of out (and of dh)
+    int act = 0;                        // NM_ACT_*
+    // gradients of the gated block
+    const void *dh = nullptr;           // [m] rows of lddh values
+    int64_t lddh = 0;
+    void *da = nullptr, *dat = nullptr; // [m x n], [n x ldt]
+    int64_t ldt = 0;
+    float *bias_parts = nullptr;        // [16-row-of-tokens groups of waves x n] or null
+    void *out2 = nullptr;               // second half of interleaved rows
+    int interleaved = 0;
+};
+
+// Tiles that the products are built for, by what they write.
+constexpr uint32_t kScaledTiles = 1u << 1 | 1u << 3 | 1u << 6 | 1u << 12 | 1u << 15;
+constexpr uint32_t kGradTiles = 1u << 1 | 1u << 3 | 1u << 6;   // whole 64-token groups: the transposed rows' padding is written too
+constexpr uint32_t kCastTiles = 1u << 1 | 1u << 3 | 1u << 6 | 1u << 12 | 1u << 4;
+
+int launch_scaled(int kind, int tile, const BlockArgs &a, int grid, void *stream);
+int launch_gated(int kind, int tile, const BlockArgs &a, int grid, void *stream);
+int launch_gated_grad(int tile, const BlockArgs &a, int grid, void *stream);
+// C = A B^T of 16-bit rows (a.k counts bytes), to `type`.
+int launch_cast(int type, int tile, const BlockArgs &a, int grid, void *stream);
+
+// Codes [rows x ld] with a scale each -> their transpose [cols x ldt] in 16 bits, each code times the power of two
+// of its row's scale (exact); zeros from `rows` to ldt.
+struct TransposeArgs {
+    const int8_t *q;
+    const float *scale;
+    void *out;
+    int64_t ld, ldt;
+    int rows, cols;
+};
+int launch_transpose_codes(int type, const TransposeArgs &a, void *stream);
+// dst[c] = sum over rows of parts[rows x n] for the channels of interleaved rows.
+int launch_bias_sums(const float *parts, int rows, int n, int n_out, float *gate, float *up, void *stream);
+
 }  // namespace nmspmm

@@ -1,0 +1,97 @@
+// The gated block's backward pass: the gradients of g and u from one more int8
+// product, the codes transposed to 16 bits, and two products of 16-bit operands
+// (fp16 or bf16, as the activations) that give dx and the weights' gradients.
+//
+//   dx[i][t]  = sum over channels j of d[i][j] c[j] w[j][t]
+//   dw[j][t]  = sum over tokens i   of d[i][j] s[i] q[i][t]
+//
+// The scales run along the reductions, so they belong to an operand.  A scale is
+// split into a power of two, which goes to the int8 codes (exact in 16 bits), and
+// a part in [1, 2), which goes to d before it is rounded: each sum's operands
+// are rounded once, as the activations' type rounds them.
+#include "nmspmm_products.h"
+
+namespace nmspmm {
+namespace {
+
+// 64 rows x 64 columns of codes a workgroup, turned in LDS.
+template <class T>
+__global__ __launch_bounds__(256) void k_transpose_codes(TransposeArgs a, int col_blocks) {
+    __shared__ __attribute__((aligned(16))) int8_t tile[64 * 80];
+    __shared__ float power[64];
+    const int t = threadIdx.x;
+    const int r0 = (int)(blockIdx.x / col_blocks) * 64, c0 = (int)(blockIdx.x % col_blocks) * 64;
+    {
+        const int row = r0 + t / 4, col = c0 + (t & 3) * 16;
+        v4i v = {0, 0, 0, 0};
+        if (row < a.rows && col < a.cols) v = *(const v4i *)(a.q + row * a.ld + col);   // cols: a multiple of 16
+        *(v4i *)(tile + (t / 4) * 80 + (t & 3) * 16) = v;
+        if (t < 64) power[t] = r0 + t < a.rows ? scale_power(a.scale[r0 + t]) : 0.f;
+    }
+    __syncthreads();
+    const int col = c0 + t / 4, rr = (t & 3) * 16;
+    if (col >= a.cols) return;
+    T *dst = (T *)a.out + col * a.ldt + r0 + rr;                                         // ldt: a multiple of 64
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = (float)tile[(rr + h * 8 + e) * 80 + t / 4] * power[rr + h * 8 + e];
+        store8(dst + h * 8, f);
+    }
+}
+
+__global__ __launch_bounds__(1024) void k_bias_sums(const float *parts, int rows, int n, int n_out, float *gate,
+                                                    float *up) {
+    __shared__ float part[16][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int row = blockIdx.x * 64 + lane;    // of the interleaved weight
+    float s = 0.f;
+    if (row < n)
+#pragma unroll 8
+        for (int r = wave; r < rows; r += 16) s += parts[(int64_t)r * n + row];
+    part[wave][lane] = s;
+    __syncthreads();
+    const int ch = (row >> 5) * 16 + (row & 15);
+    if (wave == 0 && row < n && ch < n_out) {
+        float all = 0.f;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) all += part[w][lane];
+        float *dst = (row & 16) ? up : gate;
+        if (dst) dst[ch] = all;
+    }
+}
+
+}  // namespace
+
+int launch_gated_grad(int tile, const BlockArgs &a, int grid, void *stream) {
+    return a.type == NM_TYPE_F16
+               ? launch_product<NM_KIND_DENSE, GatedGradOut<half_t>, kGradTiles>(tile, a, grid, stream)
+               : launch_product<NM_KIND_DENSE, GatedGradOut<bf16_t>, kGradTiles>(tile, a, grid, stream);
+}
+
+int launch_cast(int type, int tile, const BlockArgs &a, int grid, void *stream) {
+    return type == NM_TYPE_F16 ? launch_product<kKindF16, CastOut<half_t>, kCastTiles>(tile, a, grid, stream)
+                               : launch_product<kKindBF16, CastOut<bf16_t>, kCastTiles>(tile, a, grid, stream);
+}
+
+int launch_transpose_codes(int type, const TransposeArgs &a, void *stream) {
+    const int col_blocks = (a.cols + 63) / 64;
+    const int64_t grid = (int64_t)col_blocks * (a.ldt / 64);
+    if (grid > 0x7fffffff) return (int)hipErrorInvalidValue;
+    if (type == NM_TYPE_F16)
+        hipLaunchKernelGGL(k_transpose_codes<half_t>, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream, a,
+                           col_blocks);
+    else
+        hipLaunchKernelGGL(k_transpose_codes<bf16_t>, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream, a,
+                           col_blocks);
+    return (int)hipGetLastError();
+}
+
+int launch_bias_sums(const float *parts, int rows, int n, int n_out, float *gate, float *up, void *stream) {
+    hipLaunchKernelGGL(k_bias_sums, dim3((n + 63) / 64), dim3(1024), 0, (hipStream_t)stream, parts, rows, n, n_out, gate,
+                       up);
+    return (int)hipGetLastError();
+}
+
+}  // namespace nmspmm

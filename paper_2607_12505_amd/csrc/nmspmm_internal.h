@@ -184,5 +184,9 @@ nm_status complete_plan(int kind, int m, int n, int k, nm_plan *plan);
 // Without an explicit plan: the tile (index into kTiles, up to kNumSchedules)
 // with the least estimated time for the planner's unsplit plan.
 int schedule_tile(int kind, int m, int n, int k, int out_mode, int planned);
+// The tile of the set (bit t: tile t) with the least estimated time.
+int schedule_among(int kind, int m, int n, int k, int out_mode, uint32_t tiles);
+// Tile order of a launch: rows of tiles walked together (0: row by row).
+int group_rows_for(int tiles_m, int tile_m);
 
 }  // namespace nmspmm

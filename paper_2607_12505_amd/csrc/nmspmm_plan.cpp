@@ -405,35 +405,64 @@ static int cost_group(int kind) {
     }
 }
 
-int schedule_tile(int kind, int m, int n, int k, int out_mode, int planned) {
-    // 32-bit divisions only: this runs in every call
-    const uint32_t cus = (uint32_t)device_cu_count();
-    uint32_t bytes = 0, split_line = 0;   // per output element; of rows that do not start on a 128-byte line
-    for (uint32_t eb : {4u, 2u, 1u})
-        if (out_mode & (eb == 4 ? NM_OUT_I32 : eb == 2 ? NM_OUT_F16 : NM_OUT_I8)) {
-            bytes += eb;
-            if ((uint64_t)n * eb % 128 != 0) split_line += eb;
-        }
-    const float mn = (float)m * (float)n * 1e-6f, out_mb = mn * (float)bytes, split_mb = mn * (float)split_line;
-    const float x_mb = (float)m * (float)k * 1e-6f;
-    const uint32_t k_steps = ((uint32_t)k + kKStep - 1) / kKStep;
-    const CostTerms *cost = kCost[cost_group(kind)];
-    auto estimate_us = [&](int t) {
+namespace {
+// The estimate of one GEMM, tile by tile.
+struct Estimate {
+    uint32_t m, n, cus, bytes = 0;
+    float k_steps, out_mb, split_mb, x_mb;
+    const CostTerms *cost;
+
+    Estimate(int kind, int m_, int n_, int k, int out_mode)
+        : m((uint32_t)m_), n((uint32_t)n_), cus((uint32_t)device_cu_count()), cost(kCost[cost_group(kind)]) {
+        // 32-bit divisions only: this runs in every call
+        uint32_t split_line = 0;   // bytes per output element of rows that do not start on a 128-byte line
+        for (uint32_t eb : {4u, 2u, 1u})
+            if (out_mode & (eb == 4 ? NM_OUT_I32 : eb == 2 ? NM_OUT_F16 : NM_OUT_I8)) {
+                bytes += eb;
+                if ((uint64_t)n * eb % 128 != 0) split_line += eb;
+            }
+        const float mn = (float)m * (float)n * 1e-6f;
+        out_mb = mn * (float)bytes;
+        split_mb = mn * (float)split_line;
+        x_mb = (float)m * (float)k * 1e-6f;
+        k_steps = (float)(((uint32_t)k + kKStep - 1) / kKStep);
+    }
+    float us(int t) const {
         const CostTerms &c = cost[t];
         const uint32_t tn = (uint32_t)kTiles[t].tile_n(), tm = (uint32_t)kTiles[t].tile_m();
-        const uint32_t tiles = (((uint32_t)n + tn - 1) / tn) * (((uint32_t)m + tm - 1) / tm);   // below 2^29
-        const float steps = (float)(kTiles[t].layout == kKSliced ? (k_steps + 3) / 4 : k_steps);
+        const uint32_t tiles = ((n + tn - 1) / tn) * ((m + tm - 1) / tm);   // below 2^29
+        const float steps = kTiles[t].layout == kKSliced ? (float)(((uint32_t)k_steps + 3) / 4) : k_steps;
         const float rounds = (float)((tiles + cus - 1) / cus), mean = (float)tiles / (float)cus;
         return c.launch + steps * (c.chain + c.round_steps * rounds + c.mean_steps * mean) +
                rounds * (c.rounds + c.round_bytes * (float)bytes) + c.out_mb * out_mb + c.split_line_mb * split_mb +
                c.x_mb * x_mb;
-    };
+    }
+};
+}  // namespace
+
+int schedule_tile(int kind, int m, int n, int k, int out_mode, int planned) {
+    const Estimate estimate(kind, m, n, k, out_mode);
     int best = planned;
-    float least = (k > kFittedK ? 0.88f : 0.97f) * estimate_us(planned);
+    float least = (k > kFittedK ? 0.88f : 0.97f) * estimate.us(planned);
     for (int t = 0; t < kNumSchedules; ++t) {
         if (!tile_built(kind, t)) continue;
-        const float us = estimate_us(t);
+        const float us = estimate.us(t);
         if (us < least) {
+            least = us;
+            best = t;
+        }
+    }
+    return best;
+}
+
+int schedule_among(int kind, int m, int n, int k, int out_mode, uint32_t tiles) {
+    const Estimate estimate(kind, m, n, k, out_mode);
+    int best = -1;
+    float least = 0.f;
+    for (int t = 0; t < kNumSchedules; ++t) {
+        if (!((tiles >> t) & 1)) continue;
+        const float us = estimate.us(t);
+        if (best < 0 || us < least) {
             least = us;
             best = t;
         }

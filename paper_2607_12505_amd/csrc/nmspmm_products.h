@@ -1,0 +1,417 @@
+// Epilogues of the products of a transformer block, on the k-loop of
+// nmspmm_gemm.h: scales for each token and channel, the gate of a gated
+// feed-forward block, its gradients, and plain 16-bit results.
+#pragma once
+
+#include "nmspmm_block.h"
+#include "nmspmm_gemm.h"
+#include "nmspmm_values.h"
+
+namespace nmspmm {
+namespace {
+
+// Pieces of rows whose start has only the alignment of their values (the
+// hardware takes wide global accesses at any address of 2 bytes or more).
+typedef unsigned int v4u_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef unsigned int v2u_any __attribute__((ext_vector_type(2), aligned(2)));
+
+template <class T>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    typedef T v2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, v2{(T)a, (T)b});
+}
+template <class T>
+__device__ __forceinline__ v2u pack4_of(const v4f &f) {
+    return v2u{pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3])};
+}
+
+// 16 bytes (16 / sizeof(T) channels from ch) of a row of n channels.
+template <class T>
+__device__ __forceinline__ void store_piece(T *row, int ch, int n, const v4i &v, bool stream) {
+    constexpr int PER = 16 / sizeof(T);
+    if (ch + PER <= n) {
+        if (stream)
+            __builtin_nontemporal_store(__builtin_bit_cast(v4u, v), (v4u_any *)(row + ch));
+        else
+            *(v4u_any *)(row + ch) = __builtin_bit_cast(v4u, v);
+    } else {
+        typedef T vec __attribute__((ext_vector_type(PER)));
+        const vec t = __builtin_bit_cast(vec, v);
+#pragma unroll
+        for (int e = 0; e < PER; ++e)
+            if (ch + e < n) row[ch + e] = t[e];
+    }
+}
+
+// The wave's accumulators (or what was made of them) as rows of type T.
+template <class G, class T, class Acc, class Value, class Row>
+__device__ __forceinline__ void store_tile(int8_t *stg, int lane, const Acc (&acc)[G::FN][G::FM], int ch0, int n,
+                                           bool stream, const Value &value, const Row &row_of) {
+    store_rows<G, (int)sizeof(T)>(
+        stg, lane, acc,
+        [&](int i, int j, const Acc &v, int8_t *dst) {
+            const v4f f = value(i, j, v);
+            if constexpr (sizeof(T) == 4)
+                *(v4f *)dst = f;
+            else
+                *(v2u *)dst = pack4_of<T>(f);
+        },
+        [&](int row, int ch, const v4i &v) {
+            T *p = (T *)row_of(row, (T *)nullptr);
+            if (p && ch0 + ch < n) store_piece<T>(p, ch0 + ch, n, v, stream);
+        });
+}
+
+template <class F>
+__device__ __forceinline__ void by_type(int type, const F &f) {
+    if (type == NM_TYPE_F16)
+        f((half_t *)nullptr);
+    else if (type == NM_TYPE_BF16)
+        f((bf16_t *)nullptr);
+    else
+        f((float *)nullptr);
+}
+
+// The scales of the wave's tokens: token fragment j, lane % 16.
+template <class G>
+__device__ __forceinline__ void load_row_scales(const BlockArgs &a, const TileAt &at, float (&sx)[G::FM]) {
+#pragma unroll
+    for (int j = 0; j < G::FM; ++j) {
+        const int tok = at.tok + j * 16 + (at.lane & 15);
+        sx[j] = a.row_scale[tok < a.m ? tok : a.m - 1];
+    }
+}
+
+__device__ __forceinline__ v4f scaled_value(const v4i &v, float sx, const v4f &c, const v4f &b) {
+    v4f f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = __builtin_fmaf((float)v[e] * sx, c[e], b[e]);
+    return f;
+}
+
+// y = T(acc * sx[token] * c[channel] + b[channel]): the int32 sum is exact, three
+// roundings in binary32 and the one to T.
+struct ScaledOut {
+    static __device__ bool scaled(const BlockArgs &) { return true; }
+    static __device__ const float *first(const BlockArgs &a) { return a.scale; }
+    static __device__ const float *second(const BlockArgs &a) { return a.qscale; }
+
+    template <class G, class Mul>
+    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at,
+                                                  const v4i (&acc)[G::FN][G::FM], int8_t *stg, const Mul &multiplier,
+                                                  int *) {
+        float sx[G::FM];
+        load_row_scales<G>(a, at, sx);
+        by_type(a.type, [&](auto *t) {
+            using T = typename std::remove_pointer<decltype(t)>::type;
+            store_tile<G, T>(
+                stg, at.lane, acc, at.ch, a.n_out, (a.stream_out & sizeof(T)) != 0,
+                [&](int i, int j, const v4i &v) {
+                    return scaled_value(v, sx[j], multiplier(0, i), a.qscale ? multiplier(1, i) : v4f{0, 0, 0, 0});
+                },
+                [&](int row, T *) -> T * {
+                    return at.tok + row < a.m ? (T *)a.out + (int64_t)(at.tok + row) * a.ldo : nullptr;
+                });
+        });
+    }
+};
+
+// act(g) and its derivative.  The exponential is the hardware's (2^x within an
+// ulp, its argument rounded to binary32), the reciprocal within an ulp: a few
+// 2^-24 of act(g), under the rounding to T of what they enter.
+__device__ __forceinline__ float sigmoid(float g) {
+    return __builtin_amdgcn_rcpf(1.f + __expf(-g));
+}
+__device__ __forceinline__ void act_and_slope(int act, float g, float &f, float &df) {
+    if (act == NM_ACT_SILU) {
+        const float s = sigmoid(g);
+        f = g * s;
+        df = s * __builtin_fmaf(g, 1.f - s, 1.f);
+    } else if (act == NM_ACT_SIGMOID) {
+        f = sigmoid(g);
+        df = f * (1.f - f);
+    } else if (act == NM_ACT_RELU) {
+        f = g > 0.f || g != g ? g : 0.f;
+        df = g > 0.f ? 1.f : 0.f;
+    } else if (act == NM_ACT_GELU) {
+        const float p = 0.5f * erfcf(-0.70710678118654752f * g);
+        f = g * p;
+        df = __builtin_fmaf(0.39894228040143268f * g, __expf(-0.5f * g * g), p);
+    } else {   // NM_ACT_GELU_TANH: tanh(v) = 2 sigmoid(2 v) - 1
+        const float in = 0.79788456080286536f * __builtin_fmaf(0.044715f * g * g, g, g);
+        const float p = sigmoid(2.f * in);   // (1 + tanh) / 2
+        f = g * p;
+        df = __builtin_fmaf(2.f * g * p * (1.f - p), 0.79788456080286536f * __builtin_fmaf(0.134145f * g, g, 1.f), p);
+    }
+}
+__device__ __forceinline__ float act_of(int act, float g) {
+    float f, df;
+    act_and_slope(act, g, f, df);
+    return f;
+}
+
+// A tile's rows of the interleaved weight: 16 gate channels, the same 16 up
+// channels, the next 16 ...  So fragments 2 i and 2 i + 1 of a wave hold g and u
+// of the same channels in the same lanes.
+template <class G>
+struct HalfTile {
+    static constexpr int FN = G::FN / 2, FM = G::FM;
+    static constexpr int stage_rows(int eb) { return 16 * FN * eb >= 64 ? 16 : 1024 / (16 * FN * eb); }
+    static constexpr int stage_bytes(int eb) { return stage_rows(eb) * (FN * 16 * eb + 16); }
+    static_assert(G::FN % 2 == 0 && stage_bytes(2) <= G::STG && stage_bytes(4) <= G::STG, "gated tile");
+};
+
+// h = T(act(g) * u).
+struct GatedOut {
+    static __device__ bool scaled(const BlockArgs &) { return true; }
+    static __device__ const float *first(const BlockArgs &a) { return a.scale; }
+    static __device__ const float *second(const BlockArgs &a) { return a.qscale; }
+
+    template <class G, class Mul>
+    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at,
+                                                  const v4i (&acc)[G::FN][G::FM], int8_t *stg, const Mul &multiplier,
+                                                  int *) {
+        using H = HalfTile<G>;
+        float sx[G::FM];
+        load_row_scales<G>(a, at, sx);
+        v4f h[H::FN][H::FM];
+#pragma unroll
+        for (int i = 0; i < H::FN; ++i) {
+            const v4f cg = multiplier(0, 2 * i), cu = multiplier(0, 2 * i + 1);
+            const v4f zero = {0, 0, 0, 0};
+            const v4f bg = a.qscale ? multiplier(1, 2 * i) : zero, bu = a.qscale ? multiplier(1, 2 * i + 1) : zero;
+#pragma unroll
+            for (int j = 0; j < H::FM; ++j) {
+                const v4f g = scaled_value(acc[2 * i][j], sx[j], cg, bg);
+                const v4f u = scaled_value(acc[2 * i + 1][j], sx[j], cu, bu);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[i][j][e] = act_of(a.act, g[e]) * u[e];
+            }
+        }
+        by_type(a.type, [&](auto *t) {
+            using T = typename std::remove_pointer<decltype(t)>::type;
+            store_tile<H, T>(
+                stg, at.lane, h, at.ch / 2, a.n_out, (a.stream_out & sizeof(T)) != 0,
+                [&](int, int, const v4f &v) { return v; },
+                [&](int row, T *) -> T * {
+                    return at.tok + row < a.m ? (T *)a.out + (int64_t)(at.tok + row) * a.ldo : nullptr;
+                });
+        });
+    }
+};
+
+// A positive scale as power of two times a value in [1, 2): codes times the power
+// are exact in 16 bits, so a product with a scale along the reduction needs no
+// rounding but that of the other operand.  0 and NaN: 0 and NaN times 1.
+__device__ __forceinline__ float scale_power(float s) {
+    return s != s ? s : __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, s) & 0x7F800000u);
+}
+__device__ __forceinline__ float scale_part(float s) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, s) & 0x7FFFFFFFu;
+    return b < 0x00800000u || b >= 0x7F800000u ? 1.f : __builtin_bit_cast(float, (b & 0x007FFFFFu) | 0x3F800000u);
+}
+
+// From the recomputed g and u and dh:  dg = dh u act'(g), du = dh act(g), written
+// for the two products that follow, with the part of the scale that their 16-bit
+// codes leave out: by rows for dx (times the channel's), transposed for the
+// weights' gradients (times the token's).  Their sums over the wave's tokens
+// go to bias_parts in binary32.
+template <class T>
+struct GatedGradOut {
+    static __device__ bool scaled(const BlockArgs &) { return true; }
+    static __device__ const float *first(const BlockArgs &a) { return a.scale; }
+    static __device__ const float *second(const BlockArgs &a) { return a.qscale; }
+
+    template <class G, class Mul>
+    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at,
+                                                  const v4i (&acc)[G::FN][G::FM], int8_t *stg, const Mul &multiplier,
+                                                  int *) {
+        constexpr int FN = G::FN, FM = G::FM;
+        const int lane = at.lane, lg = lane >> 4, lt = lane & 15;
+        float sx[FM];
+        load_row_scales<G>(a, at, sx);
+        v4f d[FN][FM];
+#pragma unroll
+        for (int i = 0; i < FN; i += 2) {
+            const v4f cg = multiplier(0, i), cu = multiplier(0, i + 1), zero = {0, 0, 0, 0};
+            const v4f bg = a.qscale ? multiplier(1, i) : zero, bu = a.qscale ? multiplier(1, i + 1) : zero;
+            const int ch = at.ch / 2 + i * 8 + 4 * lg;
+#pragma unroll
+            for (int j = 0; j < FM; ++j) {
+                const int tok = at.tok + j * 16 + lt;
+                const v4f g = scaled_value(acc[i][j], sx[j], cg, bg), u = scaled_value(acc[i + 1][j], sx[j], cu, bu);
+                float dh[4] = {0, 0, 0, 0};
+                if (tok < a.m) {
+                    const T *p = (const T *)a.dh + (int64_t)tok * a.lddh + ch;
+                    if (ch + 4 <= a.n_out) {
+                        typedef T v4t __attribute__((ext_vector_type(4)));
+                        const v4t t = __builtin_bit_cast(v4t, (v2u)(*(const v2u_any *)p));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) dh[e] = (float)t[e];
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (ch + e < a.n_out) dh[e] = (float)p[e];
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float f, df;
+                    act_and_slope(a.act, g[e], f, df);
+                    // tokens past the last one have no gradient, whatever their row holds
+                    d[i][j][e] = tok < a.m ? dh[e] * u[e] * df : 0.f;
+                    d[i + 1][j][e] = tok < a.m ? dh[e] * f : 0.f;
+                }
+            }
+        }
+        store_tile<G, T>(
+            stg, lane, d, at.ch, a.n, false,
+            [&](int i, int, const v4f &v) {
+                const v4f c = multiplier(0, i);
+                return v4f{v[0] * scale_part(c[0]), v[1] * scale_part(c[1]), v[2] * scale_part(c[2]),
+                           v[3] * scale_part(c[3])};
+            },
+            [&](int row, T *) -> T * {
+                return at.tok + row < a.m ? (T *)a.da + (int64_t)(at.tok + row) * a.n : nullptr;
+            });
+        // transposed: 16 channels x FM * 16 tokens at a time through the staging area
+        constexpr int TROW = FM * 16 * 2 + 16;       // bytes of a staged channel, padded
+        constexpr int CPR = FM * 2;                  // 16-byte pieces of it
+        static_assert(16 * TROW <= G::STG, "transposed staging");
+#pragma unroll
+        for (int i = 0; i < FN; ++i) {
+#pragma unroll
+            for (int j = 0; j < FM; ++j) {
+                const float part = scale_part(sx[j]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    *(T *)(stg + (4 * lg + e) * TROW + (j * 16 + lt) * 2) = (T)(d[i][j][e] * part);
+            }
+            for (int c = lane; c < 16 * CPR; c += 64) {
+                const int row = c / CPR, tok = at.tok + (c % CPR) * 8, ch = at.ch + i * 16 + row;
+                const v4i v = *(const v4i *)(stg + row * TROW + (c % CPR) * 16);
+                if (ch < a.n && tok < a.ldt) *(v4i *)((T *)a.dat + (int64_t)ch * a.ldt + tok) = v;
+            }
+        }
+        if (!a.bias_parts) return;
+        float *parts = a.bias_parts + (int64_t)(at.tok / (FM * 16)) * a.n;
+#pragma unroll
+        for (int i = 0; i < FN; ++i) {
+            v4f s = d[i][0];
+#pragma unroll
+            for (int j = 1; j < FM; ++j) s += d[i][j];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float x = s[e];
+                x += dpp<0xB1>(0.f, x);
+                x += dpp<0x4E>(0.f, x);
+                x += dpp<0x141>(0.f, x);
+                x += dpp<0x140>(0.f, x);
+                s[e] = x;
+            }
+            const int ch = at.ch + i * 16 + 4 * lg;
+            if (lt == 0 && ch < a.n) *(v4f *)(parts + ch) = s;
+        }
+    }
+};
+
+// T(acc); interleaved rows go to two outputs.  With split_k > 1 the splits' sums
+// meet in the workspace as in the int8 kernels, added in their order.
+template <class T>
+struct CastOut {
+    static __device__ bool scaled(const BlockArgs &) { return false; }
+    static __device__ const float *first(const BlockArgs &) { return nullptr; }
+    static __device__ const float *second(const BlockArgs &) { return nullptr; }
+
+    static __device__ __forceinline__ T *row_at(const BlockArgs &a, int row) {
+        if (row >= a.m) return nullptr;
+        if (!a.interleaved) return (T *)a.out + (int64_t)row * a.ldo;
+        const int r = (row >> 5) * 16 + (row & 15);
+        return r < a.interleaved ? (T *)((row & 16) ? a.out2 : a.out) + (int64_t)r * a.ldo : nullptr;
+    }
+
+    template <class G, class Mul>
+    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at,
+                                                  const v4f (&acc)[G::FN][G::FM], int8_t *stg, const Mul &,
+                                                  int *s_last) {
+        if (a.split_k == 1) {
+            store_tile<G, T>(
+                stg, at.lane, acc, at.ch, a.n_out, (a.stream_out & sizeof(T)) != 0,
+                [&](int, int, const v4f &v) { return v; },
+                [&](int row, T *) -> T * { return row_at(a, at.tok + row); });
+            return;
+        }
+        const __amdgpu_buffer_rsrc_t r =
+            __builtin_amdgcn_make_buffer_rsrc(a.partials, 0, a.split_k * a.m * a.n * 4, kBufferFlags);
+        store_rows<G, 4>(
+            stg, at.lane, acc, [&](int, int, const v4f &v, int8_t *dst) { *(v4f *)dst = v; },
+            [&](int row, int ch, const v4i &v) {
+                if (at.tok + row < a.m && at.ch + ch < a.n)
+                    __builtin_amdgcn_raw_buffer_store_b128(
+                        __builtin_bit_cast(v4u, v), r, ((at.split * a.m + at.tok + row) * a.n + at.ch + ch) << 2, 0, kSc1);
+            });
+        if (!arrive_last(a, at.tm * a.tiles_n + at.tn, s_last)) return;
+        const int ch = at.ch + at.lane % G::CPR * 4;
+        for (int r0 = at.lane / G::CPR; r0 < G::FM * 16; r0 += G::RPI) {
+            const int row = at.tok + r0;
+            if (row >= a.m || ch >= a.n) continue;
+            v4f sum = {0, 0, 0, 0};
+#pragma unroll 4
+            for (int sp = 0; sp < a.split_k; ++sp)
+                sum += __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(
+                                                   r, ((sp * a.m + row) * a.n + ch) << 2, 0, kSc1));
+            T *p = row_at(a, row);
+            if (!p) continue;
+            if (ch + 4 <= a.n_out) {
+                *(v2u_any *)(p + ch) = pack4_of<T>(sum);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (ch + e < a.n_out) p[ch + e] = (T)sum[e];
+            }
+        }
+    }
+};
+
+template <int KIND, int WN, int WM, int FN, int FM, int NST, class EPI>
+__global__ __launch_bounds__(64 * WN * WM)
+__attribute__((amdgpu_waves_per_eu(Geometry<KIND, WN, WM, FN, FM, NST>::WAVES))) void k_product(BlockArgs a) {
+    using G = Geometry<KIND, WN, WM, FN, FM, NST>;
+    __shared__ __attribute__((aligned(1024))) int8_t lds[G::LDSB + G::MULB];
+    __shared__ uint2 lut[Kind<KIND>::LUT];
+    __shared__ int s_last;
+    gemm_tile<KIND, WN, WM, FN, FM, NST, EPI>(a, lds, lut, &s_last);
+}
+
+template <int KIND, class EPI, uint32_t TILES, int T = 0>
+int launch_product(int tile, const BlockArgs &a, int grid, void *stream) {
+    if constexpr (T < kNumSchedules) {
+        if constexpr ((TILES >> T) & 1)
+            if (tile == T) {
+                constexpr TileCfg t = kTiles[T];
+                hipLaunchKernelGGL((k_product<KIND, t.wn, t.wm, t.fn, t.fm, t.nst, EPI>), dim3(grid),
+                                   dim3(64 * t.wn * t.wm), 0, (hipStream_t)stream, a);
+                return (int)hipGetLastError();
+            }
+        return launch_product<KIND, EPI, TILES, T + 1>(tile, a, grid, stream);
+    }
+    return (int)hipErrorInvalidValue;
+}
+
+template <class EPI, uint32_t TILES>
+int launch_kinds(int kind, int tile, const BlockArgs &a, int grid, void *stream) {
+    switch (kind) {
+        case NM_KIND_SP42: return launch_product<NM_KIND_SP42, EPI, TILES>(tile, a, grid, stream);
+        case NM_KIND_C14: return launch_product<NM_KIND_C14, EPI, TILES>(tile, a, grid, stream);
+        case NM_KIND_DENSE: return launch_product<NM_KIND_DENSE, EPI, TILES>(tile, a, grid, stream);
+        case NM_KIND_C18: return launch_product<NM_KIND_C18, EPI, TILES>(tile, a, grid, stream);
+        case NM_KIND_C28: return launch_product<NM_KIND_C28, EPI, TILES>(tile, a, grid, stream);
+        case NM_KIND_MK3: return launch_product<NM_KIND_MK3, EPI, TILES>(tile, a, grid, stream);
+        case NM_KIND_MK4: return launch_product<NM_KIND_MK4, EPI, TILES>(tile, a, grid, stream);
+        case NM_KIND_MK5: return launch_product<NM_KIND_MK5, EPI, TILES>(tile, a, grid, stream);
+    }
+    return (int)hipErrorInvalidValue;
+}
+
+}  // namespace
+}  // namespace nmspmm

@@ -38,6 +38,8 @@ EXPORTED = (
     "nm_gemm_i8_dense_out_expand",
     # around the linears (bound in nmblock.py)
     "nm_quantize_rows", "nm_norm_residual", "nm_norm_residual_backward_workspace", "nm_norm_residual_backward",
+    "nm_linear_workspace", "nm_gemm_i8_scaled", "nm_linear_i8", "nm_gated_i8", "nm_gated", "nm_gated_backward_workspace",
+    "nm_gated_backward",
 )
 NM_NOALLOC_SCRATCH_BYTES = 16384 + (32 << 20)
 
@@ -97,7 +99,7 @@ def lib() -> ctypes.CDLL:
         except ImportError:
             pass
         L = ctypes.CDLL(LIB_PATH)
-        vp, i32, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
+        vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t
         pd, pp = ctypes.POINTER(NmDesc), ctypes.POINTER(NmPlan)
         sig = {
             "nm_status_string": ([i32], ctypes.c_char_p),
@@ -126,10 +128,17 @@ def lib() -> ctypes.CDLL:
                                     ctypes.POINTER(NmExpandJob)], i32),
             "nm_gemm_i8_dense_out_expand": ([vp, i32, vp, i32, i32, ctypes.POINTER(NmOutputs), vp, sz, vp, pp,
                                              ctypes.POINTER(NmExpandJob)], i32),
-            "nm_quantize_rows": ([vp, ctypes.c_int64, i32, i32, i32, vp, vp, vp], i32),
+            "nm_quantize_rows": ([vp, i64, i32, i32, i32, vp, vp, vp], i32),
             "nm_norm_residual": ([vp, vp], i32),
             "nm_norm_residual_backward_workspace": ([i32, i32, i32, ctypes.POINTER(sz)], i32),
             "nm_norm_residual_backward": ([vp, vp, sz, vp], i32),
+            "nm_linear_workspace": ([vp, i32, i32, ctypes.POINTER(sz)], i32),
+            "nm_gemm_i8_scaled": ([vp, vp, i32, vp, vp, i64, i32, vp, sz, vp], i32),
+            "nm_linear_i8": ([vp, i64, i32, i32, vp, vp, i64, i32, vp, sz, vp], i32),
+            "nm_gated_i8": ([vp, vp, i32, vp, i32, vp, i64, i32, vp, sz, vp], i32),
+            "nm_gated": ([vp, i64, i32, i32, vp, i32, vp, i64, i32, vp, sz, vp], i32),
+            "nm_gated_backward_workspace": ([vp, i32, ctypes.POINTER(sz)], i32),
+            "nm_gated_backward": ([vp, vp, vp, sz, vp], i32),
         }
         for name, (args, res) in sig.items():
             f = getattr(L, name)

@@ -126,3 +126,78 @@ def norm_grads(dz, dres, y, res, pre, post, gate, alpha):
     if gate is not None:
         out["dgate"] = tuple(t.reshape(groups, m // groups, d).sum(1).reshape(gate.shape) for t in (dt * u, tm * um))
     return out
+
+
+def weight(g, n, k, N=8, M=8):
+    """Random int8 weight [n x k] (CPU) with at most N nonzeros in each window of M, and its scales."""
+    w = torch.randint(-127, 128, (n, k), generator=g, dtype=torch.int64)
+    if N < M:
+        keep = torch.rand(n, k // M, M, generator=g).argsort(2).argsort(2) < N
+        w = w * keep.view(n, k)
+    return w.to(torch.int8), torch.exp(torch.randn(n, generator=g)) * 1e-3
+
+
+def product(q, s, w, c, b):
+    """(y, magnitude) of the scaled product in 64 bits; q holds k codes a row.  Magnitude: each of its terms once,
+    for the four roundings in binary32 (the sum's conversion, two products, the addition)."""
+    sums = q.double().cpu() @ w.double().cpu().t()
+    y = sums * s.double().cpu()[:, None] * c.double().cpu()
+    mag = y.abs()
+    if b is not None:
+        y, mag = y + b.double().cpu(), mag + b.double().cpu().abs()
+    return y, mag
+
+
+def act(g, name):
+    """act(g) and its derivative in 64 bits."""
+    s = torch.sigmoid(g)
+    if name == "silu":
+        return g * s, s * (1 + g * (1 - s))
+    if name == "sigmoid":
+        return s, s * (1 - s)
+    if name == "relu":
+        return torch.where(g > 0, g, torch.zeros_like(g)), (g > 0).double()
+    if name == "gelu":
+        p = 0.5 * torch.erfc(-g / 2 ** 0.5)
+        return g * p, p + g * torch.exp(-g * g / 2) / (2 * torch.pi) ** 0.5
+    a = (2 / torch.pi) ** 0.5
+    t = torch.tanh(a * (g + 0.044715 * g ** 3))
+    return 0.5 * g * (1 + t), 0.5 * (1 + t) + 0.5 * g * (1 - t * t) * a * (1 + 3 * 0.044715 * g * g)
+
+
+def gated(q, s, wg, cg, bg, wu, cu, bu, name):
+    """(h, magnitude) in 64 bits: with the errors of g and u (4 e of their magnitudes; slopes of act are below 1.2)
+    and of act itself: the exponential's argument and result are within 2 e (1 + |g|), so act(g) is within
+    8 e (1 + g^2) of its value."""
+    g, gm = product(q, s, wg, cg, bg)
+    u, um = product(q, s, wu, cu, bu)
+    f, _ = act(g, name)
+    return f * u, u.abs() * (1.2 * gm + 2 * (1 + g * g)) + f.abs() * um
+
+
+def gated_grads(q, s, wg, cg, bg, wu, cu, bu, name, dh, dtype):
+    """{name: (gradient, room)} in 64 bits; room: what the operands' one rounding to dtype and the sums in binary32
+    may add to the gradient's own rounding."""
+    g, gm = product(q, s, wg, cg, bg)
+    u, um = product(q, s, wu, cu, bu)
+    f, df = act(g, name)
+    dh = dh.double().cpu()
+    dg, du = dh * u * df, dh * f
+    # errors of dg and du in binary32 (second derivatives of act are below 1.2, slopes within 8 e (1 + |g|^3))
+    eg = dh.abs() * 4 * E * (um * (df.abs() + 1) + u.abs() * (1.2 * gm + 2 * (1 + g.abs() ** 3)))
+    eu = dh.abs() * 4 * E * (1.2 * gm + 2 * (1 + g * g))
+    x = q.double().cpu() * s.double().cpu()[:, None]
+    wg, wu = wg.double().cpu() * cg.double().cpu()[:, None], wu.double().cpu() * cu.double().cpu()[:, None]
+    m, n = dg.shape
+    unit = UNIT[dtype] + (K + n / 16) * E
+    out = {"dx": (dg @ wg + du @ wu,
+                  (dg.abs() * unit + eg) @ wg.abs() + (du.abs() * unit + eu) @ wu.abs()
+                  + TINY[dtype] * (wg.abs() / cg.double().cpu()[:, None] + wu.abs() / cu.double().cpu()[:, None]).sum(0))}
+    unit = UNIT[dtype] + (K + m / 16) * E
+    sub = TINY[dtype] * q.double().cpu().abs().sum(0)       # codes times a power of two, beside d's subnormal step
+    out["dw_gate"] = (dg.t() @ x, (dg.abs() * unit + eg).t() @ x.abs() + sub)
+    out["dw_up"] = (du.t() @ x, (du.abs() * unit + eu).t() @ x.abs() + sub)
+    if bg is not None:
+        out["dbias_gate"] = (dg.sum(0), (dg.abs() * (K + m / 16) * E + eg).sum(0))
+        out["dbias_up"] = (du.sum(0), (du.abs() * (K + m / 16) * E + eu).sum(0))
+    return out

@@ -1,0 +1,162 @@
+"""The int8 product with scales for each token and channel, against the plain form in 64 bits (bounds: block_util)."""
+import pytest
+import torch
+
+import block_util as bu
+from paper_2607_12505_amd import nmblock as nb
+
+pytestmark = pytest.mark.gpu
+PATTERNS = [(8, 8), (2, 4), (1, 4), (1, 8), (2, 8), (3, 8), (4, 8), (5, 8), (3, 4)]
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def check(x, w, c, b, got, dtype):
+    q, s = bu.codes(x)
+    want, mag = bu.product(q, s, w, c, b)
+    bu.close(got, want, dtype, mag, 4)
+
+
+# one token, the edges of 16-token and 64-token tiles, odd everything, more k-steps than a ring holds
+SHAPES = [(1, 64, 64), (1, 1024, 1000), (2, 4096, 48), (3, 17, 5), (7, 1, 1), (15, 128, 33), (16, 129, 64),
+          (17, 771, 1001), (33, 384, 96), (64, 2048, 16), (65, 1021, 130), (130, 640, 257), (333, 100, 515),
+          (600, 1536, 384)]
+
+
+@pytest.mark.parametrize("T", bu.TYPES)
+@pytest.mark.parametrize("m,k,n", SHAPES)
+def test_dense(T, m, k, n):
+    g = gen(m * 7 + k + n)
+    x = (torch.randn(m, k, generator=g) * torch.exp(torch.randn(m, 1, generator=g))).to(T).cuda()
+    w, c = bu.weight(g, n, k)
+    b = torch.randn(n, generator=g) if n % 2 else None
+    lin = nb.ScaledWeight.from_int8(w, c, bias=b)
+    check(x, w, c, b, nb.linear_i8(x, lin), T)
+
+
+@pytest.mark.parametrize("N,M", PATTERNS)
+@pytest.mark.parametrize("m,k,n", [(1, 512, 64), (5, 144, 24), (16, 1024, 100), (40, 256, 52), (197, 768, 384),
+                                   (1100, 128, 260)])
+def test_patterns(N, M, m, k, n):
+    g = gen(N * 100 + M + m)
+    x = torch.randn(m, k, generator=g).to(torch.bfloat16).cuda()
+    w, c = bu.weight(g, n, k, N, M)
+    b = torch.randn(n, generator=g)
+    lin = nb.ScaledWeight.from_int8(w, c, bias=b, N=N, M=M)
+    got = nb.linear_i8(x, lin, out_dtype=torch.float32)
+    check(x, w, c, b, got, torch.float32)
+    q, s = nb.quantize_rows(x)
+    assert torch.equal(nb.gemm_i8_scaled(q, s, lin, out_dtype=torch.float32), got)
+
+
+# every tile that large shapes run: tall, wide, long reductions, and the expanded form of compact weights
+@pytest.mark.parametrize("N,M", [(8, 8), (2, 4), (2, 8), (4, 8)])
+@pytest.mark.parametrize("m,k,n", [(18464, 1024, 1024), (4000, 256, 4096), (9000, 2048, 512), (30000, 64, 200)])
+def test_large_shapes_by_sampled_rows(N, M, m, k, n):
+    g = gen(m + N)
+    x = torch.randn(m, k, generator=g).half().cuda()
+    w, c = bu.weight(g, n, k, N, M)
+    lin = nb.ScaledWeight.from_int8(w, c, N=N, M=M)
+    out = torch.full((m + 2, n), 7.0, dtype=torch.half, device="cuda")
+    got = nb.linear_i8(x, lin, out=out[:m])
+    rows = torch.cat([torch.arange(0, 4), torch.arange(m - 4, m), torch.randint(0, m, (120,), generator=g)])
+    check(x[rows], w, c, None, got[rows], torch.half)
+    assert (out[m:] == 7).all()
+
+
+def test_strided_rows_and_outputs():
+    g = gen(1)
+    w, c = bu.weight(g, 100, 96)
+    lin = nb.ScaledWeight.from_int8(w, c)
+    wide = torch.randn(50, 3, 97, generator=g).half().cuda()
+    x = wide[:, 1, :96]
+    out = torch.full((50, 131), 3.0, dtype=torch.half, device="cuda")
+    got = nb.linear_i8(x, lin, out=out[:, 7:107])
+    check(x, w, c, None, got, torch.half)
+    assert (out[:, :7] == 3).all() and (out[:, 107:] == 3).all()
+    y = nb.linear_i8(wide.view(-1, 97)[:, :96], lin)
+    assert torch.equal(y.view(50, 3, 100)[:, 1], got)
+    three = wide[:, :, :96].contiguous()
+    assert torch.equal(nb.linear_i8(three, lin), y.view(50, 3, 100))
+
+
+def test_rows_of_zeros_infinities_and_nan():
+    g = gen(2)
+    w, c = bu.weight(g, 40, 64)
+    b = torch.randn(40, generator=g)
+    lin = nb.ScaledWeight.from_int8(w, c, bias=b)
+    x = torch.randn(6, 64, generator=g)
+    x[1], x[2, 3], x[3, 5] = 0, float("inf"), float("nan")
+    x[4] = 1e-35                                       # below 2^-100: counts as zero
+    y = nb.linear_i8(x.cuda(), lin).cpu()
+    assert torch.equal(y[1], b) and torch.equal(y[4], b)
+    assert y[2].isnan().all() and y[3].isnan().all()
+    check(x[[0, 5]], w, c, b, y[[0, 5]], torch.float32)
+
+
+def test_largest_sums():
+    # every code at its largest: the sums of 2^17 - 16 products stay in int32
+    k = (1 << 17) - 16
+    w = torch.full((16, k), -127, dtype=torch.int8)
+    w[1] = 127
+    lin = nb.ScaledWeight.from_int8(w, torch.ones(16))
+    y = nb.linear_i8(torch.ones(2, k).cuda(), lin).cpu()
+    want = 127.0 * k
+    assert ((y[:, 1] - want).abs() <= 4 * bu.E * want).all() and ((y[:, 0] + want).abs() <= 4 * bu.E * want).all()
+
+
+def test_empty_batch_weights_from_floats_and_streams():
+    g = gen(3)
+    W = (0.02 * torch.randn(130, 200, generator=g)).cuda()
+    lin = nb.ScaledWeight.from_float(W)
+    assert nb.linear_i8(torch.empty(0, 200, device="cuda").half(), lin).shape == (0, 130)
+    x = torch.randn(70, 200, generator=g).cuda()
+    q, c = bu.codes(W)
+    y = nb.linear_i8(x, lin)
+    check(x, q, c, None, y, torch.float32)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    z = nb.linear_i8(x, lin, stream=side)
+    side.synchronize()
+    assert torch.equal(y, z)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        z = nb.linear_i8(x, lin)
+    for _ in range(3):
+        z.fill_(0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, z)
+
+
+def test_refusals():
+    w, c = bu.weight(gen(4), 32, 64)
+    lin = nb.ScaledWeight.from_int8(w, c)
+    x = torch.zeros(4, 64, device="cuda").half()
+    q, s = nb.quantize_rows(x)
+    gw = nb.GatedWeight.from_int8(w, c, w, c)
+    bad = [
+        lambda: nb.linear_i8(x.cpu(), lin),
+        lambda: nb.linear_i8(x[:, :63], lin),
+        lambda: nb.linear_i8(x.double(), lin),
+        lambda: nb.linear_i8(x.t(), lin),
+        lambda: nb.linear_i8(x, gw),
+        lambda: nb.linear_i8(x, lin, out=torch.empty(4, 31, device="cuda").half()),
+        lambda: nb.linear_i8(x, lin, out=torch.empty(4, 32, device="cuda")),
+        lambda: nb.gemm_i8_scaled(q[:, :48], s, lin),
+        lambda: nb.gemm_i8_scaled(q, s[:3], lin),
+        lambda: nb.gemm_i8_scaled(q, s.half(), lin),
+        lambda: nb.gemm_i8_scaled(q, s, gw),
+        lambda: nb.ScaledWeight.from_int8(w.float(), c),
+        lambda: nb.ScaledWeight.from_int8(w, c[:5]),
+        lambda: nb.ScaledWeight.from_int8(w, c, bias=c[:5]),
+        lambda: nb.gated_ffn(x, lin),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail(f"call {i} was accepted")
+    with pytest.raises(nb.NmError):
+        nb.ScaledWeight.from_int8(w, c, N=2, M=4)          # more than two nonzeros in a window

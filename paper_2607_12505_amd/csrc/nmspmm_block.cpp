@@ -196,7 +196,7 @@ nm_status check_weight(const nm_scaled_weight *w, bool gated) {
 // Whether a compact weight is expanded once for the call, and the bytes of that.
 int64_t expansion(const nm_desc &d, int m) {
     nm_plan plan;
-    if (!kind_is_compact(d.kind) || make_plan(d.kind, m, d.n, d.k, NM_OUT_F16, &plan) != NM_OK) return 0;
+    if (m <= kFewTokens || !kind_is_compact(d.kind) || make_plan(d.kind, m, d.n, d.k, NM_OUT_F16, &plan) != NM_OK) return 0;
     return plan.expand ? plan.expand_bytes : 0;
 }
 
@@ -245,7 +245,15 @@ struct Product {
     int type;
     bool gated;
     int act;
+    const void *x = nullptr;    // values in place of codes (few tokens)
+    int64_t ldx = 0;
+    int xtype = 0;
 };
+
+// Whether the kernel of few tokens makes the codes of these rows itself.
+bool takes_values(const void *x, int64_t ldx, int m, int k) {
+    return few_takes_values(m, k) && ldx % 8 == 0 && aligned(x, 16);
+}
 
 // ws: room for the expanded weight where there is one.
 nm_status run_product(const Product &p, char *ws, void *stream) {
@@ -253,6 +261,23 @@ nm_status run_product(const Product &p, char *ws, void *stream) {
     int kind = d.kind;
     const int8_t *vals = p.w->vals;
     const uint8_t *meta = p.w->meta;
+    if (p.m <= kFewTokens) {
+        BlockArgs a;
+        fill_product(a, p.m, *p.w);
+        a.X = p.xq;
+        a.A = vals;
+        a.meta = meta;
+        a.row_scale = p.sx;
+        a.x = p.x;
+        a.ldx = p.ldx;
+        a.xtype = p.xtype;
+        a.kx = p.w->k;
+        a.out = p.out;
+        a.ldo = p.ldo;
+        a.type = p.type;
+        a.act = p.act;
+        return launch_few(kind, p.gated, a, stream) == 0 ? NM_OK : NM_ERR_HIP;
+    }
     if (expansion(d, p.m)) {
         int8_t *out = (int8_t *)ws;
         if (launch_expand(kind, vals, meta, d.n, d.k, out, stream) != 0) return NM_ERR_HIP;
@@ -312,6 +337,13 @@ nm_status product_of_rows(const void *x, int64_t ldx, int xtype, int m, const nm
     if (ldx < w->k) return NM_ERR_SHAPE;
     if (m == 0) return NM_OK;
     if (!x || !aligned(x, type_bytes(xtype))) return NM_ERR_ARG;
+    if (takes_values(x, ldx, m, w->k)) {
+        Product p = {nullptr, nullptr, m, w, out, ldo, type, gated, act};
+        p.x = x;
+        p.ldx = ldx;
+        p.xtype = xtype;
+        return run_product(p, nullptr, stream);
+    }
     const nm_desc &d = *w->desc;
     const size_t codes = codes_bytes(m, d.k), need = codes + (size_t)expansion(d, m);
     if (!ws || ws_bytes < need || !aligned(ws, 256)) return NM_ERR_WORKSPACE;

@@ -67,6 +67,10 @@ struct BlockArgs : GemmArgs {
     int n_out = 0;
     int type = 0;                       // NM_TYPE_* of out (and of dh)
     int act = 0;                        // NM_ACT_*
+    // few tokens: activations as values instead of codes (rows of ldx, kx of them)
+    const void *x = nullptr;
+    int64_t ldx = 0;
+    int xtype = 0, kx = 0;
     // gradients of the gated block
     const void *dh = nullptr;           // [m] rows of lddh values
     int64_t lddh = 0;
@@ -82,6 +86,10 @@ constexpr uint32_t kScaledTiles = 1u << 1 | 1u << 3 | 1u << 6 | 1u << 12 | 1u <<
 constexpr uint32_t kGradTiles = 1u << 1 | 1u << 3 | 1u << 6;   // whole 64-token groups: the transposed rows' padding is written too
 constexpr uint32_t kCastTiles = 1u << 1 | 1u << 3 | 1u << 6 | 1u << 12 | 1u << 4;
 
+// Up to kFewTokens tokens take the streaming kernel; few_takes_values: also as values.
+constexpr int kFewTokens = 64;
+bool few_takes_values(int m, int k);
+int launch_few(int kind, bool gated, const BlockArgs &a, void *stream);
 int launch_scaled(int kind, int tile, const BlockArgs &a, int grid, void *stream);
 int launch_gated(int kind, int tile, const BlockArgs &a, int grid, void *stream);
 int launch_gated_grad(int tile, const BlockArgs &a, int grid, void *stream);

@@ -82,10 +82,17 @@ __device__ __forceinline__ void load_row_scales(const BlockArgs &a, const TileAt
     }
 }
 
+// The empty statement keeps the value in binary32: left alone, the compiler
+// rounds some products straight to binary16, and a token would not have the same
+// bits from every kernel.
 __device__ __forceinline__ v4f scaled_value(const v4i &v, float sx, const v4f &c, const v4f &b) {
     v4f f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = __builtin_fmaf((float)v[e] * sx, c[e], b[e]);
+    for (int e = 0; e < 4; ++e) {
+        float x = __builtin_fmaf((float)v[e] * sx, c[e], b[e]);
+        asm("" : "+v"(x));
+        f[e] = x;
+    }
     return f;
 }
 
@@ -150,6 +157,12 @@ __device__ __forceinline__ float act_of(int act, float g) {
     return f;
 }
 
+__device__ __forceinline__ float gate_times(int act, float g, float u) {
+    float x = act_of(act, g) * u;
+    asm("" : "+v"(x));   // in binary32 before its rounding to T, as scaled_value
+    return x;
+}
+
 // A tile's rows of the interleaved weight: 16 gate channels, the same 16 up
 // channels, the next 16 ...  So fragments 2 i and 2 i + 1 of a wave hold g and u
 // of the same channels in the same lanes.
@@ -185,7 +198,7 @@ struct GatedOut {
                 const v4f g = scaled_value(acc[2 * i][j], sx[j], cg, bg);
                 const v4f u = scaled_value(acc[2 * i + 1][j], sx[j], cu, bu);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) h[i][j][e] = act_of(a.act, g[e]) * u[e];
+                for (int e = 0; e < 4; ++e) h[i][j][e] = gate_times(a.act, g[e], u[e]);
             }
         }
         by_type(a.type, [&](auto *t) {

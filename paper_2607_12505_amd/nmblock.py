@@ -18,71 +18,107 @@ from __future__ import annotations
 import ctypes
 from typing import NamedTuple, Optional
 
-from .nmspmm import (NM_LAYOUT_DENSE, DeviceWeight, NmDesc, NmError, _check, _need, _ptr, _stream, _torch,  # noqa: F401
-                     compress, compress_size, lib)
+from .nmspmm import (NM_ERR_WORKSPACE, NM_LAYOUT_DENSE, NM_OK, DeviceWeight, NmDesc, NmError, _check, compress,
+                     compress_size, lib)
 
 NM_TYPE_F16, NM_TYPE_BF16, NM_TYPE_F32 = 1, 2, 3
 NM_NORM_NONE, NM_NORM_RMS, NM_NORM_LAYER = 0, 1, 2
-_NORMS = {"none": NM_NORM_NONE, "rms": NM_NORM_RMS, "layer": NM_NORM_LAYER}
-_types = None
+_NORMS = {"rms": NM_NORM_RMS, "layer": NM_NORM_LAYER}
 
 
-def _type_of(t, name: str) -> int:
-    global _types
-    if _types is None:
-        torch = _torch()
-        _types = {torch.float16: NM_TYPE_F16, torch.bfloat16: NM_TYPE_BF16, torch.float32: NM_TYPE_F32}
-    code = _types.get(t.dtype)
+class _Runtime:
+    """What every call looks up, looked up once: a call of one token takes a few microseconds of host time, which
+    imports inside functions and Stream objects would double."""
+
+    def __init__(self):
+        import torch
+        L = lib()
+        self.torch = torch
+        self.f32, self.i8, self.u8 = torch.float32, torch.int8, torch.uint8
+        self.types = {torch.float16: NM_TYPE_F16, torch.bfloat16: NM_TYPE_BF16, torch.float32: NM_TYPE_F32}
+        self.device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self.raw_stream = raw or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+        self.quantize, self.norm, self.norm_grad = L.nm_quantize_rows, L.nm_norm_residual, L.nm_norm_residual_backward
+        self.linear, self.linear_codes = L.nm_linear_i8, L.nm_gemm_i8_scaled
+        self.gated, self.gated_codes, self.gated_grad = L.nm_gated, L.nm_gated_i8, L.nm_gated_backward
+
+
+_rt: Optional[_Runtime] = None
+
+
+def _runtime() -> _Runtime:
+    global _rt
+    if _rt is None:
+        _rt = _Runtime()
+    return _rt
+
+
+def _index(t, name: str, rt: _Runtime) -> int:
+    """The device of a call: the first tensor's, which has to be the current one (kernels go to its streams)."""
+    if not t.is_cuda:
+        raise ValueError(f"{name}: must be a device tensor")
+    dev = t.get_device()
+    if dev != rt.device():
+        raise ValueError(f"{name}: on cuda:{dev}, but the current device is cuda:{rt.device()}")
+    return dev
+
+
+def _on(t, name: str, dev: int):
+    if t.get_device() != dev:
+        raise ValueError(f"{name}: on {t.device}, expected cuda:{dev}")
+
+
+def _type_of(t, name: str, rt: _Runtime) -> int:
+    code = rt.types.get(t.dtype)
     if code is None:
         raise ValueError(f"{name}: dtype {t.dtype}, expected float16, bfloat16 or float32")
     return code
 
 
-def _rows(t, name: str, width: Optional[int] = None):
-    """(t as [rows x channels], its row stride); refuses what has no such view."""
-    if t.dim() != 2:
-        if t.dim() == 0 or not t.is_contiguous():
-            raise ValueError(f"{name}: must be two-dimensional, or contiguous with channels last")
-        t = t.view(-1, t.shape[-1])
-    m, k = t.shape
-    if width is not None and k != width:
-        raise ValueError(f"{name}: {k} channels, expected {width}")
-    if k > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name}: channels must be consecutive")
-    return t, (t.stride(0) if m > 1 else max(k, 1))
+def _rows(t, name: str):
+    """(rows, channels, row stride) of [..., channels]; refuses what has no such view."""
+    if t.dim() == 2:
+        m, k = t.shape
+        s0, s1 = t.stride()
+        if s1 != 1 and k > 1:
+            raise ValueError(f"{name}: channels must be consecutive")
+        return m, k, (s0 if m > 1 else k)
+    if t.dim() == 0 or not t.is_contiguous():
+        raise ValueError(f"{name}: must be two-dimensional, or contiguous with channels last")
+    k = t.shape[-1]
+    return (t.numel() // k if k else 0), k, k
 
 
-def _same(t, name: str, like):
-    if t.dtype != like.dtype:
-        raise ValueError(f"{name}: dtype {t.dtype}, expected {like.dtype}")
-    if t.device != like.device:
-        raise ValueError(f"{name}: on {t.device}, expected {like.device}")
+def _param(t, name: str, shape, dtype, dev: int):
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, expected contiguous {dtype} {shape}")
+    _on(t, name, dev)
 
 
-def _on_current_device(t, name: str):
-    if not t.is_cuda:
-        raise ValueError(f"{name}: must be a device tensor")
-    if t.get_device() != _torch().cuda.current_device():
-        raise ValueError(f"{name}: on {t.device}, but the current device is {_torch().cuda.current_device()}")
+def _ptr(t):
+    return None if t is None else t.data_ptr()
 
 
-def _empty(shape, dtype, like, stream):
+def _handle(stream, dev: int, rt: _Runtime) -> int:
+    return rt.raw_stream(dev) if stream is None else stream.cuda_stream
+
+
+def _empty(shape, dtype, like, stream, rt: _Runtime):
     """Memory of the call's stream: torch's allocator orders its reuse there."""
-    torch = _torch()
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
+    torch = rt.torch
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(stream.cuda_stream, device=like.device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
 
 
-def _output(given, name: str, shape, dtype, like, stream):
+def _output(given, name: str, shape, dtype, like, stream, rt: _Runtime):
     if given is None:
-        return _empty(shape, dtype, like, stream)
-    _need(given, name, (dtype,), shape)
-    if given.device != like.device:
-        raise ValueError(f"{name}: on {given.device}, expected {like.device}")
+        return _empty(shape, dtype, like, stream, rt)
+    _param(given, name, tuple(shape), dtype, like.get_device())
     return given
 
 
@@ -95,14 +131,13 @@ def padded(k: int) -> int:
 
 def quantize_rows(x, xq=None, scale=None, stream=None):
     """nm_quantize_rows: (codes int8 [rows x padded(k)], scales float32 [rows]) of x."""
-    _on_current_device(x, "x")
-    code = _type_of(x, "x")
-    x, ld = _rows(x, "x")
-    m, k = x.shape
-    torch = _torch()
-    xq = _output(xq, "xq", (m, padded(k)), torch.int8, x, stream)
-    scale = _output(scale, "scale", (m,), torch.float32, x, stream)
-    _check(lib().nm_quantize_rows(x.data_ptr(), ld, code, m, k, xq.data_ptr(), scale.data_ptr(), _stream(stream)),
+    rt = _rt or _runtime()
+    dev = _index(x, "x", rt)
+    code = _type_of(x, "x", rt)
+    m, k, ld = _rows(x, "x")
+    xq = _output(xq, "xq", (m, padded(k)), rt.i8, x, stream, rt)
+    scale = _output(scale, "scale", (m,), rt.f32, x, stream, rt)
+    _check(rt.quantize(x.data_ptr(), ld, code, m, k, xq.data_ptr(), scale.data_ptr(), _handle(stream, dev, rt)),
            "nm_quantize_rows")
     return xq, scale
 
@@ -132,67 +167,75 @@ class NmNormGradArgs(ctypes.Structure):
 
 
 class Norm:
-    """A norm of the channels: kind "rms" or "layer", float32 weight and bias [d] (None: 1 and 0), eps."""
+    """A norm of the channels: kind "rms" or "layer", float32 weight and bias [d] (None: 1 and 0), eps.
+
+    The tensors are checked here, once, and read at every call: change their values in place."""
 
     def __init__(self, kind: str, weight=None, bias=None, eps: float = 1e-6):
-        if kind not in ("rms", "layer"):
+        if kind not in _NORMS:
             raise ValueError(f"norm: kind {kind!r}, expected 'rms' or 'layer'")
         if not eps > 0:
             raise ValueError("norm: eps must be positive")
-        self.kind, self.weight, self.bias, self.eps = kind, weight, bias, float(eps)
+        import torch
+        for t, name in ((weight, "weight"), (bias, "bias")):
+            if t is not None and (t.dtype != torch.float32 or t.dim() != 1 or not t.is_contiguous() or not t.is_cuda):
+                raise ValueError(f"norm: {name} must be a contiguous float32 vector on the device")
+        if weight is not None and bias is not None and (weight.shape != bias.shape or weight.device != bias.device):
+            raise ValueError("norm: weight and bias differ in size or device")
+        one = weight if weight is not None else bias
+        self.kind, self.eps = kind, float(eps)
+        # aliases: their memory stays even if the caller's tensors are given other data
+        self.weight = None if weight is None else weight.detach()
+        self.bias = None if bias is None else bias.detach()
+        self._d = None if one is None else one.shape[0]
+        self._dev = None if one is None else one.get_device()
+        self._args = NmNorm(_NORMS[kind], self.eps, _ptr(self.weight), _ptr(self.bias))
 
-    def _args(self, d: int, like, name: str) -> NmNorm:
-        torch = _torch()
-        for t, what in ((self.weight, "weight"), (self.bias, "bias")):
-            if t is not None:
-                _need(t, f"{name}.{what}", (torch.float32,), (d,))
-                if t.device != like.device:
-                    raise ValueError(f"{name}.{what}: on {t.device}, expected {like.device}")
-        return NmNorm(_NORMS[self.kind], self.eps, _ptr(self.weight), _ptr(self.bias))
+    def _for(self, d: int, dev: int, name: str) -> NmNorm:
+        if self._d is not None and (self._d != d or self._dev != dev):
+            raise ValueError(f"{name}: of {self._d} channels on cuda:{self._dev}, expected {d} on cuda:{dev}")
+        return self._args
 
 
-def _norm_args(norm: Optional[Norm], d, like, name) -> NmNorm:
-    return NmNorm() if norm is None else norm._args(d, like, name)
-
-
-def _gate(gate, m: int, d: int, like) -> int:
+def _gate(gate, m: int, d: int, dev: int, rt: _Runtime) -> int:
     """Checks the gate [groups x d] (or [d]) and returns groups."""
     if gate is None:
         return 1
-    torch = _torch()
     groups = gate.shape[0] if gate.dim() == 2 else 1
-    _need(gate, "gate", (torch.float32,), (groups, d) if gate.dim() == 2 else (d,))
-    if gate.device != like.device:
-        raise ValueError(f"gate: on {gate.device}, expected {like.device}")
+    if gate.dtype != rt.f32 or gate.dim() not in (1, 2) or gate.shape[-1] != d or not gate.is_contiguous():
+        raise ValueError(f"gate: {gate.dtype} {tuple(gate.shape)}, expected contiguous float32 [{d}] or [groups x {d}]")
+    _on(gate, "gate", dev)
     if groups < 1 or m % groups:
         raise ValueError(f"gate: {groups} groups do not divide {m} tokens")
     return groups
 
 
-def _around(y, r, pre, post, gate, alpha, res, stream):
+def _around(y, r, pre, post, gate, alpha, res, stream, rt):
     like, name = (y, "y") if y is not None else (r, "r")
     if like is None:
         raise ValueError("y and r: at least one is needed")
-    _on_current_device(like, name)
+    dev = _index(like, name, rt)
     a = NmNormArgs()
-    a.type = _type_of(like, name)
-    shape, m, d = like.shape, 0, 0
+    a.type = _type_of(like, name, rt)
     if y is not None:
-        y2, a.ldy = _rows(y, "y")
-        a.y = y2.data_ptr()
-        m, d = y2.shape
+        m, d, a.ldy = _rows(y, "y")
+        a.y = y.data_ptr()
     if r is not None:
-        _same(r, "r", like)
-        r2, a.ldr = _rows(r, "r", d if y is not None else None)
-        if y is not None and r2.shape[0] != m:
-            raise ValueError(f"r: {r2.shape[0]} tokens, expected {m}")
-        a.r = r2.data_ptr()
-        m, d = r2.shape
-    a.m, a.d, a.groups, a.gate, a.alpha = m, d, _gate(gate, m, d, like), _ptr(gate), alpha
-    a.post, a.pre = _norm_args(post, d, like, "post"), _norm_args(pre, d, like, "pre")
-    res = _output(res, "res", shape, like.dtype, like, stream)
+        mr, dr, a.ldr = _rows(r, "r")
+        if y is not None and (mr != m or dr != d or r.dtype != y.dtype):
+            raise ValueError(f"r: {r.dtype} [{mr} x {dr}], expected {y.dtype} [{m} x {d}]")
+        _on(r, "r", dev)
+        a.r, m, d = r.data_ptr(), mr, dr
+    a.m, a.d, a.groups, a.alpha = m, d, _gate(gate, m, d, dev, rt), alpha
+    if gate is not None:
+        a.gate = gate.data_ptr()
+    if post is not None:
+        a.post = post._for(d, dev, "post")
+    if pre is not None:
+        a.pre = pre._for(d, dev, "pre")
+    res = _output(res, "res", like.shape, like.dtype, like, stream, rt)
     a.res = res.data_ptr()
-    return a, like, res
+    return a, like, res, _handle(stream, dev, rt)
 
 
 def norm_residual(y, r, pre: Optional[Norm] = None, post: Optional[Norm] = None, gate=None, alpha: float = 1.0,
@@ -201,13 +244,14 @@ def norm_residual(y, r, pre: Optional[Norm] = None, post: Optional[Norm] = None,
 
     y (the block's output) or r (the residual stream) may be None.  gate: float32 [d], or [groups x d] with a row
     for each of `groups` equal runs of tokens.  Without `pre` there is no z (None)."""
-    a, like, res = _around(y, r, pre, post, gate, alpha, res, stream)
+    rt = _rt or _runtime()
+    a, like, res, at = _around(y, r, pre, post, gate, alpha, res, stream, rt)
     if pre is not None:
-        z = _output(z, "z", res.shape, like.dtype, like, stream)
+        z = _output(z, "z", res.shape, like.dtype, like, stream, rt)
         a.z = z.data_ptr()
     elif z is not None:
         raise ValueError("z: given without a norm for it")
-    _check(lib().nm_norm_residual(ctypes.byref(a), _stream(stream)), "nm_norm_residual")
+    _check(rt.norm(ctypes.byref(a), at), "nm_norm_residual")
     return res, z
 
 
@@ -216,12 +260,12 @@ def norm_residual_i8(y, r, pre: Norm, post: Optional[Norm] = None, gate=None, al
     """norm_residual with the codes of z and their scales in its place: (res, zq int8 [rows x padded(d)], zs)."""
     if pre is None:
         raise ValueError("pre: the codes are those of a norm's rows")
-    a, like, res = _around(y, r, pre, post, gate, alpha, res, stream)
-    torch = _torch()
-    zq = _output(zq, "zq", (a.m, padded(a.d)), torch.int8, like, stream)
-    zs = _output(zs, "zs", (a.m,), torch.float32, like, stream)
+    rt = _rt or _runtime()
+    a, like, res, at = _around(y, r, pre, post, gate, alpha, res, stream, rt)
+    zq = _output(zq, "zq", (a.m, padded(a.d)), rt.i8, like, stream, rt)
+    zs = _output(zs, "zs", (a.m,), rt.f32, like, stream, rt)
     a.zq, a.zs = zq.data_ptr(), zs.data_ptr()
-    _check(lib().nm_norm_residual(ctypes.byref(a), _stream(stream)), "nm_norm_residual")
+    _check(rt.norm(ctypes.byref(a), at), "nm_norm_residual")
     return res, zq, zs
 
 
@@ -245,44 +289,71 @@ def norm_residual_backward(dz, dres, y, res, pre: Optional[Norm] = None, post: O
         raise ValueError("dz and dres: at least one is needed")
     if dz is not None and pre is None:
         raise ValueError("dz: given without its norm")
-    _on_current_device(like, name)
-    a = NmNormGradArgs()
-    a.type = _type_of(like, name)
-    flat, _ = _rows(like, name)
-    m, d = flat.shape
-    for t, what, ld in ((dz, "dz", "lddz"), (dres, "dres", "lddres"), (y, "y", "ldy"), (res, "res", "ldres")):
-        if t is None:
-            continue
-        _same(t, what, like)
-        t2, stride = _rows(t, what, d)
-        if t2.shape[0] != m:
-            raise ValueError(f"{what}: {t2.shape[0]} tokens, expected {m}")
-        setattr(a, what, t2.data_ptr())
-        setattr(a, ld, stride)
     if pre is not None and res is None:
         raise ValueError("res: needed for the gradient of its norm")
     if y is None and (post is not None or gate is not None):
         raise ValueError("y: needed for the gradients of its norm and gate")
-    a.m, a.d, a.groups, a.gate, a.alpha = m, d, _gate(gate, m, d, like), _ptr(gate), alpha
-    a.post, a.pre = _norm_args(post, d, like, "post"), _norm_args(pre, d, like, "pre")
-    torch = _torch()
-    f32 = torch.float32
-    dy = _empty(like.shape, like.dtype, like, stream) if y is not None else None
-    dr = _empty(like.shape, like.dtype, like, stream)
-    dgate = _empty(gate.shape, f32, like, stream) if gate is not None else None
-    params = []
-    for norm in (pre, post):
-        for t in (norm.weight, norm.bias) if norm is not None else (None, None):
-            params.append(_empty((d,), f32, like, stream) if t is not None else None)
-    a.dy, a.dr, a.dgate = _ptr(dy), _ptr(dr), _ptr(dgate)
-    a.dpre_weight, a.dpre_bias, a.dpost_weight, a.dpost_bias = (_ptr(p) for p in params)
+    rt = _rt or _runtime()
+    dev = _index(like, name, rt)
+    a = NmNormGradArgs()
+    a.type = _type_of(like, name, rt)
+    m, d, _ = _rows(like, name)
+
+    def given(t, what):
+        mt, dt, ld = _rows(t, what)
+        if mt != m or dt != d or t.dtype != like.dtype:
+            raise ValueError(f"{what}: {t.dtype} [{mt} x {dt}], expected {like.dtype} [{m} x {d}]")
+        _on(t, what, dev)
+        return t.data_ptr(), ld
+
+    if dz is not None:
+        a.dz, a.lddz = given(dz, "dz")
+    if dres is not None:
+        a.dres, a.lddres = given(dres, "dres")
+    if y is not None:
+        a.y, a.ldy = given(y, "y")
+    if res is not None:
+        a.res, a.ldres = given(res, "res")
+    a.m, a.d, a.groups, a.alpha = m, d, _gate(gate, m, d, dev, rt), alpha
+    dr = _empty(like.shape, like.dtype, like, stream, rt)
+    a.dr = dr.data_ptr()
+    dy = dgate = dqw = dqb = dpw = dpb = None
+    if y is not None:
+        dy = _empty(like.shape, like.dtype, like, stream, rt)
+        a.dy = dy.data_ptr()
+    # the parameters' gradients: rows of one buffer (groups for the gate, then the norms' weights and biases)
+    wanted = [pre is not None and pre.weight is not None, pre is not None and pre.bias is not None,
+              post is not None and post.weight is not None, post is not None and post.bias is not None]
+    rows = (a.groups if gate is not None else 0) + sum(wanted)
+    sums = _empty((rows, d), rt.f32, like, stream, rt) if rows else None
+    at = 0
+    if gate is not None:
+        a.gate = gate.data_ptr()
+        dgate = sums[:a.groups] if gate.dim() == 2 else sums[0]
+        a.dgate = dgate.data_ptr()
+        at = a.groups
+    if pre is not None:
+        a.pre = pre._for(d, dev, "pre")
+        if wanted[0]:
+            dqw, at = sums[at], at + 1
+            a.dpre_weight = dqw.data_ptr()
+        if wanted[1]:
+            dqb, at = sums[at], at + 1
+            a.dpre_bias = dqb.data_ptr()
+    if post is not None:
+        a.post = post._for(d, dev, "post")
+        if wanted[2]:
+            dpw, at = sums[at], at + 1
+            a.dpost_weight = dpw.data_ptr()
+        if wanted[3]:
+            dpb = sums[at]
+            a.dpost_bias = dpb.data_ptr()
     need = ctypes.c_size_t()
     _check(lib().nm_norm_residual_backward_workspace(m, d, a.groups, ctypes.byref(need)),
            "nm_norm_residual_backward_workspace")
-    ws = _empty((need.value,), torch.uint8, like, stream) if need.value else None
-    _check(lib().nm_norm_residual_backward(ctypes.byref(a), _ptr(ws), need.value, _stream(stream)),
-           "nm_norm_residual_backward")
-    return NormGrads(dy, dr, dgate, *params)
+    ws = _empty((need.value,), rt.u8, like, stream, rt) if need.value else None
+    _check(rt.norm_grad(ctypes.byref(a), _ptr(ws), need.value, _handle(stream, dev, rt)), "nm_norm_residual_backward")
+    return NormGrads(dy, dr, dgate, dqw, dqb, dpw, dpb)
 
 
 # ---------------------------------------------------------------- scaled int8 products
@@ -305,7 +376,7 @@ class NmGatedGradArgs(ctypes.Structure):
 
 
 def _device_i8(W, name: str, device):
-    torch = _torch()
+    torch = _runtime().torch
     if not torch.is_tensor(W):
         W = torch.from_numpy(W)
     if W.dtype != torch.int8 or W.dim() != 2:
@@ -314,7 +385,7 @@ def _device_i8(W, name: str, device):
 
 
 def _vector(v, name: str, n: int, like):
-    torch = _torch()
+    torch = _runtime().torch
     v = torch.as_tensor(v, dtype=torch.float32, device=like.device)
     if v.shape != (n,):
         raise ValueError(f"{name}: shape {tuple(v.shape)}, expected ({n},)")
@@ -337,7 +408,7 @@ class ScaledWeight:
 
     def __init__(self, weight: DeviceWeight, scale, bias, n: int, k: int):
         self.weight, self.scale, self.bias, self.n, self.k = weight, scale, bias, n, k
-        self.device = weight.vals.device
+        self.device, self._dev, self._kp = weight.vals.device, weight.vals.get_device(), padded(k)
         self._c = NmScaledWeight(ctypes.pointer(weight.desc), _ptr(weight.vals),
                                  _ptr(weight.meta) if weight.desc.meta_bytes else None, _ptr(scale), _ptr(bias), n, k)
         self._ref = ctypes.byref(self._c)
@@ -349,7 +420,7 @@ class ScaledWeight:
         cols = padded(W.shape[1])
         desc = compress_size(rows, cols, N, M)
         if desc.layout == NM_LAYOUT_DENSE:
-            return DeviceWeight(_pad(W, rows, cols).view(-1), W.new_empty(0).view(_torch().uint8), desc)
+            return DeviceWeight(_pad(W, rows, cols).view(-1), W.new_empty(0, dtype=_runtime().u8), desc)
         return DeviceWeight.from_packed(compress(_pad(W, rows, cols).cpu().numpy(), N, M), W.device)
 
     @classmethod
@@ -367,17 +438,16 @@ class ScaledWeight:
         q, scale = quantize_rows(W)
         return cls.from_int8(q[:, :W.shape[1]], scale, bias)
 
-    def _workspace(self, m: int, xtype: int, like, stream):
+    def _need(self, m: int, xtype: int) -> int:
+        """Workspace bytes of a product: a size by tokens and type, not a buffer."""
         need = self._needs.get((m, xtype))
-        if need is None:      # a size by tokens and type: not a buffer
+        if need is None:
             size = ctypes.c_size_t()
             _check(lib().nm_linear_workspace(self._ref, m, xtype, ctypes.byref(size)), "nm_linear_workspace")
             if len(self._needs) > 256:
                 self._needs.clear()
             need = self._needs[m, xtype] = size.value
-        if not need:
-            return None, 0
-        return _empty((need,), _torch().uint8, like, stream), need
+        return need
 
 
 class GatedWeight(ScaledWeight):
@@ -394,7 +464,7 @@ class GatedWeight(ScaledWeight):
         rows = (gate.shape[0] + 31) & ~31
         shape = (rows // 16, 16) + tuple(gate.shape[1:])
         pads = [_pad(t, rows, *t.shape[1:]).view(shape) for t in (gate, up)]
-        return _torch().stack(pads, 1).view(2 * rows, *gate.shape[1:])
+        return _runtime().torch.stack(pads, 1).view(2 * rows, *gate.shape[1:])
 
     @classmethod
     def from_int8(cls, Wg, scale_gate, Wu, scale_up, bias_gate=None, bias_up=None, act: str = "silu", N: int = 8,
@@ -423,62 +493,71 @@ class GatedWeight(ScaledWeight):
         return cls.from_int8(qg[:, :k], sg, qu[:, :k], su, bias_gate, bias_up, act=act, trainable=True)
 
 
-def _product_out(out, shape, dtype, like, stream):
-    """(output, its row stride): rows may lie apart in a given one."""
+def _product_out(out, m: int, shape, dtype, like, stream, rt):
+    """(output, its type, its row stride): rows may lie apart in a given one."""
     if out is None:
-        return _empty(shape, dtype, like, stream), shape[-1]
-    if out.dtype != dtype or tuple(out.shape) != tuple(shape) or out.device != like.device:
-        raise ValueError(f"out: {out.dtype} {tuple(out.shape)} on {out.device}, expected {dtype} {tuple(shape)} on "
-                         f"{like.device}")
-    flat, ld = _rows(out, "out")
-    return out, ld
+        code = rt.types.get(dtype)
+        if code is None:
+            raise ValueError(f"out_dtype: {dtype}, expected float16, bfloat16 or float32")
+        return _empty(shape, dtype, like, stream, rt), code, shape[-1]
+    if out.dtype != dtype or tuple(out.shape) != tuple(shape):
+        raise ValueError(f"out: {out.dtype} {tuple(out.shape)}, expected {dtype} {tuple(shape)}")
+    _on(out, "out", like.get_device())
+    return out, _type_of(out, "out", rt), _rows(out, "out")[2]
 
 
 def _of_rows(x, w: ScaledWeight, out, out_dtype, stream, gated: bool):
-    _on_current_device(x, "x")
-    if x.device != w.device:
+    rt = _rt or _runtime()
+    dev = _index(x, "x", rt)
+    if dev != w._dev:
         raise ValueError(f"x: on {x.device}, expected {w.device}")
-    xtype = _type_of(x, "x")
-    flat, ld = _rows(x, "x", w.k)
-    m = flat.shape[0]
-    dtype = x.dtype if out_dtype is None else out_dtype
-    out, ldo = _product_out(out, (*x.shape[:-1], w.n), dtype, x, stream)
-    ws, need = w._workspace(m, xtype, x, stream)
-    wp = None if ws is None else ws.data_ptr()
-    if gated:
-        _check(lib().nm_gated(flat.data_ptr(), ld, xtype, m, w._ref, w._act, out.data_ptr(), ldo, _type_of(out, "out"),
-                              wp, need, _stream(stream)), "nm_gated")
-    else:
-        _check(lib().nm_linear_i8(flat.data_ptr(), ld, xtype, m, w._ref, out.data_ptr(), ldo, _type_of(out, "out"), wp,
-                                  need, _stream(stream)), "nm_linear_i8")
+    xtype = _type_of(x, "x", rt)
+    m, k, ld = _rows(x, "x")
+    if k != w.k:
+        raise ValueError(f"x: {k} channels, expected {w.k}")
+    shape = (m, w.n) if x.dim() == 2 else (*x.shape[:-1], w.n)
+    out, otype, ldo = _product_out(out, m, shape, out_dtype or x.dtype, x, stream, rt)
+    at = _handle(stream, dev, rt)
+    # a few tokens need no workspace: it is allocated when the library asks for it
+    ws, need = None, 0
+    while True:
+        wp = None if ws is None else ws.data_ptr()
+        if gated:
+            st = rt.gated(x.data_ptr(), ld, xtype, m, w._ref, w._act, out.data_ptr(), ldo, otype, wp, need, at)
+        else:
+            st = rt.linear(x.data_ptr(), ld, xtype, m, w._ref, out.data_ptr(), ldo, otype, wp, need, at)
+        if st != NM_ERR_WORKSPACE or ws is not None:
+            break
+        need = w._need(m, xtype)
+        ws = _empty((need,), rt.u8, x, stream, rt)
+    if st != NM_OK:
+        raise NmError(st, "nm_gated" if gated else "nm_linear_i8")
     return out
 
 
-def _codes_in(xq, sx, w: ScaledWeight) -> int:
-    torch = _torch()
-    _on_current_device(xq, "xq")
-    if xq.dim() != 2:
-        raise ValueError(f"xq: {xq.dim()}-D, expected [tokens x {padded(w.k)}]")
-    m = xq.shape[0]
-    _need(xq, "xq", (torch.int8,), (m, padded(w.k)))
-    _need(sx, "sx", (torch.float32,), (m,))
-    for t, name in ((xq, "xq"), (sx, "sx")):
-        if t.device != w.device:
-            raise ValueError(f"{name}: on {t.device}, expected {w.device}")
-    return m
+def _codes_in(xq, sx, w: ScaledWeight, rt):
+    """(tokens, device) of codes and scales for w."""
+    dev = _index(xq, "xq", rt)
+    m = xq.shape[0] if xq.dim() else 0
+    _param(xq, "xq", (m, w._kp), rt.i8, w._dev)
+    _param(sx, "sx", (m,), rt.f32, w._dev)
+    return m, dev
 
 
 def _of_codes(xq, sx, w: ScaledWeight, out, out_dtype, stream, gated: bool):
-    m = _codes_in(xq, sx, w)
-    out, ldo = _product_out(out, (m, w.n), out.dtype if out is not None else out_dtype, xq, stream)
-    ws, need = w._workspace(m, 0, xq, stream)
-    wp = None if ws is None else ws.data_ptr()
+    rt = _rt or _runtime()
+    m, dev = _codes_in(xq, sx, w, rt)
+    dtype = out.dtype if out is not None else out_dtype or rt.torch.float16
+    out, otype, ldo = _product_out(out, m, (m, w.n), dtype, xq, stream, rt)
+    need = w._need(m, 0)
+    ws = _empty((need,), rt.u8, xq, stream, rt) if need else None
+    at = _handle(stream, dev, rt)
     if gated:
-        _check(lib().nm_gated_i8(xq.data_ptr(), sx.data_ptr(), m, w._ref, w._act, out.data_ptr(), ldo,
-                                 _type_of(out, "out"), wp, need, _stream(stream)), "nm_gated_i8")
+        _check(rt.gated_codes(xq.data_ptr(), sx.data_ptr(), m, w._ref, w._act, out.data_ptr(), ldo, otype, _ptr(ws),
+                              need, at), "nm_gated_i8")
     else:
-        _check(lib().nm_gemm_i8_scaled(xq.data_ptr(), sx.data_ptr(), m, w._ref, out.data_ptr(), ldo,
-                                       _type_of(out, "out"), wp, need, _stream(stream)), "nm_gemm_i8_scaled")
+        _check(rt.linear_codes(xq.data_ptr(), sx.data_ptr(), m, w._ref, out.data_ptr(), ldo, otype, _ptr(ws), need,
+                               at), "nm_gemm_i8_scaled")
     return out
 
 
@@ -494,7 +573,7 @@ def gemm_i8_scaled(xq, sx, w: ScaledWeight, out=None, out_dtype=None, stream=Non
     out_dtype (float16 without it)."""
     if isinstance(w, GatedWeight):
         raise ValueError("w: a gated block's weight")
-    return _of_codes(xq, sx, w, out, out_dtype or _torch().float16, stream, False)
+    return _of_codes(xq, sx, w, out, out_dtype, stream, False)
 
 
 def gated_ffn(x, w: GatedWeight, out=None, out_dtype=None, stream=None):
@@ -508,7 +587,7 @@ def gated_ffn_i8(xq, sx, w: GatedWeight, out=None, out_dtype=None, stream=None):
     """nm_gated_i8: the same of codes and scales; of out_dtype (float16 without it)."""
     if not isinstance(w, GatedWeight):
         raise ValueError("w: not a gated block's weight")
-    return _of_codes(xq, sx, w, out, out_dtype or _torch().float16, stream, True)
+    return _of_codes(xq, sx, w, out, out_dtype, stream, True)
 
 
 class GatedGrads(NamedTuple):
@@ -527,26 +606,26 @@ def gated_ffn_backward(xq, sx, w: GatedWeight, dh, stream=None) -> GatedGrads:
         raise ValueError("w: not a gated block's weight")
     if w.weight.desc.layout != NM_LAYOUT_DENSE:
         raise ValueError("w: the backward pass takes dense layouts")
-    torch = _torch()
-    m = _codes_in(xq, sx, w)
-    if dh.dtype not in (torch.float16, torch.bfloat16):
-        raise ValueError(f"dh: dtype {dh.dtype}, expected float16 or bfloat16")
-    if dh.device != w.device:
-        raise ValueError(f"dh: on {dh.device}, expected {w.device}")
-    flat, ld = _rows(dh, "dh", w.n)
-    if flat.shape[0] != m:
-        raise ValueError(f"dh: {flat.shape[0]} tokens, expected {m}")
-    T, f32 = dh.dtype, torch.float32
-    dx = _empty((m, w.k), T, dh, stream)
-    dwg, dwu = _empty((w.n, w.k), T, dh, stream), _empty((w.n, w.k), T, dh, stream)
+    rt = _rt or _runtime()
+    m, dev = _codes_in(xq, sx, w, rt)
+    T, f32 = dh.dtype, rt.f32
+    code = _type_of(dh, "dh", rt)
+    if code == NM_TYPE_F32:
+        raise ValueError(f"dh: dtype {T}, expected float16 or bfloat16")
+    mh, n, ld = _rows(dh, "dh")
+    if mh != m or n != w.n:
+        raise ValueError(f"dh: [{mh} x {n}], expected [{m} x {w.n}]")
+    _on(dh, "dh", dev)
+    dx = _empty((m, w.k), T, dh, stream, rt)
+    dwg, dwu = _empty((w.n, w.k), T, dh, stream, rt), _empty((w.n, w.k), T, dh, stream, rt)
     dbg = dbu = None
     if w.bias is not None:
-        dbg, dbu = _empty((w.n,), f32, dh, stream), _empty((w.n,), f32, dh, stream)
+        dbg, dbu = _empty((w.n,), f32, dh, stream, rt), _empty((w.n,), f32, dh, stream, rt)
     need = ctypes.c_size_t()
     _check(lib().nm_gated_backward_workspace(w._ref, m, ctypes.byref(need)), "nm_gated_backward_workspace")
-    ws = _empty((need.value,), torch.uint8, dh, stream) if need.value else None
-    a = NmGatedGradArgs(xq.data_ptr(), sx.data_ptr(), flat.data_ptr(), ld, m, w._act, _type_of(dh, "dh"), _ptr(dx),
-                        _ptr(dwg), _ptr(dwu), _ptr(dbg), _ptr(dbu))
-    _check(lib().nm_gated_backward(ctypes.byref(a), w._ref, _ptr(ws), need.value, _stream(stream)),
+    ws = _empty((need.value,), rt.u8, dh, stream, rt) if need.value else None
+    a = NmGatedGradArgs(xq.data_ptr(), sx.data_ptr(), dh.data_ptr(), ld, m, w._act, code, dx.data_ptr(),
+                        dwg.data_ptr(), dwu.data_ptr(), _ptr(dbg), _ptr(dbu))
+    _check(rt.gated_grad(ctypes.byref(a), w._ref, _ptr(ws), need.value, _handle(stream, dev, rt)),
            "nm_gated_backward")
     return GatedGrads(dx, dwg, dwu, dbg, dbu)

@@ -173,3 +173,15 @@ def test_refusals():
         with pytest.raises(ValueError):
             call()
             pytest.fail(f"call {i} was accepted")
+
+
+@pytest.mark.parametrize("T", bu.TYPES)
+def test_a_token_has_the_same_bits_in_every_batch(T):
+    # one token, a few, and a batch of tiles run different kernels on the same sums
+    for N, M in ((8, 8), (2, 4), (4, 8)):
+        x, w, (wg, cg, bg, *_), _ = case(700, 256, 100, T, True, N, M)
+        lin = nb.ScaledWeight.from_int8(wg, cg, bias=bg, N=N, M=M)
+        for call, weight in ((nb.gated_ffn, w), (nb.linear_i8, lin)):
+            all_ = call(x, weight)
+            for part in (1, 3, 20, 50):
+                assert torch.equal(call(x[:part], weight), all_[:part])

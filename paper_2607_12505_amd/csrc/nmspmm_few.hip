@@ -8,7 +8,7 @@
 // here and in a large batch.
 //
 // Activations come as codes (each wave reads its own k-steps of them, from L2),
-// or, for the few tokens whose values fit 32 a thread, as values: every workgroup
+// or, for the few tokens whose values fit 16 a thread, as values: every workgroup
 // then makes the codes itself, in LDS, while its first weights are on their
 // way.  That repeats a row's codes once for each 16 channels, and saves a launch.
 #include "nmspmm_products.h"
@@ -37,7 +37,7 @@ __device__ __forceinline__ void few_values(const void *x, int64_t at, float (&f)
 
 // Codes of m rows of x (k a multiple of 8, at most 8 * kFewCodes * 512 values in
 // all) into LDS rows of `pitch` bytes, zeros from k on, and their scales.
-constexpr int kFewCodes = 4;
+constexpr int kFewCodes = 2;
 __device__ __forceinline__ void few_codes(const BlockArgs &a, int8_t *xs, int pitch, float *scales, uint32_t *tops) {
     const int tid = threadIdx.x, per = a.kx / 8, chunks = a.m * per;
     float f[kFewCodes][8];
@@ -99,8 +99,9 @@ template <int KIND, int FN, int FM, bool CODES>
 __global__ __launch_bounds__(64 * kFewWaves) void k_few(BlockArgs a) {
     using K = Kind<KIND>;
     constexpr bool kDense = KIND == NM_KIND_DENSE, kMask = K::NV > 0;
-    // the codes, then the partial sums; m * k <= 16384 codes and at most 136 bytes of padding a row
-    __shared__ __attribute__((aligned(16))) int8_t lds[CODES ? kFewWaves * FM * FN * 1024 : 8 * kFewCodes * 512 + 16 * 136];
+    // the codes, then the partial sums; m * k <= 8192 codes and at most 136 bytes of padding a row
+    constexpr int kSums = kFewWaves * FM * FN * 1024, kCodes = CODES ? 0 : 8 * kFewCodes * 64 * kFewWaves + 16 * 136;
+    __shared__ __attribute__((aligned(16))) int8_t lds[kSums > kCodes ? kSums : kCodes];
     __shared__ uint2 lut[K::LUT];
     __shared__ float scales[16];
     __shared__ uint32_t tops[16];
@@ -240,10 +241,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few(BlockArgs a) {
     }
     by_type(a.type, [&](auto *p) {
         using T = typename std::remove_pointer<decltype(p)>::type;
-        T *row = (T *)a.out + (int64_t)tok * a.ldo;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (ch + e < a.n_out) row[ch + e] = (T)v[0][e];
+        store_four<T>(a, tok, ch, v[0]);
     });
 }
 

@@ -795,5 +795,284 @@ __device__ __forceinline__ void gemm_tile(const ARGS &a, int8_t *lds, uint2 *lut
                             lds + wave * G::STG, multiplier, s_last);
 }
 
+// k_gemm_ks, mask layouts: expands lane `lane`'s part of a compact block and
+// writes it to the LDS weight area of a slot: block bl of the tile (16 rows),
+// as swizzled dense rows.
+template <int KIND>
+__device__ __forceinline__ void expand_to_lds(const WRegs<KIND> &r, const uint2 *lut, int8_t *wslot, int bl,
+                                              int lane) {
+    v4i c0, c1;
+    expand_dense<KIND>(r, lut, c0, c1);
+    const int row = bl * 16 + (lane & 15);
+    const int ch = 2 * (lane >> 4);                          // the lane's first 16-byte chunk of the row
+    int8_t *rowp = wslot + row * 128;
+    *(v4i *)(rowp + ((ch ^ (row & 7)) << 4)) = c0;
+    *(v4i *)(rowp + (((ch + 1) ^ (row & 7)) << 4)) = c1;
+}
+
+// ---------------------------------------------------------------------------
+// k-sliced variant for shapes with few output tiles (small token counts).
+// Each of the 4 waves computes the whole tile_n x tile_m tile over its own
+// quarter of the k-steps (k-step s goes to wave s % 4), through a ring of
+// LDS slots that only it fills and reads: no workgroup barrier in the main
+// loop, and FN x FM matrix instructions per wave per k-step to cover the LDS
+// latency.  The four partial tiles are added through LDS at the end -- a
+// split of the reduction merged in the final stage without leaving the CU.
+
+template <int KIND, int FN, int FM, int NST>
+struct GeometryKS {
+    using K = Kind<KIND>;
+    // 1:4, 1:8 and 2:8: the compact bytes reach the ring by direct-to-LDS
+    // loads like X (RAWV value bytes and RAWM position bytes per k-step, the
+    // positions padded to 4 bytes per lane), and the compute stage expands
+    // them into the 4:2 operand in registers (no expanded copy in LDS)
+    static constexpr bool kRaw = K::kDecode && K::kSp;
+    static constexpr int BN = FN * 16;
+    static constexpr int BM = FM * 16;
+    static constexpr int XB = BM * 128;
+    static constexpr int WVB = kRaw ? 0 : K::kSp ? (BN / 16) * kVBlock : BN * 128;
+    static constexpr int WMB = kRaw ? 0 : K::kSp ? (BN / 16) * kMBlock : 0;
+    static constexpr int RAWV = kRaw ? FN * 64 * K::VB : 0;
+    static constexpr int RAWM = kRaw ? FN * 256 : 0;
+    static constexpr int SLOT = XB + WVB + WMB + RAWV + RAWM;
+    static constexpr int XI = BM / 8;                                  // X loads per k-step (one wave)
+    static constexpr int WI = kRaw ? FN * (K::VB / 4 + 1)
+                              : K::kDecode ? FN * K::LOADS : KIND == NM_KIND_SP42 ? FN * 2 : BN / 8;
+    static constexpr int DMA = XI + WI;
+    static constexpr int RING = 4 * NST * SLOT <= 160 * 1024 - 4096 ? NST : (160 * 1024 - 4096) / (4 * SLOT);
+    static constexpr int ROWB = BN * 4 + 16;                           // padded staged row (int32)
+    static constexpr int RED = 4 * BM * ROWB;
+    static constexpr int LDSB = 4 * RING * SLOT > RED ? 4 * RING * SLOT : RED;
+    static constexpr int CPR = BN / 4;                                 // 16-byte chunks per output row
+    static_assert(RING >= 2 && BM % 8 == 0 && BN % 16 == 0, "tile shape");
+};
+
+template <int KIND, int FN, int FM, int NST, class EPI, class ARGS>
+__device__ __forceinline__ void gemm_tile_ks(const ARGS &a, int8_t *lds, uint2 *lut, int *s_last) {
+    using G = GeometryKS<KIND, FN, FM, NST>;
+    using K = Kind<KIND>;
+    constexpr int BN = G::BN, BM = G::BM, R = G::RING;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t *)lds;
+
+    const int lid = map_block(blockIdx.x, (int)gridDim.x < a.gemm_grid ? (int)gridDim.x : a.gemm_grid);
+    const int tn = lid % a.tiles_n;
+    const int rest = lid / a.tiles_n;
+    const int split = rest % a.split_k;
+    const int tm = rest / a.split_k;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lg = lane >> 4;
+    const int tok0 = tm * BM;
+    const int ch0 = tn * BN;
+    const int s_begin = (int)((int64_t)split * a.k_steps / a.split_k);
+    const int s_end = (int)((int64_t)(split + 1) * a.k_steps / a.split_k);
+    const int nsteps = s_end - s_begin > wave ? (s_end - s_begin - wave + 3) / 4 : 0;  // this wave's k-steps
+    const int f0 = ch0 >> 4;
+    const uint32_t ring = lds0 + wave * R * G::SLOT;
+    int8_t *ringp = lds + wave * R * G::SLOT;
+
+    v4i acc[FN][FM];
+#pragma unroll
+    for (int i = 0; i < FN; ++i)
+#pragma unroll
+        for (int j = 0; j < FM; ++j) acc[i][j] = v4i{0, 0, 0, 0};
+
+    // k-step s into slot st of this wave's ring (same clamping rules as above):
+    // X, and the stored weight kinds
+    auto issue = [&](int s, int st) {
+        const uint32_t slot = ring + st * G::SLOT;
+#pragma unroll
+        for (int j = 0; j < BM / 8; ++j) {
+            const int r = 8 * j + (lane >> 3);
+            const int c = (lane & 7) ^ (r & 7);
+            const int tok = tok0 + r < a.m ? tok0 + r : a.m - 1;
+            const int kk = s * 128 + c * 16 < a.k ? s * 128 + c * 16 : a.k - 16;
+            dma16(a.X + (size_t)tok * a.k + kk, slot + j * 1024);
+        }
+        if constexpr (KIND == NM_KIND_SP42) {
+#pragma unroll
+            for (int bl = 0; bl < BN / 16; ++bl) {
+                int f = f0 + bl;
+                f = f < a.n_frags ? f : a.n_frags - 1;
+                const size_t b = (size_t)f * a.k_steps + s;
+                dma16(a.A + b * kVBlock + lane * 16, slot + G::XB + bl * kVBlock);
+                dma4(a.meta + b * kMBlock + lane * 4, slot + G::XB + G::WVB + bl * kMBlock);
+            }
+        } else if constexpr (KIND == NM_KIND_DENSE) {
+#pragma unroll
+            for (int j = 0; j < BN / 8; ++j) {
+                const int r = 8 * j + (lane >> 3);
+                const int c = (lane & 7) ^ (r & 7);
+                const int row = ch0 + r < a.n ? ch0 + r : a.n - 1;
+                const int kk = s * 128 + c * 16;
+                if (s * 128 + 128 <= a.k) {
+                    dma16(a.A + (size_t)row * a.k + kk, slot + G::XB + j * 1024);
+                } else {  // tail k-step of a dense weight: zeros past k
+                    v4i v = v4i{0, 0, 0, 0};
+                    if (kk < a.k) v = *(const v4i *)(a.A + (size_t)row * a.k + kk);
+                    *(v4i *)(ringp + st * G::SLOT + G::XB + j * 1024 + lane * 16) = v;
+                }
+            }
+        } else if constexpr (G::kRaw) {
+            // the FN compact blocks as stored: value bytes as whole dwords
+            // (dword i of a block by lane i % 64 of load i / 64), positions one
+            // dword per lane (2-byte positions: lanes 32-63 repeat lanes 0-31,
+            // landing in the unused half of the 256-byte area)
+            constexpr int VB = K::VB, MB = K::MB;
+#pragma unroll
+            for (int bl = 0; bl < FN; ++bl) {
+                int f = f0 + bl;
+                f = f < a.n_frags ? f : a.n_frags - 1;
+                const size_t b = (size_t)f * a.k_steps + s;
+                const int8_t *vb = a.A + b * 64 * VB;
+#pragma unroll
+                for (int i = 0; i < VB / 4; ++i)
+                    dma4(vb + (i * 64 + lane) * 4, slot + G::XB + G::WVB + G::WMB + bl * 64 * VB + i * 256);
+                const uint8_t *mb = a.meta + b * 64 * MB;
+                dma4(mb + (MB == 4 ? lane : (lane & 31)) * 4, slot + G::XB + G::WVB + G::WMB + G::RAWV + bl * 256);
+            }
+        }
+    };
+    // mask layouts (3:8-5:8; the loop below calls these only for them): the
+    // FN blocks of k-step s into registers, and their expansion into dense
+    // rows of slot st
+    WRegs<KIND> wr[FN];
+    auto wload_step = [&](int s) {
+        if constexpr (K::kDecode) {
+#pragma unroll
+            for (int bl = 0; bl < FN; ++bl) {
+                int f = f0 + bl;
+                f = f < a.n_frags ? f : a.n_frags - 1;
+                const size_t b = (size_t)f * a.k_steps + s;
+                wload<KIND>(wr[bl], a.A + (b * 64 + lane) * K::VB, a.meta + (b * 64 + lane) * K::MB);
+            }
+        }
+    };
+    auto expand_step = [&](int st) {
+        if constexpr (K::NV > 0) {
+#pragma unroll
+            for (int bl = 0; bl < FN; ++bl) expand_to_lds<KIND>(wr[bl], lut, ringp + st * G::SLOT + G::XB, bl, lane);
+        }
+    };
+    // 1:4, 1:8, 2:8: block bl of slot st's compact bytes, read from the ring
+    // and expanded into this lane's 4:2 operand (values and position word)
+    auto raw_operand = [&](int st, int bl, v4i &av, int &ai) {
+        if constexpr (G::kRaw) {
+            constexpr int VB = K::VB, MB = K::MB;
+            const int8_t *raw = ringp + st * G::SLOT + G::XB;
+            WRegs<KIND> r;
+            const int8_t *v = raw + bl * 64 * VB + lane * VB;
+            if constexpr (VB == 8) {
+                const v2u t = *(const v2u *)v;
+                r.v[0] = t[0];
+                r.v[1] = t[1];
+            } else {
+                static_assert(VB == 4, "compact 4:2 value bytes per lane");
+                r.v[0] = *(const uint32_t *)v;
+            }
+            const int8_t *m = raw + G::RAWV + bl * 256 + lane * MB;
+            r.m = MB == 4 ? *(const uint32_t *)m : (uint32_t) * (const uint16_t *)m;
+            uint32_t idx;
+            expand_sp42<KIND>(r, lut, av, idx);
+            ai = (int)idx;
+        }
+    };
+    auto compute = [&](int st) {
+        const int8_t *xs = ringp + st * G::SLOT;
+        const int8_t *ws = xs + G::XB;
+        if constexpr (K::kSp) {
+            v4i av[FN];
+            int ai[FN];
+#pragma unroll
+            for (int i = 0; i < FN; ++i) {
+                if constexpr (G::kRaw) {
+                    raw_operand(st, i, av[i], ai[i]);
+                } else {
+                    av[i] = *(const v4i *)(ws + i * kVBlock + lane * 16);
+                    ai[i] = *(const int *)(ws + G::WVB + i * kMBlock + lane * 4);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < FM; ++j) {
+                const int r = j * 16 + (lane & 15);
+                const int8_t *rowp = xs + r * 128;
+                const v4i blo = *(const v4i *)(rowp + ((lg ^ (r & 7)) << 4));
+                const v4i bhi = *(const v4i *)(rowp + (((lg + 4) ^ (r & 7)) << 4));
+                const v8i b = {blo[0], blo[1], blo[2], blo[3], bhi[0], bhi[1], bhi[2], bhi[3]};
+#pragma unroll
+                for (int i = 0; i < FN; ++i)
+                    acc[i][j] = __builtin_amdgcn_smfmac_i32_16x16x128_i8(av[i], b, acc[i][j], ai[i], 0, 0);
+            }
+        } else {
+            v4i alo[FN], ahi[FN];
+#pragma unroll
+            for (int i = 0; i < FN; ++i) {
+                const int r = i * 16 + (lane & 15);
+                const int8_t *rowp = ws + r * 128;
+                alo[i] = *(const v4i *)(rowp + ((lg ^ (r & 7)) << 4));
+                ahi[i] = *(const v4i *)(rowp + (((lg + 4) ^ (r & 7)) << 4));
+            }
+#pragma unroll
+            for (int j = 0; j < FM; ++j) {
+                const int r = j * 16 + (lane & 15);
+                const int8_t *rowp = xs + r * 128;
+                const v4i blo = *(const v4i *)(rowp + ((lg ^ (r & 7)) << 4));
+                const v4i bhi = *(const v4i *)(rowp + (((lg + 4) ^ (r & 7)) << 4));
+#pragma unroll
+                for (int i = 0; i < FN; ++i) {
+                    acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(alo[i], blo, acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(ahi[i], bhi, acc[i][j], 0, 0, 0);
+                }
+            }
+        }
+    };
+
+    // k-step t of this wave is s_begin + wave + 4 t
+#pragma unroll
+    for (int i = 0; i < R - 1; ++i)
+        if (i < nsteps) issue(s_begin + wave + 4 * i, i);
+    if constexpr (G::kRaw) {
+        fill_lut<KIND>(lut, tid, 256);
+        __syncthreads();
+    } else if constexpr (K::kDecode) {
+        // the lookup table is built while the first loads are in flight
+        if (nsteps > 0) wload_step(s_begin + wave);
+        fill_lut<KIND>(lut, tid, 256);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < R - 1; ++i)
+            if (i < nsteps) {
+                expand_step(i);
+                if (i + 1 < nsteps) wload_step(s_begin + wave + 4 * (i + 1));
+            }
+    }
+    for (int t = 0; t < nsteps; ++t) {
+        const int later = nsteps - 1 - t < R - 2 ? nsteps - 1 - t : R - 2;
+        wait_later<R - 2, G::DMA>(later);  // this wave's slot t is in LDS, its reads of slot t-1 done
+        const int nx = t + R - 1;
+        if (nx < nsteps) {
+            if constexpr (K::kDecode && !G::kRaw) {
+                expand_step(nx % R);
+                issue(s_begin + wave + 4 * nx, nx % R);
+                if (nx + 1 < nsteps) wload_step(s_begin + wave + 4 * (nx + 1));
+            } else {
+                issue(s_begin + wave + 4 * nx, nx % R);
+            }
+        }
+        compute(t % R);
+    }
+
+    // Add the four waves' partial tiles through LDS, then write rows.
+    __syncthreads();  // every wave is done with its ring
+    int8_t *stg = lds + wave * BM * G::ROWB;
+#pragma unroll
+    for (int j = 0; j < FM; ++j)
+#pragma unroll
+        for (int i = 0; i < FN; ++i)
+            *(v4i *)(stg + (j * 16 + (lane & 15)) * G::ROWB + (i * 16 + 4 * lg) * 4) = acc[i][j];
+    __syncthreads();
+    EPI::template finish_ks<G>(a, TileAt{tok0, ch0, split, tm, tn, lane}, lds, s_last);
+}
+
 }  // namespace
 }  // namespace nmspmm

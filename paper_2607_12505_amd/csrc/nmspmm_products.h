@@ -96,6 +96,30 @@ __device__ __forceinline__ v4f scaled_value(const v4i &v, float sx, const v4f &c
     return f;
 }
 
+// The k-sliced tile: the sum of its four waves' parts for 4 channels of a token,
+// and where they go.
+template <class G>
+__device__ __forceinline__ v4i sum_ks(const int8_t *lds, int row, int cc) {
+    v4i v = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) v += *(const v4i *)(lds + w * G::BM * G::ROWB + row * G::ROWB + cc * 16);
+    return v;
+}
+template <class T>
+__device__ __forceinline__ void store_four(const BlockArgs &a, int tok, int ch, const v4f &f) {
+    T *row = (T *)a.out + (int64_t)tok * a.ldo;
+    if (ch + 4 <= a.n_out) {
+        if constexpr (sizeof(T) == 4)
+            *(v4u_any *)(row + ch) = __builtin_bit_cast(v4u, f);
+        else
+            *(v2u_any *)(row + ch) = pack4_of<T>(f);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (ch + e < a.n_out) row[ch + e] = (T)f[e];
+    }
+}
+
 // y = T(acc * sx[token] * c[channel] + b[channel]): the int32 sum is exact, three
 // roundings in binary32 and the one to T.
 struct ScaledOut {
@@ -119,6 +143,21 @@ struct ScaledOut {
                 [&](int row, T *) -> T * {
                     return at.tok + row < a.m ? (T *)a.out + (int64_t)(at.tok + row) * a.ldo : nullptr;
                 });
+        });
+    }
+
+    template <class G>
+    static __device__ __forceinline__ void finish_ks(const BlockArgs &a, const TileAt &at, const int8_t *lds, int *) {
+        const int cc = threadIdx.x % G::CPR, ch = at.ch + cc * 4;   // the same channels for every row of this thread
+        const int c = ch < a.n ? ch : 0;
+        const v4f scale = *(const v4f *)(a.scale + c), bias = a.qscale ? *(const v4f *)(a.qscale + c) : v4f{0, 0, 0, 0};
+        by_type(a.type, [&](auto *t) {
+            using T = typename std::remove_pointer<decltype(t)>::type;
+            for (int p = threadIdx.x; p < G::BM * G::CPR; p += 256) {
+                const int row = p / G::CPR, tok = at.tok + row;
+                if (tok >= a.m || ch >= a.n_out) continue;
+                store_four<T>(a, tok, ch, scaled_value(sum_ks<G>(lds, row, cc), a.row_scale[tok], scale, bias));
+            }
         });
     }
 };
@@ -209,6 +248,30 @@ struct GatedOut {
                 [&](int row, T *) -> T * {
                     return at.tok + row < a.m ? (T *)a.out + (int64_t)(at.tok + row) * a.ldo : nullptr;
                 });
+        });
+    }
+
+    template <class G>
+    static __device__ __forceinline__ void finish_ks(const BlockArgs &a, const TileAt &at, const int8_t *lds, int *) {
+        constexpr int HPR = G::CPR / 2;                            // 4-channel chunks of a row of h
+        const int hc = threadIdx.x % HPR, cc = hc / 4 * 8 + hc % 4, ch = at.ch / 2 + hc * 4;
+        const int c = at.ch + cc * 4 < a.n ? at.ch + cc * 4 : 0;   // gate; the up channels are 16 rows on
+        const v4f zero = {0, 0, 0, 0}, cg = *(const v4f *)(a.scale + c), cu = *(const v4f *)(a.scale + c + 16);
+        const v4f bg = a.qscale ? *(const v4f *)(a.qscale + c) : zero;
+        const v4f bu = a.qscale ? *(const v4f *)(a.qscale + c + 16) : zero;
+        by_type(a.type, [&](auto *t) {
+            using T = typename std::remove_pointer<decltype(t)>::type;
+            for (int p = threadIdx.x; p < G::BM * HPR; p += 256) {
+                const int row = p / HPR, tok = at.tok + row;
+                if (tok >= a.m || ch >= a.n_out) continue;
+                const float sx = a.row_scale[tok];
+                const v4f g = scaled_value(sum_ks<G>(lds, row, cc), sx, cg, bg);
+                const v4f u = scaled_value(sum_ks<G>(lds, row, cc + 4), sx, cu, bu);
+                v4f h;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[e] = gate_times(a.act, g[e], u[e]);
+                store_four<T>(a, tok, ch, h);
+            }
         });
     }
 };
@@ -396,14 +459,27 @@ __attribute__((amdgpu_waves_per_eu(Geometry<KIND, WN, WM, FN, FM, NST>::WAVES)))
     gemm_tile<KIND, WN, WM, FN, FM, NST, EPI>(a, lds, lut, &s_last);
 }
 
+template <int KIND, int FN, int FM, int NST, class EPI>
+__global__ __launch_bounds__(256) void k_product_ks(BlockArgs a) {
+    using G = GeometryKS<KIND, FN, FM, NST>;
+    __shared__ __attribute__((aligned(1024))) int8_t lds[G::LDSB];
+    __shared__ uint2 lut[Kind<KIND>::LUT];
+    __shared__ int s_last;
+    gemm_tile_ks<KIND, FN, FM, NST, EPI>(a, lds, lut, &s_last);
+}
+
 template <int KIND, class EPI, uint32_t TILES, int T = 0>
 int launch_product(int tile, const BlockArgs &a, int grid, void *stream) {
     if constexpr (T < kNumSchedules) {
         if constexpr ((TILES >> T) & 1)
             if (tile == T) {
                 constexpr TileCfg t = kTiles[T];
-                hipLaunchKernelGGL((k_product<KIND, t.wn, t.wm, t.fn, t.fm, t.nst, EPI>), dim3(grid),
-                                   dim3(64 * t.wn * t.wm), 0, (hipStream_t)stream, a);
+                if constexpr (t.layout == kKSliced)
+                    hipLaunchKernelGGL((k_product_ks<KIND, t.fn, t.fm, t.nst, EPI>), dim3(grid), dim3(kThreads), 0,
+                                       (hipStream_t)stream, a);
+                else
+                    hipLaunchKernelGGL((k_product<KIND, t.wn, t.wm, t.fn, t.fm, t.nst, EPI>), dim3(grid),
+                                       dim3(64 * t.wn * t.wm), 0, (hipStream_t)stream, a);
                 return (int)hipGetLastError();
             }
         return launch_product<KIND, EPI, TILES, T + 1>(tile, a, grid, stream);

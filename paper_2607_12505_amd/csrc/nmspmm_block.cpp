@@ -356,32 +356,37 @@ nm_status product_of_rows(const void *x, int64_t ldx, int xtype, int m, const nm
 
 // ---------------------------------------------------------------- gated backward
 
-// Pieces of the workspace, in their order; sizes in bytes, offsets filled by the constructor.
+// A product of 16-bit operands: [m x n] outputs over k bytes of each row.
+struct CastPlan {
+    int tile, split;
+    int64_t m, n;
+    CastPlan(int64_t m_, int64_t n_, int64_t k_bytes) : m(m_), n(n_) {
+        tile = schedule_among(NM_KIND_DENSE, (int)m, (int)n, (int)k_bytes, NM_OUT_F16, kCastTiles);
+        // few tiles and a long reduction: split until every compute unit has a
+        // workgroup, with 16 k-steps or more each
+        const TileCfg &t = kTiles[tile];
+        const int64_t tiles = ((m + t.tile_m() - 1) / t.tile_m()) * ((n + t.tile_n() - 1) / t.tile_n());
+        split = 1;
+        while (split < 8 && tiles * split < device_cu_count() && k_bytes / kKStep / (2 * split) >= 16 &&
+               tiles <= kMaxSplitTiles && 2 * split * m * n * 4 < ((int64_t)1 << 31))
+            split *= 2;
+    }
+    int64_t split_bytes() const { return split > 1 ? (int64_t)kCounterBytes + split * m * n * 4 : 0; }
+};
+
+// Pieces of the workspace, in their order.
 struct GradPlan {
     int64_t rows_w, cols, ldt;     // 2 n', k rounded up to 16, tokens rounded up to 64
-    int grad_tile, dx_tile, dw_tile, dw_split;
+    CastPlan dx, dw;
+    int grad_tile, parts_rows;
     size_t at_da, at_dat, at_xt, at_wt, at_parts, at_split, bytes;
-    int parts_rows;
 
-    GradPlan(const nm_scaled_weight &w, int m) {
-        const nm_desc &d = *w.desc;
-        rows_w = d.n;
-        cols = d.k;
-        ldt = (int64_t)(m + 63) / 64 * 64;
-        grad_tile = schedule_among(NM_KIND_DENSE, m, d.n, d.k, NM_OUT_I32, kGradTiles);
-        dx_tile = schedule_among(NM_KIND_DENSE, m, d.k, (int)(2 * rows_w), NM_OUT_F16, kCastTiles);
-        const int k_bytes = (int)(2 * ldt);
-        dw_tile = schedule_among(NM_KIND_DENSE, d.n, d.k, k_bytes, NM_OUT_F16, kCastTiles);
+    GradPlan(const nm_scaled_weight &w, int m)
+        : rows_w(w.desc->n), cols(w.desc->k), ldt((int64_t)(m + 63) / 64 * 64), dx(m, cols, 2 * rows_w),
+          dw(rows_w, cols, 2 * ldt) {
+        grad_tile = schedule_among(NM_KIND_DENSE, m, w.desc->n, w.desc->k, NM_OUT_I32, kGradTiles);
         const TileCfg &g = kTiles[grad_tile];
         parts_rows = (m + g.tile_m() - 1) / g.tile_m() * g.wm;
-        // the weights' gradient has few tiles and a long reduction: split until
-        // every compute unit has two workgroups, with 16 k-steps or more each
-        const TileCfg &t = kTiles[dw_tile];
-        const int64_t tiles = ((rows_w + t.tile_m() - 1) / t.tile_m()) * ((cols + t.tile_n() - 1) / t.tile_n());
-        dw_split = 1;
-        while (dw_split < 8 && tiles * dw_split < device_cu_count() && k_bytes / kKStep / (2 * dw_split) >= 16 &&
-               tiles <= kMaxSplitTiles && 2 * dw_split * rows_w * cols * 4 < ((int64_t)1 << 31))
-            dw_split *= 2;
         size_t at = 0;
         auto take = [&](int64_t n) {
             const size_t here = at;
@@ -393,7 +398,9 @@ struct GradPlan {
         at_xt = take(cols * ldt * 2);
         at_wt = take(cols * rows_w * 2);
         at_parts = take((int64_t)parts_rows * rows_w * 4);
-        at_split = take(dw_split > 1 ? (int64_t)kCounterBytes + dw_split * rows_w * cols * 4 : 0);
+        // the two products' partial sums, one after the other; the counters at
+        // its start are left at zero by the first
+        at_split = take(dx.split_bytes() > dw.split_bytes() ? dx.split_bytes() : dw.split_bytes());
         bytes = at;
     }
 };
@@ -504,6 +511,11 @@ extern "C" nm_status nm_gated_backward(const nm_gated_grad_args *args, const nm_
     c.n_out = w->k;
     c.ldo = w->k;
     c.n_frags = (d.k + kFragRows - 1) / kFragRows;
+    if (p.dx.split > 1 || p.dw.split > 1) {
+        c.counters = (int32_t *)(base + p.at_split);
+        c.partials = (int32_t *)(base + p.at_split + kCounterBytes);
+        if (launch_zero(c.counters, kCounterBytes, stream) != 0) return NM_ERR_HIP;
+    }
     if (g.dx) {
         if (launch_transpose_codes(g.type, {w->vals, w->scale, base + p.at_wt, d.k, p.rows_w, d.n, d.k}, stream) != 0)
             return NM_ERR_HIP;
@@ -513,8 +525,9 @@ extern "C" nm_status nm_gated_backward(const nm_gated_grad_args *args, const nm_
         c.k_steps = c.k / kKStep;
         c.out = g.dx;
         c.stream_out = aligned(g.dx, 128) ? stream_out_for(g.m, w->k, c.k) : 0;
-        grid = place_tiles(c, p.dx_tile);
-        if (launch_cast(g.type, p.dx_tile, c, grid, stream) != 0) return NM_ERR_HIP;
+        c.split_k = p.dx.split;
+        grid = place_tiles(c, p.dx.tile);
+        if (launch_cast(g.type, p.dx.tile, c, grid, stream) != 0) return NM_ERR_HIP;
     }
     if (g.dw_gate) {
         if (launch_transpose_codes(g.type, {g.xq, g.sx, base + p.at_xt, d.k, p.ldt, g.m, d.k}, stream) != 0)
@@ -527,15 +540,10 @@ extern "C" nm_status nm_gated_backward(const nm_gated_grad_args *args, const nm_
         c.out = g.dw_gate;
         c.out2 = g.dw_up;
         c.interleaved = w->n;
-        c.split_k = p.dw_split;
-        if (p.dw_split > 1) {
-            c.counters = (int32_t *)(base + p.at_split);
-            c.partials = (int32_t *)(base + p.at_split + kCounterBytes);
-            if (launch_zero(c.counters, kCounterBytes, stream) != 0) return NM_ERR_HIP;
-        }
+        c.split_k = p.dw.split;
         c.stream_out = 0;
-        grid = place_tiles(c, p.dw_tile);
-        if (launch_cast(g.type, p.dw_tile, c, grid, stream) != 0) return NM_ERR_HIP;
+        grid = place_tiles(c, p.dw.tile);
+        if (launch_cast(g.type, p.dw.tile, c, grid, stream) != 0) return NM_ERR_HIP;
     }
     return NM_OK;
 }

@@ -12,6 +12,8 @@
 // difference of two sums, which cancels where the mean is large).
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "nmspmm_block.h"
 #include "nmspmm_values.h"
 
@@ -23,35 +25,47 @@ typedef unsigned int v2u __attribute__((ext_vector_type(2)));
 // A lane's part of a row: CH chunks of VEC consecutive channels, chunk c of
 // lane l of the team at channel (c * lanes + l) * VEC.  VEC = 8 needs d % 8 == 0
 // and 16-byte aligned rows; any other row goes one channel at a time.
+// As loaded: 16-bit values stay two to a register until they are used.
 template <class T, int VEC, int CH>
 struct Part {
-    T v[CH][VEC];
+    typename std::conditional<VEC == 8, Raw8<T>, T>::type v[CH];
+    __device__ __forceinline__ void get(float (&f)[CH][VEC]) const {
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if constexpr (VEC == 8) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[c][e] = (float)v[c].v[e];
+            } else {
+                f[c][0] = (float)v[c];
+            }
+    }
 };
 
+// Channels past d are zero; a row of null is.
 template <class T, int VEC, int CH>
 __device__ __forceinline__ void load_part(Part<T, VEC, CH> &p, const T *row, int d, int at, int step) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int ch = at + c * step;
         if constexpr (VEC == 8) {
-            Raw8<T> t = {};
-            if (ch < d) t = load8(row + ch);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) p.v[c][e] = t.v[e];
+            p.v[c] = {};
+            if (ch < d) p.v[c] = load8(row + ch);
         } else {
-            p.v[c][0] = ch < d ? row[ch] : (T)0.f;
+            p.v[c] = ch < d ? row[ch] : (T)0.f;
         }
     }
 }
+// A parameter of the lane's channels, `absent` where there is none and zero past d:
+// a lane without channels adds nothing to any sum.
 template <int VEC, int CH>
 __device__ __forceinline__ void load_param(float (&p)[CH][VEC], const float *row, float absent, int d, int at,
                                            int step) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const bool in = row && at + c * step < d;
+        const bool in = at + c * step < d;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) p[c][e] = absent;
-        if (in) {
+        for (int e = 0; e < VEC; ++e) p[c][e] = in ? absent : 0.f;
+        if (row && in) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) p[c][e] = row[at + c * step + e];
         }
@@ -128,13 +142,8 @@ __global__ __launch_bounds__(team_threads(WPR)) void k_norm_residual(NormArgs a)
         if (a.groups > 1)
             load_param(gate, a.gate + (int64_t)(live ? row / a.per_group : 0) * a.d, 1.f, a.d, at, step);
         float v[CH][VEC], rf[CH][VEC];
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                v[c][e] = (float)y.v[c][e];
-                rf[c][e] = (float)r.v[c][e];
-            }
+        y.get(v);
+        r.get(rf);
         fetch(row + (int)gridDim.x * TEAMS);
 
         if (a.post.kind != NM_NORM_NONE) {
@@ -150,7 +159,7 @@ __global__ __launch_bounds__(team_threads(WPR)) void k_norm_residual(NormArgs a)
         for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
-                v[c][e] = at + c * step < a.d ? __builtin_fmaf(gate[c][e], v[c][e], a.alpha * rf[c][e]) : 0.f;
+                v[c][e] = __builtin_fmaf(gate[c][e], v[c][e], a.alpha * rf[c][e]);
         if (a.res && live) store_part((T *)a.res + (int64_t)row * a.d, v, a.d, at, step);
         if (!a.z && !a.zq) continue;
 
@@ -170,8 +179,7 @@ __global__ __launch_bounds__(team_threads(WPR)) void k_norm_residual(NormArgs a)
 #pragma unroll
             for (int c = 0; c < CH; ++c)
 #pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    top = larger(top, at + c * step < a.d ? magnitude(v[c][e]) : 0.f);
+                for (int e = 0; e < VEC; ++e) top = larger(top, magnitude(v[c][e]));
             const RowScale rs = row_scale(red.largest(top));
             if (live) {
                 if (lane == 0) a.zs[row] = rs.scale;
@@ -193,6 +201,37 @@ __global__ __launch_bounds__(team_threads(WPR)) void k_norm_residual(NormArgs a)
     }
 }
 
+// The norms' parameters of the backward pass in LDS, where registers are short:
+// as a team's lanes read them, 16 bytes a lane and instruction (VEC = 8: the
+// first four channels of every chunk, then the last four).
+template <int VEC, int CH, int LANES>
+struct SharedParam {
+    static constexpr int SIZE = LANES * CH * VEC;
+    float *at0;
+    __device__ void fill(const float *src, float absent, int d) const {
+        for (int ch = threadIdx.x; ch < SIZE; ch += blockDim.x) {
+            const int to = VEC == 8 ? (ch % 8 / 4) * (LANES * CH * 4) + ch / 8 * 4 + ch % 4 : ch;
+            at0[to] = ch < d ? (src ? src[ch] : absent) : 0.f;
+        }
+    }
+    __device__ __forceinline__ void get(float (&f)[CH][VEC], int lane) const {
+        typedef float v4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            if constexpr (VEC == 8) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const v4 t = *(const v4 *)(at0 + h * (LANES * CH * 4) + (c * LANES + lane) * 4);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) f[c][4 * h + e] = t[e];
+                }
+            } else {
+                f[c][0] = at0[c * LANES + lane];
+            }
+        }
+    }
+};
+
 // --------------------------------------------------------------- backward
 // With hat(v) the normalised row and t = dout * weight, a norm's gradient is
 //   dv = (t - [mean(t)] - hat * mean(t * hat)) / deviation     ([]: layer norm)
@@ -205,11 +244,18 @@ __global__ __launch_bounds__(team_threads(WPR)) void k_norm_residual(NormArgs a)
 // the workgroups in k_norm_sums: every addition has its place, so results do not
 // change from run to run.  A gate that is shared by fewer tokens than all is
 // finished, or put aside for k_norm_sums, whenever the team reaches the group's end.
-template <class T, int VEC, int CH, int WPR>
-__global__ __launch_bounds__(team_threads(WPR)) void k_norm_residual_backward(NormGradArgs a) {
+// Waves of a SIMD that the register budget is made for.
+constexpr int grad_waves(int wpr, int vec, bool post) { return wpr == 16 || (vec == 8 && !post) ? 4 : 3; }
+
+// POST: whether there is a norm after the block (its sums are 40 % of the registers).
+template <class T, int VEC, int CH, int WPR, bool POST>
+__global__ __launch_bounds__(team_threads(WPR)) __attribute__((amdgpu_waves_per_eu(grad_waves(WPR, VEC, POST)))) void k_norm_residual_backward(
+    NormGradArgs a) {
     constexpr int TEAMS = team_threads(WPR) / 64 / WPR, LANES = 64 * WPR;
     __shared__ float box[TEAMS][2][2][WPR];
-    extern __shared__ __attribute__((aligned(16))) float joined[];     // TEAMS > 1: one sum of every team but the first
+    // the parameters, then (TEAMS > 1) one sum of every team but the first
+    using Shared = SharedParam<VEC, CH, LANES>;
+    extern __shared__ __attribute__((aligned(16))) float joined[];
     const int team = threadIdx.x / LANES, lane = threadIdx.x % LANES;
     RowReduce<WPR> red{box[team], lane >> 6};
     const int at = lane * VEC, step = LANES * VEC;
@@ -217,17 +263,25 @@ __global__ __launch_bounds__(team_threads(WPR)) void k_norm_residual_backward(No
     const int first = (int)(blockIdx.x * TEAMS + team) * a.run;
     const int end = first + a.run < a.m ? first + a.run : a.m;
     const bool layer_q = a.pre.kind == NM_NORM_LAYER, layer_p = a.post.kind == NM_NORM_LAYER;
-    const bool has_q = a.pre.kind != NM_NORM_NONE, has_p = a.post.kind != NM_NORM_NONE;
+    const bool has_q = a.pre.kind != NM_NORM_NONE;
+    constexpr bool has_p = POST;
 
-    float gate[CH][VEC], wq[CH][VEC], wp[CH][VEC], bp[CH][VEC];
-    load_param(wp, a.post.weight, 1.f, a.d, at, step);
-    load_param(bp, a.post.bias, 0.f, a.d, at, step);
-    load_param(wq, a.pre.weight, 1.f, a.d, at, step);
+    float gate[CH][VEC];
+    const Shared lds_wq{joined}, lds_wp{joined + Shared::SIZE}, lds_bp{joined + 2 * Shared::SIZE};
+    lds_wq.fill(a.pre.weight, 1.f, a.d);
+    if constexpr (POST) {
+        lds_wp.fill(a.post.weight, 1.f, a.d);
+        lds_bp.fill(a.post.bias, 0.f, a.d);
+    }
+    __syncthreads();
     float s_wq[CH][VEC] = {}, s_bq[CH][VEC] = {}, s_g[CH][VEC] = {}, s_wp[CH][VEC] = {}, s_bp[CH][VEC] = {};
 
     Part<T, VEC, CH> py = {}, pr = {}, pz = {}, pd = {};
     auto fetch = [&](int row) {
-        if (row >= end) return;
+        if (row >= end) {      // a team that is done takes rows of zeros along: they add nothing
+            py = pr = pz = pd = {};
+            return;
+        }
         if (a.y) load_part(py, (const T *)a.y + row * a.ldy, a.d, at, step);
         if (has_q) load_part(pr, (const T *)a.res + row * a.ldr, a.d, at, step);
         if (a.dz) load_part(pz, (const T *)a.dz + row * a.lddz, a.d, at, step);
@@ -258,15 +312,10 @@ __global__ __launch_bounds__(team_threads(WPR)) void k_norm_residual_backward(No
             load_param(gate, a.gate ? a.gate + (int64_t)group * a.d : nullptr, 1.f, a.d, at, step);
         }
         float y[CH][VEC], r[CH][VEC], dz[CH][VEC], dt[CH][VEC];
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                y[c][e] = live ? (float)py.v[c][e] : 0.f;
-                r[c][e] = live ? (float)pr.v[c][e] : 0.f;
-                dz[c][e] = live ? (float)pz.v[c][e] : 0.f;
-                dt[c][e] = live ? (float)pd.v[c][e] : 0.f;
-            }
+        py.get(y);
+        pr.get(r);
+        pz.get(dz);
+        pd.get(dt);
         fetch(row + 1);
 
         float my = has_p ? total(y) : 0.f, mr = total(r);
@@ -277,7 +326,8 @@ __global__ __launch_bounds__(team_threads(WPR)) void k_norm_residual_backward(No
         const float inv_y = has_p ? 1.f / __builtin_sqrtf(__builtin_fmaf(vy, per, a.post.eps)) : 1.f;
         if (has_q) {
             const float inv_r = 1.f / __builtin_sqrtf(__builtin_fmaf(vr, per, a.pre.eps));
-            float st = 0.f, sth = 0.f;
+            float st = 0.f, sth = 0.f, wq[CH][VEC];
+            lds_wq.get(wq, lane);
 #pragma unroll
             for (int c = 0; c < CH; ++c)
 #pragma unroll
@@ -313,14 +363,17 @@ __global__ __launch_bounds__(team_threads(WPR)) void k_norm_residual_backward(No
         }
         if (!a.y) continue;
 
-        float st = 0.f, sth = 0.f;
+        float st = 0.f, sth = 0.f, wp[CH][VEC], bp[CH][VEC];
+        if constexpr (POST) {
+            lds_wp.get(wp, lane);
+            lds_bp.get(bp, lane);
+        }
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const bool in = at + c * step < a.d;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                const float t = in ? dt[c][e] : 0.f;
-                if (has_p) {
+                const float t = dt[c][e];      // past d: times the gate's zero
+                if constexpr (POST) {
                     const float hat = y[c][e] * inv_y, g = t * gate[c][e];
                     s_g[c][e] = __builtin_fmaf(t, __builtin_fmaf(hat, wp[c][e], bp[c][e]), s_g[c][e]);
                     s_wp[c][e] = __builtin_fmaf(g, hat, s_wp[c][e]);
@@ -335,7 +388,7 @@ __global__ __launch_bounds__(team_threads(WPR)) void k_norm_residual_backward(No
                 }
             }
         }
-        if (has_p) {
+        if constexpr (POST) {
             red.sum2(st, sth);
             const float mt = layer_p ? st * per : 0.f, mth = sth * per;
 #pragma unroll
@@ -369,8 +422,10 @@ __global__ __launch_bounds__(team_threads(WPR)) void k_norm_residual_backward(No
     join(s_g, a.groups <= 1 && a.dgate ? a.parts : nullptr);
     join(s_wq, a.dpre_weight ? a.parts + span : nullptr);
     join(s_bq, a.dpre_bias ? a.parts + 2 * span : nullptr);
-    join(s_wp, a.dpost_weight ? a.parts + 3 * span : nullptr);
-    join(s_bp, a.dpost_bias ? a.parts + 4 * span : nullptr);
+    if constexpr (POST) {
+        join(s_wp, a.dpost_weight ? a.parts + 3 * span : nullptr);
+        join(s_bp, a.dpost_bias ? a.parts + 4 * span : nullptr);
+    }
 }
 
 // Adds what the workgroups and runs left: blocks 0 .. 5 * col_blocks - 1 one kind
@@ -389,7 +444,7 @@ __global__ __launch_bounds__(1024) void k_norm_sums(NormGradArgs a, int workgrou
               : kind == 3 ? a.dpost_weight : a.dpost_bias;
         if (dst && ch < a.d) {
             const float *src = a.parts + (int64_t)kind * workgroups * a.d + ch;
-#pragma unroll 8
+#pragma unroll 16
             for (int w = wave; w < workgroups; w += 16) s += src[(int64_t)w * a.d];
         }
     } else {
@@ -431,15 +486,19 @@ __global__ __launch_bounds__(team_threads(WPR)) void k_quantize_rows(QuantArgs a
         int base = 0;
         for (;; base += span) {
             load_part(p, src, a.k, base + lane * VEC, step);
+            float f[CH][VEC];
+            p.get(f);
 #pragma unroll
             for (int c = 0; c < CH; ++c)
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) top = larger(top, magnitude((float)p.v[c][e]));
+                for (int e = 0; e < VEC; ++e) top = larger(top, magnitude(f[c][e]));
             if (base + span >= a.ldq) break;
         }
         const RowScale rs = row_scale(red.largest(top));
         if (live && lane == 0) a.scale[row] = rs.scale;
         for (;; base -= span) {      // the last part is still in registers
+            float f[CH][VEC];
+            p.get(f);
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const int ch = base + lane * VEC + c * step;
@@ -447,7 +506,7 @@ __global__ __launch_bounds__(team_threads(WPR)) void k_quantize_rows(QuantArgs a
                 int8_t *dst = a.q + row * a.ldq + ch;
                 int q[VEC];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) q[e] = row_code((float)p.v[c][e], rs.inv);
+                for (int e = 0; e < VEC; ++e) q[e] = row_code(f[c][e], rs.inv);
                 if constexpr (VEC == 8)
                     *(v2u *)dst = v2u{pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7])};
                 else
@@ -483,22 +542,29 @@ int norm_by_width(const NormArgs &a, void *stream) {
     return norm_one<T, VEC, full, 16>(a, stream);
 }
 
-template <class T, int VEC, int CH, int WPR>
+template <class T, int VEC, int CH, int WPR, bool POST>
 int grad_one(const NormGradArgs &a, int workgroups, void *stream) {
-    constexpr int teams = team_threads(WPR) / 64 / WPR;
-    hipLaunchKernelGGL((k_norm_residual_backward<T, VEC, CH, WPR>), dim3(workgroups), dim3(team_threads(WPR)),
-                       (teams - 1) * a.d * 4, (hipStream_t)stream, a);
+    constexpr int teams = team_threads(WPR) / 64 / WPR, params = SharedParam<VEC, CH, 64 * WPR>::SIZE * (POST ? 3 : 1);
+    const int sums = (teams - 1) * a.d;      // once the parameters are no longer needed
+    hipLaunchKernelGGL((k_norm_residual_backward<T, VEC, CH, WPR, POST>), dim3(workgroups), dim3(team_threads(WPR)),
+                       (params > sums ? params : sums) * 4, (hipStream_t)stream, a);
     return (int)hipGetLastError();
 }
-template <class T, int VEC>
+template <class T, int VEC, bool POST>
 int grad_by_width(const NormGradArgs &a, int workgroups, void *stream) {
     constexpr int half = 8 / VEC;
-    if (a.d <= 512) return grad_one<T, VEC, half, 1>(a, workgroups, stream);
-    if (a.d <= 1024) return grad_one<T, VEC, half, 2>(a, workgroups, stream);
-    if (a.d <= 2048) return grad_one<T, VEC, half, 4>(a, workgroups, stream);
-    if (a.d <= 4096) return grad_one<T, VEC, half, 8>(a, workgroups, stream);
-    if (a.d <= 8192) return grad_one<T, VEC, half, 16>(a, workgroups, stream);
-    return grad_one<T, VEC, 2 * half, 16>(a, workgroups, stream);
+    if (a.d <= 512) return grad_one<T, VEC, half, 1, POST>(a, workgroups, stream);
+    if (a.d <= 1024) return grad_one<T, VEC, half, 2, POST>(a, workgroups, stream);
+    if (a.d <= 2048) return grad_one<T, VEC, half, 4, POST>(a, workgroups, stream);
+    if (a.d <= 4096) return grad_one<T, VEC, half, 8, POST>(a, workgroups, stream);
+    if (a.d <= 8192) return grad_one<T, VEC, half, 16, POST>(a, workgroups, stream);
+    return grad_one<T, VEC, 2 * half, 16, POST>(a, workgroups, stream);
+}
+template <class T>
+int grad_of(bool vec, const NormGradArgs &a, int workgroups, void *stream) {
+    const bool post = a.post.kind != NM_NORM_NONE && a.y;
+    if (vec) return post ? grad_by_width<T, 8, true>(a, workgroups, stream) : grad_by_width<T, 8, false>(a, workgroups, stream);
+    return post ? grad_by_width<T, 1, true>(a, workgroups, stream) : grad_by_width<T, 1, false>(a, workgroups, stream);
 }
 
 template <class T, int VEC, int CH, int WPR>
@@ -525,7 +591,7 @@ static int grad_teams(int d) { return d <= 512 ? 4 : d <= 1024 ? 2 : 1; }
 
 NormGradShape norm_grad_shape(int m, int d) {
     const int teams = grad_teams(d);
-    const int most = device_cu_count() * (d <= 2048 ? 4 : 2);
+    const int most = device_cu_count() * (d <= 2048 ? 3 : d <= 4096 ? 2 : 1);
     const int want = (m + teams - 1) / teams, workgroups = want < most ? want : most;
     NormGradShape s;
     s.teams = teams;
@@ -546,15 +612,9 @@ int launch_norm_residual(int type, bool vec, const NormArgs &a, void *stream) {
 int launch_norm_residual_backward(int type, bool vec, const NormGradArgs &a, int workgroups, void *stream) {
     int err = (int)hipErrorInvalidValue;
     switch (type) {
-        case NM_TYPE_F16:
-            err = vec ? grad_by_width<half_t, 8>(a, workgroups, stream) : grad_by_width<half_t, 1>(a, workgroups, stream);
-            break;
-        case NM_TYPE_BF16:
-            err = vec ? grad_by_width<bf16_t, 8>(a, workgroups, stream) : grad_by_width<bf16_t, 1>(a, workgroups, stream);
-            break;
-        case NM_TYPE_F32:
-            err = vec ? grad_by_width<float, 8>(a, workgroups, stream) : grad_by_width<float, 1>(a, workgroups, stream);
-            break;
+        case NM_TYPE_F16: err = grad_of<half_t>(vec, a, workgroups, stream); break;
+        case NM_TYPE_BF16: err = grad_of<bf16_t>(vec, a, workgroups, stream); break;
+        case NM_TYPE_F32: err = grad_of<float>(vec, a, workgroups, stream); break;
     }
     if (err != 0) return err;
     const int col_blocks = (a.d + 63) / 64;

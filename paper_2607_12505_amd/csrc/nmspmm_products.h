@@ -164,7 +164,11 @@ struct ScaledOut {
 
 // act(g) and its derivative.  The exponential is the hardware's (2^x within an
 // ulp, its argument rounded to binary32), the reciprocal within an ulp: a few
-// 2^-24 of act(g), under the rounding to T of what they enter.
+// 2^-24 of act(g), under the rounding to T of what they enter.  The normal
+// distribution function of gelu is formula 7.1.26 of Abramowitz and Stegun,
+// Handbook of Mathematical Functions (1964): erf within 1.5e-7, on the
+// exponential that the derivative needs as well.  (erfcf of the library took half of the backward pass's
+// first kernel.)
 __device__ __forceinline__ float sigmoid(float g) {
     return __builtin_amdgcn_rcpf(1.f + __expf(-g));
 }
@@ -180,9 +184,16 @@ __device__ __forceinline__ void act_and_slope(int act, float g, float &f, float 
         f = g > 0.f || g != g ? g : 0.f;
         df = g > 0.f ? 1.f : 0.f;
     } else if (act == NM_ACT_GELU) {
-        const float p = 0.5f * erfcf(-0.70710678118654752f * g);
+        const float x = __builtin_fabsf(0.70710678118654752f * g), e = __expf(-x * x);
+        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.f));
+        float q = __builtin_fmaf(1.061405429f, t, -1.453152027f);
+        q = __builtin_fmaf(q, t, 1.421413741f);
+        q = __builtin_fmaf(q, t, -0.284496736f);
+        q = __builtin_fmaf(q, t, 0.254829592f);
+        const float tail = 0.5f * q * t * e;          // of the side that g is on
+        const float p = g > 0.f ? 1.f - tail : tail;
         f = g * p;
-        df = __builtin_fmaf(0.39894228040143268f * g, __expf(-0.5f * g * g), p);
+        df = __builtin_fmaf(0.39894228040143268f * g, e, p);
     } else {   // NM_ACT_GELU_TANH: tanh(v) = 2 sigmoid(2 v) - 1
         const float in = 0.79788456080286536f * __builtin_fmaf(0.044715f * g * g, g, g);
         const float p = sigmoid(2.f * in);   // (1 + tanh) / 2

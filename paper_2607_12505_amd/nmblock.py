@@ -149,6 +149,9 @@ class NmNorm(ctypes.Structure):
                 ("bias", ctypes.c_void_p)]
 
 
+_NO_NORM = NmNorm()
+
+
 class NmNormArgs(ctypes.Structure):
     _fields_ = [("y", ctypes.c_void_p), ("r", ctypes.c_void_p), ("ldy", ctypes.c_int64), ("ldr", ctypes.c_int64),
                 ("type", ctypes.c_int32), ("m", ctypes.c_int32), ("d", ctypes.c_int32), ("groups", ctypes.c_int32),
@@ -215,26 +218,23 @@ def _around(y, r, pre, post, gate, alpha, res, stream, rt):
     if like is None:
         raise ValueError("y and r: at least one is needed")
     dev = _index(like, name, rt)
-    a = NmNormArgs()
-    a.type = _type_of(like, name, rt)
+    code = _type_of(like, name, rt)
+    yp = rp = None
+    ldy = ldr = 0
     if y is not None:
-        m, d, a.ldy = _rows(y, "y")
-        a.y = y.data_ptr()
+        m, d, ldy = _rows(y, "y")
+        yp = y.data_ptr()
     if r is not None:
-        mr, dr, a.ldr = _rows(r, "r")
+        mr, dr, ldr = _rows(r, "r")
         if y is not None and (mr != m or dr != d or r.dtype != y.dtype):
             raise ValueError(f"r: {r.dtype} [{mr} x {dr}], expected {y.dtype} [{m} x {d}]")
         _on(r, "r", dev)
-        a.r, m, d = r.data_ptr(), mr, dr
-    a.m, a.d, a.groups, a.alpha = m, d, _gate(gate, m, d, dev, rt), alpha
-    if gate is not None:
-        a.gate = gate.data_ptr()
-    if post is not None:
-        a.post = post._for(d, dev, "post")
-    if pre is not None:
-        a.pre = pre._for(d, dev, "pre")
+        rp, m, d = r.data_ptr(), mr, dr
+    groups, gp = (1, None) if gate is None else (_gate(gate, m, d, dev, rt), gate.data_ptr())
     res = _output(res, "res", like.shape, like.dtype, like, stream, rt)
-    a.res = res.data_ptr()
+    a = NmNormArgs(yp, rp, ldy, ldr, code, m, d, groups, gp, alpha,
+                   _NO_NORM if post is None else post._for(d, dev, "post"),
+                   _NO_NORM if pre is None else pre._for(d, dev, "pre"), res.data_ptr())
     return a, like, res, _handle(stream, dev, rt)
 
 
@@ -295,65 +295,44 @@ def norm_residual_backward(dz, dres, y, res, pre: Optional[Norm] = None, post: O
         raise ValueError("y: needed for the gradients of its norm and gate")
     rt = _rt or _runtime()
     dev = _index(like, name, rt)
-    a = NmNormGradArgs()
-    a.type = _type_of(like, name, rt)
+    code = _type_of(like, name, rt)
     m, d, _ = _rows(like, name)
 
     def given(t, what):
+        if t is None:
+            return None, 0
         mt, dt, ld = _rows(t, what)
         if mt != m or dt != d or t.dtype != like.dtype:
             raise ValueError(f"{what}: {t.dtype} [{mt} x {dt}], expected {like.dtype} [{m} x {d}]")
         _on(t, what, dev)
         return t.data_ptr(), ld
 
-    if dz is not None:
-        a.dz, a.lddz = given(dz, "dz")
-    if dres is not None:
-        a.dres, a.lddres = given(dres, "dres")
-    if y is not None:
-        a.y, a.ldy = given(y, "y")
-    if res is not None:
-        a.res, a.ldres = given(res, "res")
-    a.m, a.d, a.groups, a.alpha = m, d, _gate(gate, m, d, dev, rt), alpha
+    (zp, ldz), (sp, lds), (yp, ldy), (rp, ldr) = given(dz, "dz"), given(dres, "dres"), given(y, "y"), given(res, "res")
+    groups, gp = (1, None) if gate is None else (_gate(gate, m, d, dev, rt), gate.data_ptr())
     dr = _empty(like.shape, like.dtype, like, stream, rt)
-    a.dr = dr.data_ptr()
-    dy = dgate = dqw = dqb = dpw = dpb = None
-    if y is not None:
-        dy = _empty(like.shape, like.dtype, like, stream, rt)
-        a.dy = dy.data_ptr()
-    # the parameters' gradients: rows of one buffer (groups for the gate, then the norms' weights and biases)
-    wanted = [pre is not None and pre.weight is not None, pre is not None and pre.bias is not None,
-              post is not None and post.weight is not None, post is not None and post.bias is not None]
-    rows = (a.groups if gate is not None else 0) + sum(wanted)
-    sums = _empty((rows, d), rt.f32, like, stream, rt) if rows else None
-    at = 0
-    if gate is not None:
-        a.gate = gate.data_ptr()
-        dgate = sums[:a.groups] if gate.dim() == 2 else sums[0]
-        a.dgate = dgate.data_ptr()
-        at = a.groups
-    if pre is not None:
-        a.pre = pre._for(d, dev, "pre")
-        if wanted[0]:
-            dqw, at = sums[at], at + 1
-            a.dpre_weight = dqw.data_ptr()
-        if wanted[1]:
-            dqb, at = sums[at], at + 1
-            a.dpre_bias = dqb.data_ptr()
-    if post is not None:
-        a.post = post._for(d, dev, "post")
-        if wanted[2]:
-            dpw, at = sums[at], at + 1
-            a.dpost_weight = dpw.data_ptr()
-        if wanted[3]:
-            dpb = sums[at]
-            a.dpost_bias = dpb.data_ptr()
+    dy = _empty(like.shape, like.dtype, like, stream, rt) if y is not None else None
+    # the parameters' gradients are rows of one buffer: the gate's, then the norms' weights and biases
+    wanted = [t is not None for n in (pre, post) for t in ((n.weight, n.bias) if n is not None else (None, None))]
+    rows = (groups if gate is not None else 0) + sum(wanted)
+    dgate, params, dgp = None, [None] * 4, None
+    if rows:
+        sums = _empty((rows, d), rt.f32, like, stream, rt)
+        each = sums.unbind(0) if gate is None or groups == 1 else sums[groups:].unbind(0)
+        if gate is not None:
+            dgate = sums[:groups] if gate.dim() == 2 else each[0]
+            dgp = dgate.data_ptr()
+        left = iter(each[1:] if gate is not None and groups == 1 else each)
+        params = [next(left) if want else None for want in wanted]
+    a = NmNormGradArgs(yp, rp, zp, sp, ldy, ldr, ldz, lds, code, m, d, groups, gp, alpha,
+                       _NO_NORM if post is None else post._for(d, dev, "post"),
+                       _NO_NORM if pre is None else pre._for(d, dev, "pre"), _ptr(dy), dr.data_ptr(), dgp,
+                       *[_ptr(t) for t in params])
     need = ctypes.c_size_t()
     _check(lib().nm_norm_residual_backward_workspace(m, d, a.groups, ctypes.byref(need)),
            "nm_norm_residual_backward_workspace")
     ws = _empty((need.value,), rt.u8, like, stream, rt) if need.value else None
     _check(rt.norm_grad(ctypes.byref(a), _ptr(ws), need.value, _handle(stream, dev, rt)), "nm_norm_residual_backward")
-    return NormGrads(dy, dr, dgate, dqw, dqb, dpw, dpb)
+    return NormGrads(dy, dr, dgate, *params)
 
 
 # ---------------------------------------------------------------- scaled int8 products

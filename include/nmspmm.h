@@ -454,7 +454,7 @@ nm_status nm_quantize_f16(const uint16_t *x, int64_t count, float inv_scale, int
  * x device [m x k] of `type`, row stride ldx >= k; xq device int8 [m x kp]
  * with kp = k rounded up to a multiple of 16, the padding zero, 16-byte
  * aligned; scale device float32 [m].  m == 0 is a no-op.  Asynchronous on
- * `stream`.  Errors: NM_ERR_SHAPE (m < 0 or >= 2^30, k < 1 or >= 2^30, ldx < k),
+ * `stream`.  Errors: NM_ERR_SHAPE (m < 0 or >= 2^30, k < 1 or >= 2^28, ldx < k),
  * NM_ERR_ARG (NULL or misaligned pointer, unknown type), NM_ERR_HIP. */
 nm_status nm_quantize_rows(const void *x, int64_t ldx, int type, int m, int k, int8_t *xq, float *scale,
                            void *stream);

@@ -105,7 +105,9 @@ struct TransposeArgs {
     int64_t ld, ldt;
     int rows, cols;
 };
-int launch_transpose_codes(int type, const TransposeArgs &a, void *stream);
+// Two such (rows 0: none) and `counters` (or null) set to zero, in one launch.
+int launch_transpose_codes(int type, const TransposeArgs &a, const TransposeArgs &b, int *counters, int count,
+                           void *stream);
 // dst[c] = sum over rows of parts[rows x n] for the channels of interleaved rows.
 int launch_bias_sums(const float *parts, int rows, int n, int n_out, float *gate, float *up, void *stream);
 

@@ -16,11 +16,17 @@ namespace {
 
 // 64 rows x 64 columns of codes a workgroup, turned in LDS.
 template <class T>
-__global__ __launch_bounds__(256) void k_transpose_codes(TransposeArgs a, int col_blocks) {
+__global__ __launch_bounds__(256) void k_transpose_codes(TransposeArgs first, TransposeArgs second, int first_blocks,
+                                                         int *counters, int count) {
     __shared__ __attribute__((aligned(16))) int8_t tile[64 * 80];
     __shared__ float power[64];
     const int t = threadIdx.x;
-    const int r0 = (int)(blockIdx.x / col_blocks) * 64, c0 = (int)(blockIdx.x % col_blocks) * 64;
+    if (counters && blockIdx.x == 0)
+        for (int i = t; i < count; i += 256) counters[i] = 0;
+    const bool is_first = (int)blockIdx.x < first_blocks;
+    const TransposeArgs a = is_first ? first : second;
+    const int block = is_first ? blockIdx.x : blockIdx.x - first_blocks, col_blocks = (a.cols + 63) / 64;
+    const int r0 = block / col_blocks * 64, c0 = block % col_blocks * 64;
     {
         const int row = r0 + t / 4, col = c0 + (t & 3) * 16;
         v4i v = {0, 0, 0, 0};
@@ -75,16 +81,16 @@ int launch_cast(int type, int tile, const BlockArgs &a, int grid, void *stream) 
                                : launch_product<kKindBF16, CastOut<bf16_t>, kCastTiles>(tile, a, grid, stream);
 }
 
-int launch_transpose_codes(int type, const TransposeArgs &a, void *stream) {
-    const int col_blocks = (a.cols + 63) / 64;
-    const int64_t grid = (int64_t)col_blocks * (a.ldt / 64);
-    if (grid > 0x7fffffff) return (int)hipErrorInvalidValue;
+int launch_transpose_codes(int type, const TransposeArgs &a, const TransposeArgs &b, int *counters, int count,
+                           void *stream) {
+    const int64_t na = a.rows ? (a.cols + 63) / 64 * (a.ldt / 64) : 0, nb = b.rows ? (b.cols + 63) / 64 * (b.ldt / 64) : 0;
+    if (na + nb > 0x7fffffff) return (int)hipErrorInvalidValue;
     if (type == NM_TYPE_F16)
-        hipLaunchKernelGGL(k_transpose_codes<half_t>, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream, a,
-                           col_blocks);
+        hipLaunchKernelGGL(k_transpose_codes<half_t>, dim3((unsigned)(na + nb)), dim3(256), 0, (hipStream_t)stream, a, b,
+                           (int)na, counters, count);
     else
-        hipLaunchKernelGGL(k_transpose_codes<bf16_t>, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream, a,
-                           col_blocks);
+        hipLaunchKernelGGL(k_transpose_codes<bf16_t>, dim3((unsigned)(na + nb)), dim3(256), 0, (hipStream_t)stream, a, b,
+                           (int)na, counters, count);
     return (int)hipGetLastError();
 }
 

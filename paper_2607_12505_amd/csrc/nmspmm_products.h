@@ -123,12 +123,14 @@ __device__ __forceinline__ void store_four(const BlockArgs &a, int tok, int ch, 
 // y = T(acc * sx[token] * c[channel] + b[channel]): the int32 sum is exact, three
 // roundings in binary32 and the one to T.
 struct ScaledOut {
+    template <class G>
+    using Early = NoEarly;
     static __device__ bool scaled(const BlockArgs &) { return true; }
     static __device__ const float *first(const BlockArgs &a) { return a.scale; }
     static __device__ const float *second(const BlockArgs &a) { return a.qscale; }
 
     template <class G, class Mul>
-    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at,
+    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at, const NoEarly &,
                                                   const v4i (&acc)[G::FN][G::FM], int8_t *stg, const Mul &multiplier,
                                                   int *) {
         float sx[G::FM];
@@ -226,12 +228,14 @@ struct HalfTile {
 
 // h = T(act(g) * u).
 struct GatedOut {
+    template <class G>
+    using Early = NoEarly;
     static __device__ bool scaled(const BlockArgs &) { return true; }
     static __device__ const float *first(const BlockArgs &a) { return a.scale; }
     static __device__ const float *second(const BlockArgs &a) { return a.qscale; }
 
     template <class G, class Mul>
-    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at,
+    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at, const NoEarly &,
                                                   const v4i (&acc)[G::FN][G::FM], int8_t *stg, const Mul &multiplier,
                                                   int *) {
         using H = HalfTile<G>;
@@ -305,12 +309,37 @@ __device__ __forceinline__ float scale_part(float s) {
 // go to bias_parts in binary32.
 template <class T>
 struct GatedGradOut {
+    // dh of the wave's tokens and channels, in flight during the k-loop
+    template <class G>
+    struct Early {
+        typedef T v4t __attribute__((ext_vector_type(4)));
+        v4t dh[G::FN / 2][G::FM];
+        __device__ __forceinline__ Early(const BlockArgs &a, const TileAt &at) {
+#pragma unroll
+            for (int i = 0; i < G::FN / 2; ++i)
+#pragma unroll
+                for (int j = 0; j < G::FM; ++j) {
+                    const int tok = at.tok + j * 16 + (at.lane & 15), ch = at.ch / 2 + i * 16 + 4 * (at.lane >> 4);
+                    dh[i][j] = {};
+                    if (tok >= a.m) continue;
+                    const T *p = (const T *)a.dh + (int64_t)tok * a.lddh + ch;
+                    if (ch + 4 <= a.n_out) {
+                        dh[i][j] = __builtin_bit_cast(v4t, (v2u)(*(const v2u_any *)p));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (ch + e < a.n_out) dh[i][j][e] = p[e];
+                    }
+                }
+        }
+    };
+
     static __device__ bool scaled(const BlockArgs &) { return true; }
     static __device__ const float *first(const BlockArgs &a) { return a.scale; }
     static __device__ const float *second(const BlockArgs &a) { return a.qscale; }
 
     template <class G, class Mul>
-    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at,
+    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at, const Early<G> &early,
                                                   const v4i (&acc)[G::FN][G::FM], int8_t *stg, const Mul &multiplier,
                                                   int *) {
         constexpr int FN = G::FN, FM = G::FM;
@@ -322,32 +351,18 @@ struct GatedGradOut {
         for (int i = 0; i < FN; i += 2) {
             const v4f cg = multiplier(0, i), cu = multiplier(0, i + 1), zero = {0, 0, 0, 0};
             const v4f bg = a.qscale ? multiplier(1, i) : zero, bu = a.qscale ? multiplier(1, i + 1) : zero;
-            const int ch = at.ch / 2 + i * 8 + 4 * lg;
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
                 const int tok = at.tok + j * 16 + lt;
                 const v4f g = scaled_value(acc[i][j], sx[j], cg, bg), u = scaled_value(acc[i + 1][j], sx[j], cu, bu);
-                float dh[4] = {0, 0, 0, 0};
-                if (tok < a.m) {
-                    const T *p = (const T *)a.dh + (int64_t)tok * a.lddh + ch;
-                    if (ch + 4 <= a.n_out) {
-                        typedef T v4t __attribute__((ext_vector_type(4)));
-                        const v4t t = __builtin_bit_cast(v4t, (v2u)(*(const v2u_any *)p));
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) dh[e] = (float)t[e];
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (ch + e < a.n_out) dh[e] = (float)p[e];
-                    }
-                }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float f, df;
                     act_and_slope(a.act, g[e], f, df);
                     // tokens past the last one have no gradient, whatever their row holds
-                    d[i][j][e] = tok < a.m ? dh[e] * u[e] * df : 0.f;
-                    d[i + 1][j][e] = tok < a.m ? dh[e] * f : 0.f;
+                    const float dh = (float)early.dh[i / 2][j][e];
+                    d[i][j][e] = tok < a.m ? dh * u[e] * df : 0.f;
+                    d[i + 1][j][e] = tok < a.m ? dh * f : 0.f;
                 }
             }
         }
@@ -406,6 +421,8 @@ struct GatedGradOut {
 // meet in the workspace as in the int8 kernels, added in their order.
 template <class T>
 struct CastOut {
+    template <class G>
+    using Early = NoEarly;
     static __device__ bool scaled(const BlockArgs &) { return false; }
     static __device__ const float *first(const BlockArgs &) { return nullptr; }
     static __device__ const float *second(const BlockArgs &) { return nullptr; }
@@ -418,7 +435,7 @@ struct CastOut {
     }
 
     template <class G, class Mul>
-    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at,
+    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at, const NoEarly &,
                                                   const v4f (&acc)[G::FN][G::FM], int8_t *stg, const Mul &,
                                                   int *s_last) {
         if (a.split_k == 1) {

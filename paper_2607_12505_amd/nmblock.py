@@ -115,6 +115,13 @@ def _empty(shape, dtype, like, stream, rt: _Runtime):
         return like.new_empty(shape, dtype=dtype)
 
 
+def _like(t, stream, rt: _Runtime):
+    """Memory of t's shape and type, without gaps."""
+    if stream is None and t.is_contiguous():
+        return rt.torch.empty_like(t)
+    return _empty(t.shape, t.dtype, t, stream, rt)
+
+
 def _output(given, name: str, shape, dtype, like, stream, rt: _Runtime):
     if given is None:
         return _empty(shape, dtype, like, stream, rt)
@@ -231,7 +238,7 @@ def _around(y, r, pre, post, gate, alpha, res, stream, rt):
         _on(r, "r", dev)
         rp, m, d = r.data_ptr(), mr, dr
     groups, gp = (1, None) if gate is None else (_gate(gate, m, d, dev, rt), gate.data_ptr())
-    res = _output(res, "res", like.shape, like.dtype, like, stream, rt)
+    res = _like(like, stream, rt) if res is None else _output(res, "res", like.shape, like.dtype, like, stream, rt)
     a = NmNormArgs(yp, rp, ldy, ldr, code, m, d, groups, gp, alpha,
                    _NO_NORM if post is None else post._for(d, dev, "post"),
                    _NO_NORM if pre is None else pre._for(d, dev, "pre"), res.data_ptr())
@@ -247,7 +254,7 @@ def norm_residual(y, r, pre: Optional[Norm] = None, post: Optional[Norm] = None,
     rt = _rt or _runtime()
     a, like, res, at = _around(y, r, pre, post, gate, alpha, res, stream, rt)
     if pre is not None:
-        z = _output(z, "z", res.shape, like.dtype, like, stream, rt)
+        z = _like(res, stream, rt) if z is None else _output(z, "z", res.shape, like.dtype, like, stream, rt)
         a.z = z.data_ptr()
     elif z is not None:
         raise ValueError("z: given without a norm for it")
@@ -309,8 +316,8 @@ def norm_residual_backward(dz, dres, y, res, pre: Optional[Norm] = None, post: O
 
     (zp, ldz), (sp, lds), (yp, ldy), (rp, ldr) = given(dz, "dz"), given(dres, "dres"), given(y, "y"), given(res, "res")
     groups, gp = (1, None) if gate is None else (_gate(gate, m, d, dev, rt), gate.data_ptr())
-    dr = _empty(like.shape, like.dtype, like, stream, rt)
-    dy = _empty(like.shape, like.dtype, like, stream, rt) if y is not None else None
+    dr = _like(like, stream, rt)
+    dy = _like(like, stream, rt) if y is not None else None
     # the parameters' gradients are rows of one buffer: the gate's, then the norms' weights and biases
     wanted = [t is not None for n in (pre, post) for t in ((n.weight, n.bias) if n is not None else (None, None))]
     rows = (groups if gate is not None else 0) + sum(wanted)

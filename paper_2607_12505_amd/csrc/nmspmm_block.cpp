@@ -222,7 +222,8 @@ void fill_product(BlockArgs &a, int m, const nm_scaled_weight &w) {
 }
 
 int place_tiles(BlockArgs &a, int tile) {
-    const int tn = kTiles[tile].tile_n(), tm = kTiles[tile].tile_m();
+    const int tn = tile == kRowTile ? kRowTileN : kTiles[tile].tile_n();
+    const int tm = tile == kRowTile ? kRowTileM : kTiles[tile].tile_m();
     a.tiles_n = (a.n + tn - 1) / tn;
     a.tiles_m = (a.m + tm - 1) / tm;
     a.group_rows = group_rows_for(a.tiles_m, tm);
@@ -233,6 +234,18 @@ int place_tiles(BlockArgs &a, int tile) {
 // What the estimate of a GEMM's time is given as output: the bytes written for each weight row.
 int out_mode_for(int type, bool gated) {
     return gated ? (type == NM_TYPE_F32 ? NM_OUT_F16 : NM_OUT_I8) : type == NM_TYPE_F32 ? NM_OUT_I32 : NM_OUT_F16;
+}
+
+// The tile of a product.  Dense gated blocks with many tiles and a short reduction
+// take the tile of which two share a compute unit: one's epilogue (an exponential a
+// value) runs beside the other's products.  Of 27 random gated shapes with 0.5 to 20
+// tiles a unit, those within the rule took 0.79 to 1.02 of the time of the estimate's
+// tile (0.88 on average; 18464 x 1024 -> 2736: 127 us against 144), those outside
+// 0.90 to 1.39; 33 plain products 0.81 to 1.29, 1.08 on average.
+int product_tile(int kind, bool gated, int m, int n, int k, int out_mode) {
+    const int64_t tiles = (int64_t)((n + kRowTileN - 1) / kRowTileN) * ((m + kRowTileM - 1) / kRowTileM);
+    if (gated && kind == NM_KIND_DENSE && k <= 1536 && 2 * tiles >= 5 * device_cu_count()) return kRowTile;
+    return schedule_among(kind, m, n, k, out_mode, kScaledTiles);
 }
 
 struct Product {
@@ -301,7 +314,7 @@ nm_status run_product(const Product &p, char *ws, void *stream) {
         a.type = p.type;
         a.act = p.act;
         a.stream_out = aligned(p.out, 128) ? stream_out_for(m, (int)(p.ldo < (1 << 30) ? p.ldo : 1), d.k) : 0;
-        const int tile = schedule_among(kind, m, d.n, d.k, out_mode_for(p.type, p.gated), kScaledTiles);
+        const int tile = product_tile(kind, p.gated, m, d.n, d.k, out_mode_for(p.type, p.gated));
         const int grid = place_tiles(a, tile);
         const int err = p.gated ? launch_gated(kind, tile, a, grid, stream) : launch_scaled(kind, tile, a, grid, stream);
         if (err != 0) return NM_ERR_HIP;

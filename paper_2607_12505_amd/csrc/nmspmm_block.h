@@ -89,6 +89,8 @@ constexpr uint32_t kCastTiles = 1u << 1 | 1u << 3 | 1u << 6 | 1u << 12 | 1u << 4
 // Up to kFewTokens tokens take the streaming kernel; few_takes_values: also as values.
 constexpr int kFewTokens = 64;
 bool few_takes_values(int m, int k);
+// The tile of nmspmm_rows.h, numbered after kTiles.
+constexpr int kRowTile = kNumSchedules, kRowTileN = 256, kRowTileM = 160;
 int launch_few(int kind, bool gated, const BlockArgs &a, void *stream);
 int launch_scaled(int kind, int tile, const BlockArgs &a, int grid, void *stream);
 int launch_gated(int kind, int tile, const BlockArgs &a, int grid, void *stream);

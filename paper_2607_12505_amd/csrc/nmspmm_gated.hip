@@ -1,11 +1,26 @@
 // The gated feed-forward block: both products, the activation and their
 // product in one kernel.
 #include "nmspmm_products.h"
+#include "nmspmm_rows.h"
 
 namespace nmspmm {
+namespace {
+
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) void k_gated_rows(BlockArgs a) {
+    using G = RowGeometry<4, 2, 4, 5>;
+    static_assert(G::BN == kRowTileN && G::BM == kRowTileM, "row tile");
+    __shared__ __attribute__((aligned(1024))) int8_t lds[G::LDSB];
+    __shared__ int s_last;
+    gemm_rows<NM_KIND_DENSE, 4, 2, 4, 5, GatedOut>(a, lds, &s_last);
+}
+
+}  // namespace
 
 int launch_gated(int kind, int tile, const BlockArgs &a, int grid, void *stream) {
-    return launch_kinds<GatedOut, kScaledTiles>(kind, tile, a, grid, stream);
+    if (tile != kRowTile) return launch_kinds<GatedOut, kScaledTiles>(kind, tile, a, grid, stream);
+    if (kind != NM_KIND_DENSE) return (int)hipErrorInvalidValue;
+    hipLaunchKernelGGL(k_gated_rows, dim3(grid), dim3(512), 0, (hipStream_t)stream, a);
+    return (int)hipGetLastError();
 }
 
 }  // namespace nmspmm

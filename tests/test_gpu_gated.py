@@ -49,7 +49,9 @@ def test_patterns(N, M, m):
     bu.close(nb.gated_ffn(x, w, out_dtype=torch.float32), want, torch.float32, mag, 4)
 
 
-@pytest.mark.parametrize("N,M,m,k,n", [(8, 8, 18464, 1024, 320), (2, 4, 9000, 256, 1024), (2, 8, 20000, 512, 512)])
+# the 8-wave tiles, the tile of which two share a compute unit (with and without a short last k-step), sparse weights
+@pytest.mark.parametrize("N,M,m,k,n", [(8, 8, 18464, 1024, 320), (8, 8, 8011, 1040, 1603), (8, 8, 20000, 64, 900),
+                                       (8, 8, 30000, 17, 700), (2, 4, 9000, 256, 1024), (2, 8, 20000, 512, 512)])
 def test_large_shapes_by_sampled_rows(N, M, m, k, n):
     x, w, plain, g = case(m, k, n, torch.half, False, N, M)
     h = nb.gated_ffn(x, w)

@@ -370,21 +370,22 @@ nm_status product_of_rows(const void *x, int64_t ldx, int xtype, int m, const nm
 // ---------------------------------------------------------------- gated backward
 
 // A product of 16-bit operands, [m x n] outputs over k_bytes of each row: the
-// tile and split of the reduction with the least estimated time (us), linear in
-// nine terms and fitted per tile (non-negative least squares on relative errors,
-// near-best rows weighted most) to timings of every (tile, split) on 113 shapes, m
-// 64..20000, n to 4096, 128..20000 values of k.  Fitted to 76 of them, the choice on
-// the other 44 draws took 5.6 % longer than the best on average, one in ten 21 % or more.
+// tile and split of the reduction with the least estimated time (us).  The estimate
+// is linear in ten terms, among them rounds of one workgroup and of as many as a
+// unit holds, fitted per tile (non-negative least squares on relative errors, near-best
+// rows weighted most) to timings of every (tile, split) on 191 shapes, m 64..20000, n to
+// 4096, 128..20000 values of k.  Fitted to 108 of them, its choice on the other 83 took 1.7 %
+// longer than the best on average, for one in ten 3.7 % or more, 39 % at most.
 struct CastCost {
-    int tile;
-    float launch, chain, round_steps, mean_steps, rounds, out_mb, x_mb, split, part_mb;
+    int tile, per_cu;
+    float launch, chain, round_steps, mean_steps, full_steps, rounds, out_mb, x_mb, split, part_mb;
 };
 constexpr CastCost kCastCost[] = {
-    {1, 2.65f, 0.326f, 0.00136f, 0.229f, 0.781f, 0.0f, 0.0f, 5.47f, 0.829f},
-    {3, 2.53f, 0.225f, 0.0574f, 0.083f, 0.523f, 0.0f, 0.026f, 3.04f, 1.29f},
-    {4, 0.0f, 0.0f, 1.09f, 0.316f, 7.18f, 0.0624f, 0.00749f, 14.0f, 0.363f},
-    {6, 1.54f, 0.324f, 0.086f, 0.247f, 2.25f, 0.0f, 0.0024f, 5.75f, 0.634f},
-    {12, 0.339f, 0.0f, 0.802f, 0.207f, 5.86f, 0.0f, 0.011f, 10.1f, 0.378f},
+    {1, 3, 2.8f, 0.117f, 0.0f, 0.21f, 0.217f, 0.639f, 0.0f, 0.0f, 4.94f, 0.942f},
+    {3, 5, 2.68f, 0.147f, 0.0f, 0.141f, 0.118f, 0.412f, 0.0f, 0.0f, 2.78f, 1.45f},
+    {4, 1, 1.84f, 0.0f, 0.0f, 0.429f, 1.03f, 5.61f, 0.0427f, 0.00878f, 15.6f, 0.367f},
+    {6, 2, 1.88f, 0.0405f, 0.0f, 0.258f, 0.395f, 1.66f, 0.0f, 0.000901f, 5.12f, 0.67f},
+    {12, 1, 0.92f, 0.0f, 0.812f, 0.189f, 0.0f, 4.91f, 0.043f, 0.00755f, 11.2f, 0.38f},
 };
 struct CastPlan {
     int tile = 0, split = 1;
@@ -400,7 +401,9 @@ struct CastPlan {
                 if (s > 1 && (k_steps / s < 4 || tiles > kMaxSplitTiles || s * m * n * 4 >= ((int64_t)1 << 31))) break;
                 const float steps = (float)k_steps / (float)s, mean = (float)(tiles * s) / (float)cus;
                 const float rounds = (float)((tiles * s + cus - 1) / cus);
-                float us = c.launch + steps * (c.chain + c.round_steps * rounds + c.mean_steps * mean) +
+                const float full = (float)((tiles * s + c.per_cu * cus - 1) / (c.per_cu * cus));
+                float us = c.launch +
+                           steps * (c.chain + c.round_steps * rounds + c.mean_steps * mean + c.full_steps * full) +
                            c.rounds * rounds + c.out_mb * out_mb + c.x_mb * x_mb;
                 if (s > 1) us += c.split + c.part_mb * 2.f * (float)s * out_mb;
                 if (tile == 0 || us < least) {

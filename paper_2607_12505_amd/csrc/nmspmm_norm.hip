@@ -246,6 +246,8 @@ __global__ __launch_bounds__(team_threads(WPR)) void k_norm_residual(NormArgs a)
 template <int VEC, int CH, int LANES>
 struct SharedParam {
     static constexpr int SIZE = LANES * CH * VEC;
+    // how many of the three fit beside the rest: past 8192 channels post's bias is read from memory
+    static constexpr int FIT = 3 * SIZE * 4 <= 128 * 1024 ? 3 : 2;
     float *at0;
     __device__ void fill(const float *src, float absent, int d) const {
         for (int ch = threadIdx.x; ch < SIZE; ch += blockDim.x) {
@@ -313,7 +315,7 @@ __global__ __launch_bounds__(team_threads(WPR)) __attribute__((amdgpu_waves_per_
     lds_wq.fill(a.pre.weight, 1.f, a.d);
     if constexpr (POST) {
         lds_wp.fill(a.post.weight, 1.f, a.d);
-        lds_bp.fill(a.post.bias, 0.f, a.d);
+        if constexpr (Shared::FIT == 3) lds_bp.fill(a.post.bias, 0.f, a.d);
     }
     __syncthreads();
     float s_wq[CH][VEC] = {}, s_bq[CH][VEC] = {}, s_g[CH][VEC] = {}, s_wp[CH][VEC] = {}, s_bp[CH][VEC] = {};
@@ -407,7 +409,10 @@ __global__ __launch_bounds__(team_threads(WPR)) __attribute__((amdgpu_waves_per_
         float st = 0.f, sth = 0.f, wp[CH][VEC], bp[CH][VEC];
         if constexpr (POST) {
             lds_wp.get(wp, lane);
-            lds_bp.get(bp, lane);
+            if constexpr (Shared::FIT == 3)
+                lds_bp.get(bp, lane);
+            else
+                load_param(bp, a.post.bias, 0.f, a.d, at, step);
         }
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
@@ -598,7 +603,8 @@ int norm_by_width(const NormArgs &a, void *stream) {
 
 template <class T, int VEC, int CH, int WPR, bool POST>
 int grad_one(const NormGradArgs &a, int workgroups, void *stream) {
-    constexpr int teams = team_threads(WPR) / 64 / WPR, params = SharedParam<VEC, CH, 64 * WPR>::SIZE * (POST ? 3 : 1);
+    using Shared = SharedParam<VEC, CH, 64 * WPR>;
+    constexpr int teams = team_threads(WPR) / 64 / WPR, params = Shared::SIZE * (POST ? Shared::FIT : 1);
     const int sums = (teams - 1) * a.d;      // once the parameters are no longer needed
     hipLaunchKernelGGL((k_norm_residual_backward<T, VEC, CH, WPR, POST>), dim3(workgroups), dim3(team_threads(WPR)),
                        (params > sums ? params : sums) * 4, (hipStream_t)stream, a);

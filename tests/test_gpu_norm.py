@@ -168,6 +168,18 @@ def test_backward(T, d):
     assert (got.dpost_weight is None) == (post is None)
 
 
+@pytest.mark.parametrize("d", [8193, 8200, 12000, 16383, 16384])
+def test_backward_of_the_longest_rows(d):
+    g = gen(d)
+    m, T = 6, torch.bfloat16
+    pre, p64 = norm_of(g, d, "layer")
+    post, q64 = norm_of(g, d, "layer")
+    y, res, dz, dres = (rows(g, m, d, T) for _ in range(4))
+    gate = torch.randn(2, d, generator=g).cuda()
+    got = nb.norm_residual_backward(dz, dres, y, res, pre=pre, post=post, gate=gate)
+    check_grads(got, bu.norm_grads(dz, dres, y, res, p64, q64, gate, 1.0), T, m)
+
+
 # groups that end inside a run of rows, runs that end inside a group, one token a group, many runs a group
 @pytest.mark.parametrize("m,d,groups", [(1, 8, 1), (6, 40, 6), (4096, 24, 2), (6000, 40, 1500), (5000, 72, 5000),
                                         (9000, 136, 90), (2500, 600, 5), (1030, 2056, 103), (7000, 512, 7)])

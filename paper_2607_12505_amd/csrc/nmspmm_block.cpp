@@ -222,8 +222,7 @@ void fill_product(BlockArgs &a, int m, const nm_scaled_weight &w) {
 }
 
 int place_tiles(BlockArgs &a, int tile) {
-    const int tn = tile == kRowTile ? kRowTileN : kTiles[tile].tile_n();
-    const int tm = tile == kRowTile ? kRowTileM : kTiles[tile].tile_m();
+    const int tn = tile_n_of(tile), tm = tile_m_of(tile);
     a.tiles_n = (a.n + tn - 1) / tn;
     a.tiles_m = (a.m + tm - 1) / tm;
     a.group_rows = group_rows_for(a.tiles_m, tm);
@@ -243,7 +242,8 @@ int out_mode_for(int type, bool gated) {
 // tile (0.88 on average; 18464 x 1024 -> 2736: 127 us against 144), those outside
 // 0.90 to 1.39; 33 plain products 0.81 to 1.29, 1.08 on average.
 int product_tile(int kind, bool gated, int m, int n, int k, int out_mode) {
-    const int64_t tiles = (int64_t)((n + kRowTileN - 1) / kRowTileN) * ((m + kRowTileM - 1) / kRowTileM);
+    const int tn = tile_n_of(kRowTile), tm = tile_m_of(kRowTile);
+    const int64_t tiles = (int64_t)((n + tn - 1) / tn) * ((m + tm - 1) / tm);
     if (gated && kind == NM_KIND_DENSE && k <= 1536 && 2 * tiles >= 5 * device_cu_count()) return kRowTile;
     return schedule_among(kind, m, n, k, out_mode, kScaledTiles);
 }
@@ -387,49 +387,54 @@ constexpr CastCost kCastCost[] = {
     {6, 2, 1.88f, 0.0405f, 0.0f, 0.258f, 0.395f, 1.66f, 0.0f, 0.000901f, 5.12f, 0.67f},
     {12, 1, 0.92f, 0.0f, 0.812f, 0.189f, 0.0f, 4.91f, 0.043f, 0.00755f, 11.2f, 0.38f},
 };
-struct CastPlan {
-    int tile = 0, split = 1;
-    int64_t m, n;
-    CastPlan(int64_t m_, int64_t n_, int64_t k_bytes) : m(m_), n(n_) {
-        const int64_t k_steps = k_bytes / kKStep, cus = device_cu_count();
-        const float out_mb = (float)(m * n) * 2e-6f, x_mb = (float)(m * k_bytes) * 1e-6f;
-        float least = 0.f;
-        for (const CastCost &c : kCastCost) {
-            const TileCfg &t = kTiles[c.tile];
-            const int64_t tiles = ((m + t.tile_m() - 1) / t.tile_m()) * ((n + t.tile_n() - 1) / t.tile_n());
-            for (int s = 1; s <= 8; s *= 2) {
-                if (s > 1 && (k_steps / s < 4 || tiles > kMaxSplitTiles || s * m * n * 4 >= ((int64_t)1 << 31))) break;
-                const float steps = (float)k_steps / (float)s, mean = (float)(tiles * s) / (float)cus;
-                const float rounds = (float)((tiles * s + cus - 1) / cus);
-                const float full = (float)((tiles * s + c.per_cu * cus - 1) / (c.per_cu * cus));
-                float us = c.launch +
-                           steps * (c.chain + c.round_steps * rounds + c.mean_steps * mean + c.full_steps * full) +
-                           c.rounds * rounds + c.out_mb * out_mb + c.x_mb * x_mb;
-                if (s > 1) us += c.split + c.part_mb * 2.f * (float)s * out_mb;
-                if (tile == 0 || us < least) {
-                    least = us;
-                    tile = c.tile;
-                    split = s;
-                }
-            }
+// The best split of a product on one tile, and its estimate.
+struct CastChoice {
+    int split = 1;
+    float us = 0.f;
+};
+CastChoice cast_choice(const CastCost &c, int64_t m, int64_t n, int64_t k_bytes) {
+    const int64_t k_steps = k_bytes / kKStep, cus = device_cu_count();
+    const float out_mb = (float)(m * n) * 2e-6f, x_mb = (float)(m * k_bytes) * 1e-6f;
+    const TileCfg &t = kTiles[c.tile];
+    const int64_t tiles = ((m + t.tile_m() - 1) / t.tile_m()) * ((n + t.tile_n() - 1) / t.tile_n());
+    CastChoice best;
+    for (int s = 1; s <= 8; s *= 2) {
+        if (s > 1 && (k_steps / s < 4 || tiles > kMaxSplitTiles || s * m * n * 4 >= ((int64_t)1 << 31))) break;
+        const float steps = (float)k_steps / (float)s, mean = (float)(tiles * s) / (float)cus;
+        const float rounds = (float)((tiles * s + cus - 1) / cus);
+        const float full = (float)((tiles * s + c.per_cu * cus - 1) / (c.per_cu * cus));
+        float us = c.launch + steps * (c.chain + c.round_steps * rounds + c.mean_steps * mean + c.full_steps * full) +
+                   c.rounds * rounds + c.out_mb * out_mb + c.x_mb * x_mb;
+        if (s > 1) us += c.split + c.part_mb * 2.f * (float)s * out_mb;
+        if (s == 1 || us < best.us) {
+            best.us = us;
+            best.split = s;
         }
     }
-    int64_t split_bytes() const { return split > 1 ? (int64_t)kCounterBytes + split * m * n * 4 : 0; }
-};
-
+    return best;
+}
 // Pieces of the workspace, in their order.
 struct GradPlan {
     int64_t rows_w, cols, ldt;     // 2 n', k rounded up to 16, tokens rounded up to 64
-    CastPlan dx, dw;
-    int grad_tile, parts_rows;
-    size_t at_da, at_dat, at_xt, at_wt, at_parts, at_split, bytes;
+    int grad_tile, parts_rows, cast_tile = 0, dx_split = 1, dw_split = 1;
+    size_t at_da, at_dat, at_xt, at_wt, at_parts, at_dx_split, at_dw_split, bytes;
 
     GradPlan(const nm_scaled_weight &w, int m)
-        : rows_w(w.desc->n), cols(w.desc->k), ldt((int64_t)(m + 63) / 64 * 64), dx(m, cols, 2 * rows_w),
-          dw(rows_w, cols, 2 * ldt) {
+        : rows_w(w.desc->n), cols(w.desc->k), ldt((int64_t)(m + 63) / 64 * 64) {
         grad_tile = schedule_among(NM_KIND_DENSE, m, w.desc->n, w.desc->k, NM_OUT_I32, kGradTiles);
         const TileCfg &g = kTiles[grad_tile];
         parts_rows = (m + g.tile_m() - 1) / g.tile_m() * g.wm;
+        // dx and the weights' gradients run in one launch, on the tile that is best for both
+        float least = 0.f;
+        for (const CastCost &c : kCastCost) {
+            const CastChoice dx = cast_choice(c, m, cols, 2 * rows_w), dw = cast_choice(c, rows_w, cols, 2 * ldt);
+            if (cast_tile == 0 || dx.us + dw.us < least) {
+                least = dx.us + dw.us;
+                cast_tile = c.tile;
+                dx_split = dx.split;
+                dw_split = dw.split;
+            }
+        }
         size_t at = 0;
         auto take = [&](int64_t n) {
             const size_t here = at;
@@ -441,9 +446,9 @@ struct GradPlan {
         at_xt = take(cols * ldt * 2);
         at_wt = take(cols * rows_w * 2);
         at_parts = take((int64_t)parts_rows * rows_w * 4);
-        // the two products' partial sums, one after the other; the counters at
-        // its start are left at zero by the first
-        at_split = take(dx.split_bytes() > dw.split_bytes() ? dx.split_bytes() : dw.split_bytes());
+        // (split products: counters, then partial sums; the two counter blocks lie one after the other)
+        at_dx_split = take(2 * kCounterBytes + (dx_split > 1 ? dx_split * (int64_t)m * cols * 4 : 0));
+        at_dw_split = take(dw_split > 1 ? dw_split * rows_w * cols * 4 : 0);
         bytes = at;
     }
 };
@@ -545,37 +550,28 @@ extern "C" nm_status nm_gated_backward(const nm_gated_grad_args *args, const nm_
     if (a.bias_parts && launch_bias_sums(a.bias_parts, p.parts_rows, d.n, w->n, g.dbias_gate, g.dbias_up, stream) != 0)
         return NM_ERR_HIP;
 
-    BlockArgs c;
-    fill_product(c, g.m, *w);
-    c.scale = nullptr;
-    c.qscale = nullptr;
-    c.meta = nullptr;
-    c.n = d.k;
-    c.n_out = w->k;
-    c.ldo = w->k;
-    c.n_frags = (d.k + kFragRows - 1) / kFragRows;
-    int *counters = nullptr;
-    if (p.dx.split > 1 || p.dw.split > 1) {
-        c.counters = counters = (int32_t *)(base + p.at_split);
-        c.partials = (int32_t *)(base + p.at_split + kCounterBytes);
-    }
+    if (!g.dx && !g.dw_gate) return NM_OK;
     const TransposeArgs wt = {w->vals, w->scale, base + p.at_wt, d.k, p.rows_w, g.dx ? d.n : 0, d.k};
     const TransposeArgs xt = {g.xq, g.sx, base + p.at_xt, d.k, p.ldt, g.dw_gate ? g.m : 0, d.k};
-    if ((g.dx || g.dw_gate) &&
-        launch_transpose_codes(g.type, wt, xt, counters, (int)(kCounterBytes / 4), stream) != 0)
+    int *counters = (int *)(base + p.at_dx_split);
+    if (launch_transpose_codes(g.type, wt, xt, p.dx_split > 1 || p.dw_split > 1 ? counters : nullptr,
+                               (int)(2 * kCounterBytes / 4), stream) != 0)
         return NM_ERR_HIP;
-    if (g.dx) {
-        c.X = (const int8_t *)(base + p.at_da);
-        c.A = (const int8_t *)(base + p.at_wt);
-        c.k = (int)(2 * p.rows_w);
-        c.k_steps = c.k / kKStep;
-        c.out = g.dx;
-        c.stream_out = aligned(g.dx, 128) ? stream_out_for(g.m, w->k, c.k) : 0;
-        c.split_k = p.dx.split;
-        grid = place_tiles(c, p.dx.tile);
-        if (launch_cast(g.type, p.dx.tile, c, grid, stream) != 0) return NM_ERR_HIP;
+    CastPair pair;
+    for (BlockArgs &c : pair.part) {
+        fill_product(c, g.m, *w);
+        c.scale = nullptr;
+        c.qscale = nullptr;
+        c.meta = nullptr;
+        c.n = d.k;
+        c.n_out = w->k;
+        c.ldo = w->k;
+        c.n_frags = (d.k + kFragRows - 1) / kFragRows;
+        c.gemm_grid = 0;
     }
+    // the weights' gradients first: their reductions are the longer ones where the device is hard to fill
     if (g.dw_gate) {
+        BlockArgs &c = pair.part[0];
         c.X = (const int8_t *)(base + p.at_dat);
         c.A = (const int8_t *)(base + p.at_xt);
         c.m = d.n;
@@ -584,10 +580,25 @@ extern "C" nm_status nm_gated_backward(const nm_gated_grad_args *args, const nm_
         c.out = g.dw_gate;
         c.out2 = g.dw_up;
         c.interleaved = w->n;
-        c.split_k = p.dw.split;
+        c.split_k = p.dw_split;
+        c.counters = counters + kCounterBytes / 4;
+        c.partials = (int32_t *)(base + p.at_dw_split);
         c.stream_out = 0;
-        grid = place_tiles(c, p.dw.tile);
-        if (launch_cast(g.type, p.dw.tile, c, grid, stream) != 0) return NM_ERR_HIP;
+        place_tiles(c, p.cast_tile);
     }
+    if (g.dx) {
+        BlockArgs &c = pair.part[1];
+        c.X = (const int8_t *)(base + p.at_da);
+        c.A = (const int8_t *)(base + p.at_wt);
+        c.k = (int)(2 * p.rows_w);
+        c.k_steps = c.k / kKStep;
+        c.out = g.dx;
+        c.split_k = p.dx_split;
+        c.counters = counters;
+        c.partials = (int32_t *)(base + p.at_dx_split + 2 * kCounterBytes);
+        c.stream_out = aligned(g.dx, 128) ? stream_out_for(g.m, w->k, c.k) : 0;
+        place_tiles(c, p.cast_tile);
+    }
+    if (launch_cast(g.type, p.cast_tile, pair, stream) != 0) return NM_ERR_HIP;
     return NM_OK;
 }

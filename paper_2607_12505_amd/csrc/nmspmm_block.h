@@ -90,13 +90,25 @@ constexpr uint32_t kCastTiles = 1u << 1 | 1u << 3 | 1u << 6 | 1u << 12 | 1u << 4
 constexpr int kFewTokens = 64;
 bool few_takes_values(int m, int k);
 // The tile of nmspmm_rows.h, numbered after kTiles.
-constexpr int kRowTile = kNumSchedules, kRowTileN = 256, kRowTileM = 160;
+struct RowTile {
+    int wn, wm, fn, fm;
+    constexpr int tile_n() const { return wn * fn * kFragRows; }
+    constexpr int tile_m() const { return wm * fm * 16; }
+};
+constexpr int kRowTile = kNumSchedules;
+constexpr RowTile kRowTileShape = {4, 2, 4, 5};
+constexpr int tile_n_of(int tile) { return tile == kRowTile ? kRowTileShape.tile_n() : kTiles[tile].tile_n(); }
+constexpr int tile_m_of(int tile) { return tile == kRowTile ? kRowTileShape.tile_m() : kTiles[tile].tile_m(); }
 int launch_few(int kind, bool gated, const BlockArgs &a, void *stream);
 int launch_scaled(int kind, int tile, const BlockArgs &a, int grid, void *stream);
 int launch_gated(int kind, int tile, const BlockArgs &a, int grid, void *stream);
 int launch_gated_grad(int tile, const BlockArgs &a, int grid, void *stream);
-// C = A B^T of 16-bit rows (a.k counts bytes), to `type`.
-int launch_cast(int type, int tile, const BlockArgs &a, int grid, void *stream);
+// C = A B^T of 16-bit rows (a.k counts bytes), to `type`: one or two of them on the same tile in one launch (their
+// gemm_grid: workgroups, 0 for none).
+struct CastPair {
+    BlockArgs part[2];
+};
+int launch_cast(int type, int tile, const CastPair &a, void *stream);
 
 // Codes [rows x ld] with a scale each -> their transpose [cols x ldt] in 16 bits, each code times the power of two
 // of its row's scale (exact); zeros from `rows` to ldt.

@@ -7,11 +7,11 @@ namespace nmspmm {
 namespace {
 
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) void k_gated_rows(BlockArgs a) {
-    using G = RowGeometry<4, 2, 4, 5>;
-    static_assert(G::BN == kRowTileN && G::BM == kRowTileM, "row tile");
+    constexpr RowTile t = kRowTileShape;
+    using G = RowGeometry<t.wn, t.wm, t.fn, t.fm>;
     __shared__ __attribute__((aligned(1024))) int8_t lds[G::LDSB];
     __shared__ int s_last;
-    gemm_rows<NM_KIND_DENSE, 4, 2, 4, 5, GatedOut>(a, lds, &s_last);
+    gemm_rows<NM_KIND_DENSE, t.wn, t.wm, t.fn, t.fm, GatedOut>(a, lds, &s_last);
 }
 
 }  // namespace

@@ -47,6 +47,21 @@ __global__ __launch_bounds__(256) void k_transpose_codes(TransposeArgs first, Tr
     }
 }
 
+// Two products of 16-bit operands in one launch, workgroups [0, gemm_grid) and
+// [first, first + gemm_grid): neither alone fills the device evenly.
+template <int KIND, int WN, int WM, int FN, int FM, int NST, class EPI>
+__global__ __launch_bounds__(64 * WN * WM)
+__attribute__((amdgpu_waves_per_eu(Geometry<KIND, WN, WM, FN, FM, NST>::WAVES))) void k_cast_pair(CastPair p, int first) {
+    using G = Geometry<KIND, WN, WM, FN, FM, NST>;
+    __shared__ __attribute__((aligned(1024))) int8_t lds[G::LDSB + G::MULB];
+    __shared__ uint2 lut[Kind<KIND>::LUT];
+    __shared__ int s_last;
+    const int which = (int)blockIdx.x >= first, block = (int)blockIdx.x - (which ? first : 0);
+    const BlockArgs &a = p.part[which];
+    if (block >= a.gemm_grid) return;
+    gemm_tile<KIND, WN, WM, FN, FM, NST, EPI>(a, block, a.gemm_grid, lds, lut, &s_last);
+}
+
 __global__ __launch_bounds__(1024) void k_bias_sums(const float *parts, int rows, int n, int n_out, float *gate,
                                                     float *up) {
     __shared__ float part[16][64];
@@ -76,9 +91,31 @@ int launch_gated_grad(int tile, const BlockArgs &a, int grid, void *stream) {
                : launch_product<NM_KIND_DENSE, GatedGradOut<bf16_t>, kGradTiles>(tile, a, grid, stream);
 }
 
-int launch_cast(int type, int tile, const BlockArgs &a, int grid, void *stream) {
-    return type == NM_TYPE_F16 ? launch_product<kKindF16, CastOut<half_t>, kCastTiles>(tile, a, grid, stream)
-                               : launch_product<kKindBF16, CastOut<bf16_t>, kCastTiles>(tile, a, grid, stream);
+namespace {
+
+template <int KIND, class EPI, int T = 0>
+int launch_pair(int tile, const CastPair &p, int first, int grid, void *stream) {
+    if constexpr (T < kNumSchedules) {
+        if constexpr ((kCastTiles >> T) & 1)
+            if (tile == T) {
+                constexpr TileCfg t = kTiles[T];
+                hipLaunchKernelGGL((k_cast_pair<KIND, t.wn, t.wm, t.fn, t.fm, t.nst, EPI>), dim3(grid),
+                                   dim3(64 * t.wn * t.wm), 0, (hipStream_t)stream, p, first);
+                return (int)hipGetLastError();
+            }
+        return launch_pair<KIND, EPI, T + 1>(tile, p, first, grid, stream);
+    }
+    return (int)hipErrorInvalidValue;
+}
+
+}  // namespace
+
+int launch_cast(int type, int tile, const CastPair &p, void *stream) {
+    // the second product begins at a multiple of 8, so that its workgroups' order over the XCDs is its own
+    const int64_t first = ((int64_t)p.part[0].gemm_grid + 7) / 8 * 8, grid = first + p.part[1].gemm_grid;
+    if (grid > 0x7fffffff) return (int)hipErrorInvalidValue;
+    return type == NM_TYPE_F16 ? launch_pair<kKindF16, CastOut<half_t>>(tile, p, (int)first, (int)grid, stream)
+                               : launch_pair<kKindBF16, CastOut<bf16_t>>(tile, p, (int)first, (int)grid, stream);
 }
 
 int launch_transpose_codes(int type, const TransposeArgs &a, const TransposeArgs &b, int *counters, int count,

@@ -479,8 +479,8 @@ __device__ inline bool arrive_last(const GemmArgs &a, int tile, int *s_flag) {
     return *s_flag != 0;
 }
 
-// One workgroup's output tile: what EPI::Early loads ahead, the k-loop, then
-// EPI::finish with the wave's accumulators.  EPI also names two float arrays of the channels (multipliers,
+// One workgroup's output tile (workgroup `block` of the product's `blocks`): the
+// k-loop, then EPI::finish with the wave's accumulators.  EPI also names two float arrays of the channels (multipliers,
 // or null) whose slices of the tile come to LDS with the loads, and whether
 // they are wanted at all.
 struct TileAt {
@@ -490,14 +490,8 @@ struct TileAt {
     int lane;
 };
 
-// Nothing to load ahead.
-struct NoEarly {
-    template <class ARGS>
-    __device__ __forceinline__ NoEarly(const ARGS &, const TileAt &) {}
-};
-
 template <int KIND, int WN, int WM, int FN, int FM, int NST, class EPI, class ARGS>
-__device__ __forceinline__ void gemm_tile(const ARGS &a, int8_t *lds, uint2 *lut, int *s_last) {
+__device__ __forceinline__ void gemm_tile(const ARGS &a, int block, int blocks, int8_t *lds, uint2 *lut, int *s_last) {
     using G = Geometry<KIND, WN, WM, FN, FM, NST>;
     using K = Kind<KIND>;
     using Acc = typename K::Acc;
@@ -505,7 +499,7 @@ __device__ __forceinline__ void gemm_tile(const ARGS &a, int8_t *lds, uint2 *lut
     constexpr bool kDense = kind_is_rows(KIND);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t *)lds;
 
-    const int lid = map_block(blockIdx.x, (int)gridDim.x < a.gemm_grid ? (int)gridDim.x : a.gemm_grid);
+    const int lid = map_block(block, blocks);
     int tn, rest;
     tile_order(lid, a.tiles_n, a.tiles_m * a.split_k, a.group_rows, &tn, &rest);
     const int split = rest % a.split_k;
@@ -642,9 +636,6 @@ __device__ __forceinline__ void gemm_tile(const ARGS &a, int8_t *lds, uint2 *lut
             expand_dense<KIND>(o.r, lut, lo, hi);
         }
     };
-
-    const TileAt at = {tok0 + wm * FM * 16, ch0 + wn * FN * 16, split, tm, tn, lane};
-    const typename EPI::template Early<G> early(a, at);
 
     // The tile's multipliers, loaded so early that the epilogue does not start with
     // a load's latency: with the ring, or into a slot that the last k-step leaves free.
@@ -800,7 +791,8 @@ __device__ __forceinline__ void gemm_tile(const ARGS &a, int8_t *lds, uint2 *lut
         else
             return mreg[h][i];
     };
-    EPI::template finish<G>(a, at, early, acc, lds + wave * G::STG, multiplier, s_last);
+    EPI::template finish<G>(a, TileAt{tok0 + wm * FM * 16, ch0 + wn * FN * 16, split, tm, tn, lane}, acc,
+                            lds + wave * G::STG, multiplier, s_last);
 }
 
 // k_gemm_ks, mask layouts: expands lane `lane`'s part of a compact block and

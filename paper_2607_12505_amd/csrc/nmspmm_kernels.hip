@@ -212,15 +212,12 @@ __device__ __forceinline__ void store_chunk(const GemmArgs &a, __amdgpu_buffer_r
 
 // int32, fp16(fp32(y) * scale) and/or int8 codes q8(fp32(y) * qscale), whichever are wanted.
 struct PlainOut {
-    template <class G>
-    using Early = NoEarly;
     static __device__ bool scaled(const GemmArgs &a) { return a.split_k == 1 && (a.Yh || a.Yq); }
     static __device__ const float *first(const GemmArgs &a) { return a.Yh ? a.scale : nullptr; }
     static __device__ const float *second(const GemmArgs &a) { return a.Yq ? a.qscale : nullptr; }
 
     template <class G, class Mul>
-    static __device__ __forceinline__ void finish(const GemmArgs &a, const TileAt &at, const NoEarly &,
-                                                  const v4i (&acc)[G::FN][G::FM],
+    static __device__ __forceinline__ void finish(const GemmArgs &a, const TileAt &at, const v4i (&acc)[G::FN][G::FM],
                                                   int8_t *stg, const Mul &multiplier, int *s_last) {
         constexpr int FM = G::FM;
         const int lane = at.lane, tokw = at.tok, chw = at.ch;   // the wave's part of the tile
@@ -315,7 +312,8 @@ __attribute__((amdgpu_waves_per_eu(Geometry<KIND, WN, WM, FN, FM, NST>::WAVES)))
         expand_tail(a, (uint2 *)lds);
         return;
     }
-    gemm_tile<KIND, WN, WM, FN, FM, NST, PlainOut>(a, lds, lut, &s_last);
+    gemm_tile<KIND, WN, WM, FN, FM, NST, PlainOut>(
+        a, blockIdx.x, (int)gridDim.x < a.gemm_grid ? (int)gridDim.x : a.gemm_grid, lds, lut, &s_last);
 }
 
 template <int KIND, int FN, int FM, int NST>

@@ -123,14 +123,12 @@ __device__ __forceinline__ void store_four(const BlockArgs &a, int tok, int ch, 
 // y = T(acc * sx[token] * c[channel] + b[channel]): the int32 sum is exact, three
 // roundings in binary32 and the one to T.
 struct ScaledOut {
-    template <class G>
-    using Early = NoEarly;
     static __device__ bool scaled(const BlockArgs &) { return true; }
     static __device__ const float *first(const BlockArgs &a) { return a.scale; }
     static __device__ const float *second(const BlockArgs &a) { return a.qscale; }
 
     template <class G, class Mul>
-    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at, const NoEarly &,
+    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at,
                                                   const v4i (&acc)[G::FN][G::FM], int8_t *stg, const Mul &multiplier,
                                                   int *) {
         float sx[G::FM];
@@ -226,16 +224,23 @@ struct HalfTile {
     static_assert(G::FN % 2 == 0 && stage_bytes(2) <= G::STG && stage_bytes(4) <= G::STG, "gated tile");
 };
 
+// Two fragments of a wave's channels.
+template <class G>
+struct PairTile {
+    static constexpr int FN = 2, FM = G::FM;
+    static constexpr int stage_rows(int eb) { return 16 * FN * eb >= 64 ? 16 : 1024 / (16 * FN * eb); }
+    static constexpr int stage_bytes(int eb) { return stage_rows(eb) * (FN * 16 * eb + 16); }
+    static_assert(G::FN % 2 == 0 && stage_bytes(2) <= G::STG, "gated tile");
+};
+
 // h = T(act(g) * u).
 struct GatedOut {
-    template <class G>
-    using Early = NoEarly;
     static __device__ bool scaled(const BlockArgs &) { return true; }
     static __device__ const float *first(const BlockArgs &a) { return a.scale; }
     static __device__ const float *second(const BlockArgs &a) { return a.qscale; }
 
     template <class G, class Mul>
-    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at, const NoEarly &,
+    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at,
                                                   const v4i (&acc)[G::FN][G::FM], int8_t *stg, const Mul &multiplier,
                                                   int *) {
         using H = HalfTile<G>;
@@ -302,6 +307,25 @@ __device__ __forceinline__ float scale_part(float s) {
     return b < 0x00800000u || b >= 0x7F800000u ? 1.f : __builtin_bit_cast(float, (b & 0x007FFFFFu) | 0x3F800000u);
 }
 
+// Four values of dh from channel ch of a token; zero past the last token and channel.
+template <class T>
+__device__ __forceinline__ void load_four(const BlockArgs &a, int tok, int ch, float (&f)[4]) {
+    typedef T v4t __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = 0.f;
+    if (tok >= a.m) return;
+    const T *p = (const T *)a.dh + (int64_t)tok * a.lddh + ch;
+    if (ch + 4 <= a.n_out) {
+        const v4t t = __builtin_bit_cast(v4t, (v2u)(*(const v2u_any *)p));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = (float)t[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (ch + e < a.n_out) f[e] = (float)p[e];
+    }
+}
+
 // From the recomputed g and u and dh:  dg = dh u act'(g), du = dh act(g), written
 // for the two products that follow, with the part of the scale that their 16-bit
 // codes leave out: by rows for dx (times the channel's), transposed for the
@@ -309,110 +333,86 @@ __device__ __forceinline__ float scale_part(float s) {
 // go to bias_parts in binary32.
 template <class T>
 struct GatedGradOut {
-    // dh of the wave's tokens and channels, in flight during the k-loop
-    template <class G>
-    struct Early {
-        typedef T v4t __attribute__((ext_vector_type(4)));
-        v4t dh[G::FN / 2][G::FM];
-        __device__ __forceinline__ Early(const BlockArgs &a, const TileAt &at) {
-#pragma unroll
-            for (int i = 0; i < G::FN / 2; ++i)
-#pragma unroll
-                for (int j = 0; j < G::FM; ++j) {
-                    const int tok = at.tok + j * 16 + (at.lane & 15), ch = at.ch / 2 + i * 16 + 4 * (at.lane >> 4);
-                    dh[i][j] = {};
-                    if (tok >= a.m) continue;
-                    const T *p = (const T *)a.dh + (int64_t)tok * a.lddh + ch;
-                    if (ch + 4 <= a.n_out) {
-                        dh[i][j] = __builtin_bit_cast(v4t, (v2u)(*(const v2u_any *)p));
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (ch + e < a.n_out) dh[i][j][e] = p[e];
-                    }
-                }
-        }
-    };
-
     static __device__ bool scaled(const BlockArgs &) { return true; }
     static __device__ const float *first(const BlockArgs &a) { return a.scale; }
     static __device__ const float *second(const BlockArgs &a) { return a.qscale; }
 
     template <class G, class Mul>
-    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at, const Early<G> &early,
+    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at,
                                                   const v4i (&acc)[G::FN][G::FM], int8_t *stg, const Mul &multiplier,
                                                   int *) {
-        constexpr int FN = G::FN, FM = G::FM;
+        // one pair of fragments (the same channels of both projections) at a time: 2 FM
+        // fragments of gradients beside the accumulators still to come
+        using P = PairTile<G>;
+        constexpr int FM = G::FM;
         const int lane = at.lane, lg = lane >> 4, lt = lane & 15;
         float sx[FM];
         load_row_scales<G>(a, at, sx);
-        v4f d[FN][FM];
+        float *parts = a.bias_parts ? a.bias_parts + (int64_t)(at.tok / (FM * 16)) * a.n : nullptr;
 #pragma unroll
-        for (int i = 0; i < FN; i += 2) {
-            const v4f cg = multiplier(0, i), cu = multiplier(0, i + 1), zero = {0, 0, 0, 0};
+        for (int i = 0; i < G::FN; i += 2) {
+            const v4f zero = {0, 0, 0, 0}, c[2] = {multiplier(0, i), multiplier(0, i + 1)};
             const v4f bg = a.qscale ? multiplier(1, i) : zero, bu = a.qscale ? multiplier(1, i + 1) : zero;
+            v4f d[2][FM];
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
                 const int tok = at.tok + j * 16 + lt;
-                const v4f g = scaled_value(acc[i][j], sx[j], cg, bg), u = scaled_value(acc[i + 1][j], sx[j], cu, bu);
+                const v4f g = scaled_value(acc[i][j], sx[j], c[0], bg), u = scaled_value(acc[i + 1][j], sx[j], c[1], bu);
+                float dh[4];
+                load_four<T>(a, tok, at.ch / 2 + i * 8 + 4 * lg, dh);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float f, df;
                     act_and_slope(a.act, g[e], f, df);
                     // tokens past the last one have no gradient, whatever their row holds
-                    const float dh = (float)early.dh[i / 2][j][e];
-                    d[i][j][e] = tok < a.m ? dh * u[e] * df : 0.f;
-                    d[i + 1][j][e] = tok < a.m ? dh * f : 0.f;
+                    d[0][j][e] = tok < a.m ? dh[e] * u[e] * df : 0.f;
+                    d[1][j][e] = tok < a.m ? dh[e] * f : 0.f;
                 }
             }
-        }
-        store_tile<G, T>(
-            stg, lane, d, at.ch, a.n, false,
-            [&](int i, int, const v4f &v) {
-                const v4f c = multiplier(0, i);
-                return v4f{v[0] * scale_part(c[0]), v[1] * scale_part(c[1]), v[2] * scale_part(c[2]),
-                           v[3] * scale_part(c[3])};
-            },
-            [&](int row, T *) -> T * {
-                return at.tok + row < a.m ? (T *)a.da + (int64_t)(at.tok + row) * a.n : nullptr;
-            });
-        // transposed: 16 channels x FM * 16 tokens at a time through the staging area
-        constexpr int TROW = FM * 16 * 2 + 16;       // bytes of a staged channel, padded
-        constexpr int CPR = FM * 2;                  // 16-byte pieces of it
-        static_assert(16 * TROW <= G::STG, "transposed staging");
+            const int ch0 = at.ch + i * 16;
+            store_tile<P, T>(
+                stg, lane, d, ch0, a.n, false,
+                [&](int p, int, const v4f &v) {
+                    return v4f{v[0] * scale_part(c[p][0]), v[1] * scale_part(c[p][1]), v[2] * scale_part(c[p][2]),
+                               v[3] * scale_part(c[p][3])};
+                },
+                [&](int row, T *) -> T * {
+                    return at.tok + row < a.m ? (T *)a.da + (int64_t)(at.tok + row) * a.n : nullptr;
+                });
+            // transposed: 16 channels x FM * 16 tokens at a time through the staging area
+            constexpr int TROW = FM * 16 * 2 + 16;       // bytes of a staged channel, padded
+            constexpr int CPR = FM * 2;                  // 16-byte pieces of it
+            static_assert(16 * TROW <= G::STG, "transposed staging");
 #pragma unroll
-        for (int i = 0; i < FN; ++i) {
+            for (int p = 0; p < 2; ++p) {
 #pragma unroll
-            for (int j = 0; j < FM; ++j) {
-                const float part = scale_part(sx[j]);
+                for (int j = 0; j < FM; ++j) {
+                    const float part = scale_part(sx[j]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    *(T *)(stg + (4 * lg + e) * TROW + (j * 16 + lt) * 2) = (T)(d[i][j][e] * part);
+                    for (int e = 0; e < 4; ++e)
+                        *(T *)(stg + (4 * lg + e) * TROW + (j * 16 + lt) * 2) = (T)(d[p][j][e] * part);
+                }
+                for (int q = lane; q < 16 * CPR; q += 64) {
+                    const int row = q / CPR, tok = at.tok + (q % CPR) * 8, ch = ch0 + p * 16 + row;
+                    const v4i v = *(const v4i *)(stg + row * TROW + (q % CPR) * 16);
+                    if (ch < a.n && tok < a.ldt) *(v4i *)((T *)a.dat + (int64_t)ch * a.ldt + tok) = v;
+                }
+                if (!parts) continue;
+                v4f s = d[p][0];
+#pragma unroll
+                for (int j = 1; j < FM; ++j) s += d[p][j];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float x = s[e];
+                    x += dpp<0xB1>(0.f, x);
+                    x += dpp<0x4E>(0.f, x);
+                    x += dpp<0x141>(0.f, x);
+                    x += dpp<0x140>(0.f, x);
+                    s[e] = x;
+                }
+                const int ch = ch0 + p * 16 + 4 * lg;
+                if (lt == 0 && ch < a.n) *(v4f *)(parts + ch) = s;
             }
-            for (int c = lane; c < 16 * CPR; c += 64) {
-                const int row = c / CPR, tok = at.tok + (c % CPR) * 8, ch = at.ch + i * 16 + row;
-                const v4i v = *(const v4i *)(stg + row * TROW + (c % CPR) * 16);
-                if (ch < a.n && tok < a.ldt) *(v4i *)((T *)a.dat + (int64_t)ch * a.ldt + tok) = v;
-            }
-        }
-        if (!a.bias_parts) return;
-        float *parts = a.bias_parts + (int64_t)(at.tok / (FM * 16)) * a.n;
-#pragma unroll
-        for (int i = 0; i < FN; ++i) {
-            v4f s = d[i][0];
-#pragma unroll
-            for (int j = 1; j < FM; ++j) s += d[i][j];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float x = s[e];
-                x += dpp<0xB1>(0.f, x);
-                x += dpp<0x4E>(0.f, x);
-                x += dpp<0x141>(0.f, x);
-                x += dpp<0x140>(0.f, x);
-                s[e] = x;
-            }
-            const int ch = at.ch + i * 16 + 4 * lg;
-            if (lt == 0 && ch < a.n) *(v4f *)(parts + ch) = s;
         }
     }
 };
@@ -421,8 +421,6 @@ struct GatedGradOut {
 // meet in the workspace as in the int8 kernels, added in their order.
 template <class T>
 struct CastOut {
-    template <class G>
-    using Early = NoEarly;
     static __device__ bool scaled(const BlockArgs &) { return false; }
     static __device__ const float *first(const BlockArgs &) { return nullptr; }
     static __device__ const float *second(const BlockArgs &) { return nullptr; }
@@ -435,7 +433,7 @@ struct CastOut {
     }
 
     template <class G, class Mul>
-    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at, const NoEarly &,
+    static __device__ __forceinline__ void finish(const BlockArgs &a, const TileAt &at,
                                                   const v4f (&acc)[G::FN][G::FM], int8_t *stg, const Mul &,
                                                   int *s_last) {
         if (a.split_k == 1) {
@@ -484,7 +482,7 @@ __attribute__((amdgpu_waves_per_eu(Geometry<KIND, WN, WM, FN, FM, NST>::WAVES)))
     __shared__ __attribute__((aligned(1024))) int8_t lds[G::LDSB + G::MULB];
     __shared__ uint2 lut[Kind<KIND>::LUT];
     __shared__ int s_last;
-    gemm_tile<KIND, WN, WM, FN, FM, NST, EPI>(a, lds, lut, &s_last);
+    gemm_tile<KIND, WN, WM, FN, FM, NST, EPI>(a, blockIdx.x, gridDim.x, lds, lut, &s_last);
 }
 
 template <int KIND, int FN, int FM, int NST, class EPI>

@@ -96,8 +96,6 @@ __device__ __forceinline__ void gemm_rows(const ARGS &a, int8_t *lds, int *s_las
         wait_then_barrier<63>();
     };
 
-    const TileAt at = {tok0 + wm * FM * 16, ch0 + wn * FN * 16, split, tm, tn, lane};
-    const typename EPI::template Early<G> early(a, at);
     Acc acc[FN][FM];
 #pragma unroll
     for (int i = 0; i < FN; ++i)
@@ -142,7 +140,8 @@ __device__ __forceinline__ void gemm_rows(const ARGS &a, int8_t *lds, int *s_las
         const int ch = c0 + i * 16;
         return *(const v4f *)((h ? second : first) + (ch < a.n ? ch : 0));
     };
-    EPI::template finish<G>(a, at, early, acc, lds + wave * G::STG, multiplier, s_last);
+    EPI::template finish<G>(a, TileAt{tok0 + wm * FM * 16, ch0 + wn * FN * 16, split, tm, tn, lane}, acc,
+                            lds + wave * G::STG, multiplier, s_last);
 }
 
 }  // namespace

@@ -310,7 +310,7 @@ __global__ __launch_bounds__(team_threads(WPR)) __attribute__((amdgpu_waves_per_
     constexpr bool has_p = POST;
     const int bytes = a.d * (int)sizeof(T);
 
-    float gate[CH][VEC];
+    float gate[CH][VEC] = {};      // of a team without rows too: its zeros must stay zeros
     const Shared lds_wq{joined}, lds_wp{joined + Shared::SIZE}, lds_bp{joined + 2 * Shared::SIZE};
     lds_wq.fill(a.pre.weight, 1.f, a.d);
     if constexpr (POST) {

@@ -196,6 +196,24 @@ def test_backward_of_shared_gates(T, m, d, groups):
     assert all(torch.equal(a, b) for a, b in zip(got, again) if a is not None)      # the same bits every time
 
 
+@pytest.mark.parametrize("m,d", [(75, 1024), (1, 600), (18463, 1024), (1537, 1000), (771, 72)])
+def test_teams_without_rows_add_nothing(m, d):
+    # the last workgroup holds teams past the last token; what an earlier kernel left in registers must not
+    # enter the sums, so one that leaves NaN there runs first
+    g = gen(m)
+    T = torch.bfloat16
+    pre, p64 = norm_of(g, d, "layer")
+    post, q64 = norm_of(g, d, "layer")
+    y, res, dz, dres = (rows(g, m, d, T) for _ in range(4))
+    gate = torch.randn(d, generator=g).cuda()
+    odd = torch.full((4096, d), float("nan"), dtype=T, device="cuda")
+    nan_gate = torch.full((d,), float("nan"), device="cuda")
+    want = bu.norm_grads(dz, dres, y, res, p64, q64, gate, 1.0)
+    for _ in range(3):
+        nb.norm_residual_backward(odd, odd, odd, odd, pre=pre, post=post, gate=nan_gate)
+        check_grads(nb.norm_residual_backward(dz, dres, y, res, pre=pre, post=post, gate=gate), want, T, m)
+
+
 @pytest.mark.parametrize("T", [torch.bfloat16])
 def test_backward_of_parts(T):
     g = gen(77)

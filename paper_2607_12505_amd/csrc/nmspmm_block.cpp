@@ -245,7 +245,7 @@ int product_tile(int kind, bool gated, int m, int n, int k, int out_mode) {
     const int tn = tile_n_of(kRowTile), tm = tile_m_of(kRowTile);
     const int64_t tiles = (int64_t)((n + tn - 1) / tn) * ((m + tm - 1) / tm);
     if (gated && kind == NM_KIND_DENSE && k <= 1536 && 2 * tiles >= 5 * device_cu_count()) return kRowTile;
-    return schedule_among(kind, m, n, k, out_mode, kScaledTiles);
+    return schedule_among(kind, m, n, k, out_mode, scaled_tiles(kind));
 }
 
 struct Product {

@@ -17,7 +17,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) void k
 }  // namespace
 
 int launch_gated(int kind, int tile, const BlockArgs &a, int grid, void *stream) {
-    if (tile != kRowTile) return launch_kinds<GatedOut, kScaledTiles>(kind, tile, a, grid, stream);
+    if (tile != kRowTile) return launch_kinds<GatedOut>(kind, tile, a, grid, stream);
     if (kind != NM_KIND_DENSE) return (int)hipErrorInvalidValue;
     hipLaunchKernelGGL(k_gated_rows, dim3(grid), dim3(512), 0, (hipStream_t)stream, a);
     return (int)hipGetLastError();

@@ -513,17 +513,17 @@ int launch_product(int tile, const BlockArgs &a, int grid, void *stream) {
     return (int)hipErrorInvalidValue;
 }
 
-template <class EPI, uint32_t TILES>
+template <class EPI>
 int launch_kinds(int kind, int tile, const BlockArgs &a, int grid, void *stream) {
     switch (kind) {
-        case NM_KIND_SP42: return launch_product<NM_KIND_SP42, EPI, TILES>(tile, a, grid, stream);
-        case NM_KIND_C14: return launch_product<NM_KIND_C14, EPI, TILES>(tile, a, grid, stream);
-        case NM_KIND_DENSE: return launch_product<NM_KIND_DENSE, EPI, TILES>(tile, a, grid, stream);
-        case NM_KIND_C18: return launch_product<NM_KIND_C18, EPI, TILES>(tile, a, grid, stream);
-        case NM_KIND_C28: return launch_product<NM_KIND_C28, EPI, TILES>(tile, a, grid, stream);
-        case NM_KIND_MK3: return launch_product<NM_KIND_MK3, EPI, TILES>(tile, a, grid, stream);
-        case NM_KIND_MK4: return launch_product<NM_KIND_MK4, EPI, TILES>(tile, a, grid, stream);
-        case NM_KIND_MK5: return launch_product<NM_KIND_MK5, EPI, TILES>(tile, a, grid, stream);
+        case NM_KIND_SP42: return launch_product<NM_KIND_SP42, EPI, scaled_tiles(NM_KIND_SP42)>(tile, a, grid, stream);
+        case NM_KIND_C14: return launch_product<NM_KIND_C14, EPI, scaled_tiles(NM_KIND_C14)>(tile, a, grid, stream);
+        case NM_KIND_DENSE: return launch_product<NM_KIND_DENSE, EPI, scaled_tiles(NM_KIND_DENSE)>(tile, a, grid, stream);
+        case NM_KIND_C18: return launch_product<NM_KIND_C18, EPI, scaled_tiles(NM_KIND_C18)>(tile, a, grid, stream);
+        case NM_KIND_C28: return launch_product<NM_KIND_C28, EPI, scaled_tiles(NM_KIND_C28)>(tile, a, grid, stream);
+        case NM_KIND_MK3: return launch_product<NM_KIND_MK3, EPI, scaled_tiles(NM_KIND_MK3)>(tile, a, grid, stream);
+        case NM_KIND_MK4: return launch_product<NM_KIND_MK4, EPI, scaled_tiles(NM_KIND_MK4)>(tile, a, grid, stream);
+        case NM_KIND_MK5: return launch_product<NM_KIND_MK5, EPI, scaled_tiles(NM_KIND_MK5)>(tile, a, grid, stream);
     }
     return (int)hipErrorInvalidValue;
 }

@@ -4,7 +4,7 @@
 namespace nmspmm {
 
 int launch_scaled(int kind, int tile, const BlockArgs &a, int grid, void *stream) {
-    return launch_kinds<ScaledOut, kScaledTiles>(kind, tile, a, grid, stream);
+    return launch_kinds<ScaledOut>(kind, tile, a, grid, stream);
 }
 
 }  // namespace nmspmm

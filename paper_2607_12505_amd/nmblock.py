@@ -492,6 +492,9 @@ def _product_out(out, m: int, shape, dtype, like, stream, rt):
     return out, _type_of(out, "out", rt), _rows(out, "out")[2]
 
 
+_FEW = 16      # most tokens of a call that makes its codes in the product's own launch
+
+
 def _of_rows(x, w: ScaledWeight, out, out_dtype, stream, gated: bool):
     rt = _rt or _runtime()
     dev = _index(x, "x", rt)
@@ -504,18 +507,15 @@ def _of_rows(x, w: ScaledWeight, out, out_dtype, stream, gated: bool):
     shape = (m, w.n) if x.dim() == 2 else (*x.shape[:-1], w.n)
     out, otype, ldo = _product_out(out, m, shape, out_dtype or x.dtype, x, stream, rt)
     at = _handle(stream, dev, rt)
-    # a few tokens need no workspace: it is allocated when the library asks for it
-    ws, need = None, 0
-    while True:
-        wp = None if ws is None else ws.data_ptr()
-        if gated:
-            st = rt.gated(x.data_ptr(), ld, xtype, m, w._ref, w._act, out.data_ptr(), ldo, otype, wp, need, at)
-        else:
-            st = rt.linear(x.data_ptr(), ld, xtype, m, w._ref, out.data_ptr(), ldo, otype, wp, need, at)
-        if st != NM_ERR_WORKSPACE or ws is not None:
-            break
+    act = (w._act,) if gated else ()
+    call, args = rt.gated if gated else rt.linear, (x.data_ptr(), ld, xtype, m, w._ref, *act, out.data_ptr(), ldo, otype)
+    st = NM_ERR_WORKSPACE
+    if m <= _FEW:       # needs no workspace where the kernel makes the codes itself
+        st = call(*args, None, 0, at)
+    if st == NM_ERR_WORKSPACE:
         need = w._need(m, xtype)
         ws = _empty((need,), rt.u8, x, stream, rt)
+        st = call(*args, ws.data_ptr(), need, at)
     if st != NM_OK:
         raise NmError(st, "nm_gated" if gated else "nm_linear_i8")
     return out

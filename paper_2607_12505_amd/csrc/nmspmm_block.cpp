@@ -237,10 +237,10 @@ int out_mode_for(int type, bool gated) {
 
 // The tile of a product.  Dense gated blocks with many tiles and a short reduction
 // take the tile of which two share a compute unit: one's epilogue (an exponential a
-// value) runs beside the other's products.  Of 27 random gated shapes with 0.5 to 20
-// tiles a unit, those within the rule took 0.79 to 1.02 of the time of the estimate's
-// tile (0.88 on average; 18464 x 1024 -> 2736: 127 us against 144), those outside
-// 0.90 to 1.39; 33 plain products 0.81 to 1.29, 1.08 on average.
+// value) runs beside the other's products.  Of 28 random gated shapes with 0.5 to 20
+// tiles a unit, the 11 within the rule took 0.77 to 1.02 of the time of the estimate's
+// tile (0.87 on average; 18464 x 1024 -> 2736: 125 us against 144), those outside 0.91 to
+// 1.35; 32 plain products 0.83 to 1.29, 1.07 on average.
 int product_tile(int kind, bool gated, int m, int n, int k, int out_mode) {
     const int tn = tile_n_of(kRowTile), tm = tile_m_of(kRowTile);
     const int64_t tiles = (int64_t)((n + tn - 1) / tn) * ((m + tm - 1) / tm);

@@ -53,9 +53,10 @@ __device__ __forceinline__ void gemm_rows(const ARGS &a, int8_t *lds, int *s_las
     const int t_tail = ragged && s_end == all ? nsteps - 1 : -1;
 
     // --- loads.  Instruction q of a k-step: 16 rows, lane L row L / 4 and, at
-    // place L % 4, the row's chunk (L % 4) ^ ((row / 4) % 4): the 16 rows of an
-    // operand read lie in distinct banks.  Rows past the end read the last one.
-    const int place = ((lane & 3) ^ ((lane >> 4) & 3)) * 16;
+    // place L % 4, the row's chunk (L % 4) ^ ((row / 2) % 4): eight consecutive rows
+    // of an operand read lie in distinct banks (by row / 4 half of the LDS cycles were
+    // conflicts).  Rows past the end read the last one.
+    const int place = ((lane & 3) ^ ((lane >> 3) & 3)) * 16;
     uint32_t off[G::ND];
 #pragma unroll
     for (int c = 0; c < G::ND; ++c) {
@@ -102,7 +103,7 @@ __device__ __forceinline__ void gemm_rows(const ARGS &a, int8_t *lds, int *s_las
 #pragma unroll
         for (int j = 0; j < FM; ++j) acc[i][j] = Acc{0, 0, 0, 0};
 
-    const int sw = (lg ^ ((lane >> 2) & 3)) << 4;                        // the lane's chunk of its row
+    const int sw = (lg ^ ((lane >> 1) & 3)) << 4;                        // the lane's chunk of its row
     const int8_t *xrow = lds + (wm * FM * 16 + (lane & 15)) * 64 + sw;
     const int8_t *wrow = lds + G::XC * 1024 + (wn * FN * 16 + (lane & 15)) * 64 + sw;
 

@@ -193,10 +193,25 @@ nm_status check_weight(const nm_scaled_weight *w, bool gated) {
     return NM_OK;
 }
 
+// Whether codes of m tokens take the kernel of few tokens.  It repeats the codes for every
+// 16 channels, so it loses where they outweigh its start: of times in us against the tiles',
+// dense weights, 1024 -> 4096 with 1 token 2.7 to 3.4, with 16 3.0 to 3.4, with 32 3.5 to 3.5, with
+// 64 4.6 to 4.5; 4096 -> 1024 with 1 4.5 to 5.3, with 16 5.7 to 5.4, with 32 7.6 to 5.5; 4096 -> 4096 with 1
+// 5.9 to 6.2, with 16 6.9 to 6.3; 4096 -> 11008 with 1 10.8 to 9.8, with 16 13.8 to 9.9.  Weights of
+// 3:8 to 5:8 cost the tiles more, which expand a block for every token tile: 4096 -> 11008 at 4:8
+// with 1 7.7 to 10.7, with 16 10.7 to 10.4; 4096 -> 1024 with 32 5.9 to 6.7.
+bool takes_few(int kind, int64_t m, int64_t n, int64_t k) {
+    const bool masks = layout_mask_values(kind) > 0;
+    if (m <= 16) return masks || n * k <= (1 << 24);
+    return m <= kFewTokens && n * k <= (masks ? 1 << 24 : 1 << 22) && (masks || k <= 1024);
+}
+
 // Whether a compact weight is expanded once for the call, and the bytes of that.
 int64_t expansion(const nm_desc &d, int m) {
     nm_plan plan;
-    if (m <= kFewTokens || !kind_is_compact(d.kind) || make_plan(d.kind, m, d.n, d.k, NM_OUT_F16, &plan) != NM_OK) return 0;
+    if (takes_few(d.kind, m, d.n, d.k) || !kind_is_compact(d.kind) ||
+        make_plan(d.kind, m, d.n, d.k, NM_OUT_F16, &plan) != NM_OK)
+        return 0;
     return plan.expand ? plan.expand_bytes : 0;
 }
 
@@ -274,7 +289,7 @@ nm_status run_product(const Product &p, char *ws, void *stream) {
     int kind = d.kind;
     const int8_t *vals = p.w->vals;
     const uint8_t *meta = p.w->meta;
-    if (p.m <= kFewTokens) {
+    if (p.x || takes_few(kind, p.m, d.n, d.k)) {
         BlockArgs a;
         fill_product(a, p.m, *p.w);
         a.X = p.xq;

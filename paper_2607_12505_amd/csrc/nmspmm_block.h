@@ -89,8 +89,8 @@ constexpr uint32_t scaled_tiles(int kind) {
 constexpr uint32_t kGradTiles = 1u << 1 | 1u << 3 | 1u << 6;   // whole 64-token groups: the transposed rows' padding is written too
 constexpr uint32_t kCastTiles = 1u << 1 | 1u << 3 | 1u << 6 | 1u << 12 | 1u << 4;
 
-// Up to kFewTokens tokens take the streaming kernel; few_takes_values: also as values.
-constexpr int kFewTokens = 64;
+// The kernel of few tokens: the most that it is built for, and whether it takes them as values.
+constexpr int kFewTokens = 32;
 bool few_takes_values(int m, int k);
 // The tile of nmspmm_rows.h, numbered after kTiles.
 struct RowTile {

@@ -255,8 +255,7 @@ template <int KIND, int FN>
 int few_shape(const BlockArgs &a, void *stream) {
     if (a.x) return few_one<KIND, FN, 1, false>(a, stream);
     if (a.m <= 16) return few_one<KIND, FN, 1, true>(a, stream);
-    if (a.m <= 32) return few_one<KIND, FN, 2, true>(a, stream);
-    return few_one<KIND, FN, 4, true>(a, stream);
+    return few_one<KIND, FN, kFewTokens / 16, true>(a, stream);
 }
 template <int KIND>
 int few_kind(bool gated, const BlockArgs &a, void *stream) {
@@ -265,6 +264,8 @@ int few_kind(bool gated, const BlockArgs &a, void *stream) {
 
 }  // namespace
 
+// Values: up to 8192 of them.  At 16384 (m 4, k 4096) one launch took 7.2 us against
+// 5.7 to 6.5 for the codes and the product; at 4096 2.7 to 3.3 us against 5.
 bool few_takes_values(int m, int k) { return m <= 16 && k % 8 == 0 && (int64_t)m * (k / 8) <= kFewCodes * 64 * kFewWaves; }
 
 int launch_few(int kind, bool gated, const BlockArgs &a, void *stream) {

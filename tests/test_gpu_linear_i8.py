@@ -160,3 +160,18 @@ def test_refusals():
             pytest.fail(f"call {i} was accepted")
     with pytest.raises(nb.NmError):
         nb.ScaledWeight.from_int8(w, c, N=2, M=4)          # more than two nonzeros in a window
+
+
+# both sides of the sizes at which codes of few tokens take the tiles, and values in one launch beside them
+@pytest.mark.parametrize("N,M", [(8, 8), (2, 4), (1, 4), (3, 8)])
+@pytest.mark.parametrize("m,k,n", [(1, 4096, 4096), (1, 4096, 4112), (2, 4096, 4112), (16, 512, 200), (17, 512, 200),
+                                   (32, 1024, 72), (32, 1040, 72), (33, 1024, 72)])
+def test_few_tokens_on_either_kernel(N, M, m, k, n):
+    g = gen(m + k + n)
+    x = torch.randn(m, k, generator=g).half().cuda()
+    w, c = bu.weight(g, n, k, N, M)
+    lin = nb.ScaledWeight.from_int8(w, c, N=N, M=M)
+    q, s = nb.quantize_rows(x)
+    got = nb.gemm_i8_scaled(q, s, lin, out_dtype=torch.float32)
+    check(x, w, c, None, got, torch.float32)
+    assert torch.equal(nb.linear_i8(x, lin, out_dtype=torch.float32), got)

@@ -459,6 +459,11 @@ nm_status nm_quantize_f16(const uint16_t *x, int64_t count, float inv_scale, int
 nm_status nm_quantize_rows(const void *x, int64_t ldx, int type, int m, int k, int8_t *xq, float *scale,
                            void *stream);
 
+/* Codes that were made elsewhere, device int8 [m x k] at any address and row
+ * stride ldq >= k, as the products read them: out as xq above.  Asynchronous
+ * on `stream`; errors as nm_quantize_rows. */
+nm_status nm_pad_codes(const int8_t *q, int64_t ldq, int m, int k, int8_t *out, void *stream);
+
 /* A norm over the channels of a token: hat(v) * weight + bias with
  * hat(v) = v / sqrt(mean(v^2) + eps) (RMS) or
  * hat(v) = (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) (layer norm);

@@ -54,6 +54,14 @@ extern "C" nm_status nm_quantize_rows(const void *x, int64_t ldx, int type, int 
     return launch_quantize_rows(type, pieces(x, ldx, k, type), a, stream) == 0 ? NM_OK : NM_ERR_HIP;
 }
 
+extern "C" nm_status nm_pad_codes(const int8_t *q, int64_t ldq, int m, int k, int8_t *out, void *stream) {
+    if (m < 0 || m >= kMaxRows || k < 1 || k >= (1 << 28) || ldq < k) return NM_ERR_SHAPE;
+    if (m == 0) return NM_OK;
+    if (!q || !out || !aligned(out, 16)) return NM_ERR_ARG;
+    const PadArgs a = {q, out, ldq, round16(k), m, k};
+    return launch_pad_codes(a, stream) == 0 ? NM_OK : NM_ERR_HIP;
+}
+
 extern "C" nm_status nm_norm_residual(const nm_norm_args *args, void *stream) {
     if (!args) return NM_ERR_ARG;
     const nm_norm_args &g = *args;

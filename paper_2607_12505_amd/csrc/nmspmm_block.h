@@ -46,6 +46,16 @@ struct QuantArgs {
     int k;
 };
 
+// Rows of q as 16-byte pieces of rows of ldq bytes, zeros from k on.
+struct PadArgs {
+    const int8_t *q;
+    int8_t *out;              // [m x ldo], ldo = k rounded up to 16
+    int64_t ldq, ldo;
+    int64_t m;
+    int k;
+};
+int launch_pad_codes(const PadArgs &a, void *stream);
+
 constexpr int kMaxNormWidth = 16384;
 constexpr int64_t kMaxRows = 1 << 30;
 

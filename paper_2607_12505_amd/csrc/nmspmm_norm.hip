@@ -577,6 +577,24 @@ __global__ __launch_bounds__(team_threads(WPR)) void k_quantize_rows(QuantArgs a
     }
 }
 
+// One 16-byte piece of a padded row a thread, from any address.
+__global__ __launch_bounds__(256) void k_pad_codes(PadArgs a) {
+    typedef unsigned int v4u_bytes __attribute__((ext_vector_type(4), aligned(1)));
+    const int64_t per = a.ldo / 16, pieces = a.m * per;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / per;
+        const int c = (int)(i - row * per) * 16;
+        const int8_t *src = a.q + row * a.ldq + c;
+        v4u v = {0, 0, 0, 0};
+        if (c + 16 <= a.k) {
+            v = *(const v4u_bytes *)src;
+        } else {
+            for (int e = 0; e < a.k - c; ++e) v[e / 4] |= (unsigned)(uint8_t)src[e] << (e % 4 * 8);
+        }
+        *(v4u *)(a.out + i * 16) = v;
+    }
+}
+
 // --------------------------------------------------------------- launches
 // Waves of a team by the row's length, and workgroups that the device holds at once.
 constexpr int kResident = 8;
@@ -685,6 +703,12 @@ int launch_norm_residual_backward(int type, bool vec, const NormGradArgs &a, int
     const int64_t shared = a.groups > 1 && a.dgate ? (int64_t)a.groups * ((a.d + 63) / 64) : 0;
     hipLaunchKernelGGL(k_norm_sums, dim3((unsigned)(5 * col_blocks + shared)), dim3(1024), 0, (hipStream_t)stream, a,
                        workgroups, col_blocks);
+    return (int)hipGetLastError();
+}
+
+int launch_pad_codes(const PadArgs &a, void *stream) {
+    const int64_t want = (a.m * (a.ldo / 16) + 255) / 256, most = (int64_t)device_cu_count() * kResident;
+    hipLaunchKernelGGL(k_pad_codes, dim3((unsigned)(want < most ? want : most)), dim3(256), 0, (hipStream_t)stream, a);
     return (int)hipGetLastError();
 }
 

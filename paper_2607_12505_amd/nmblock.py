@@ -1,6 +1,7 @@
 """The operators of a transformer block around its int8 linears (C ABI in include/nmspmm.h).
 
-* `quantize_rows`: int8 codes of activation rows with a scale for each token.
+* `quantize_rows`: int8 codes of activation rows with a scale for each token; `pad_codes`: codes made elsewhere, as the
+  products read them (which take rows of an odd number of codes and pad them, or padded rows).
 * `linear_i8`, `gemm_i8_scaled`: the int8 product (dense or N:M weights) with scales for each token and channel, of
   activations or of codes already made; `ScaledWeight` holds its weight.
 * `gated_ffn`, `gated_ffn_i8`, `gated_ffn_backward`: both projections of a gated feed-forward block, the activation and
@@ -147,6 +148,18 @@ def quantize_rows(x, xq=None, scale=None, stream=None):
     _check(rt.quantize(x.data_ptr(), ld, code, m, k, xq.data_ptr(), scale.data_ptr(), _handle(stream, dev, rt)),
            "nm_quantize_rows")
     return xq, scale
+
+
+def pad_codes(q, out=None, stream=None):
+    """nm_pad_codes: codes int8 [rows x k] of any row stride as the products read them, [rows x padded(k)]."""
+    rt = _rt or _runtime()
+    dev = _index(q, "q", rt)
+    if q.dtype != rt.i8 or q.dim() != 2:
+        raise ValueError(f"q: {q.dtype} {tuple(q.shape)}, expected two-dimensional {rt.i8}")
+    m, k, ld = _rows(q, "q")
+    out = _output(out, "out", (m, padded(k)), rt.i8, q, stream, rt)
+    _check(lib().nm_pad_codes(q.data_ptr(), ld, m, k, out.data_ptr(), _handle(stream, dev, rt)), "nm_pad_codes")
+    return out
 
 
 # ---------------------------------------------------------------- norms around a block
@@ -521,18 +534,21 @@ def _of_rows(x, w: ScaledWeight, out, out_dtype, stream, gated: bool):
     return out
 
 
-def _codes_in(xq, sx, w: ScaledWeight, rt):
-    """(tokens, device) of codes and scales for w."""
+def _codes_in(xq, sx, w: ScaledWeight, stream, rt):
+    """(codes, tokens, device) of codes and scales for w: rows of w.k codes, which get their padding here, or padded."""
     dev = _index(xq, "xq", rt)
     m = xq.shape[0] if xq.dim() else 0
-    _param(xq, "xq", (m, w._kp), rt.i8, w._dev)
     _param(sx, "sx", (m,), rt.f32, w._dev)
-    return m, dev
+    if w.k != w._kp and xq.dim() == 2 and xq.shape[1] == w.k:
+        _on(xq, "xq", w._dev)
+        return pad_codes(xq, stream=stream), m, dev
+    _param(xq, "xq", (m, w._kp), rt.i8, w._dev)
+    return xq, m, dev
 
 
 def _of_codes(xq, sx, w: ScaledWeight, out, out_dtype, stream, gated: bool):
     rt = _rt or _runtime()
-    m, dev = _codes_in(xq, sx, w, rt)
+    xq, m, dev = _codes_in(xq, sx, w, stream, rt)
     dtype = out.dtype if out is not None else out_dtype or rt.torch.float16
     out, otype, ldo = _product_out(out, m, (m, w.n), dtype, xq, stream, rt)
     need = w._need(m, 0)
@@ -593,7 +609,7 @@ def gated_ffn_backward(xq, sx, w: GatedWeight, dh, stream=None) -> GatedGrads:
     if w.weight.desc.layout != NM_LAYOUT_DENSE:
         raise ValueError("w: the backward pass takes dense layouts")
     rt = _rt or _runtime()
-    m, dev = _codes_in(xq, sx, w, rt)
+    xq, m, dev = _codes_in(xq, sx, w, stream, rt)
     T, f32 = dh.dtype, rt.f32
     code = _type_of(dh, "dh", rt)
     if code == NM_TYPE_F32:

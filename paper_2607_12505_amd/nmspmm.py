@@ -37,7 +37,7 @@ EXPORTED = (
     "nm_quantize_f16", "nm_spmm_noalloc", "nm_expand_size", "nm_expand", "nm_spmm_out_expand",
     "nm_gemm_i8_dense_out_expand",
     # around the linears (bound in nmblock.py)
-    "nm_quantize_rows", "nm_norm_residual", "nm_norm_residual_backward_workspace", "nm_norm_residual_backward",
+    "nm_quantize_rows", "nm_pad_codes", "nm_norm_residual", "nm_norm_residual_backward_workspace", "nm_norm_residual_backward",
     "nm_linear_workspace", "nm_gemm_i8_scaled", "nm_linear_i8", "nm_gated_i8", "nm_gated", "nm_gated_backward_workspace",
     "nm_gated_backward",
 )
@@ -129,6 +129,7 @@ def lib() -> ctypes.CDLL:
             "nm_gemm_i8_dense_out_expand": ([vp, i32, vp, i32, i32, ctypes.POINTER(NmOutputs), vp, sz, vp, pp,
                                              ctypes.POINTER(NmExpandJob)], i32),
             "nm_quantize_rows": ([vp, i64, i32, i32, i32, vp, vp, vp], i32),
+            "nm_pad_codes": ([vp, i64, i32, i32, vp, vp], i32),
             "nm_norm_residual": ([vp, vp], i32),
             "nm_norm_residual_backward_workspace": ([i32, i32, i32, ctypes.POINTER(sz)], i32),
             "nm_norm_residual_backward": ([vp, vp, sz, vp], i32),

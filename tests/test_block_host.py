@@ -206,3 +206,15 @@ def test_m0_serves_the_loads_to_lds_alone(tmp_path):
                     assert re.fullmatch(r"s_mov_b32 m0, s\d+", text), text
                     due, writes = 3, writes + 1
     assert writes > 0
+
+
+def test_padding_codes_refuses():
+    f = L.nm_pad_codes
+    assert f(FAKE, 99, 4, 100, FAKE, NUL) == SHAPE
+    assert f(FAKE, 100, -1, 100, FAKE, NUL) == SHAPE
+    assert f(FAKE, 100, 4, 0, FAKE, NUL) == SHAPE
+    assert f(FAKE, 100, 4, 100, FAKE + 8, NUL) == ARG
+    assert f(NUL, 100, 4, 100, FAKE, NUL) == ARG
+    assert f(NUL, 100, 0, 100, NUL, NUL) == 0
+    if no_gpu():
+        assert f(FAKE + 1, 101, 4, 100, FAKE, NUL) == HIP

@@ -187,3 +187,13 @@ def test_a_token_has_the_same_bits_in_every_batch(T):
             all_ = call(x, weight)
             for part in (1, 3, 20, 50):
                 assert torch.equal(call(x[:part], weight), all_[:part])
+
+
+@pytest.mark.parametrize("m,k,n", [(5, 17, 3), (387, 131, 70)])
+def test_codes_without_padding(m, k, n):
+    x, w, plain, g = case(m, k, n, torch.bfloat16, True, act="gelu")
+    q, s = nb.quantize_rows(x)
+    dh = torch.randn(m, n, generator=g).bfloat16().cuda()
+    assert torch.equal(nb.gated_ffn_i8(q[:, :k], s, w), nb.gated_ffn_i8(q, s, w))
+    for got, want in zip(nb.gated_ffn_backward(q[:, :k].contiguous(), s, w, dh), nb.gated_ffn_backward(q, s, w, dh)):
+        assert torch.equal(got, want)

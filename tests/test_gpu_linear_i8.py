@@ -175,3 +175,27 @@ def test_few_tokens_on_either_kernel(N, M, m, k, n):
     got = nb.gemm_i8_scaled(q, s, lin, out_dtype=torch.float32)
     check(x, w, c, None, got, torch.float32)
     assert torch.equal(nb.linear_i8(x, lin, out_dtype=torch.float32), got)
+
+
+# codes without padding, with gaps between rows and at odd addresses
+@pytest.mark.parametrize("m,k,n", [(0, 7, 4), (1, 1, 5), (1, 4095, 16), (33, 17, 40), (387, 1315, 70), (70, 130, 515)])
+def test_codes_without_padding(m, k, n):
+    g = gen(m + k + n)
+    x = torch.randn(m, k, generator=g).half().cuda()
+    w, c = bu.weight(g, n, k)
+    lin = nb.ScaledWeight.from_int8(w, c)
+    q, s = nb.quantize_rows(x)
+    wide = torch.full((m, k + 5), 77, dtype=torch.int8, device="cuda")
+    wide[:, 3:3 + k] = q[:, :k]
+    assert torch.equal(nb.pad_codes(wide[:, 3:3 + k]), q)
+    want = nb.gemm_i8_scaled(q, s, lin)
+    assert torch.equal(nb.gemm_i8_scaled(q[:, :k].contiguous(), s, lin), want)
+    assert torch.equal(nb.gemm_i8_scaled(wide[:, 3:3 + k], s, lin), want)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = nb.gemm_i8_scaled(wide[:, 3:3 + k], s, lin, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got, want)
+    for bad in (q.half(), q[0] if m else q.flatten(), q.t().contiguous().t() if m > 1 and k > 1 else q.float()):
+        with pytest.raises(ValueError):
+            nb.pad_codes(bad)

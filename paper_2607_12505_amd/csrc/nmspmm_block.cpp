@@ -105,9 +105,15 @@ extern "C" nm_status nm_norm_residual_backward_workspace(int m, int d, int group
     if (st != NM_OK) return st;
     *bytes = 0;
     if (m == 0) return NM_OK;
-    const NormGradShape s = norm_grad_shape(m, d);
-    *bytes = round256((size_t)5 * s.workgroups * d * 4);
-    if (groups > 1) *bytes += (size_t)s.workgroups * s.teams * 2 * d * 4;
+    // the most of what the forms of the kernel need
+    size_t parts = 0, runs = 0;
+    for (int form = 0; form < 4; ++form) {
+        const NormGradShape s = norm_grad_shape(m, d, form & 1, form & 2);
+        if ((size_t)s.workgroups > parts) parts = s.workgroups;
+        if ((size_t)s.runs > runs) runs = s.runs;
+    }
+    *bytes = round256(5 * parts * d * 4);
+    if (groups > 1) *bytes += runs * 2 * d * 4;
     return NM_OK;
 }
 
@@ -146,7 +152,6 @@ extern "C" nm_status nm_norm_residual_backward(const nm_norm_grad_args *args, vo
     st = nm_norm_residual_backward_workspace(g.m, g.d, g.groups, &need);
     if (st != NM_OK) return st;
     if (!ws || ws_bytes < need || !aligned(ws, 16)) return NM_ERR_WORKSPACE;
-    const NormGradShape s = norm_grad_shape(g.m, g.d);
     NormGradArgs a;
     a.y = to_block ? g.y : nullptr;
     a.res = g.res;
@@ -163,7 +168,6 @@ extern "C" nm_status nm_norm_residual_backward(const nm_norm_grad_args *args, vo
     a.dpost_weight = g.dpost_weight;
     a.dpost_bias = g.dpost_bias;
     a.parts = (float *)ws;
-    a.gate_parts = (float *)((char *)ws + round256((size_t)5 * s.workgroups * g.d * 4));
     a.ldy = g.ldy;
     a.ldr = g.ldres;
     a.lddz = g.lddz;
@@ -172,11 +176,14 @@ extern "C" nm_status nm_norm_residual_backward(const nm_norm_grad_args *args, vo
     a.d = g.d;
     a.groups = g.groups;
     a.per_group = g.m / g.groups;
-    a.run = s.run;
     a.alpha = g.alpha;
     const bool vec = pieces(a.y, g.ldy, g.d, g.type) && pieces(g.res, g.ldres, g.d, g.type) &&
                      pieces(g.dz, g.lddz, g.d, g.type) && pieces(g.dres, g.lddres, g.d, g.type) &&
                      pieces(g.dy, g.d, g.d, g.type) && pieces(g.dr, g.d, g.d, g.type) && g.d % 8 == 0;
+    const NormGradShape s = norm_grad_shape(g.m, g.d, vec, a.post.kind != NM_NORM_NONE && a.y);
+    a.runs = s.runs;
+    a.turns = s.turns;
+    a.gate_parts = (float *)((char *)ws + round256((size_t)5 * s.workgroups * g.d * 4));
     return launch_norm_residual_backward(g.type, vec, a, s.workgroups, stream) == 0 ? NM_OK : NM_ERR_HIP;
 }
 

@@ -25,17 +25,17 @@ struct NormGradArgs {
     void *dy, *dr;
     float *dgate, *dpre_weight, *dpre_bias, *dpost_weight, *dpost_bias;
     float *parts;             // [5][workgroups][d]
-    float *gate_parts;        // [teams][2][d]: gate groups that several runs share
+    float *gate_parts;        // [runs][2][d]: gate groups that several runs share
     int64_t ldy, ldr, lddz, lddres;
     int m, d, groups, per_group;
-    int run;                  // rows of one team
+    int runs, turns;          // teams with rows (team t: rows t m / runs to (t + 1) m / runs), the most rows of one
     float alpha;
 };
-// Teams of waves that share a workgroup, rows that one team takes, workgroups.
+// Teams that take rows, the most rows of one, workgroups; of the form for pieces (vec) and for a norm after the block.
 struct NormGradShape {
-    int teams, run, workgroups;
+    int runs, turns, workgroups;
 };
-NormGradShape norm_grad_shape(int m, int d);
+NormGradShape norm_grad_shape(int m, int d, bool vec, bool post);
 
 struct QuantArgs {
     const void *x;

@@ -111,17 +111,6 @@ __device__ __forceinline__ void load_param(float (&p)[CH][VEC], const float *row
             for (int e = 0; e < VEC; ++e) p[c][e] = at + c * step < d ? absent : 0.f;
     }
 }
-// The lane's channels as floats in LDS.
-template <int VEC, int CH>
-__device__ __forceinline__ void store_shared(float *row, const float (&f)[CH][VEC], int d, int at, int step) {
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        if (at + c * step >= d) continue;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) row[at + c * step + e] = f[c][e];
-    }
-}
-
 template <int VEC, int CH>
 __device__ __forceinline__ float total(const float (&f)[CH][VEC]) {
     float s = 0.f;
@@ -245,6 +234,7 @@ __global__ __launch_bounds__(team_threads(WPR)) void k_norm_residual(NormArgs a)
 // first four channels of every chunk, then the last four).
 template <int VEC, int CH, int LANES>
 struct SharedParam {
+    typedef float v4 __attribute__((ext_vector_type(4)));
     static constexpr int SIZE = LANES * CH * VEC;
     // how many of the three fit beside the rest: past 8192 channels post's bias is read from memory
     static constexpr int FIT = 3 * SIZE * 4 <= 128 * 1024 ? 3 : 2;
@@ -255,8 +245,22 @@ struct SharedParam {
             at0[to] = ch < d ? (src ? src[ch] : absent) : 0.f;
         }
     }
+    // The first channel of a piece: four floats, or one.
+    static __device__ __forceinline__ int channel(int place) {
+        return VEC == 8 ? place % (LANES * CH) * 8 + place / (LANES * CH) * 4 : place;
+    }
+    __device__ __forceinline__ void put(const float (&f)[CH][VEC], int lane) const {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            if constexpr (VEC == 8) {
+                *(v4 *)(at0 + (c * LANES + lane) * 4) = v4{f[c][0], f[c][1], f[c][2], f[c][3]};
+                *(v4 *)(at0 + (LANES * CH + c * LANES + lane) * 4) = v4{f[c][4], f[c][5], f[c][6], f[c][7]};
+            } else {
+                at0[c * LANES + lane] = f[c][0];
+            }
+        }
+    }
     __device__ __forceinline__ void get(float (&f)[CH][VEC], int lane) const {
-        typedef float v4 __attribute__((ext_vector_type(4)));
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             if constexpr (VEC == 8) {
@@ -283,34 +287,64 @@ struct SharedParam {
 // A team takes a run of consecutive rows and sums for its channels what the
 // parameters' gradients need; the teams of a workgroup join their sums in LDS,
 // the workgroups in k_norm_sums: every addition has its place, so results do not
-// change from run to run.  A gate that is shared by fewer tokens than all is
+// change from run to run.  A workgroup is as many teams as a compute unit holds,
+// so that few sums are left to join.  A gate that is shared by fewer tokens than all is
 // finished, or put aside for k_norm_sums, whenever the team reaches the group's end.
+// 1 / sqrt(v), within an ulp (the hardware's, which takes no denormals): the root and quotient
+// rounded one after the other, as the forward pass has them, took 40 of a row's 500 instructions.
+__device__ __forceinline__ float inverse_root(float v) {
+    const bool tiny = v < 0x1p-100f;
+    return __builtin_amdgcn_rsqf(tiny ? v * 0x1p64f : v) * (tiny ? 0x1p32f : 1.f);
+}
+// The first row of a run, and the run of a row.
+__host__ __device__ constexpr int first_row(int64_t run, int m, int runs) { return (int)(run * m / runs); }
+__device__ constexpr int run_of(int64_t row, int m, int runs) { return (int)(((row + 1) * runs - 1) / m); }
 // Waves of a SIMD that the register budget is made for.
 constexpr int grad_waves(int wpr, int vec, int ch, bool post) {
     return wpr == 16 ? 4 : ch * vec > 8 ? 2 : vec == 8 && !post ? 4 : 3;
 }
 
+constexpr int grad_teams(int wpr, int vec, int ch, bool post) {
+    if (wpr >= 8 && (post || vec == 1 || wpr == 16)) return 1;
+    return 4 * grad_waves(wpr, vec, ch, post) / wpr;
+}
+
 // POST: whether there is a norm after the block (its sums are 40 % of the registers).
 template <class T, int VEC, int CH, int WPR, bool POST>
-__global__ __launch_bounds__(team_threads(WPR)) __attribute__((amdgpu_waves_per_eu(grad_waves(WPR, VEC, CH, POST)))) void k_norm_residual_backward(
-    NormGradArgs a) {
-    constexpr int TEAMS = team_threads(WPR) / 64 / WPR, LANES = 64 * WPR;
+__global__ __launch_bounds__(64 * WPR *grad_teams(WPR, VEC, CH, POST))
+__attribute__((amdgpu_waves_per_eu(grad_waves(WPR, VEC, CH, POST)))) void k_norm_residual_backward(NormGradArgs a) {
+    constexpr int TEAMS = grad_teams(WPR, VEC, CH, POST), LANES = 64 * WPR, SUMS = POST ? 5 : 3;
     __shared__ float box[TEAMS][2][2][WPR];
-    // the parameters, then (TEAMS > 1) one sum of every team but the first
+    // the parameters, then (TEAMS > 1) the sums of every team
     using Shared = SharedParam<VEC, CH, LANES>;
-    extern __shared__ __attribute__((aligned(16))) float joined[];
+    constexpr int PARAMS = Shared::SIZE * (POST ? Shared::FIT : 1), ALL = TEAMS > 1 ? TEAMS * SUMS * Shared::SIZE : 0;
+    __shared__ __attribute__((aligned(16))) float joined[PARAMS > ALL ? PARAMS : ALL];
     const int team = __builtin_amdgcn_readfirstlane(threadIdx.x / LANES), lane = threadIdx.x % LANES;
     RowReduce<WPR> red{box[team], lane >> 6};
     const int at = lane * VEC, step = LANES * VEC;
     const float per = 1.f / (float)a.d;
-    const int first = (int)(blockIdx.x * TEAMS + team) * a.run;
-    const int end = first + a.run < a.m ? first + a.run : a.m;
+    const int run = blockIdx.x * TEAMS + team;
+    const int first = run < a.runs ? first_row(run, a.m, a.runs) : a.m;
+    const int end = run < a.runs ? first_row(run + 1, a.m, a.runs) : a.m;
     const bool layer_q = a.pre.kind == NM_NORM_LAYER, layer_p = a.post.kind == NM_NORM_LAYER;
     const bool has_q = a.pre.kind != NM_NORM_NONE;
     constexpr bool has_p = POST;
     const int bytes = a.d * (int)sizeof(T);
 
     float gate[CH][VEC] = {};      // of a team without rows too: its zeros must stay zeros
+    float s_wq[CH][VEC] = {}, s_bq[CH][VEC] = {}, s_g[CH][VEC] = {}, s_wp[CH][VEC] = {}, s_bp[CH][VEC] = {};
+    Part<T, VEC, CH> py = {}, pr = {}, pz = {}, pd = {};
+    auto fetch = [&](int row) {
+        // a team that is done takes rows of zeros along: they add nothing
+        const int n = row < end ? bytes : 0;
+        const int64_t r = row < end ? row : 0;
+        // (and so does one without the tensor: no branch)
+        load_part(py, row_of(a.y, r * a.ldy * (int)sizeof(T), a.y ? n : 0), at, step);
+        load_part(pr, row_of(a.res, r * a.ldr * (int)sizeof(T), has_q ? n : 0), at, step);
+        load_part(pz, row_of(a.dz, r * a.lddz * (int)sizeof(T), a.dz ? n : 0), at, step);
+        load_part(pd, row_of(a.dres, r * a.lddres * (int)sizeof(T), a.dres ? n : 0), at, step);
+    };
+    fetch(first);
     const Shared lds_wq{joined}, lds_wp{joined + Shared::SIZE}, lds_bp{joined + 2 * Shared::SIZE};
     lds_wq.fill(a.pre.weight, 1.f, a.d);
     if constexpr (POST) {
@@ -318,34 +352,21 @@ __global__ __launch_bounds__(team_threads(WPR)) __attribute__((amdgpu_waves_per_
         if constexpr (Shared::FIT == 3) lds_bp.fill(a.post.bias, 0.f, a.d);
     }
     __syncthreads();
-    float s_wq[CH][VEC] = {}, s_bq[CH][VEC] = {}, s_g[CH][VEC] = {}, s_wp[CH][VEC] = {}, s_bp[CH][VEC] = {};
-
-    Part<T, VEC, CH> py = {}, pr = {}, pz = {}, pd = {};
-    auto fetch = [&](int row) {
-        // a team that is done takes rows of zeros along: they add nothing
-        const int n = row < end ? bytes : 0;
-        const int64_t r = row < end ? row : 0;
-        if (a.y) load_part(py, row_of(a.y, r * a.ldy * (int)sizeof(T), n), at, step);
-        if (has_q) load_part(pr, row_of(a.res, r * a.ldr * (int)sizeof(T), n), at, step);
-        if (a.dz) load_part(pz, row_of(a.dz, r * a.lddz * (int)sizeof(T), n), at, step);
-        if (a.dres) load_part(pd, row_of(a.dres, r * a.lddres * (int)sizeof(T), n), at, step);
-    };
     int group = -1;
     auto group_done = [&]() {
         // a group within this run is finished; one that other runs share is put
         // aside, in place 0 if the run began with it (or within it), else in 1
-        const bool whole = group * a.per_group >= first && (group + 1) * a.per_group <= first + a.run;
+        const bool whole = group * a.per_group >= first && (group + 1) * a.per_group <= end;
         const float *dst = whole ? a.dgate + (int64_t)group * a.d
-                                 : a.gate_parts + ((int64_t)(first / a.run) * 2 + (group == first / a.per_group ? 0 : 1)) * a.d;
+                                 : a.gate_parts + ((int64_t)run * 2 + (group == first / a.per_group ? 0 : 1)) * a.d;
         store_part<float>(row_of(dst, 0, a.d * 4), s_g, at, step);
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int e = 0; e < VEC; ++e) s_g[c][e] = 0.f;
     };
-    fetch(first);
-    // every team of the workgroup makes a.run turns: the reductions hold barriers
-    for (int i = 0; i < a.run; ++i) {
+    // every team of the workgroup makes as many turns: the reductions hold barriers
+    for (int i = 0; i < a.turns; ++i) {
         const int row = first + i;
         const bool live = row < end;
         if (WPR == 1 && !live) break;
@@ -366,9 +387,9 @@ __global__ __launch_bounds__(team_threads(WPR)) __attribute__((amdgpu_waves_per_
         float vy = has_p ? centre(y, layer_p ? my * per : 0.f, a.d, at, step) : 0.f;
         float vr = centre(r, layer_q ? mr * per : 0.f, a.d, at, step);
         red.sum2(vy, vr);
-        const float inv_y = has_p ? 1.f / __builtin_sqrtf(__builtin_fmaf(vy, per, a.post.eps)) : 1.f;
+        const float inv_y = has_p ? inverse_root(__builtin_fmaf(vy, per, a.post.eps)) : 1.f;
         if (has_q) {
-            const float inv_r = 1.f / __builtin_sqrtf(__builtin_fmaf(vr, per, a.pre.eps));
+            const float inv_r = inverse_root(__builtin_fmaf(vr, per, a.pre.eps));
             float st = 0.f, sth = 0.f, wq[CH][VEC];
             lds_wq.get(wq, lane);
 #pragma unroll
@@ -396,13 +417,13 @@ __global__ __launch_bounds__(team_threads(WPR)) __attribute__((amdgpu_waves_per_
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) dt[c][e] += dz[c][e];
         }
-        if (a.dr && live) {
+        {
             float out[CH][VEC];
 #pragma unroll
             for (int c = 0; c < CH; ++c)
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) out[c][e] = a.alpha * dt[c][e];
-            store_part<T>(row_of(a.dr, (int64_t)row * bytes, bytes), out, at, step);
+            store_part<T>(row_of(a.dr, (int64_t)row * bytes, a.dr && live ? bytes : 0), out, at, step);
         }
         if (!a.y) continue;
 
@@ -442,35 +463,47 @@ __global__ __launch_bounds__(team_threads(WPR)) __attribute__((amdgpu_waves_per_
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) dt[c][e] = inv_y * (dt[c][e] - mt - y[c][e] * mth);
         }
-        if (a.dy && live) store_part<T>(row_of(a.dy, (int64_t)row * bytes, bytes), dt, at, step);
+        store_part<T>(row_of(a.dy, (int64_t)row * bytes, a.dy && live ? bytes : 0), dt, at, step);
     }
     if (a.groups > 1 && group >= 0 && a.dgate) group_done();
 
     // this workgroup's sums, in the order gate, pre weight, pre bias, post weight, post bias
-    auto join = [&](float (&s)[CH][VEC], float *dst) {
-        if (!dst) return;
-        if constexpr (TEAMS > 1) {
-            __syncthreads();
-            if (team > 0) store_shared(joined + (team - 1) * a.d, s, a.d, at, step);
-            __syncthreads();
-            if (team == 0) {
-#pragma unroll
-                for (int c = 0; c < CH; ++c)
-                    if (at + c * step < a.d)
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e)
-                            for (int t = 1; t < TEAMS; ++t) s[c][e] += joined[(t - 1) * a.d + at + c * step + e];
-            }
-        }
-        if (team == 0) store_part<float>(row_of(dst, (int64_t)blockIdx.x * a.d * 4, a.d * 4), s, at, step);
-    };
+    float *const dst[5] = {a.groups <= 1 ? a.dgate : nullptr, a.dpre_weight, a.dpre_bias, a.dpost_weight, a.dpost_bias};
     const int64_t span = (int64_t)gridDim.x * a.d;
-    join(s_g, a.groups <= 1 && a.dgate ? a.parts : nullptr);
-    join(s_wq, a.dpre_weight ? a.parts + span : nullptr);
-    join(s_bq, a.dpre_bias ? a.parts + 2 * span : nullptr);
-    if constexpr (POST) {
-        join(s_wp, a.dpost_weight ? a.parts + 3 * span : nullptr);
-        join(s_bp, a.dpost_bias ? a.parts + 4 * span : nullptr);
+    float *parts = a.parts + (int64_t)blockIdx.x * a.d;
+    if constexpr (TEAMS == 1) {
+        const auto put = [&](int kind, const float (&f)[CH][VEC]) {
+            if (dst[kind]) store_part<float>(row_of(parts + kind * span, 0, a.d * 4), f, at, step);
+        };
+        put(0, s_g);
+        put(1, s_wq);
+        put(2, s_bq);
+        if constexpr (POST) {
+            put(3, s_wp);
+            put(4, s_bp);
+        }
+    } else {
+        constexpr int PER = VEC == 8 ? 4 : 1;
+        typedef float piece __attribute__((ext_vector_type(PER)));
+        __syncthreads();                         // the parameters have been read
+        const Shared mine{joined + team * (SUMS * Shared::SIZE)};
+        const auto leave = [&](int kind, const float (&f)[CH][VEC]) { Shared{mine.at0 + kind * Shared::SIZE}.put(f, lane); };
+        leave(0, s_g);
+        leave(1, s_wq);
+        leave(2, s_bq);
+        if constexpr (POST) {
+            leave(3, s_wp);
+            leave(4, s_bp);
+        }
+        __syncthreads();
+        for (int q = threadIdx.x; q < SUMS * Shared::SIZE / PER; q += TEAMS * LANES) {
+            const int kind = q / (Shared::SIZE / PER), place = q % (Shared::SIZE / PER), ch = Shared::channel(place);
+            if (ch >= a.d || !dst[kind]) continue;
+            piece sum = *(const piece *)(joined + q * PER);
+#pragma unroll
+            for (int t = 1; t < TEAMS; ++t) sum += *(const piece *)(joined + t * (SUMS * Shared::SIZE) + q * PER);
+            *(piece *)(parts + kind * span + ch) = sum;
+        }
     }
 }
 
@@ -517,11 +550,11 @@ __global__ __launch_bounds__(1024) void k_norm_sums(NormGradArgs a, int workgrou
     } else {
         const int wide = (a.d + 63) / 64, b = blockIdx.x - 5 * col_blocks;
         const int group = b / wide, ch = (b % wide) * 64 + (threadIdx.x & 63);
-        const int t0 = group * a.per_group / a.run, t1 = ((group + 1) * a.per_group - 1) / a.run;
+        const int t0 = run_of(group * a.per_group, a.m, a.runs), t1 = run_of((group + 1) * a.per_group - 1, a.m, a.runs);
         if (t0 == t1) return;              // within one run: finished there
         if (ch < a.d)
             for (int t = t0 + (threadIdx.x >> 6); t <= t1; t += 16)
-                s += a.gate_parts[((int64_t)2 * t + (group == t * a.run / a.per_group ? 0 : 1)) * a.d + ch];
+                s += a.gate_parts[((int64_t)2 * t + (group == first_row(t, a.m, a.runs) / a.per_group ? 0 : 1)) * a.d + ch];
         add_turns<64>(part, s, a.dgate + (int64_t)group * a.d + ch, ch < a.d);
     }
 }
@@ -621,11 +654,8 @@ int norm_by_width(const NormArgs &a, void *stream) {
 
 template <class T, int VEC, int CH, int WPR, bool POST>
 int grad_one(const NormGradArgs &a, int workgroups, void *stream) {
-    using Shared = SharedParam<VEC, CH, 64 * WPR>;
-    constexpr int teams = team_threads(WPR) / 64 / WPR, params = Shared::SIZE * (POST ? Shared::FIT : 1);
-    const int sums = (teams - 1) * a.d;      // once the parameters are no longer needed
-    hipLaunchKernelGGL((k_norm_residual_backward<T, VEC, CH, WPR, POST>), dim3(workgroups), dim3(team_threads(WPR)),
-                       (params > sums ? params : sums) * 4, (hipStream_t)stream, a);
+    hipLaunchKernelGGL((k_norm_residual_backward<T, VEC, CH, WPR, POST>), dim3(workgroups),
+                       dim3(64 * WPR * grad_teams(WPR, VEC, CH, POST)), 0, (hipStream_t)stream, a);
     return (int)hipGetLastError();
 }
 template <class T, int VEC, bool POST>
@@ -668,17 +698,17 @@ int quant_by_width(const QuantArgs &a, void *stream) {
 
 }  // namespace
 
-// Waves of a backward team, and the workgroups and rows of a team's run for m rows.
-static int grad_teams(int d) { return d <= 512 ? 4 : d <= 1024 ? 2 : 1; }
-
-NormGradShape norm_grad_shape(int m, int d) {
-    const int teams = grad_teams(d);
-    const int most = device_cu_count() * (d <= 2048 ? 3 : d <= 4096 ? 2 : 1);
-    const int want = (m + teams - 1) / teams, workgroups = want < most ? want : most;
+// Workgroups of the backward kernel for m rows, one a compute unit, and the rows of a
+// run: as many as another's or one more.
+NormGradShape norm_grad_shape(int m, int d, bool vec, bool post) {
+    const int v = vec ? 8 : 1, half = 8 / v;
+    const int wpr = d <= 512 ? 1 : d <= 1024 ? 2 : d <= 2048 ? 4 : d <= 4096 || (d <= 8192 && vec && post) ? 8 : 16;
+    const int ch = d > 8192 || (d > 4096 && vec && post) ? 2 * half : half;
+    const int teams = grad_teams(wpr, v, ch, post), most = device_cu_count(), want = (m + teams - 1) / teams;
     NormGradShape s;
-    s.teams = teams;
-    s.run = (m + workgroups * teams - 1) / (workgroups * teams);
-    s.workgroups = (m + s.run * teams - 1) / (s.run * teams);
+    s.workgroups = want < most ? want : most;
+    s.runs = s.workgroups * teams < m ? s.workgroups * teams : m;
+    s.turns = (m + s.runs - 1) / s.runs;
     return s;
 }
 

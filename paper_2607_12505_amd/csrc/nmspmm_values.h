@@ -53,6 +53,25 @@ __device__ __forceinline__ float wave_sum(float x) {
     x += dpp<0x143, 0xC>(0.f, x);
     return last_lane(x);
 }
+// Two sums in one: lanes 0 to 31 end with that of a, the others with that of b.  After the
+// swap of a's upper half with b's lower one an addition joins both halves of both; then
+// rows 16 lanes apart, and the steps of wave_sum within a row.
+__device__ __forceinline__ float wave_sums(float a, float b) {
+    const auto half = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b),
+                                                       false, false);
+    const float y = __builtin_bit_cast(float, (uint32_t)half[0]) + __builtin_bit_cast(float, (uint32_t)half[1]);
+    const auto row = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, y), __builtin_bit_cast(uint32_t, y),
+                                                      false, false);
+    float x = __builtin_bit_cast(float, (uint32_t)row[0]) + __builtin_bit_cast(float, (uint32_t)row[1]);
+    x += dpp<0xB1>(0.f, x);
+    x += dpp<0x4E>(0.f, x);
+    x += dpp<0x141>(0.f, x);
+    x += dpp<0x140>(0.f, x);
+    return x;
+}
+__device__ __forceinline__ float lane_of(float x, int lane) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
+}
 // The larger of two magnitudes; a NaN, or an infinity, wins: the bits of a
 // float without its sign are ordered as the values are, NaN above infinity.
 __device__ __forceinline__ float larger(float a, float b) {
@@ -81,13 +100,12 @@ struct RowReduce {
     int wave;          // of the row
     int turn = 0;
     __device__ void sum2(float &a, float &b) {
-        a = wave_sum(a);
-        b = wave_sum(b);
-        if constexpr (WPR > 1) {
-            if ((threadIdx.x & 63) == 0) {
-                box[turn][0][wave] = a;
-                box[turn][1][wave] = b;
-            }
+        const float both = wave_sums(a, b);
+        if constexpr (WPR == 1) {
+            a = lane_of(both, 0);
+            b = lane_of(both, 32);
+        } else {
+            if ((threadIdx.x & 31) == 0) box[turn][(threadIdx.x >> 5) & 1][wave] = both;
             __syncthreads();
             a = b = 0.f;
 #pragma unroll

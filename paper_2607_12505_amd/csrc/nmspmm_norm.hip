@@ -457,11 +457,12 @@ __attribute__((amdgpu_waves_per_eu(grad_waves(WPR, VEC, CH, POST)))) void k_norm
         }
         if constexpr (POST) {
             red.sum2(st, sth);
-            const float mt = layer_p ? st * per : 0.f, mth = sth * per;
+            const float mt = layer_p ? st * per * inv_y : 0.f, mth = sth * per * inv_y;
 #pragma unroll
             for (int c = 0; c < CH; ++c)
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) dt[c][e] = inv_y * (dt[c][e] - mt - y[c][e] * mth);
+                for (int e = 0; e < VEC; ++e)
+                    dt[c][e] = __builtin_fmaf(-y[c][e], mth, __builtin_fmaf(dt[c][e], inv_y, -mt));
         }
         store_part<T>(row_of(a.dy, (int64_t)row * bytes, a.dy && live ? bytes : 0), dt, at, step);
     }

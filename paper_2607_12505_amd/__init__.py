@@ -2,6 +2,8 @@
 
 The compute lives in ``libnmspmm.so`` (hand-written HIP kernels behind a C
 ABI, declared in ``include/nmspmm.h``).  ``paper_2607_12505_amd.nmspmm`` is the
-thin ctypes binding; importing this package does not load the library.
+thin ctypes binding; ``paper_2607_12505_amd.nmblock`` binds the operators of a
+transformer block around the GEMM.  Importing this package does not load the
+library.
 """
-__all__ = ["nmspmm", "workloads"]
+__all__ = ["nmblock", "nmspmm", "workloads"]

@@ -241,8 +241,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few(BlockArgs a) {
     int ch = f0 * 16 + 4 * lg;
     if constexpr (FN == 2) {
         ch = blockIdx.x * 16 + 4 * lg;
+        by_act(a.act, [&](auto act) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[0][e] = gate_times(a.act, v[0][e], v[1][e]);
+            for (int e = 0; e < 4; ++e) v[0][e] = gate_times(decltype(act)::value, v[0][e], v[1][e]);
+        });
     }
     by_type(a.type, [&](auto *p) {
         using T = typename std::remove_pointer<decltype(p)>::type;

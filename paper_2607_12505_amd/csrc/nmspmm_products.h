@@ -213,6 +213,19 @@ __device__ __forceinline__ float act_of(int act, float g) {
     return f;
 }
 
+// The activation as a constant to f: decided once for all values that f makes, whose
+// exponentials then overlap (decided at each value they ran one after the other).
+template <class F>
+__device__ __forceinline__ void by_act(int act, const F &f) {
+    switch (act) {
+        case NM_ACT_SILU: f(std::integral_constant<int, NM_ACT_SILU>{}); break;
+        case NM_ACT_GELU: f(std::integral_constant<int, NM_ACT_GELU>{}); break;
+        case NM_ACT_GELU_TANH: f(std::integral_constant<int, NM_ACT_GELU_TANH>{}); break;
+        case NM_ACT_RELU: f(std::integral_constant<int, NM_ACT_RELU>{}); break;
+        default: f(std::integral_constant<int, NM_ACT_SIGMOID>{}); break;
+    }
+}
+
 __device__ __forceinline__ float gate_times(int act, float g, float u) {
     float x = act_of(act, g) * u;
     asm("" : "+v"(x));   // in binary32 before its rounding to T, as scaled_value
@@ -264,8 +277,10 @@ struct GatedOut {
             for (int j = 0; j < H::FM; ++j) {
                 const v4f g = scaled_value(acc[2 * i][j], sx[j], cg, bg);
                 const v4f u = scaled_value(acc[2 * i + 1][j], sx[j], cu, bu);
+                by_act(a.act, [&](auto act) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) h[i][j][e] = gate_times(a.act, g[e], u[e]);
+                    for (int e = 0; e < 4; ++e) h[i][j][e] = gate_times(decltype(act)::value, g[e], u[e]);
+                });
             }
         }
         by_type(a.type, [&](auto *t) {
@@ -296,8 +311,10 @@ struct GatedOut {
                 const v4f g = scaled_value(sum_ks<G>(lds, row, cc), sx, cg, bg);
                 const v4f u = scaled_value(sum_ks<G>(lds, row, cc + 4), sx, cu, bu);
                 v4f h;
+                by_act(a.act, [&](auto act) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) h[e] = gate_times(a.act, g[e], u[e]);
+                    for (int e = 0; e < 4; ++e) h[e] = gate_times(decltype(act)::value, g[e], u[e]);
+                });
                 store_four<T>(a, tok, ch, h);
             }
         });
@@ -364,20 +381,34 @@ struct GatedGradOut {
             const v4f zero = {0, 0, 0, 0}, c[2] = {multiplier(0, i), multiplier(0, i + 1)};
             const v4f bg = a.qscale ? multiplier(1, i) : zero, bu = a.qscale ? multiplier(1, i + 1) : zero;
             v4f d[2][FM];
+            float dh[FM][4];
 #pragma unroll
-            for (int j = 0; j < FM; ++j) {
-                const int tok = at.tok + j * 16 + lt;
-                const v4f g = scaled_value(acc[i][j], sx[j], c[0], bg), u = scaled_value(acc[i + 1][j], sx[j], c[1], bu);
-                float dh[4];
-                load_four<T>(a, tok, at.ch / 2 + i * 8 + 4 * lg, dh);
+            for (int j = 0; j < FM; ++j) load_four<T>(a, at.tok + j * 16 + lt, at.ch / 2 + i * 8 + 4 * lg, dh[j]);
+            by_act(a.act, [&](auto act) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float f, df;
-                    act_and_slope(a.act, g[e], f, df);
-                    // tokens past the last one have no gradient, whatever their row holds
-                    d[0][j][e] = tok < a.m ? dh[e] * u[e] * df : 0.f;
-                    d[1][j][e] = tok < a.m ? dh[e] * f : 0.f;
+                for (int j = 0; j < FM; ++j) {
+                    const v4f g = scaled_value(acc[i][j], sx[j], c[0], bg);
+                    const v4f u = scaled_value(acc[i + 1][j], sx[j], c[1], bu);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float f, df;
+                        act_and_slope(decltype(act)::value, g[e], f, df);
+                        d[0][j][e] = dh[j][e] * u[e] * df;
+                        d[1][j][e] = dh[j][e] * f;
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
+            });
+            // tokens past the last one have no gradient, whatever their row holds
+            if (at.tok + FM * 16 > a.m) {
+#pragma unroll
+                for (int j = 0; j < FM; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const bool live = at.tok + j * 16 + lt < a.m;
+                        d[0][j][e] = live ? d[0][j][e] : 0.f;
+                        d[1][j][e] = live ? d[1][j][e] : 0.f;
+                    }
             }
             const int ch0 = at.ch + i * 16;
             store_tile<P, T>(

@@ -267,10 +267,11 @@ int out_mode_for(int type, bool gated) {
 
 // The tile of a product.  Dense gated blocks with many tiles and a short reduction
 // take the tile of which two share a compute unit: one's epilogue (an exponential a
-// value) runs beside the other's products.  Of 28 random gated shapes with 0.5 to 20
-// tiles a unit, the 11 within the rule took 0.77 to 1.02 of the time of the estimate's
-// tile (0.87 on average; 18464 x 1024 -> 2736: 125 us against 144), those outside 0.91 to
-// 1.35; 32 plain products 0.83 to 1.29, 1.07 on average.
+// value) runs beside the other's products.  Of 42 gated shapes with 0.5 to 12 tiles a unit, the
+// 15 within the rule took 0.80 to 1.03 of the time of the estimate's tile (0.92 on
+// average; 18464 x 1024 -> 2736: 120.5 us against 128.1).  Outside it (28 shapes, before the
+// activation was decided once for four values) 0.91 to 1.35; 32 plain products 0.83 to 1.29,
+// 1.07 on average.
 int product_tile(int kind, bool gated, int m, int n, int k, int out_mode) {
     const int tn = tile_n_of(kRowTile), tm = tile_m_of(kRowTile);
     const int64_t tiles = (int64_t)((n + tn - 1) / tn) * ((m + tm - 1) / tm);

@@ -272,10 +272,20 @@ int out_mode_for(int type, bool gated) {
 // average; 18464 x 1024 -> 2736: 120.5 us against 128.1).  Outside it (28 shapes, before the
 // activation was decided once for four values) 0.91 to 1.35; 32 plain products 0.83 to 1.29,
 // 1.07 on average.
+//   A 4:2 operand and a long reduction take the 4-slot ring where its tiles fit the
+// device at once, two a compute unit: the deeper ring covers the load latency that few
+// workgroups leave bare.  Of 11 random shapes within the rule, operands out of L2, 10 took
+// 0.79 to 0.95 of the estimate's tile and one 0.98 (1906 x 1200 -> 1504 10.5 us against 11.7);
+// 13 of k 320 to 900 at that many tiles 0.97 to 1.10; past two a unit 31 shapes 1.12 to 1.47.
 int product_tile(int kind, bool gated, int m, int n, int k, int out_mode) {
     const int tn = tile_n_of(kRowTile), tm = tile_m_of(kRowTile);
     const int64_t tiles = (int64_t)((n + tn - 1) / tn) * ((m + tm - 1) / tm);
     if (gated && kind == NM_KIND_DENSE && k <= 1536 && 2 * tiles >= 5 * device_cu_count()) return kRowTile;
+    if (kind == NM_KIND_SP42 && k >= 1024) {
+        const TileCfg &t = kTiles[kDeepTile];
+        const int64_t deep = (int64_t)((n + t.tile_n() - 1) / t.tile_n()) * ((m + t.tile_m() - 1) / t.tile_m());
+        if (deep > device_cu_count() && deep <= 2 * device_cu_count()) return kDeepTile;
+    }
     return schedule_among(kind, m, n, k, out_mode, scaled_tiles(kind));
 }
 

@@ -91,10 +91,11 @@ struct BlockArgs : GemmArgs {
     int interleaved = 0;
 };
 
+constexpr int kDeepTile = 13;    // of kTiles: 128 ch x 64 tok, 4-slot ring
 // Tiles that the products are built for, by what they write.
 constexpr uint32_t scaled_tiles(int kind) {
     return 1u << 1 | 1u << 3 | 1u << 6 | 1u << 7 | 1u << 8 | 1u << 9 | 1u << 10 | 1u << 12 | 1u << 15 |
-           (tile_built(kind, 13) ? 1u << 13 : 0u);
+           (tile_built(kind, kDeepTile) ? 1u << kDeepTile : 0u);
 }
 constexpr uint32_t kGradTiles = 1u << 1 | 1u << 3 | 1u << 6;   // whole 64-token groups: the transposed rows' padding is written too
 constexpr uint32_t kCastTiles = 1u << 1 | 1u << 3 | 1u << 6 | 1u << 12 | 1u << 4;

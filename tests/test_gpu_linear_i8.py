@@ -199,3 +199,20 @@ def test_codes_without_padding(m, k, n):
     for bad in (q.half(), q[0] if m else q.flatten(), q.t().contiguous().t() if m > 1 and k > 1 else q.float()):
         with pytest.raises(ValueError):
             nb.pad_codes(bad)
+
+
+# a 4:2 operand with a long reduction and one to two 64-token tiles a compute unit: the 4-slot ring, with a short last
+# k-step, ragged channels and tokens, and just past the rule (513 tiles)
+@pytest.mark.parametrize("N,M", [(2, 4), (1, 4)])
+@pytest.mark.parametrize("m,k,n", [(1906, 1200, 1504), (4070, 1024, 1000), (2061, 1300, 1001), (3585, 1024, 1152)])
+def test_long_reductions_by_sampled_rows(N, M, m, k, n):
+    g = gen(m + N)
+    x = torch.randn(m, k, generator=g).half().cuda()
+    w, c = bu.weight(g, n, k, N, M)
+    b = torch.randn(n, generator=g)
+    lin = nb.ScaledWeight.from_int8(w, c, bias=b, N=N, M=M)
+    out = torch.full((m + 2, n), 7.0, dtype=torch.half, device="cuda")
+    got = nb.linear_i8(x, lin, out=out[:m])
+    rows = torch.cat([torch.arange(0, 4), torch.arange(m - 4, m), torch.randint(0, m, (120,), generator=g)])
+    check(x[rows], w, c, b, got[rows], torch.half)
+    assert (out[m:] == 7).all()

@@ -12,8 +12,8 @@
 // then makes the codes itself, in LDS, while its first weights are on their
 // way.  That repeats a row's codes once for each 16 channels, and saves a launch.
 //
-// Measured: one token as values, dense 1024 -> 4096 4.2 us, gated 1024 -> 2736 (twice the
-// weight rows) 5.1 us.  A token's weights are 4 to 6 MB, under 1 us at the memory's rate: what is
+// Measured: one token as values, dense 1024 -> 4096 4.3 us, gated 1024 -> 2736 (twice the
+// weight rows) 4.8 us.  A token's weights are 4 to 6 MB, under 1 us at the memory's rate: what is
 // left is the launch, the wait for x and the weights one after the other, and the sums.  A
 // long weight streams: 4096 -> 11008 from codes, 45 MB, 10.8 us (4.2 TB/s).
 #include "nmspmm_products.h"

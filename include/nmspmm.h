@@ -482,9 +482,9 @@ typedef struct nm_norm {
 /* A block's end and the next one's beginning, for m tokens of d channels:
  *   u = post(y);  res = alpha * r + gate * u;  z = pre(res)
  * y the block's output and r the residual stream (either may be NULL: then its
- * term is absent); gate device float32 [groups x d], row i / (m / groups) for
- * token i (groups divides m), or NULL (1, groups = 1).  Outputs, each of
- * which may be NULL: res and z of `type`, and the codes zq (int8 [m x dp], dp =
+ * term is absent, with post and gate or alpha, whatever they hold); gate
+ * device float32 [groups x d], row i / (m / groups) for token i (groups divides
+ * m), or NULL (1, groups = 1).  Outputs, each of which may be NULL: res and z of `type`, and the codes zq (int8 [m x dp], dp =
  * d rounded up to 16) with scales zs (float32 [m]) of z as nm_quantize_rows
  * defines them.  z is computed from res before its rounding to `type`.
  * res may be r or y itself (same row stride d), no other overlap.  d <= 16384. */

@@ -76,11 +76,13 @@ extern "C" nm_status nm_norm_residual(const nm_norm_args *args, void *stream) {
     for (const void *p : {g.y, g.r, (const void *)g.res, (const void *)g.z})
         if (!aligned(p, eb)) return NM_ERR_ARG;
     if (!aligned(g.gate, 4) || !aligned(g.zs, 4) || !aligned(g.zq, 16)) return NM_ERR_ARG;
+    // an absent term is absent whole: a norm's bias, a gate or alpha times nothing adds nothing, whatever they hold
+    static const nm_norm none = {NM_NORM_NONE, 0.f, nullptr, nullptr};
     NormArgs a;
     a.y = g.y;
     a.r = g.r;
-    a.gate = g.gate;
-    a.post = as_read(g.post);
+    a.gate = g.y ? g.gate : nullptr;
+    a.post = g.y ? as_read(g.post) : none;
     a.pre = as_read(g.pre);
     a.res = g.res;
     a.z = g.z;
@@ -91,9 +93,9 @@ extern "C" nm_status nm_norm_residual(const nm_norm_args *args, void *stream) {
     a.ldq = round16(g.d);
     a.m = g.m;
     a.d = g.d;
-    a.groups = g.groups;
-    a.per_group = g.m / g.groups;
-    a.alpha = g.alpha;
+    a.groups = g.y ? g.groups : 1;
+    a.per_group = g.m / a.groups;
+    a.alpha = g.r ? g.alpha : 0.f;
     const bool vec = pieces(g.y, g.ldy, g.d, g.type) && pieces(g.r, g.ldr, g.d, g.type) &&
                      pieces(g.res, g.d, g.d, g.type) && pieces(g.z, g.d, g.d, g.type) && g.d % 8 == 0;
     return launch_norm_residual(g.type, vec, a, stream) == 0 ? NM_OK : NM_ERR_HIP;

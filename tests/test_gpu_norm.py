@@ -331,3 +331,32 @@ def test_refusals():
     wide = torch.zeros(2, 16400, dtype=torch.float16, device="cuda")
     with pytest.raises(nb.NmError):
         nb.norm_residual(wide, wide)
+
+
+@pytest.mark.parametrize("T", bu.TYPES)
+@pytest.mark.parametrize("m,d,groups", [(1, 64, 1), (6, 100, 3), (40, 1032, 40), (9, 2049, 1)])
+@pytest.mark.parametrize("post_kind", ["rms", "layer"])
+def test_absent_block_output_adds_nothing(T, m, d, groups, post_kind):
+    # neither the norm's bias nor a gate, whatever it holds, enters a sum whose y is absent
+    g = gen(m + d)
+    pre, p64 = norm_of(g, d, "layer")
+    post, q64 = norm_of(g, d, post_kind)
+    gate = torch.randn(groups, d, generator=g).cuda()
+    gate[-1, 0], gate[0, -1] = float("inf"), float("nan")
+    r = rows(g, m, d, T, pad=8)
+    want = bu.norm_residual(None, r, p64, q64, gate, 0.75)
+    res, z = nb.norm_residual(None, r, pre=pre, post=post, gate=gate, alpha=0.75)
+    bu.close(res, want[0], T, want[2])
+    bu.close(z, want[1], T, want[3])
+    plain = nb.norm_residual_i8(None, r, pre=pre, alpha=0.75)
+    for a, b in zip(nb.norm_residual_i8(None, r, pre=pre, post=post, gate=gate, alpha=0.75), plain):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("alpha", [float("inf"), float("nan")])
+def test_absent_residual_adds_nothing(alpha):
+    g = gen(21)
+    pre, _ = norm_of(g, 72, "layer")
+    y = rows(g, 5, 72, torch.float32)
+    for a, b in zip(nb.norm_residual(y, None, pre=pre, alpha=alpha), nb.norm_residual(y, None, pre=pre)):
+        assert torch.equal(a, b)

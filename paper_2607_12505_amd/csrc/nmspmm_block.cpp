@@ -21,6 +21,7 @@ bool valid_norm(const nm_norm &n) {
     return (n.kind == NM_NORM_RMS || n.kind == NM_NORM_LAYER) && n.eps > 0.f && aligned(n.weight, 4) &&
            aligned(n.bias, 4);
 }
+constexpr nm_norm kNoNorm = {NM_NORM_NONE, 0.f, nullptr, nullptr};
 nm_norm as_read(nm_norm n) {
     if (n.kind == NM_NORM_NONE) n.weight = n.bias = nullptr;
     return n;
@@ -77,12 +78,11 @@ extern "C" nm_status nm_norm_residual(const nm_norm_args *args, void *stream) {
         if (!aligned(p, eb)) return NM_ERR_ARG;
     if (!aligned(g.gate, 4) || !aligned(g.zs, 4) || !aligned(g.zq, 16)) return NM_ERR_ARG;
     // an absent term is absent whole: a norm's bias, a gate or alpha times nothing adds nothing, whatever they hold
-    static const nm_norm none = {NM_NORM_NONE, 0.f, nullptr, nullptr};
     NormArgs a;
     a.y = g.y;
     a.r = g.r;
     a.gate = g.y ? g.gate : nullptr;
-    a.post = g.y ? as_read(g.post) : none;
+    a.post = g.y ? as_read(g.post) : kNoNorm;
     a.pre = as_read(g.pre);
     a.res = g.res;
     a.z = g.z;
@@ -161,7 +161,7 @@ extern "C" nm_status nm_norm_residual_backward(const nm_norm_grad_args *args, vo
     a.dres = g.dres;
     a.gate = g.gate;
     a.post = as_read(g.post);
-    a.pre = as_read(g.pre);
+    a.pre = g.dz ? as_read(g.pre) : kNoNorm;     // without dz nothing comes through it, whatever res holds
     a.dy = g.dy;
     a.dr = g.dr;
     a.dgate = g.dgate;

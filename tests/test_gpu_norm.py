@@ -360,3 +360,19 @@ def test_absent_residual_adds_nothing(alpha):
     y = rows(g, 5, 72, torch.float32)
     for a, b in zip(nb.norm_residual(y, None, pre=pre, alpha=alpha), nb.norm_residual(y, None, pre=pre)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("T", bu.TYPES)
+@pytest.mark.parametrize("m,d,post_kind", [(5, 64, None), (70, 100, "rms"), (9, 2049, "layer"), (300, 512, None)])
+def test_absent_gradient_of_z_adds_nothing(T, m, d, post_kind):
+    # without dz nothing comes through the norm before the next block, whatever the residual rows hold
+    g = gen(m + d)
+    pre, p64 = norm_of(g, d, "layer")
+    post, q64 = norm_of(g, d, post_kind)
+    y, res, dres = (rows(g, m, d, T) for _ in range(3))
+    gate = torch.randn(d, generator=g).cuda()
+    res = res.clone()
+    res[0, 0], res[m // 2, d - 1], res[m - 1] = float("inf"), float("nan"), -float("inf")
+    got = nb.norm_residual_backward(None, dres, y, res, pre=pre, post=post, gate=gate, alpha=0.5)
+    check_grads(got, bu.norm_grads(None, dres, y, res, p64, q64, gate, 0.5), T, m)
+    assert (got.dpre_weight == 0).all() and (got.dpre_bias == 0).all()

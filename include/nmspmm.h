@@ -581,9 +581,9 @@ nm_status nm_gated(const void *x, int64_t ldx, int xtype, int m, const nm_scaled
  * and the bias gradients, the sums of dg and du over tokens (binary32).  g and u
  * are computed again in binary32; dg and du enter the products rounded to `type`
  * (NM_TYPE_F16 or NM_TYPE_BF16) once, times the fraction, in [1, 2), of the scale
- * that runs along the sum (its power of two goes to the codes, exactly): in
+ * that runs along the sum (its power of two and sign go to the codes, exactly): in
  * binary16 dg and du have to stay below half of its largest value, and scales
- * below 1024; of scales below 2^-24 a code keeps what binary16's subnormals hold.  dh [m] rows of lddh >= n, dx
+ * within 1024 of 0; of scales below 2^-24 a code keeps what binary16's subnormals hold.  dh [m] rows of lddh >= n, dx
  * [m x k], dw_* [n x k] without gaps, of `type`; dbias_* float32 [n]; any output may be
  * NULL.  The weight's layout must be NM_LAYOUT_DENSE (NM_ERR_UNSUPPORTED
  * otherwise).  With m == 0 the weight and bias gradients are set to zero.  The

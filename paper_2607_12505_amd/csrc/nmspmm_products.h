@@ -321,11 +321,11 @@ struct GatedOut {
     }
 };
 
-// A positive scale as power of two times a value in [1, 2): codes times the power
-// are exact in 16 bits, so a product with a scale along the reduction needs no
+// A scale as power of two, with its sign, times a value in [1, 2): codes times the
+// power are exact in 16 bits, so a product with a scale along the reduction needs no
 // rounding but that of the other operand.  0 and NaN: 0 and NaN times 1.
 __device__ __forceinline__ float scale_power(float s) {
-    return s != s ? s : __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, s) & 0x7F800000u);
+    return s != s ? s : __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, s) & 0xFF800000u);
 }
 __device__ __forceinline__ float scale_part(float s) {
     const uint32_t b = __builtin_bit_cast(uint32_t, s) & 0x7FFFFFFFu;

@@ -197,3 +197,29 @@ def test_codes_without_padding(m, k, n):
     assert torch.equal(nb.gated_ffn_i8(q[:, :k], s, w), nb.gated_ffn_i8(q, s, w))
     for got, want in zip(nb.gated_ffn_backward(q[:, :k].contiguous(), s, w, dh), nb.gated_ffn_backward(q, s, w, dh)):
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("T", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("m,k,n", [(5, 17, 3), (130, 96, 40), (1000, 48, 70)])
+def test_scales_of_either_sign(T, m, k, n):
+    # a channel (or token) with a negative scale is the negated codes with the positive one
+    act = ACTS[(m + k) % 5]
+    x, _, (wg, cg, bg, wu, cu, bu_, _), g = case(m, k, n, T, True, act=act)
+    q, s = nb.quantize_rows(x)
+    dh = torch.randn(m, n, generator=g).to(T).cuda()
+    sg, su, ss = (torch.where(torch.rand(c, generator=g) < 0.5, -1, 1) for c in (n, n, m))
+
+    def weight(a, b, c, d):
+        return nb.GatedWeight.from_int8(a, b, c, d, bias_gate=bg, bias_up=bu_, act=act, trainable=True)
+
+    def flip(w, sign):
+        return (w * sign[:, None]).to(torch.int8)
+
+    signed, codes = weight(wg, cg * sg, wu, cu * su), weight(flip(wg, sg), cg, flip(wu, su), cu)
+    neg = flip(q, ss.cuda())
+    assert torch.equal(nb.gated_ffn_i8(q, s * ss.cuda(), signed), nb.gated_ffn_i8(neg, s, codes))
+    got = nb.gated_ffn_backward(q, s * ss.cuda(), signed, dh)
+    want = bu.gated_grads(neg[:, :k], s, flip(wg, sg), cg, bg, flip(wu, su), cu, bu_, act, dh, T)
+    check_grads(got, want, T)
+    for a, b in zip(got, nb.gated_ffn_backward(neg, s, codes, dh)):
+        assert torch.equal(a, b)

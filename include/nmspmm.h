@@ -547,8 +547,9 @@ typedef struct nm_scaled_weight {
  * the sum exact, scaled in binary32 (as (sum * sx) * scale + bias) and rounded once to
  * `type`.  xq device int8 [m x desc->k], sx device float32 [m], as
  * nm_quantize_rows writes them (what the padding of xq holds does not matter); y
- * device [m] rows of ldy >= n values.  nm_linear_i8 takes x instead (device [m]
- * rows of ldx >= k values of xtype) and makes the codes itself.
+ * device [m] rows of ldy >= n values, apart from xq, sx and the weight.
+ * nm_linear_i8 takes x instead (device [m] rows of ldx >= k values of xtype) and
+ * makes the codes itself; its y may share memory with x.
  * ws: nm_linear_workspace bytes of device memory, any content, 256-byte
  * aligned (NULL where that is 0); xtype 0 asks for the size that
  * nm_gemm_i8_scaled needs.  m == 0 is a no-op.  The sums of a row hold in int32

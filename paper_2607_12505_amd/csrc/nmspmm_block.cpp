@@ -311,6 +311,15 @@ bool takes_values(const void *x, int64_t ldx, int m, int k) {
     return few_takes_values(m, k) && ldx % 8 == 0 && aligned(x, 16);
 }
 
+// Whether m rows of `wide_a` bytes every `step_a` from a and m of b share a byte.  Rows of
+// one stride that lie side by side do not.
+bool rows_meet(const void *a, int64_t step_a, int64_t wide_a, const void *b, int64_t step_b, int64_t wide_b, int m) {
+    const int64_t off = (int64_t)((uintptr_t)b - (uintptr_t)a);
+    if (off >= (m - 1) * step_a + wide_a || -off >= (m - 1) * step_b + wide_b) return false;
+    const int64_t side = ((off % step_a) + step_a) % step_a;
+    return step_a != step_b || side < wide_a || side + wide_b > step_a;
+}
+
 // ws: room for the expanded weight where there is one.
 nm_status run_product(const Product &p, char *ws, void *stream) {
     const nm_desc &d = *p.w->desc;
@@ -393,7 +402,11 @@ nm_status product_of_rows(const void *x, int64_t ldx, int xtype, int m, const nm
     if (ldx < w->k) return NM_ERR_SHAPE;
     if (m == 0) return NM_OK;
     if (!x || !aligned(x, type_bytes(xtype))) return NM_ERR_ARG;
-    if (takes_values(x, ldx, m, w->k)) {
+    // (a workgroup of that kernel reads x while others have written their outputs: where the two share
+    // memory the codes are made first)
+    const int xb = type_bytes(xtype), ob = type_bytes(type);
+    if (takes_values(x, ldx, m, w->k) &&
+        !rows_meet(x, ldx * xb, (int64_t)w->k * xb, out, ldo * ob, (int64_t)w->n * ob, m)) {
         Product p = {nullptr, nullptr, m, w, out, ldo, type, gated, act};
         p.x = x;
         p.ldx = ldx;

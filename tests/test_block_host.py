@@ -218,3 +218,21 @@ def test_padding_codes_refuses():
     assert f(NUL, 100, 0, 100, NUL, NUL) == 0
     if no_gpu():
         assert f(FAKE + 1, 101, 4, 100, FAKE, NUL) == HIP
+
+
+def test_outputs_in_the_memory_of_x_are_not_written_while_it_is_read():
+    # few tokens of values go to one kernel that reads x until its end and needs no workspace; where the output shares
+    # memory with x the codes are made first, in a workspace
+    f, g, lin, gated = L.nm_linear_i8, L.nm_gated, weight(k=64), weight(n=32, k=64)
+    x, one = FAKE, NUL
+    meets = [(x, 64, 1, 64, 4), (x + 2, 64, 1, 64, 4), (x - 64, 64, 1, 64, 1), (x + 3 * 128 + 126, 64, 1, 64, 4),
+             (x, 64, 3, 64, 4), (x + 64, 128, 1, 128, 4), (x + 192, 128, 1, 128, 4), (x, 100, 1, 64, 16)]
+    apart = [(x - 512, 64, 1, 64, 4), (x + 4 * 128, 64, 1, 64, 4), (x + 128, 128, 1, 128, 4), (x - 128, 128, 1, 128, 4),
+             (x + 128, 64, 1, 64, 1)]
+    for out, ldo, otype, ldx, m in meets:
+        assert f(x, ldx, 1, m, ctypes.byref(lin), out, ldo, otype, one, 0, NUL) == WS, (out - x, ldo, otype, ldx, m)
+        if out % 128 == 0:
+            assert g(x, ldx, 1, m, ctypes.byref(gated), 1, out, ldo, otype, one, 0, NUL) == WS
+    if no_gpu():       # (the launch fails: the one kernel was chosen)
+        for out, ldo, otype, ldx, m in apart:
+            assert f(x, ldx, 1, m, ctypes.byref(lin), out, ldo, otype, one, 0, NUL) == HIP, (out - x, ldo, ldx, m)

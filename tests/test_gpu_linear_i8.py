@@ -216,3 +216,23 @@ def test_long_reductions_by_sampled_rows(N, M, m, k, n):
     rows = torch.cat([torch.arange(0, 4), torch.arange(m - 4, m), torch.randint(0, m, (120,), generator=g)])
     check(x[rows], w, c, b, got[rows], torch.half)
     assert (out[m:] == 7).all()
+
+
+# one kernel of values, and codes first: in place, shifted by less than a row, in the columns beside x
+@pytest.mark.parametrize("m", [1, 2, 7, 16, 17, 300])
+@pytest.mark.parametrize("T", [torch.float16, torch.float32])
+def test_outputs_in_the_memory_of_x(m, T):
+    g = gen(m)
+    k = 256
+    (w, c), (v, e) = bu.weight(g, k, k), bu.weight(g, k, k)
+    x = torch.randn(m, k, generator=g).to(T).cuda()
+    for call, weight in ((nb.linear_i8, nb.ScaledWeight.from_int8(w, c)),
+                         (nb.gated_ffn, nb.GatedWeight.from_int8(w, c, v, e))):
+        want = call(x, weight)
+        same = x.clone()
+        assert torch.equal(call(same, weight, out=same), want)
+        for shift in (8, 64, k):
+            wide = torch.zeros(m, 2 * k, dtype=T, device="cuda")
+            wide[:, :k] = x
+            assert torch.equal(call(wide[:, :k], weight, out=wide[:, shift:shift + k]), want)
+            assert torch.equal(wide[:, :min(shift, k)], x[:, :shift])

@@ -376,3 +376,33 @@ def test_absent_gradient_of_z_adds_nothing(T, m, d, post_kind):
     got = nb.norm_residual_backward(None, dres, y, res, pre=pre, post=post, gate=gate, alpha=0.5)
     check_grads(got, bu.norm_grads(None, dres, y, res, p64, q64, gate, 0.5), T, m)
     assert (got.dpre_weight == 0).all() and (got.dpre_bias == 0).all()
+
+
+# more groups than runs of rows: the sums of a group that runs share are found from the runs' ends
+@pytest.mark.parametrize("T", [torch.float16, torch.float32])
+@pytest.mark.parametrize("m,d,groups", [(12000, 40, 4000), (12345, 16, 4115), (9999, 24, 3333), (20000, 72, 10000),
+                                        (6150, 520, 3075), (1030, 9000, 515)])
+def test_backward_of_more_groups_than_runs(T, m, d, groups):
+    g = gen(m + groups)
+    pre, p64 = norm_of(g, d, "rms", with_bias=False)
+    post, q64 = norm_of(g, d, "layer")
+    y, res, dz = (rows(g, m, d, T) for _ in range(3))
+    gate = torch.randn(groups, d, generator=g).cuda()
+    got = nb.norm_residual_backward(dz, None, y, res, pre=pre, post=post, gate=gate)
+    check_grads(got, bu.norm_grads(dz, None, y, res, p64, q64, gate, 1.0), T, m)
+    again = nb.norm_residual_backward(dz, None, y, res, pre=pre, post=post, gate=gate)
+    assert all(torch.equal(a, b) for a, b in zip(got, again) if a is not None)
+
+
+def test_backward_of_a_gate_for_each_of_millions_of_groups():
+    # (more than 2^32 work items if every group had a workgroup for its sums)
+    groups, d = (1 << 22) + 5, 3
+    g = torch.Generator(device="cuda").manual_seed(1)
+    y, dres = (torch.randn(3 * groups, d, generator=g, device="cuda") for _ in range(2))
+    gate = torch.randn(groups, d, generator=g, device="cuda")
+    del_me = torch.full((groups, d), float("nan"), device="cuda")
+    del del_me                                      # (what the gate's gradient may be given)
+    got = nb.norm_residual_backward(None, dres, y, None, gate=gate, alpha=2.0)
+    assert torch.equal(got.dr, 2 * dres) and torch.equal(got.dy, dres * gate.repeat_interleave(3, 0))
+    terms = (dres.double() * y.double()).view(groups, 3, d)
+    assert ((got.dgate - terms.sum(1)).abs() <= 3 * bu.E * terms.abs().sum(1)).all()

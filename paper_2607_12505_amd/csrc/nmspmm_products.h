@@ -168,13 +168,20 @@ struct ScaledOut {
     }
 };
 
-// act(g) and its derivative.  The exponential is the hardware's (2^x within an
-// ulp, its argument rounded to binary32), the reciprocal within an ulp: a few
-// 2^-24 of act(g), under the rounding to T of what they enter.  The normal
-// distribution function of gelu is formula 7.1.26 of Abramowitz and Stegun,
-// Handbook of Mathematical Functions (1964): erf within 1.5e-7, on the
-// exponential that the derivative needs as well.  (erfcf of the library took half of the backward pass's
-// first kernel.)
+// act(g) and its derivative.  In steps of 2^-24 of the value: the exponential of sigmoid
+// is the hardware's (2^x within an ulp, 2 steps) of an argument that is rounded to binary32, the
+// reciprocal within an ulp, so silu and sigmoid are within 6 + 2 |g| steps and
+// tanh gelu within 6 + 8 a, a = 2 sqrt(2 / pi) (|g| + 0.044715 |g|^3) its sigmoid's argument: under the
+// rounding to binary16 or bfloat16 wherever the value is above 2^-100, in binary32 a few bits
+// less in the far negative tail.
+//   The normal distribution function of gelu: its tail at x = |g| is exp(-x^2 / 2) r(t), r a
+// polynomial of t = 1 / (1 + p x).  p and the eight coefficients were fitted here (least squares,
+// weighted until the largest relative error was least) to exp(x^2 / 2) erfc(x / sqrt(2)) / 2 for x to 16:
+// 1.3e-7 of its value.  The roundings of the square and of its product with log2(e) / 2
+// come back as a correction of the exponential, so gelu is within 32 steps down to g = -12,
+// and 0 past -13.  (Formula 7.1.26 of Abramowitz and Stegun, Handbook of Mathematical
+// Functions, 1964, is shorter but holds in absolute terms only: 1.6e-3 of gelu(-5).  erfcf of the
+// library took half of the backward pass's first kernel.)
 __device__ __forceinline__ float sigmoid(float g) {
     return __builtin_amdgcn_rcpf(1.f + __expf(-g));
 }
@@ -190,13 +197,24 @@ __device__ __forceinline__ void act_and_slope(int act, float g, float &f, float 
         f = g > 0.f || g != g ? g : 0.f;
         df = g > 0.f ? 1.f : 0.f;
     } else if (act == NM_ACT_GELU) {
-        const float x = __builtin_fabsf(0.70710678118654752f * g), e = __expf(-x * x);
-        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.f));
-        float q = __builtin_fmaf(1.061405429f, t, -1.453152027f);
-        q = __builtin_fmaf(q, t, 1.421413741f);
-        q = __builtin_fmaf(q, t, -0.284496736f);
-        q = __builtin_fmaf(q, t, 0.254829592f);
-        const float tail = 0.5f * q * t * e;          // of the side that g is on
+        // past 16 the tail is 0, and an infinite square would make NaN of its correction
+        const float x = __builtin_fminf(__builtin_fabsf(g), 16.f), h = x * x, h_lost = __builtin_fmaf(x, x, -h);
+        constexpr float kHalf = -0.72134752f, kHalfLost = -9.6298e-9f;        // -log2(e) / 2
+        const float y = kHalf * h;
+        float lost = __builtin_fmaf(kHalf, h, -y);
+        lost = __builtin_fmaf(kHalf, h_lost, lost);
+        lost = __builtin_fmaf(kHalfLost, h, lost);
+        float e = __builtin_amdgcn_exp2f(y);
+        e = __builtin_fmaf(e, 0.69314718f * lost, e);
+        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.30759144f, x, 1.f));
+        float q = __builtin_fmaf(0.03628652f, t, -0.14714111f);
+        q = __builtin_fmaf(q, t, 0.16965123f);
+        q = __builtin_fmaf(q, t, -0.025647799f);
+        q = __builtin_fmaf(q, t, 0.11512103f);
+        q = __builtin_fmaf(q, t, 0.10576676f);
+        q = __builtin_fmaf(q, t, 0.12327715f);
+        q = __builtin_fmaf(q, t, 0.12268628f);
+        const float tail = q * t * e;                 // of the side that g is on
         const float p = g > 0.f ? 1.f - tail : tail;
         f = g * p;
         df = __builtin_fmaf(0.39894228040143268f * g, e, p);

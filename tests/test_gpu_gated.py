@@ -223,3 +223,21 @@ def test_scales_of_either_sign(T, m, k, n):
     check_grads(got, want, T)
     for a, b in zip(got, nb.gated_ffn_backward(neg, s, codes, dh)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("T", bu.TYPES)
+def test_gelu_keeps_its_relative_accuracy_in_the_tail(T):
+    # g is given exactly (one code of 1 a row, its scale |g|), u is 1.  In units of 2^-24 of the result: the fitted
+    # tail 2.6; its argument, a rounded product and sum and a reciprocal within an ulp, 2.5 times up to 2.6; eight steps of
+    # Horner's rule at 1.75 times their result 14; the exponential and its correction 4; three products 3: 31.
+    g = torch.cat([torch.linspace(-12, 12, 4001), torch.tensor([0.0, 100.0, 3e38, -100.0, -1e30])])
+    q = torch.zeros(len(g), 16, dtype=torch.int8)
+    q[:, 0] = torch.sign(g)
+    one, zero = torch.ones(3, 1, dtype=torch.int8), torch.zeros(3)
+    w = nb.GatedWeight.from_int8(one, zero + 1, 0 * one, zero + 1, bias_gate=zero, bias_up=zero + 1, act="gelu")
+    h = nb.gated_ffn_i8(q.cuda(), g.abs().cuda(), w, out_dtype=T)
+    v = g.double()
+    want = (v * 0.5 * torch.special.erfc(-v / 2 ** 0.5))[:, None].expand(-1, 3)
+    if T == torch.float16:
+        want = torch.where(want > 65519.0, torch.inf, want)
+    bu.close(h, want, T, want.abs(), 32)

@@ -12,7 +12,9 @@
 Tensors are device tensors of float16, bfloat16 or float32, [..., channels] with consecutive channels; two-dimensional
 inputs may have any row stride.  Parameters are float32.  Every call enqueues its kernels on `stream` (a
 torch.cuda.Stream; the current one without it) and returns; outputs that are not given are allocated for that stream.
-There is no fallback: a missing library raises.
+Tensors are used as they are: no call records an autograd graph, and outputs never require gradients (the gradients are
+the `_backward` functions' to give).  A given output counts as modified in place, so that torch refuses to go back through
+what it held.  There is no fallback: a missing library raises.
 """
 from __future__ import annotations
 
@@ -124,11 +126,17 @@ def _like(t, stream, rt: _Runtime):
     return _empty(t.shape, t.dtype, t, stream, rt)
 
 
+def _written(t, rt: _Runtime):
+    """t, its version moved as torch's own in-place operations move it."""
+    rt.torch.autograd.graph.increment_version(t)
+    return t
+
+
 def _output(given, name: str, shape, dtype, like, stream, rt: _Runtime):
     if given is None:
         return _empty(shape, dtype, like, stream, rt)
     _param(given, name, tuple(shape), dtype, like.get_device())
-    return given
+    return _written(given, rt)
 
 
 def padded(k: int) -> int:
@@ -503,7 +511,8 @@ def _product_out(out, m: int, shape, dtype, like, stream, rt):
     if out.dtype != dtype or tuple(out.shape) != tuple(shape):
         raise ValueError(f"out: {out.dtype} {tuple(out.shape)}, expected {dtype} {tuple(shape)}")
     _on(out, "out", like.get_device())
-    return out, _type_of(out, "out", rt), _rows(out, "out")[2]
+    code, ld = _type_of(out, "out", rt), _rows(out, "out")[2]
+    return _written(out, rt), code, ld
 
 
 _FEW = 16      # most tokens of a call that makes its codes in the product's own launch

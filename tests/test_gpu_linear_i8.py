@@ -236,3 +236,37 @@ def test_outputs_in_the_memory_of_x(m, T):
             wide[:, :k] = x
             assert torch.equal(call(wide[:, :k], weight, out=wide[:, shift:shift + k]), want)
             assert torch.equal(wide[:, :min(shift, k)], x[:, :shift])
+
+
+def test_given_outputs_count_as_written():
+    # torch refuses to go back through a tensor that was overwritten after it was saved
+    x = torch.randn(20, 64, device="cuda").half()
+    pre = nb.Norm("rms", torch.ones(64).cuda())
+    like = {"res": x.clone(), "z": x.clone()}
+    nb.norm_residual(x, x, pre=pre, **like)
+    q, s = nb.quantize_rows(x)
+    codes = {"zq": q.clone(), "zs": s.clone(), "res": x.clone()}
+    nb.norm_residual_i8(x, None, pre=pre, **codes)
+    rows_ = {"xq": q.clone(), "scale": s.clone()}
+    nb.quantize_rows(x, **rows_)
+    padded = q.clone()
+    nb.pad_codes(q, out=padded)
+    one = torch.ones(64, 64, dtype=torch.int8)
+    lin = nb.ScaledWeight.from_int8(one, torch.ones(64))
+    gated = nb.GatedWeight.from_int8(one, torch.ones(64), one, torch.ones(64))
+    outs = [x.clone() for _ in range(4)]
+    nb.linear_i8(x, lin, out=outs[0])
+    nb.gemm_i8_scaled(q, s, lin, out=outs[1])
+    nb.gated_ffn(x, gated, out=outs[2])
+    nb.gated_ffn_i8(q, s, gated, out=outs[3])
+    for t in (*like.values(), *codes.values(), *rows_.values(), padded, *outs):
+        assert t._version == 1
+
+
+def test_given_outputs_of_inference_mode():
+    one = torch.ones(32, 32, dtype=torch.int8)
+    lin = nb.ScaledWeight.from_int8(one, torch.ones(32))
+    with torch.inference_mode():
+        x = torch.ones(3, 32, device="cuda")
+        out = torch.empty(3, 32, device="cuda")
+        assert (nb.linear_i8(x, lin, out=out) - 32).abs().max() < 1e-4 and nb.quantize_rows(x, scale=out[:, 0].clone())

@@ -210,23 +210,35 @@ nm_status check_weight(const nm_scaled_weight *w, bool gated) {
     return NM_OK;
 }
 
-// Whether codes of m tokens take the kernel of few tokens.  It repeats the codes for every
-// 16 channels, so it loses where they outweigh its start: of times in us against the tiles',
-// dense weights, 1024 -> 4096 with 1 token 2.7 to 3.4, with 16 3.0 to 3.4, with 32 3.5 to 3.5, with
-// 64 4.6 to 4.5; 4096 -> 1024 with 1 4.5 to 5.3, with 16 5.7 to 5.4, with 32 7.6 to 5.5; 4096 -> 4096 with 1
-// 5.9 to 6.2, with 16 6.9 to 6.3; 4096 -> 11008 with 1 10.8 to 9.8, with 16 13.8 to 9.9.  Weights of
-// 3:8 to 5:8 cost the tiles more, which expand a block for every token tile: 4096 -> 11008 at 4:8
-// with 1 7.7 to 10.7, with 16 10.7 to 10.4; 4096 -> 1024 with 32 5.9 to 6.7.
-bool takes_few(int kind, int64_t m, int64_t n, int64_t k) {
-    const bool masks = layout_mask_values(kind) > 0;
-    if (m <= 16) return masks || n * k <= (1 << 24);
-    return m <= kFewTokens && n * k <= (masks ? 1 << 24 : 1 << 22) && (masks || k <= 1024);
+// Whether codes of m tokens take the kernel of few tokens (n: rows of the weight).  It
+// repeats the codes for every 16 channels, so it loses where they outweigh its start,
+// and with long dense rows of both projections of a gated block.  Times against the tiles'
+// in us, weights from memory, on a grid of k 256 to 16384, n 512 to 32768 (gated: k 512 to 4096) and m to 32:
+//   dense 1024 -> 4096 with 1 token 3.3 to 4.2, with 32 4.1 to 4.6; 4096 -> 4096 with 16 7.2 to 7.2;
+//     2048 -> 6144 with 4 5.6 to 5.4, with 16 6.5 to 5.5; 1024 -> 16384 with 8 5.9 to 6.1, with 16 6.6 to 6.2;
+//     4096 -> 11008 with 16 15.1 to 12.3
+//   gated dense 1024 -> 2 x 4096 with 16 4.7 to 5.0; 2048 -> 2 x 1024 with 4 4.7 to 4.6, with 16 5.1 to 4.6;
+//     4096 -> 2 x 2048 with 1 7.8 to 7.3; 1024 -> 2 x 2048 with 32 4.5 to 4.1, 512 -> 2 x 4096 3.8 to 4.0
+//   2:4 4096 -> 4096 with 16 5.8 to 6.2; 2048 -> 8192 with 8 5.0 to 5.2, with 16 5.6 to 5.3
+//   4:8 (weights of 3:8 to 5:8 cost the tiles more, which expand a block for every token tile) 4096 ->
+//     4096 with 16 5.8 to 9.8, with 32 7.5 to 9.7; 4096 -> 16384 with 16 15.3 to 13.9; 1024 -> 8192 with 32
+//     5.1 to 5.2, 1024 -> 16384 7.9 to 6.7, 2048 -> 6144 7.4 to 6.8
+// Within the rule the grid's worst are 1.12 (dense 256 -> 32768 with 16, 5.8 to 5.2) and 1.10 (4:8 4096 -> 16384 with 16).
+bool takes_few(int kind, bool gated, int64_t m, int64_t n, int64_t k) {
+    const bool dense = kind == NM_KIND_DENSE;
+    if (m > kFewTokens) return false;
+    if (layout_mask_values(kind) > 0)
+        return m <= 16 || (n * k <= 1 << 24 && (n <= 4096 || (n <= 8192 && k <= 1024)));
+    if (m > 16) return n * k <= 1 << 22 && n <= 8192 && k <= (dense && gated ? 512 : 1024);
+    if (n * k > 1 << 24) return false;
+    if (dense && gated) return k <= 1024 || (k <= 2048 && m <= 4);
+    return n <= 4096 || (m * n * k <= 1 << 27 && (!dense || k <= 1024));
 }
 
 // Whether a compact weight is expanded once for the call, and the bytes of that.
 int64_t expansion(const nm_desc &d, int m) {
     nm_plan plan;
-    if (takes_few(d.kind, m, d.n, d.k) || !kind_is_compact(d.kind) ||
+    if (!kind_is_compact(d.kind) || takes_few(d.kind, false, m, d.n, d.k) ||   // (a compact kind: gated or not)
         make_plan(d.kind, m, d.n, d.k, NM_OUT_F16, &plan) != NM_OK)
         return 0;
     return plan.expand ? plan.expand_bytes : 0;
@@ -326,7 +338,7 @@ nm_status run_product(const Product &p, char *ws, void *stream) {
     int kind = d.kind;
     const int8_t *vals = p.w->vals;
     const uint8_t *meta = p.w->meta;
-    if (p.x || takes_few(kind, p.m, d.n, d.k)) {
+    if (p.x || takes_few(kind, p.gated, p.m, d.n, d.k)) {
         BlockArgs a;
         fill_product(a, p.m, *p.w);
         a.X = p.xq;

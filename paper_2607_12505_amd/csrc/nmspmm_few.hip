@@ -14,8 +14,9 @@
 //
 // Measured: one token as values, dense 1024 -> 4096 4.3 us, gated 1024 -> 2736 (twice the
 // weight rows) 4.8 us.  A token's weights are 4 to 6 MB, under 1 us at the memory's rate: what is
-// left is the launch, the wait for x and the weights one after the other, and the sums.  A
-// long weight streams: 4096 -> 11008 from codes, 45 MB, 10.8 us (4.2 TB/s).
+// left is the launch, the wait for x and the weights one after the other, and the sums.  From
+// codes, weights from memory: dense 4096 -> 4096, 17 MB, 6.3 us (2.7 TB/s); 4:8 4096 ->
+// 11008, 28 MB as stored, 8.6 us (3.3 TB/s).
 #include "nmspmm_products.h"
 
 namespace nmspmm {

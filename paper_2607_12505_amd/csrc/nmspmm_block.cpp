@@ -12,7 +12,7 @@ bool aligned(const void *p, int to) { return ((uintptr_t)p & (uintptr_t)(to - 1)
 
 // Whether rows of `width` values with this stride are whole 16-byte pieces at
 // 16-byte boundaries (8 values of a 16-bit type at once, 4 + 4 of binary32).
-bool pieces(const void *p, int64_t ld, int width, int type) {
+bool pieces(const void *p, int64_t ld, int width) {
     return !p || (aligned(p, 16) && ld % 8 == 0 && width % 8 == 0);
 }
 
@@ -52,7 +52,7 @@ extern "C" nm_status nm_quantize_rows(const void *x, int64_t ldx, int type, int 
     a.ldq = round16(k);
     a.m = m;
     a.k = k;
-    return launch_quantize_rows(type, pieces(x, ldx, k, type), a, stream) == 0 ? NM_OK : NM_ERR_HIP;
+    return launch_quantize_rows(type, pieces(x, ldx, k), a, stream) == 0 ? NM_OK : NM_ERR_HIP;
 }
 
 extern "C" nm_status nm_pad_codes(const int8_t *q, int64_t ldq, int m, int k, int8_t *out, void *stream) {
@@ -96,8 +96,8 @@ extern "C" nm_status nm_norm_residual(const nm_norm_args *args, void *stream) {
     a.groups = g.y ? g.groups : 1;
     a.per_group = g.m / a.groups;
     a.alpha = g.r ? g.alpha : 0.f;
-    const bool vec = pieces(g.y, g.ldy, g.d, g.type) && pieces(g.r, g.ldr, g.d, g.type) &&
-                     pieces(g.res, g.d, g.d, g.type) && pieces(g.z, g.d, g.d, g.type) && g.d % 8 == 0;
+    const bool vec = pieces(g.y, g.ldy, g.d) && pieces(g.r, g.ldr, g.d) &&
+                     pieces(g.res, g.d, g.d) && pieces(g.z, g.d, g.d) && g.d % 8 == 0;
     return launch_norm_residual(g.type, vec, a, stream) == 0 ? NM_OK : NM_ERR_HIP;
 }
 
@@ -179,9 +179,9 @@ extern "C" nm_status nm_norm_residual_backward(const nm_norm_grad_args *args, vo
     a.groups = g.groups;
     a.per_group = g.m / g.groups;
     a.alpha = g.alpha;
-    const bool vec = pieces(a.y, g.ldy, g.d, g.type) && pieces(g.res, g.ldres, g.d, g.type) &&
-                     pieces(g.dz, g.lddz, g.d, g.type) && pieces(g.dres, g.lddres, g.d, g.type) &&
-                     pieces(g.dy, g.d, g.d, g.type) && pieces(g.dr, g.d, g.d, g.type) && g.d % 8 == 0;
+    const bool vec = pieces(a.y, g.ldy, g.d) && pieces(g.res, g.ldres, g.d) &&
+                     pieces(g.dz, g.lddz, g.d) && pieces(g.dres, g.lddres, g.d) &&
+                     pieces(g.dy, g.d, g.d) && pieces(g.dr, g.d, g.d) && g.d % 8 == 0;
     const NormGradShape s = norm_grad_shape(g.m, g.d, vec, a.post.kind != NM_NORM_NONE && a.y);
     a.runs = s.runs;
     a.turns = s.turns;

@@ -86,7 +86,7 @@ struct BlockArgs : GemmArgs {
     int64_t lddh = 0;
     void *da = nullptr, *dat = nullptr; // [m x n], [n x ldt]
     int64_t ldt = 0;
-    float *bias_parts = nullptr;        // [16-row-of-tokens groups of waves x n] or null
+    float *bias_parts = nullptr;        // [rows of waves x n] or null: a row for each wave's tokens of a tile
     void *out2 = nullptr;               // second half of interleaved rows
     int interleaved = 0;
 };

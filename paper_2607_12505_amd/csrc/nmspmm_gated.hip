@@ -10,8 +10,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) void k
     constexpr RowTile t = kRowTileShape;
     using G = RowGeometry<t.wn, t.wm, t.fn, t.fm>;
     __shared__ __attribute__((aligned(1024))) int8_t lds[G::LDSB];
-    __shared__ int s_last;
-    gemm_rows<NM_KIND_DENSE, t.wn, t.wm, t.fn, t.fm, GatedOut>(a, lds, &s_last);
+    gemm_rows<t.wn, t.wm, t.fn, t.fm, GatedOut>(a, lds);
 }
 
 }  // namespace

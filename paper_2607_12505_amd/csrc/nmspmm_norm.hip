@@ -716,9 +716,8 @@ int grad_by_width(const NormGradArgs &a, int workgroups, void *stream) {
     if (a.d <= 4096) return grad_one<T, VEC, half, 8, POST>(a, workgroups, stream);
     // 16 waves leave a wave 128 registers: with both norms' sums 8 waves of twice the
     // channels are faster (2048 x 8192 bf16: 73 us against 139)
-    if constexpr (VEC == 8 && POST)
-        if (a.d <= 8192) return grad_one<T, VEC, 2 * half, 8, POST>(a, workgroups, stream);
-    if (a.d <= 8192) return grad_one<T, VEC, half, 16, POST>(a, workgroups, stream);
+    constexpr bool wide = VEC == 8 && POST;
+    if (a.d <= 8192) return grad_one<T, VEC, wide ? 2 * half : half, wide ? 8 : 16, POST>(a, workgroups, stream);
     return grad_one<T, VEC, 2 * half, 16, POST>(a, workgroups, stream);
 }
 template <class T>

@@ -1,4 +1,4 @@
-// A k-loop for products whose operands are both plain rows (a dense weight) and
+// A k-loop for int8 products whose operands are both plain rows (a dense weight) and
 // whose epilogue is long: tiles of 256 x 160 on 8 waves whose ring of three 64-byte
 // k-steps takes half of a compute unit's LDS, so two workgroups share it and one
 // multiplies while the other starts, waits at its barrier or runs its epilogue.  At
@@ -28,29 +28,25 @@ struct RowGeometry {
     static constexpr int stage_bytes(int eb) { return stage_rows(eb) * (FN * 16 * eb + 16); }
     static constexpr int STG = stage_bytes(4) > stage_bytes(1) ? stage_bytes(4) : stage_bytes(1);
     static constexpr int LDSB = R * SLOT;
-    static_assert(NW * STG <= LDSB && 2 * (LDSB + 64) <= 160 * 1024 && 64 % CPR == 0, "two workgroups a compute unit");
+    static_assert(NW * STG <= LDSB && 2 * LDSB <= 160 * 1024 && 64 % CPR == 0, "two workgroups a compute unit");
 };
 
-template <int KIND, int WN, int WM, int FN, int FM, class EPI, class ARGS>
-__device__ __forceinline__ void gemm_rows(const ARGS &a, int8_t *lds, int *s_last) {
+template <int WN, int WM, int FN, int FM, class EPI, class ARGS>
+__device__ __forceinline__ void gemm_rows(const ARGS &a, int8_t *lds) {
     using G = RowGeometry<WN, WM, FN, FM>;
-    using Acc = typename Kind<KIND>::Acc;
     constexpr int BN = G::BN, BM = G::BM, NW = G::NW, R = G::R;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t *)lds;
 
     const int lid = map_block(blockIdx.x, gridDim.x);
-    int tn, rest;
-    tile_order(lid, a.tiles_n, a.tiles_m * a.split_k, a.group_rows, &tn, &rest);
-    const int split = rest % a.split_k, tm = rest / a.split_k;
+    int tn, tm;
+    tile_order(lid, a.tiles_n, a.tiles_m, a.group_rows, &tn, &tm);
     const int tid = threadIdx.x, lane = tid & 63, lg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wn = wave % WN, wm = wave / WN;
     const int tok0 = tm * BM, ch0 = tn * BN;
-    const int all = (a.k + 63) >> 6;
-    const int s_begin = (int)((int64_t)split * all / a.split_k), s_end = (int)((int64_t)(split + 1) * all / a.split_k);
-    const int nsteps = s_end - s_begin;
+    const int nsteps = (a.k + 63) >> 6;
     const int ragged = a.k & 63;                                         // bytes of the last k-step, if it is short
-    const int t_tail = ragged && s_end == all ? nsteps - 1 : -1;
+    const int t_tail = ragged ? nsteps - 1 : -1;
 
     // --- loads.  Instruction q of a k-step: 16 rows, lane L row L / 4 and, at
     // place L % 4, the row's chunk (L % 4) ^ ((row / 2) % 4): eight consecutive rows
@@ -73,7 +69,7 @@ __device__ __forceinline__ void gemm_rows(const ARGS &a, int8_t *lds, int *s_las
             const int q = NW * c + wave;
             const bool x = NW * c + NW <= G::XC || (NW * c < G::XC && q < G::XC);
             const int l = NW * c + NW <= G::NC || q < G::NC ? live : 0;
-            dma16o_if((x ? xp : wp) + (uint64_t)(s_begin + t) * 64, off[c], lds0 + st * G::SLOT + q * 1024,
+            dma16o_if((x ? xp : wp) + (uint64_t)t * 64, off[c], lds0 + st * G::SLOT + q * 1024,
                       __builtin_amdgcn_readfirstlane(l));
         }
     };
@@ -97,11 +93,11 @@ __device__ __forceinline__ void gemm_rows(const ARGS &a, int8_t *lds, int *s_las
         wait_then_barrier<63>();
     };
 
-    Acc acc[FN][FM];
+    v4i acc[FN][FM];
 #pragma unroll
     for (int i = 0; i < FN; ++i)
 #pragma unroll
-        for (int j = 0; j < FM; ++j) acc[i][j] = Acc{0, 0, 0, 0};
+        for (int j = 0; j < FM; ++j) acc[i][j] = v4i{0, 0, 0, 0};
 
     const int sw = (lg ^ ((lane >> 1) & 3)) << 4;                        // the lane's chunk of its row
     const int8_t *xrow = lds + (wm * FM * 16 + (lane & 15)) * 64 + sw;
@@ -129,7 +125,7 @@ __device__ __forceinline__ void gemm_rows(const ARGS &a, int8_t *lds, int *s_las
 #pragma unroll
         for (int j = 0; j < FM; ++j)
 #pragma unroll
-            for (int i = 0; i < FN; ++i) acc[i][j] = mfma_rows<KIND>(w[i], x[j], acc[i][j]);
+            for (int i = 0; i < FN; ++i) acc[i][j] = mfma_rows<NM_KIND_DENSE>(w[i], x[j], acc[i][j]);
         st = st + 1 == R ? 0 : st + 1;
     }
     wait_only<0>();
@@ -141,8 +137,8 @@ __device__ __forceinline__ void gemm_rows(const ARGS &a, int8_t *lds, int *s_las
         const int ch = c0 + i * 16;
         return *(const v4f *)((h ? second : first) + (ch < a.n ? ch : 0));
     };
-    EPI::template finish<G>(a, TileAt{tok0 + wm * FM * 16, ch0 + wn * FN * 16, split, tm, tn, lane}, acc,
-                            lds + wave * G::STG, multiplier, s_last);
+    EPI::template finish<G>(a, TileAt{tok0 + wm * FM * 16, ch0 + wn * FN * 16, 0, tm, tn, lane}, acc,
+                            lds + wave * G::STG, multiplier, nullptr);
 }
 
 }  // namespace

@@ -241,3 +241,18 @@ def test_gelu_keeps_its_relative_accuracy_in_the_tail(T):
     if T == torch.float16:
         want = torch.where(want > 65519.0, torch.inf, want)
     bu.close(h, want, T, want.abs(), 32)
+
+
+# the tile of which two workgroups share a compute unit: every type of its staging, biases, activations and a last k-step
+# of 16, 48 and 64 bytes
+@pytest.mark.parametrize("T", bu.TYPES)
+@pytest.mark.parametrize("m,k,n,act", [(20011, 208, 701, "gelu"), (18464, 1000, 830, "relu"), (33000, 64, 515, "gelu_tanh"),
+                                       (20000, 72, 700, "sigmoid")])
+def test_two_workgroups_a_unit_by_sampled_rows(T, m, k, n, act):
+    x, w, plain, g = case(m, k, n, T, True, act=act)
+    out = torch.full((m + 1, n + 5), 7.0, dtype=T, device="cuda")
+    h = nb.gated_ffn(x, w, out=out[:m, 2:n + 2])
+    rows = torch.cat([torch.arange(0, 4), torch.arange(m - 4, m), torch.randint(0, m, (100,), generator=g)])
+    want, mag = bu.gated(*bu.codes(x[rows]), *plain)
+    bu.close(h[rows], want, T, mag, 4)
+    assert (out[m:] == 7).all() and (out[:, :2] == 7).all() and (out[:, n + 2:] == 7).all()

@@ -270,3 +270,24 @@ def test_given_outputs_of_inference_mode():
         x = torch.ones(3, 32, device="cuda")
         out = torch.empty(3, 32, device="cuda")
         assert (nb.linear_i8(x, lin, out=out) - 32).abs().max() < 1e-4 and nb.quantize_rows(x, scale=out[:, 0].clone())
+
+
+@pytest.mark.parametrize("N,M", [(8, 8), (2, 4)])
+def test_codes_past_2_to_the_32_bytes(N, M):
+    # the kernels address codes with 32-bit offsets: such a batch goes in parts, here of 32000 and 1003 tokens
+    g = gen(N)
+    m, k, n = 33003, (1 << 17) - 16, 20
+    (w, c), (v, e) = bu.weight(g, n, k, N, M), bu.weight(g, n, k, N, M)
+    c, e = c / 1e4, e / 1e4
+    q = torch.randint(-127, 128, (m, k), generator=torch.Generator(device="cuda").manual_seed(N), device="cuda",
+                      dtype=torch.int8)
+    s = torch.exp(torch.randn(m, generator=g)).cuda()
+    lin = nb.ScaledWeight.from_int8(w, c, N=N, M=M)
+    gated = nb.GatedWeight.from_int8(w, c, v, e, act="relu", N=N, M=M)
+    y, h = nb.gemm_i8_scaled(q, s, lin, out_dtype=torch.float32), nb.gated_ffn_i8(q, s, gated, out_dtype=torch.float32)
+    rows = torch.cat([torch.arange(0, 3), torch.arange(31998, 32003), torch.arange(m - 3, m),
+                      torch.randint(0, m, (20,), generator=g)])
+    want, mag = bu.product(q[rows.cuda()], s[rows.cuda()], w, c, None)
+    bu.close(y[rows.cuda()], want, torch.float32, mag, 4)
+    want, mag = bu.gated(q[rows.cuda()], s[rows.cuda()], w, c, None, v, e, None, "relu")
+    bu.close(h[rows.cuda()], want, torch.float32, mag, 4)

@@ -521,9 +521,11 @@ __attribute__((amdgpu_waves_per_eu(grad_waves(WPR, VEC, CH, POST)))) void k_norm
 // col_blocks - 1 take one kind of sum and 16 channels each, 64 groups of 16 lanes
 // going through the workgroups in turn.  The others join the gate groups that several
 // runs share: few groups, of many runs each, 64 channels a workgroup, 16 waves going through
-// the runs; many, of few runs each, 256 channels a wave.  Such a group holds the first row
-// of a run, so where there are more groups than runs those of the runs' first rows
-// are enough.  256 workgroups' sums of 1024 channels: 5.2 MB, 4.0 us.
+// the runs; many groups (MANY: under 16 runs each), 256 channels a wave.  Such a group
+// holds the first row of a run, so where there are more groups than runs those of the
+// runs' first rows are enough.  256 workgroups' sums of 1024 channels: 5.2 MB, 4.0 us.  The
+// whole backward pass of 18464 x 1024 bf16 with 1154 groups takes 54 us (a workgroup for each
+// group and 64 channels: 105), with a group a token 85 (858).
 template <int WIDE>
 __device__ __forceinline__ void add_turns(float *part, float s, float *dst, bool in) {
     constexpr int TURNS = 1024 / WIDE;
@@ -545,16 +547,7 @@ __device__ __forceinline__ void add_turns(float *part, float s, float *dst, bool
     }
 }
 
-// Where the groups that runs share are looked for: at each group, or at the runs' ends.
-struct GateSums {
-    bool by_run, by_wave;
-    int places, pieces;          // and the pieces of a row of channels
-    __host__ __device__ GateSums(const NormGradArgs &a)
-        : by_run(a.groups >= a.runs), by_wave(a.runs < 16 * (int64_t)a.groups), places(by_run ? a.runs - 1 : a.groups),
-          pieces(by_wave ? (a.d + 255) / 256 : (a.d + 63) / 64) {}
-    int workgroups() const { return by_wave ? (places * pieces + 15) / 16 : places * pieces; }
-};
-
+template <bool MANY>
 __global__ __launch_bounds__(1024) void k_norm_sums(NormGradArgs a, int workgroups, int col_blocks) {
     __shared__ float part[64 * 17];
     float s = 0.f;
@@ -571,40 +564,37 @@ __global__ __launch_bounds__(1024) void k_norm_sums(NormGradArgs a, int workgrou
         }
         add_turns<16>(part, s, dst + ch, ch < a.d);
     } else {
-        const GateSums sums(a);
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-        const int b = (int)blockIdx.x - 5 * col_blocks, item = sums.by_wave ? b * 16 + wave : b;
-        const int place = item / sums.pieces, piece = item % sums.pieces;
-        if (place >= sums.places) return;
-        const int group = sums.by_run ? first_row(place + 1, a.m, a.runs) / a.per_group : place;
+        const int b = blockIdx.x - 5 * col_blocks;
+        const int wide = MANY ? (a.d + 255) / 256 : (a.d + 63) / 64;
+        const int item = MANY ? b * 16 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : b;
+        const bool by_run = MANY && a.groups >= a.runs;
+        const int place = item / wide, group = by_run ? first_row(place + 1, a.m, a.runs) / a.per_group : place;
+        if (MANY && place >= (by_run ? a.runs - 1 : a.groups)) return;
         const int t0 = run_of(group * a.per_group, a.m, a.runs), t1 = run_of((group + 1) * a.per_group - 1, a.m, a.runs);
-        if (t0 == t1) return;                       // within one run: finished there
-        if (sums.by_run && t0 != place) return;     // begins in another run, whose end has it (or a later one's)
+        if (t0 == t1) return;              // within one run: finished there
+        if (by_run && t0 != place) return; // begins in another run, whose end has it (or a later one's)
         const auto left = [&](int t) {
             return a.gate_parts + ((int64_t)2 * t + (group == first_row(t, a.m, a.runs) / a.per_group ? 0 : 1)) * a.d;
         };
         float *dst = a.dgate + (int64_t)group * a.d;
-        if (sums.by_wave) {
+        if constexpr (MANY) {
+            const int ch0 = item % wide * 256 + (threadIdx.x & 63);
             float sum[4] = {};
             for (int t = t0; t <= t1; ++t) {
                 const float *src = left(t);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int ch = piece * 256 + q * 64 + lane;
-                    if (ch < a.d) sum[q] += src[ch];
-                }
+                for (int q = 0; q < 4; ++q)
+                    if (ch0 + q * 64 < a.d) sum[q] += src[ch0 + q * 64];
             }
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int ch = piece * 256 + q * 64 + lane;
-                if (ch < a.d) dst[ch] = sum[q];
-            }
-            return;
+            for (int q = 0; q < 4; ++q)
+                if (ch0 + q * 64 < a.d) dst[ch0 + q * 64] = sum[q];
+        } else {
+            const int ch = item % wide * 64 + (threadIdx.x & 63);
+            if (ch < a.d)
+                for (int t = t0 + (threadIdx.x >> 6); t <= t1; t += 16) s += left(t)[ch];
+            add_turns<64>(part, s, dst + ch, ch < a.d);
         }
-        const int ch = piece * 64 + lane;
-        if (ch < a.d)
-            for (int t = t0 + wave; t <= t1; t += 16) s += left(t)[ch];
-        add_turns<64>(part, s, dst + ch, ch < a.d);
     }
 }
 
@@ -778,9 +768,14 @@ int launch_norm_residual_backward(int type, bool vec, const NormGradArgs &a, int
     }
     if (err != 0) return err;
     const int col_blocks = (a.d + 15) / 16;
-    const int shared = a.groups > 1 && a.dgate ? GateSums(a).workgroups() : 0;
-    hipLaunchKernelGGL(k_norm_sums, dim3(5 * col_blocks + shared), dim3(1024), 0, (hipStream_t)stream, a,
-                       workgroups, col_blocks);
+    const bool shared = a.groups > 1 && a.dgate, many = shared && a.runs < 16 * (int64_t)a.groups;
+    const int places = a.groups < a.runs ? a.groups : a.runs - 1;     // where shared groups are looked for
+    if (many)
+        hipLaunchKernelGGL(k_norm_sums<true>, dim3(5 * col_blocks + (places * ((a.d + 255) / 256) + 15) / 16), dim3(1024),
+                           0, (hipStream_t)stream, a, workgroups, col_blocks);
+    else
+        hipLaunchKernelGGL(k_norm_sums<false>, dim3(5 * col_blocks + (shared ? places * ((a.d + 63) / 64) : 0)),
+                           dim3(1024), 0, (hipStream_t)stream, a, workgroups, col_blocks);
     return (int)hipGetLastError();
 }
 

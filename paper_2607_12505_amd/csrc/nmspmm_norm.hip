@@ -141,7 +141,9 @@ constexpr int team_threads(int wpr) { return wpr > 4 ? 64 * wpr : 256; }
 
 // --------------------------------------------------------------- forward
 // Bound by memory: 18464 x 1024 bf16 (layer norm before, gate) 27.3 us, 5.5 TB/s of the rows
-// read and written, where a copy of 512 MiB reaches 5.3.  One token of 1024: 2.4 us.
+// read and written, where a copy of 512 MiB reaches 5.3; a gate for each token adds its 4 bytes a
+// channel, 37.6 us for 28.8 in a graph.  One token of 1024: 2.4 us.  Past 8192 channels 16 waves of
+// 128 registers hold 16 values a lane and spill 83 to 129: 4096 x 12288 bf16 210 us, 1.9 TB/s.
 template <class T, int VEC, int CH, int WPR>
 __global__ __launch_bounds__(team_threads(WPR)) void k_norm_residual(NormArgs a) {
     constexpr int TEAMS = team_threads(WPR) / 64 / WPR;
@@ -299,6 +301,9 @@ struct SharedParam {
 // behind a branch, whose two sides would copy registers.  Short batches are bound by
 // what surrounds the rows: with workgroups of 4 waves the 1536 x 1024 sums of three times
 // as many workgroups took 25.8 us to leave and add, now 16.7; 12608 x 384 fp16 18.9 us.
+//   Registers spill in the forms beside these: 6 to 54 of binary32 rows without a norm after
+// (18464 x 1024 111 us, 2048 x 8192 145), 25 to 111 of odd rows past 512 channels with one (4096 x 1021 bf16
+// 32 us), 115 and more past 8192 channels (512 x 16384 bf16 93 us, with both norms 236).
 // 1 / sqrt(v), within an ulp (the hardware's, which takes no denormals): the root and quotient
 // rounded one after the other, as the forward pass has them, took 40 of a row's 500 instructions.
 __device__ __forceinline__ float inverse_root(float v) {

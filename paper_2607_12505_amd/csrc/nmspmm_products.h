@@ -272,7 +272,7 @@ struct PairTile {
 
 // h = T(act(g) * u).  g and u never reach memory: a product of both and an elementwise pass
 // after it would write and read 4 m n values more.  18464 x 1024 -> 2736 dense 120 us on the
-// tile of nmspmm_rows.h, 1.72 POP/s; 1576 x 768 -> 2048 13.2 us.
+// tile of nmspmm_rows.h, 1.72 POP/s, with gelu 5 % more; 1576 x 768 -> 2048 13.2 us.
 struct GatedOut {
     static __device__ bool scaled(const BlockArgs &) { return true; }
     static __device__ const float *first(const BlockArgs &a) { return a.scale; }
@@ -373,7 +373,7 @@ __device__ __forceinline__ void load_four(const BlockArgs &a, int tok, int ch, f
 // for the two products that follow, with the part of the scale that their 16-bit
 // codes leave out: by rows for dx (times the channel's), transposed for the
 // weights' gradients (times the token's).  Their sums over the wave's tokens
-// go to bias_parts in binary32.  6304 x 768 -> 2048 bf16 with gelu 58.4 us: bound by this
+// go to bias_parts in binary32.  6304 x 768 -> 2048 bf16 with gelu 60 us: bound by this
 // epilogue (act and slope of 12.9 M values, 103 MB written and 26 read); its int8
 // products are 11 at the rate of a bare loop of them.
 template <class T>

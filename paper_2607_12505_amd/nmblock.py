@@ -613,7 +613,8 @@ class GatedGrads(NamedTuple):
 
 def gated_ffn_backward(xq, sx, w: GatedWeight, dh, stream=None) -> GatedGrads:
     """nm_gated_backward: from dh [tokens x n] (float16 or bfloat16) at the codes that the forward pass used; the
-    gradients pass straight through the rounding to codes.  w must be of a dense layout."""
+    gradients pass straight through the rounding to codes.  The gradients of g and u are rounded to dh's type before
+    their products with x and the weights.  w must be of a dense layout."""
     if not isinstance(w, GatedWeight):
         raise ValueError("w: not a gated block's weight")
     if w.weight.desc.layout != NM_LAYOUT_DENSE:

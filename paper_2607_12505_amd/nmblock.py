@@ -272,7 +272,8 @@ def norm_residual(y, r, pre: Optional[Norm] = None, post: Optional[Norm] = None,
     """nm_norm_residual: (res, z) with u = post(y), res = alpha r + gate u, z = pre(res).
 
     y (the block's output; post and gate go with it) or r (the residual stream) may be None.  gate: float32 [d], or
-    [groups x d] with a row for each of `groups` equal runs of tokens.  Without `pre` there is no z (None)."""
+    [groups x d] with a row for each of `groups` equal runs of tokens.  Without `pre` there is no z (None).  res may be y
+    or r itself; no output may overlap an input otherwise."""
     rt = _rt or _runtime()
     a, like, res, at = _around(y, r, pre, post, gate, alpha, res, stream, rt)
     if pre is not None:

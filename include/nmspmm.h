@@ -603,6 +603,128 @@ nm_status nm_gated_backward_workspace(const nm_scaled_weight *w, int m, size_t *
 nm_status nm_gated_backward(const nm_gated_grad_args *args, const nm_scaled_weight *w, void *ws, size_t ws_bytes,
                             void *stream);
 
+/* ---------------------------------------------------------------- attention
+ * The attention half of a transformer block: rotary positions on queries and keys,
+ * and differential attention, with their backward passes.  Bound in nmattention.py.
+ *
+ * Tensors of heads have consecutive channels and any strides (in values, not
+ * negative) between tokens, heads and sequences, so they may lie inside the rows of a
+ * product of all projections or in a cache.  Pointers need the alignment of their
+ * type only; heads that are whole 16-byte pieces at 16-byte boundaries take the
+ * fast path.  The same inputs give the same bits. */
+
+/* Rotary positions with several axes (time, height, width, ...).  Pair i of a head's
+ * channels, (u, w) = (x[i], x[pairs + i]), or (x[2 i], x[2 i + 1]) if interleaved,
+ * turns by a = pos[axis[i]][token] * freq[i]:
+ *   out = (u cos a - w sin a, u sin a + w cos a)
+ * channels from 2 pairs on are copied.  back != 0 turns by -a: the gradient.
+ * Angles are made in 64 bits, the rotation in binary32, rounded once.
+ * Up to two tensors of the same tokens, d and type in one launch (queries and keys): part[1]
+ * with heads = 0 is absent.  out may be x (with its strides), no other overlap.  pos: device
+ * int32 (or float32 if pos_float), [axes] rows ld_pos apart; freq: device float64
+ * [pairs], axis: device int32 [pairs], each 0 .. axes - 1 (others are taken as the nearest).
+ * 1 <= pairs, 2 pairs <= d <= 1024.  tokens == 0 is a no-op.  Asynchronous on
+ * `stream`.  Errors: NM_ERR_ARG (NULL or misaligned pointer, unknown type, no heads),
+ * NM_ERR_SHAPE (a size or stride out of range), NM_ERR_HIP. */
+typedef struct nm_rotary_part {
+    const void *x;
+    void *out;
+    int64_t x_token, x_head, out_token, out_head;
+    int32_t heads;
+} nm_rotary_part;
+typedef struct nm_rotary_args {
+    nm_rotary_part part[2];
+    const void *pos;
+    int64_t ld_pos;
+    const double *freq;
+    const int32_t *axis;
+    int64_t tokens;
+    int32_t type, pos_float, pairs, d, axes, interleaved, back;
+} nm_rotary_args;
+nm_status nm_rotary(const nm_rotary_args *args, void *stream);
+
+/* Differential attention.  Head h of H has two softmax maps over keys,
+ *   p_i = softmax over the keys that the row sees of scale * (q[2 h + i] . k[2 g + i]), i = 0, 1
+ *   o[h] = (p_0 - lam[h] p_1) v[g]
+ * g = h / (H / Hk) the key head that H / Hk heads share: q has 2 H heads of d channels, k 2 Hk,
+ * v Hk of dv, o H of dv.  Row r of a sequence of nq rows and nk keys sees key j where
+ *   -left <= j - (r + nk - nq) <= right     (left, right < 0: no bound)
+ * so left = -1, right = 0 is the causal mask with the last row at the last key.  A row
+ * that sees no key gives zero.  Sequences, `batch` of them, are padded: tensors [batch x tq]
+ * and [batch x tk], of which the first q_lens[b] rows and k_lens[b] keys count (device
+ * int32 [batch]; NULL: all); or packed behind each other: q_offsets and k_offsets, device
+ * int32 [batch + 1], with tq and tk at least the longest lengths and total_q, total_k
+ * rows in all (the batch strides are not read).  Lengths and offsets outside the tensors are
+ * taken as the nearest inside.  Rows of o behind a sequence's end stay as they were; what q, k
+ * and v hold there does not matter.  Within a sequence a key that a row does not see has
+ * no weight for it, but where v there is infinite or NaN, the row may be NaN.
+ *
+ * lam: `value`, float32 [H]; or, with value NULL, made from learned vectors of n channels,
+ *   exp(q1 . k1) - exp(q2 . k2) + init
+ * float32 [n] for all heads, or [H x n] with per_head.
+ *
+ * Scores, sums and products are in binary32; the maps are rounded to the type once before the
+ * product with v (the matrix instructions' operand).  kept and stats (both or neither NULL) are what
+ * the backward pass reads: kept, device int16 [rows x H x 2 x dv], codes of p_i v; stats, device float32
+ * [2 H x (1 + ceil(dv / 128)) x rows]: the base-2 logarithm of a map's sum (plus infinity where a row sees none), then
+ * the scale of the codes of each 128 channels, their largest magnitude / 32767 (NaN where one is not finite).
+ * rows = batch * tq, or total_q.
+ * type: NM_TYPE_F16 or NM_TYPE_BF16.  d <= 128, dv <= 256; scale > 0.  q, k, v apart from the outputs.
+ * ws: nm_diff_attention_workspace bytes of device memory, any content, 16-byte
+ * aligned (NULL where that is 0; it depends on sizes alone).  Without rows it is a no-op.
+ * Errors: NM_ERR_ARG (NULL or misaligned pointer, another type, scale not positive or not finite), NM_ERR_SHAPE (a size or
+ * stride out of range: sequences of 2^28 rows, token strides of 2^22 values), NM_ERR_WORKSPACE, NM_ERR_HIP. */
+typedef struct nm_heads {
+    void *p;
+    int64_t batch, token, head;   /* strides in values */
+} nm_heads;
+typedef struct nm_tokens {
+    int32_t batch, tq, tk;
+    int32_t left, right;
+    const int32_t *q_offsets, *k_offsets, *q_lens, *k_lens;
+    int64_t total_q, total_k;
+} nm_tokens;
+typedef struct nm_diff_weight {
+    const float *value;
+    const float *q1, *k1, *q2, *k2;
+    float init;
+    int32_t n, per_head;
+} nm_diff_weight;
+typedef struct nm_diff_args {
+    nm_heads q, k, v, o;
+    int16_t *kept;
+    float *stats;
+    nm_tokens tokens;
+    nm_diff_weight weight;
+    int32_t type, H, Hk, d, dv;
+    float scale;
+} nm_diff_args;
+nm_status nm_diff_attention_workspace(const nm_diff_args *args, size_t *bytes);
+nm_status nm_diff_attention(const nm_diff_args *args, void *ws, size_t ws_bytes, void *stream);
+
+/* Its backward pass from grad_o, at kept and stats as the forward pass stored them:
+ *   dp = grad_o v^T;  D_i = sum over keys of p_i dp
+ *   dv = (p_0 - lam p_1)^T grad_o;  ds_0 = p_0 (dp - D_0);  ds_1 = -lam p_1 (dp - D_1)
+ *   dq_i = scale ds_i k_i;  dk_i = scale ds_i^T q_i;  dlam = -sum over rows of D_1
+ * dk and dv are summed over the heads that share them; dq1, dk1, dq2, dk2 (with value NULL) are the learned
+ * vectors' gradients, of their shapes, dlam float32 [H]; all have to be given.  p_0 - lam p_1 and ds_i are
+ * rounded to the type once before their products: in binary16 ds has to stay below its largest value.  Rows and keys
+ * behind a sequence's end stay as they were.  With batch == 0 the weights' gradients are set to zero.
+ * No output may overlap an input or another output (dq, dk and dv may lie inside the rows of one
+ * buffer).  ws: nm_diff_attention_backward_workspace bytes, as above. */
+typedef struct nm_diff_grad_args {
+    nm_heads q, k, v, grad_o, dq, dk, dv;
+    const int16_t *kept;
+    const float *stats;
+    float *dlam, *dq1, *dk1, *dq2, *dk2;
+    nm_tokens tokens;
+    nm_diff_weight weight;
+    int32_t type, H, Hk, d, dv_width;
+    float scale;
+} nm_diff_grad_args;
+nm_status nm_diff_attention_backward_workspace(const nm_diff_grad_args *args, size_t *bytes);
+nm_status nm_diff_attention_backward(const nm_diff_grad_args *args, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

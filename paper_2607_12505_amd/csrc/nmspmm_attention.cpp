@@ -1,0 +1,285 @@
+// C entry points of rotary positions and differential attention: argument checks,
+// workspaces and dispatch (host only).
+#include <cmath>
+
+#include "nmspmm_attn_internal.h"
+
+using namespace nmspmm;
+
+namespace {
+
+bool aligned(const void *p, int to) { return ((uintptr_t)p & (uintptr_t)(to - 1)) == 0; }
+size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// Whether heads of `width` 16-bit values are whole pieces of `values` values at their boundaries.
+bool pieces(const nm_heads &t, int width, int values) {
+    return aligned(t.p, 2 * values) && t.token % values == 0 && t.head % values == 0 && t.batch % values == 0 &&
+           width % values == 0;
+}
+
+nm_status check_tokens(const nm_tokens &t) {
+    if (t.batch < 0 || t.tq < 0 || t.tk < 0 || t.batch >= (1 << 24) || t.tq >= kMaxAttnTokens ||
+        t.tk >= kMaxAttnTokens)
+        return NM_ERR_SHAPE;
+    if (!t.q_offsets != !t.k_offsets) return NM_ERR_ARG;
+    if (t.q_offsets) {
+        if (t.q_lens || t.k_lens) return NM_ERR_ARG;
+        if (t.total_q < 0 || t.total_k < 0 || t.total_q >= (1ll << 31) || t.total_k >= (1ll << 31)) return NM_ERR_SHAPE;
+    }
+    for (const int32_t *p : {t.q_offsets, t.k_offsets, t.q_lens, t.k_lens})
+        if (!aligned(p, 4)) return NM_ERR_ARG;
+    return NM_OK;
+}
+
+nm_status check_heads(int type, int H, int Hk, int d, int dv, float scale) {
+    if (type != NM_TYPE_F16 && type != NM_TYPE_BF16) return NM_ERR_ARG;
+    if (H < 1 || Hk < 1 || H % Hk != 0 || H >= (1 << 16) || d < 1 || d > kMaxHeadWidth || dv < 1 || dv > kMaxValueWidth)
+        return NM_ERR_SHAPE;
+    return scale > 0.f && std::isfinite(scale) ? NM_OK : NM_ERR_ARG;
+}
+
+nm_status check_weight(const nm_diff_weight &w) {
+    if (w.value) return aligned(w.value, 4) ? NM_OK : NM_ERR_ARG;
+    if (w.n < 1 || w.n >= (1 << 20)) return NM_ERR_SHAPE;
+    for (const float *p : {w.q1, w.k1, w.q2, w.k2})
+        if (!p || !aligned(p, 4)) return NM_ERR_ARG;
+    return NM_OK;
+}
+
+// A tensor's strides; its pointer where it has rows.
+nm_status check_tensor(const nm_heads &t, bool rows) {
+    if (t.token < 0 || t.head < 0 || t.batch < 0 || t.token >= kMaxTokenStride) return NM_ERR_SHAPE;
+    return (!rows || t.p) && aligned(t.p, 2) ? NM_OK : NM_ERR_ARG;
+}
+
+Heads heads_of(const nm_heads &t) { return {(char *)t.p, t.batch, t.token, t.head}; }
+
+int64_t rows_of(const nm_tokens &t) { return t.q_offsets ? t.total_q : (int64_t)t.batch * t.tq; }
+int64_t keys_of(const nm_tokens &t) { return t.k_offsets ? t.total_k : (int64_t)t.batch * t.tk; }
+
+void fill(AttnArgs &a, const nm_tokens &t, const nm_diff_weight &w, int H, int Hk, int d, int dv, float scale) {
+    a = AttnArgs{};
+    a.q_offsets = t.q_offsets;
+    a.k_offsets = t.k_offsets;
+    a.q_lens = t.q_lens;
+    a.k_lens = t.k_lens;
+    a.total_q = t.total_q;
+    a.total_k = t.total_k;
+    a.rows = rows_of(t);
+    a.batch = t.batch;
+    a.tq = t.tq;
+    a.tk = t.tk;
+    a.H = H;
+    a.Hk = Hk;
+    a.group = H / Hk;
+    a.d = d;
+    a.dv = dv;
+    // no bound is one that no pair of positions reaches; larger ones say the same
+    const int most = 1 << 29;
+    a.left = t.left < 0 || t.left > most ? most : t.left;
+    a.right = t.right < 0 || t.right > most ? most : t.right;
+    a.scale = scale;
+    a.stat_rows = stat_rows_of(dv);
+    a.scale2 = scale * 1.4426950408889634f;
+    a.weight = w;
+}
+
+// How the forward pass is cut: 128 rows a workgroup that shares its tiles of keys, or 32 rows, with the
+// keys in `splits` parts that a second kernel joins.
+struct Cut {
+    bool wide;
+    int row_tiles, splits;
+};
+Cut cut_of(const nm_tokens &t, int H, int Hk) {
+    const int64_t rows = (int64_t)t.tq * (H / Hk), heads = (int64_t)t.batch * Hk;
+    const int cus = device_cu_count();
+    const int64_t wide_groups = heads * ((rows + 127) / 128);
+    Cut c;
+    c.wide = rows > 64 && (wide_groups >= cus || t.tk <= 1024);
+    const int tile = c.wide ? kRowTileWide : kRowTileNarrow;
+    c.row_tiles = (int)((rows + tile - 1) / tile);
+    c.splits = 1;
+    if (!c.wide) {
+        const int64_t groups = heads * c.row_tiles, key_tiles = (t.tk + kKeyTileNarrow - 1) / kKeyTileNarrow;
+        int64_t splits = groups ? 4 * cus / groups : 1;
+        if (splits > key_tiles) splits = key_tiles;
+        if (splits > 256) splits = 256;
+        c.splits = splits > 1 ? (int)splits : 1;
+    }
+    return c;
+}
+size_t parts_bytes(const nm_tokens &t, int H, int dv, int splits) {
+    return splits > 1 ? (size_t)t.batch * H * t.tq * splits * (2 * dv + 4) * 4 : 0;
+}
+bool grid_fits(int64_t n) { return n < (1ll << 31); }
+
+}  // namespace
+
+// ---------------------------------------------------------------- rotary positions
+
+extern "C" nm_status nm_rotary(const nm_rotary_args *args, void *stream) {
+    if (!args) return NM_ERR_ARG;
+    const nm_rotary_args &g = *args;
+    if (g.type < NM_TYPE_F16 || g.type > NM_TYPE_F32) return NM_ERR_ARG;
+    if (g.tokens < 0 || g.tokens >= (1ll << 31) || g.pairs < 1 || g.d < 2 * (int64_t)g.pairs || g.d > kMaxRotaryWidth ||
+        g.axes < 1 || g.ld_pos < 0)
+        return NM_ERR_SHAPE;
+    const int eb = g.type == NM_TYPE_F32 ? 4 : 2;
+    int64_t heads = 0;
+    bool vec = g.d % 8 == 0 && (g.interleaved ? g.pairs % 4 == 0 : g.pairs % 8 == 0);
+    for (const nm_rotary_part &p : g.part) {
+        if (p.heads < 0 || p.x_token < 0 || p.x_head < 0 || p.out_token < 0 || p.out_head < 0) return NM_ERR_SHAPE;
+        heads += p.heads;
+        if (p.heads == 0 || g.tokens == 0) continue;
+        if (!p.x || !p.out || !aligned(p.x, eb) || !aligned(p.out, eb)) return NM_ERR_ARG;
+        vec = vec && aligned(p.x, 16) && aligned(p.out, 16) && p.x_token % 8 == 0 && p.x_head % 8 == 0 &&
+              p.out_token % 8 == 0 && p.out_head % 8 == 0;
+    }
+    if (heads >= (1 << 16)) return NM_ERR_SHAPE;
+    if (heads == 0) return NM_ERR_ARG;
+    if (g.tokens == 0) return NM_OK;
+    if (!g.pos || !g.freq || !g.axis || !aligned(g.pos, 4) || !aligned(g.freq, 8) || !aligned(g.axis, 4))
+        return NM_ERR_ARG;
+    RotaryArgs a;
+    for (int i = 0; i < 2; ++i) {
+        const nm_rotary_part &p = g.part[i];
+        a.part[i] = {p.x, p.out, p.x_token, p.x_head, p.out_token, p.out_head, p.heads};
+    }
+    a.pos = g.pos;
+    a.ld_pos = g.ld_pos;
+    a.freq = g.freq;
+    a.axis = g.axis;
+    a.tokens = g.tokens;
+    a.pos_float = g.pos_float != 0;
+    a.pairs = g.pairs;
+    a.d = g.d;
+    a.interleaved = g.interleaved != 0;
+    a.axes = g.axes;
+    a.sign = g.back ? -1.f : 1.f;
+    return launch_rotary(g.type, vec, a, stream) == 0 ? NM_OK : NM_ERR_HIP;
+}
+
+// ---------------------------------------------------------------- differential attention
+
+static nm_status check_forward(const nm_diff_args *args) {
+    if (!args) return NM_ERR_ARG;
+    const nm_diff_args &g = *args;
+    nm_status st = check_heads(g.type, g.H, g.Hk, g.d, g.dv, g.scale);
+    if (st == NM_OK) st = check_tokens(g.tokens);
+    return st;
+}
+
+extern "C" nm_status nm_diff_attention_workspace(const nm_diff_args *args, size_t *bytes) {
+    if (!bytes) return NM_ERR_ARG;
+    const nm_status st = check_forward(args);
+    if (st != NM_OK) return st;
+    *bytes = parts_bytes(args->tokens, args->H, args->dv, cut_of(args->tokens, args->H, args->Hk).splits);
+    return NM_OK;
+}
+
+extern "C" nm_status nm_diff_attention(const nm_diff_args *args, void *ws, size_t ws_bytes, void *stream) {
+    nm_status st = check_forward(args);
+    if (st == NM_OK) st = check_weight(args->weight);
+    if (st != NM_OK) return st;
+    const nm_diff_args &g = *args;
+    const int64_t rows = rows_of(g.tokens), keys = keys_of(g.tokens);
+    for (const nm_heads *t : {&g.q, &g.k, &g.v, &g.o})
+        if ((st = check_tensor(*t, (t == &g.k || t == &g.v ? keys : rows) > 0)) != NM_OK) return st;
+    if (!aligned(g.kept, 16) || !aligned(g.stats, 4) || !g.kept != !g.stats) return NM_ERR_ARG;
+    if (rows == 0 || g.tokens.batch == 0 || g.tokens.tq == 0) return NM_OK;
+    const Cut c = cut_of(g.tokens, g.H, g.Hk);
+    const size_t need = parts_bytes(g.tokens, g.H, g.dv, c.splits);
+    if (need && (!ws || ws_bytes < need || !aligned(ws, 16))) return NM_ERR_WORKSPACE;
+    AttnArgs a;
+    fill(a, g.tokens, g.weight, g.H, g.Hk, g.d, g.dv, g.scale);
+    if (!grid_fits((int64_t)a.batch * a.Hk * c.row_tiles * c.splits * 2) ||
+        !grid_fits((int64_t)a.batch * a.H * a.tq))
+        return NM_ERR_SHAPE;
+    a.q = heads_of(g.q);
+    a.k = heads_of(g.k);
+    a.v = heads_of(g.v);
+    a.o = heads_of(g.o);
+    a.kept = g.kept;
+    a.stats = g.stats;
+    a.vec = pieces(g.q, g.d, 8) && pieces(g.k, g.d, 8) && pieces(g.v, g.dv, 8);
+    a.vec_out = pieces(g.o, g.dv, 4);
+    a.row_tiles = c.row_tiles;
+    a.splits = c.splits;
+    a.chunks = value_chunks(width_class(g.d, g.dv), g.dv);
+    a.parts = (float *)ws;
+    if (launch_diff_forward(g.type, width_class(g.d, g.dv), c.wide, a, stream) != 0) return NM_ERR_HIP;
+    if (c.splits > 1 && launch_diff_join(g.type, a, stream) != 0) return NM_ERR_HIP;
+    return NM_OK;
+}
+
+static nm_status check_backward(const nm_diff_grad_args *args) {
+    if (!args) return NM_ERR_ARG;
+    const nm_diff_grad_args &g = *args;
+    nm_status st = check_heads(g.type, g.H, g.Hk, g.d, g.dv_width, g.scale);
+    if (st == NM_OK) st = check_tokens(g.tokens);
+    return st;
+}
+static int64_t grad_row_tiles(const nm_diff_grad_args &g) {
+    return ((int64_t)g.tokens.tq * (g.H / g.Hk) + 127) / 128;
+}
+static size_t delta_bytes(const nm_diff_grad_args &g) { return round256((size_t)2 * g.H * rows_of(g.tokens) * 4); }
+
+extern "C" nm_status nm_diff_attention_backward_workspace(const nm_diff_grad_args *args, size_t *bytes) {
+    if (!bytes) return NM_ERR_ARG;
+    const nm_status st = check_backward(args);
+    if (st != NM_OK) return st;
+    *bytes = delta_bytes(*args) + (size_t)args->H * args->tokens.batch * grad_row_tiles(*args) * 16;
+    return NM_OK;
+}
+
+extern "C" nm_status nm_diff_attention_backward(const nm_diff_grad_args *args, void *ws, size_t ws_bytes,
+                                                void *stream) {
+    nm_status st = check_backward(args);
+    if (st == NM_OK) st = check_weight(args->weight);
+    if (st != NM_OK) return st;
+    const nm_diff_grad_args &g = *args;
+    const int64_t rows = rows_of(g.tokens), keys = keys_of(g.tokens);
+    for (const nm_heads *t : {&g.q, &g.grad_o, &g.dq})
+        if ((st = check_tensor(*t, rows > 0)) != NM_OK) return st;
+    for (const nm_heads *t : {&g.k, &g.v, &g.dk, &g.dv})
+        if ((st = check_tensor(*t, keys > 0)) != NM_OK) return st;
+    if (!g.dlam || !aligned(g.dlam, 4) || !aligned(g.kept, 16) || !aligned(g.stats, 4) ||
+        (rows > 0 && (!g.kept || !g.stats)))
+        return NM_ERR_ARG;
+    if (!g.weight.value)
+        for (const float *p : {g.dq1, g.dk1, g.dq2, g.dk2})
+            if (!p || !aligned(p, 4)) return NM_ERR_ARG;
+    size_t need = 0;
+    st = nm_diff_attention_backward_workspace(args, &need);
+    if (st != NM_OK) return st;
+    if (need && (!ws || ws_bytes < need || !aligned(ws, 16))) return NM_ERR_WORKSPACE;
+    AttnArgs a;
+    fill(a, g.tokens, g.weight, g.H, g.Hk, g.d, g.dv_width, g.scale);
+    const int64_t row_tiles = grad_row_tiles(g), key_tiles = (g.tokens.tk + kGradKeys - 1) / kGradKeys;
+    if (!grid_fits((int64_t)a.batch * a.Hk * row_tiles * 4) || !grid_fits((int64_t)a.batch * a.Hk * key_tiles + 1))
+        return NM_ERR_SHAPE;
+    a.q = heads_of(g.q);
+    a.k = heads_of(g.k);
+    a.v = heads_of(g.v);
+    a.grad = heads_of(g.grad_o);
+    a.dq = heads_of(g.dq);
+    a.dk = heads_of(g.dk);
+    a.dv_ = heads_of(g.dv);
+    a.kept = (int16_t *)g.kept;
+    a.stats = (float *)g.stats;
+    a.vec = pieces(g.q, g.d, 8) && pieces(g.k, g.d, 8) && pieces(g.v, g.dv_width, 8) && pieces(g.grad_o, g.dv_width, 8);
+    a.vec_out = pieces(g.dq, g.d, 4) && pieces(g.dk, g.d, 4) && pieces(g.dv, g.dv_width, 4);
+    a.row_tiles = (int)row_tiles;
+    a.key_tiles = (int)key_tiles;
+    a.delta = (float *)ws;
+    a.dlam_parts = (float *)((char *)ws + delta_bytes(g));
+    a.dlam_count = (int)((int64_t)a.batch * row_tiles * 4);
+    a.dlam = g.dlam;
+    a.dq1 = g.dq1;
+    a.dk1 = g.dk1;
+    a.dq2 = g.dq2;
+    a.dk2 = g.dk2;
+    const int cls = width_class(g.d, g.dv_width);
+    if (a.batch > 0 && row_tiles > 0 && launch_diff_grad_q(g.type, cls, a, stream) != 0) return NM_ERR_HIP;
+    return launch_diff_grad_k(g.type, cls, a, stream) == 0 ? NM_OK : NM_ERR_HIP;
+}

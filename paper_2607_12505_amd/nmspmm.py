@@ -40,6 +40,9 @@ EXPORTED = (
     "nm_quantize_rows", "nm_pad_codes", "nm_norm_residual", "nm_norm_residual_backward_workspace", "nm_norm_residual_backward",
     "nm_linear_workspace", "nm_gemm_i8_scaled", "nm_linear_i8", "nm_gated_i8", "nm_gated", "nm_gated_backward_workspace",
     "nm_gated_backward",
+    # attention (bound in nmattention.py)
+    "nm_rotary", "nm_diff_attention_workspace", "nm_diff_attention", "nm_diff_attention_backward_workspace",
+    "nm_diff_attention_backward",
 )
 NM_NOALLOC_SCRATCH_BYTES = 16384 + (32 << 20)
 
@@ -140,6 +143,11 @@ def lib() -> ctypes.CDLL:
             "nm_gated": ([vp, i64, i32, i32, vp, i32, vp, i64, i32, vp, sz, vp], i32),
             "nm_gated_backward_workspace": ([vp, i32, ctypes.POINTER(sz)], i32),
             "nm_gated_backward": ([vp, vp, vp, sz, vp], i32),
+            "nm_rotary": ([vp, vp], i32),
+            "nm_diff_attention_workspace": ([vp, ctypes.POINTER(sz)], i32),
+            "nm_diff_attention": ([vp, vp, sz, vp], i32),
+            "nm_diff_attention_backward_workspace": ([vp, ctypes.POINTER(sz)], i32),
+            "nm_diff_attention_backward": ([vp, vp, sz, vp], i32),
         }
         for name, (args, res) in sig.items():
             f = getattr(L, name)

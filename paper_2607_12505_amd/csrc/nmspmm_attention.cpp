@@ -84,26 +84,26 @@ void fill(AttnArgs &a, const nm_tokens &t, const nm_diff_weight &w, int H, int H
     a.weight = w;
 }
 
-// How the forward pass is cut: 128 rows a workgroup that shares its tiles of keys, or 32 rows, with the
+// How the forward pass is cut: workgroups of many rows that share their tiles of keys, or of few rows, with the
 // keys in `splits` parts that a second kernel joins.
 struct Cut {
     bool wide;
     int row_tiles, splits;
 };
-Cut cut_of(const nm_tokens &t, int H, int Hk) {
+Cut cut_of(const nm_tokens &t, int H, int Hk, int cls) {
     const int64_t rows = (int64_t)t.tq * (H / Hk), heads = (int64_t)t.batch * Hk;
     const int cus = device_cu_count();
-    const int64_t wide_groups = heads * ((rows + 127) / 128);
+    const int64_t wide_groups = heads * ((rows + wide_rows(cls) - 1) / wide_rows(cls));
     Cut c;
     c.wide = rows > 64 && (wide_groups >= cus || t.tk <= 1024);
-    const int tile = c.wide ? kRowTileWide : kRowTileNarrow;
+    const int tile = c.wide ? wide_rows(cls) : kFewRows;
     c.row_tiles = (int)((rows + tile - 1) / tile);
     c.splits = 1;
     if (!c.wide) {
-        const int64_t groups = heads * c.row_tiles, key_tiles = (t.tk + kKeyTileNarrow - 1) / kKeyTileNarrow;
+        const int64_t groups = heads * c.row_tiles, key_tiles = (t.tk + kFewRowsKeys - 1) / kFewRowsKeys;
         int64_t splits = groups ? 4 * cus / groups : 1;
         if (splits > key_tiles) splits = key_tiles;
-        if (splits > 256) splits = 256;
+        if (splits > kMaxSplits) splits = kMaxSplits;
         c.splits = splits > 1 ? (int)splits : 1;
     }
     return c;
@@ -173,7 +173,7 @@ extern "C" nm_status nm_diff_attention_workspace(const nm_diff_args *args, size_
     if (!bytes) return NM_ERR_ARG;
     const nm_status st = check_forward(args);
     if (st != NM_OK) return st;
-    *bytes = parts_bytes(args->tokens, args->H, args->dv, cut_of(args->tokens, args->H, args->Hk).splits);
+    *bytes = parts_bytes(args->tokens, args->H, args->dv, cut_of(args->tokens, args->H, args->Hk, width_class(args->d, args->dv)).splits);
     return NM_OK;
 }
 
@@ -187,13 +187,13 @@ extern "C" nm_status nm_diff_attention(const nm_diff_args *args, void *ws, size_
         if ((st = check_tensor(*t, (t == &g.k || t == &g.v ? keys : rows) > 0)) != NM_OK) return st;
     if (!aligned(g.kept, 16) || !aligned(g.stats, 4) || !g.kept != !g.stats) return NM_ERR_ARG;
     if (rows == 0 || g.tokens.batch == 0 || g.tokens.tq == 0) return NM_OK;
-    const Cut c = cut_of(g.tokens, g.H, g.Hk);
+    const Cut c = cut_of(g.tokens, g.H, g.Hk, width_class(g.d, g.dv));
     const size_t need = parts_bytes(g.tokens, g.H, g.dv, c.splits);
     if (need && (!ws || ws_bytes < need || !aligned(ws, 16))) return NM_ERR_WORKSPACE;
     AttnArgs a;
     fill(a, g.tokens, g.weight, g.H, g.Hk, g.d, g.dv, g.scale);
-    if (!grid_fits((int64_t)a.batch * a.Hk * c.row_tiles * c.splits * 2) ||
-        !grid_fits((int64_t)a.batch * a.H * a.tq))
+    if (!grid_fits((int64_t)a.batch * a.Hk * c.row_tiles * c.splits) ||
+        !grid_fits((int64_t)a.batch * a.H * a.tq) || !grid_fits((int64_t)a.tq * a.group))
         return NM_ERR_SHAPE;
     a.q = heads_of(g.q);
     a.k = heads_of(g.k);
@@ -205,7 +205,6 @@ extern "C" nm_status nm_diff_attention(const nm_diff_args *args, void *ws, size_
     a.vec_out = pieces(g.o, g.dv, 4);
     a.row_tiles = c.row_tiles;
     a.splits = c.splits;
-    a.chunks = value_chunks(width_class(g.d, g.dv), g.dv);
     a.parts = (float *)ws;
     if (launch_diff_forward(g.type, width_class(g.d, g.dv), c.wide, a, stream) != 0) return NM_ERR_HIP;
     if (c.splits > 1 && launch_diff_join(g.type, a, stream) != 0) return NM_ERR_HIP;
@@ -220,7 +219,7 @@ static nm_status check_backward(const nm_diff_grad_args *args) {
     return st;
 }
 static int64_t grad_row_tiles(const nm_diff_grad_args &g) {
-    return ((int64_t)g.tokens.tq * (g.H / g.Hk) + 127) / 128;
+    return ((int64_t)g.tokens.tq * (g.H / g.Hk) + kGradRows - 1) / kGradRows;
 }
 static size_t delta_bytes(const nm_diff_grad_args &g) { return round256((size_t)2 * g.H * rows_of(g.tokens) * 4); }
 
@@ -256,7 +255,7 @@ extern "C" nm_status nm_diff_attention_backward(const nm_diff_grad_args *args, v
     AttnArgs a;
     fill(a, g.tokens, g.weight, g.H, g.Hk, g.d, g.dv_width, g.scale);
     const int64_t row_tiles = grad_row_tiles(g), key_tiles = (g.tokens.tk + kGradKeys - 1) / kGradKeys;
-    if (!grid_fits((int64_t)a.batch * a.Hk * row_tiles * 4) || !grid_fits((int64_t)a.batch * a.Hk * key_tiles + 1))
+    if (!grid_fits((int64_t)a.batch * a.Hk * row_tiles * 4) || !grid_fits((int64_t)a.tq * a.group) || !grid_fits((int64_t)a.batch * a.Hk * key_tiles + 1))
         return NM_ERR_SHAPE;
     a.q = heads_of(g.q);
     a.k = heads_of(g.k);

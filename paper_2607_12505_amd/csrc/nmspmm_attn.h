@@ -42,13 +42,13 @@ struct Mfma<bf16_t> {
     }
 };
 
-// Values 8 c .. 8 c + 7 of C, rounded once: a B operand.
+// Eight values of C (8 c .. 8 c + 7), rounded once: a B operand.
 template <class T>
-__device__ __forceinline__ v8s pack(const float (&f)[16], int c) {
+__device__ __forceinline__ v8s pack(const float (&f)[8]) {
     typedef T v8 __attribute__((ext_vector_type(8)));
     v8 r;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = (T)f[8 * c + e];
+    for (int e = 0; e < 8; ++e) r[e] = (T)f[e];
     return __builtin_bit_cast(v8s, r);
 }
 
@@ -65,9 +65,6 @@ __device__ __forceinline__ float half_max(float x) {
 }
 
 // ---------------------------------------------------------------- tiles in LDS
-// A tile is rows of CPR 16-byte pieces.  Piece c of row r lies at place c ^ swizzle(r):
-// the rows of an A or B operand (16 lanes at one piece) and the 4 rows of a turned
-// one (16 lanes at 32 bytes of each) then lie in distinct banks.
 // LDS is addressed by bytes from its start.
 template <class V>
 __device__ __forceinline__ V lds_load(uint32_t at) {
@@ -75,12 +72,6 @@ __device__ __forceinline__ V lds_load(uint32_t at) {
 }
 __device__ __forceinline__ uint32_t lds_start(char *lds) {
     return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
-}
-template <int CPR>
-__device__ __forceinline__ int swizzle(int r) {
-    if constexpr (CPR == 4) return ((r >> 1 & 1) * 2) ^ (r >> 2 & 1) ^ ((r >> 3 & 1) * 2);
-    if constexpr (CPR == 8) return ((r & 1) * 2) ^ ((r >> 1 & 1) * 4) ^ (r >> 2 & 1) ^ ((r >> 3 & 1) * 2);
-    return ((r & 1) * 4) ^ ((r >> 1 & 1) * 10) ^ (r >> 2 & 1) ^ ((r >> 3 & 1) * 2);
 }
 
 // 16 bytes a lane straight to LDS, lane l's at lds + 16 l (lds wave-uniform); zeros
@@ -110,57 +101,146 @@ __device__ __forceinline__ void arrive() {
     asm volatile("" ::: "memory");
 }
 
-// ROWS rows of `width` values into LDS: rows from `left` on and columns from `width` on
-// are zero, whatever memory holds there.  In whole pieces at 16-byte boundaries the
-// loads go straight to LDS and arrive later; otherwise a value at a time, at once.
+// The same with this wave's newest N loads still under way.
+template <int N>
+__device__ __forceinline__ void arrive_but() {
+    static_assert(N >= 0 && N < 64, "vmcnt range");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// ROWS rows of CPR 16-byte pieces in LDS.  One load of a wave fills 1024 bytes, a group of
+// 64 / CPR rows.  Which rows make a group, and a gap of 16 bytes for each step of a group's
+// number, put the rows of an operand (16 lanes at one piece) and the 4 rows of a turned one
+// (32 lanes at 64 bytes of each) in distinct banks.  A row's place is a sum over the bits of its
+// number, so an operand is read at one address of its lane and constants.
 template <class T, int CPR, int ROWS, int WAVES>
 struct Tile {
-    static constexpr int LOADS = ROWS * CPR / (64 * WAVES), BYTES = ROWS * CPR * 16;
-    static_assert(LOADS * 64 * WAVES == ROWS * CPR, "whole loads");
-    static __device__ __forceinline__ void load(const T *p, int64_t stride, int left, int width, bool vec, uint32_t lds,
-                                                int wave, int lane) {
-        left = left < 0 ? 0 : left < ROWS ? left : ROWS;
-        if (vec) {
-            const v4i buffer = buffer_of(p, left ? ((left - 1) * stride + width) * 2 : 0);
+    static constexpr int GROUPS = ROWS * CPR / 64;
+    static_assert(ROWS == 32 || ROWS == 64 || ROWS == 128, "rows");
+    // bits of a row's number in the place within its group, then in the group's number, from the lowest
+    static constexpr int order(int n) {
+        constexpr int few[4][6] = {{0, 1, 4, 3, 2, 5}, {1, 4, 3, 2, 0, 5}, {4, 3, 2, 0, 1, 5}, {4, 2, 3, 0, 1, 5}};
+        constexpr int many[4][6] = {{0, 1, 4, 5, 2, 3}, {1, 4, 5, 2, 3, 0}, {4, 5, 2, 3, 0, 1}, {4, 2, 3, 0, 1, 5}};
+        constexpr int kind = CPR == 4 ? 0 : CPR == 8 ? 1 : CPR == 16 ? 2 : 3;
+        return n == 6 ? 6 : ROWS == 32 ? few[kind][n] : many[kind][n];
+    }
+    static constexpr int PLACE_BITS = CPR == 4 ? 4 : CPR == 8 ? 3 : CPR == 16 ? 2 : 1;
+    // 16-byte steps of a group's gap
+    static constexpr int gap(int group) {
+        if (ROWS == 32 && CPR == 8) return (group & 1) + (group >> 1 & 1) * 4;
+        if (ROWS == 32 && CPR == 16) return (group & 1) + (group >> 1 & 1) * 4 + (group >> 2 & 1) * 8;
+        return group;
+    }
+    static constexpr int BYTES = GROUPS * 1024 + (gap(GROUPS - 1) * 16 + 127) / 128 * 128;
+    static constexpr __host__ __device__ int group_at(int group) { return group * 1024 + gap(group) * 16; }
+    // where a row lies, and the rows of a group and place
+    static constexpr __host__ __device__ int place_of(int row) {
+        int place = 0, group = 0;
+        for (int n = 0; n < 7; ++n) {
+            const int bit = row >> order(n) & 1;
+            if (n < PLACE_BITS)
+                place |= bit << n;
+            else
+                group |= bit << (n - PLACE_BITS);
+        }
+        return group_at(group) + place * CPR * 16;
+    }
+    static constexpr __host__ __device__ int row_of_place(int place) {
+        int row = 0;
+        for (int n = 0; n < PLACE_BITS; ++n) row |= (place >> n & 1) << order(n);
+        return row;
+    }
+    static constexpr __host__ __device__ int row_of_group(int group) {
+        int row = 0;
+        for (int n = PLACE_BITS; n < 7; ++n) row |= (group >> (n - PLACE_BITS) & 1) << order(n);
+        return row;
+    }
+
+    // The A or B operand of the rows row .. row + 31 (row: a multiple of 32), k = 16 c .. 16 c + 15, at
+    // the address of this lane's part of it.
+    static __device__ __forceinline__ uint32_t rows_lane(int lane) { return place_of(lane & 31) + (lane >> 5) * 16; }
+    static __device__ __forceinline__ v8s rows(uint32_t at, int row, int c) {
+        return lds_load<v8s>(at + (place_of(row) + c * 32));
+    }
+    // The A operand of 32 columns from 32 x with k over the rows row .. row + 15 (row: a
+    // multiple of 16) in the order that values of C have (above).  A read gives 16 lanes 4 rows x 16
+    // columns: lane i gives the address of 4 columns of row i / 4 and gets the 4 rows of column i.
+    static __device__ __forceinline__ uint32_t turned_lane(int lane) {
+        return place_of((lane & 15) >> 2 | (lane >> 5) << 2) + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+    }
+    static __device__ __forceinline__ v8s turned(uint32_t at, int row, int x) {
+        const v4s a = read4(at + (place_of(row) + x * 64)), b = read4(at + (place_of(row + 8) + x * 64));
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    static __device__ __forceinline__ v4s read4(uint32_t at) {
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)(uintptr_t)at);
+    }
+};
+
+// Loads of tile after tile of rows, of one tensor or of two `second` values apart (their tiles one behind the
+// other): rows behind the last and columns from `width` on are zero, whatever memory holds there.  In whole
+// pieces at 16-byte boundaries the loads go straight to LDS and arrive later (LOADS of them by every
+// wave); otherwise a value at a time, at once.  What a load needs but its tile's base is made once.
+template <class T, int CPR, int ROWS, int WAVES, int TENSORS>
+struct Feed {
+    using Place = Tile<T, CPR, ROWS, WAVES>;
+    static constexpr int GROUPS = Place::GROUPS, LOADS = TENSORS * GROUPS / WAVES;
+    static constexpr bool SPREAD = GROUPS < WAVES;          // waves share out the tensors too
+    static constexpr int EACH = SPREAD ? 1 : GROUPS / WAVES; // loads of one tensor
+    static_assert(TENSORS * GROUPS % WAVES == 0 && (SPREAD || GROUPS % WAVES == 0), "as many loads by every wave");
+    const T *p;
+    int64_t stride, second, bytes;      // bytes: from p to the end of the last row
+    int left, width, first;             // rows left; this wave's first group
+    uint32_t offset[EACH];              // of a lane; past any buffer where its piece is not of the columns
+    bool vec;
+    __device__ __forceinline__ Feed(const T *from, int64_t row_stride, int64_t tensor_stride, int rows, int columns, bool whole,
+                                    int wave, int lane)
+        : p(from), stride(row_stride), second(tensor_stride), bytes(((int64_t)(rows - 1) * row_stride + columns) * 2),
+          left(rows), width(columns), vec(whole) {
+        first = SPREAD ? wave % GROUPS : wave;
+        if (SPREAD) p += wave / GROUPS * second;
+        const int c = lane % CPR;
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int id = (i * WAVES + wave) * 64 + lane, row = id / CPR, c = (id % CPR) ^ swizzle<CPR>(row);
-                const uint32_t offset = c * 8 < width ? (uint32_t)(row * (uint32_t)stride * 2 + c * 16) : 0x80000000u;
-                dma16(buffer, offset, lds + (i * WAVES + wave) * 1024);
+        for (int i = 0; i < EACH; ++i)
+            offset[i] = c * 8 < width ? (uint32_t)(Place::row_of_place(lane / CPR) + Place::row_of_group(i * WAVES + first)) *
+                                                (uint32_t)stride * 2 + c * 16
+                                      : 0x80000000u;
+    }
+    __device__ __forceinline__ void load(uint32_t lds, int wave, int lane) {
+        if (SPREAD) lds += wave / GROUPS * Place::BYTES;
+        if (vec) {
+            const int records = left <= 0 ? 0 : bytes < 0x7FFFFFFF ? (int)bytes : 0x7FFFFFFF;
+#pragma unroll
+            for (int t = 0; t < (SPREAD ? 1 : TENSORS); ++t) {
+                const v4i buffer = buffer_of(p + t * second, records);
+#pragma unroll
+                for (int i = 0; i < EACH; ++i)
+                    dma16(buffer, offset[i], lds + t * Place::BYTES + Place::group_at(i * WAVES + first));
             }
         } else {
+            typedef T v8 __attribute__((ext_vector_type(8)));
+            const int c = lane % CPR * 8;
 #pragma unroll 1
-            for (int i = 0; i < LOADS; ++i) {
-                const int id = (i * WAVES + wave) * 64 + lane, row = id / CPR, c = (id % CPR) ^ swizzle<CPR>(row);
-                typedef T v8 __attribute__((ext_vector_type(8)));
+            for (int n = 0; n < LOADS; ++n) {
+                const int t = n / EACH, group = n % EACH * WAVES + first;
+                const int row = Place::row_of_group(group) + Place::row_of_place(lane / CPR);
+                const T *from = p + t * second + row * stride;
                 v8 v;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     v[e] = (T)0.f;
-                    if (row < left && c * 8 + e < width) v[e] = p[row * stride + c * 8 + e];
+                    if (row < left && c + e < width) v[e] = from[c + e];
                 }
-                *(__attribute__((address_space(3))) v8 *)(uintptr_t)(lds + id * 16) = v;
+                *(__attribute__((address_space(3))) v8 *)(uintptr_t)(lds + t * Place::BYTES + Place::group_at(group) +
+                                                                    lane * 16) = v;
             }
         }
-    }
-    // The A or B operand of 32 rows from `row` (a multiple of 32): k = 16 c .. 16 c + 15.
-    static __device__ __forceinline__ v8s rows(uint32_t lds, int row, int c, int lane) {
-        const int r = row + (lane & 31);
-        return lds_load<v8s>(lds + (r * CPR + ((2 * c + (lane >> 5)) ^ swizzle<CPR>(r & 15))) * 16);
-    }
-    // The A operand of 32 columns from 32 x with k over the rows row .. row + 15 (row: a
-    // multiple of 16) in the order that values of C have (above).
-    static __device__ __forceinline__ v8s turned(uint32_t lds, int row, int x, int lane) {
-        const int quad = (lane >> 5) * 4 + ((lane & 15) >> 2);
-        const int piece = 4 * x + 2 * (lane >> 4 & 1) + (lane >> 1 & 1), low = 8 * (lane & 1);
-        const v4s a = read4(lds + ((row + quad) * CPR + (piece ^ swizzle<CPR>(quad))) * 16 + low);
-        const v4s b = read4(lds + ((row + 8 + quad) * CPR + (piece ^ swizzle<CPR>(8 + quad))) * 16 + low);
-        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-    }
-    // 4 rows x 16 columns of 16 bits for 16 lanes: lane i gives the address of 4 columns of row
-    // i / 4 and gets the 4 rows of column i.
-    static __device__ __forceinline__ v4s read4(uint32_t at) {
-        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)(uintptr_t)at);
+        p += ROWS * stride;
+        bytes -= ROWS * stride * 2;
+        left -= ROWS;
     }
 };
 
@@ -278,10 +358,84 @@ __device__ __forceinline__ Weight weight_of(const nm_diff_weight &w, int head, i
 }
 
 // Workgroups are dispatched round-robin over the 8 XCDs; those of one head (which share its
-// keys) run on one of them, whose L2 then holds the keys.
+// keys) run on one of them, whose L2 then holds the keys.  Under a causal mask work falls along
+// a head's tiles: the second 32 of an XCD (which has 32 compute units) go backwards, so that
+// the two workgroups that a compute unit starts with are a long and a short one (2 x 4096 rows of
+// 8 heads: 160 us, in order 199).
 __device__ __forceinline__ int near_block(int bid, int count) {
-    const int xcd = bid & 7, local = bid >> 3, per = count >> 3, left = count & 7;
-    return xcd < left ? xcd * (per + 1) + local : left * (per + 1) + (xcd - left) * per + local;
+    const int xcd = bid & 7, per = count >> 3, left = count & 7;
+    const int mine = xcd < left ? per + 1 : per, before = xcd < left ? xcd * (per + 1) : left * (per + 1) + (xcd - left) * per;
+    int local = bid >> 3;
+    if (local >> 5 == 1) {
+        const int from = 32, to = mine < 64 ? mine : 64;
+        local = from + to - 1 - local;
+    }
+    return before + local;
+}
+
+// The rows of a workgroup: `TILE` of the rows (token t, head g of the group) number t * group + g that
+// share a key head, 32 a block; a lane's row is the block's number lane % 32.
+struct RowTile {
+    Sequence s;
+    int b, hk, tile, start, rows;
+    bool valid;           // lanes behind the last row repeat it and store nothing
+    int t, g, head;
+    int first, last;      // keys that the lane's row sees
+    // what the block's rows see, one of them or all: rows rise with t, and so do both ends
+    int block_low, block_high, block_full, block_end;
+    int low, high;        // what the workgroup's rows see
+};
+__device__ __forceinline__ int token_of(const AttnArgs &a, int number) {
+    return a.group == 1 ? number : (int)((uint32_t)number / (uint32_t)a.group);
+}
+template <int TILE>
+__device__ __forceinline__ RowTile row_tile(const AttnArgs &a, int id, int lane, int block) {
+    RowTile r;
+    r.tile = a.row_tiles - 1 - id % a.row_tiles;      // the long rows of a causal mask first
+    id /= a.row_tiles;
+    r.hk = id % a.Hk;
+    r.b = id / a.Hk;
+    r.s = sequence(a, r.b);
+    r.start = r.tile * TILE;
+    r.rows = r.s.nq * a.group - r.start;              // (tq * group < 2^31)
+    r.rows = r.rows < TILE ? r.rows : TILE;
+    const int mine = block * 32 + (lane & 31);
+    r.valid = mine < r.rows;
+    const int number = r.start + (r.valid ? mine : r.rows - 1);
+    r.t = token_of(a, number);
+    r.g = number - r.t * a.group;
+    r.head = r.hk * a.group + r.g;
+    r.first = first_seen(a, r.s, r.t);
+    r.last = last_seen(a, r.s, r.t);
+    r.block_low = __builtin_amdgcn_readlane(r.first, 0);
+    r.block_full = __builtin_amdgcn_readlane(r.first, 31);
+    r.block_end = __builtin_amdgcn_readlane(r.last, 0);
+    r.block_high = block * 32 < r.rows ? __builtin_amdgcn_readlane(r.last, 31) : -1;
+    r.low = first_seen(a, r.s, token_of(a, r.start));
+    r.high = last_seen(a, r.s, token_of(a, r.start + r.rows - 1));
+    return r;
+}
+// lam of the lane's head, made by the whole wave for each head of the group.
+__device__ __forceinline__ float row_weight(const AttnArgs &a, const RowTile &r, int lane) {
+    float lam = 0.f;
+    for (int k = 0; k < a.group; ++k) {
+        const float w = weight_of(a.weight, r.hk * a.group + k, lane).lam;
+        lam = k == r.g ? w : lam;
+    }
+    return lam;
+}
+// Scores of 32 keys from j0 for the lane's row, of keys that it does not see minus infinity.
+template <int MAPS>
+__device__ __forceinline__ void hide(const RowTile &r, int j0, int lane, v16f (&z)[MAPS]) {
+    const int at = j0 + 4 * (lane >> 5) - r.first;
+    const uint32_t span = (uint32_t)(r.last - r.first);
+    const bool none = r.last < r.first;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const bool seen = !none && (uint32_t)(at + 8 * (e / 4) + e % 4) <= span;
+#pragma unroll
+        for (int i = 0; i < MAPS; ++i) z[i][e] = seen ? z[i][e] : -__builtin_inff();
+    }
 }
 
 }  // namespace

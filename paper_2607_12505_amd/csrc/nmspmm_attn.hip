@@ -2,10 +2,10 @@
 // row sees, o = (p1 - lam p2) v.
 //
 // One pass over the keys.  The ratio of the maps' sums is not known before the last
-// key, so each map has its own running maximum, sum and product with v; both products
-// share v's operands.  Scores are made transposed (keys x rows): a lane holds
-// keys of one row of q, so maximum and sum are a lane's own but for one exchange of
-// halves, and the maps go into the product with v as they lie (nmspmm_attn.h).
+// key, so each map has its own running maximum, sum and product with v.  Scores are made
+// transposed (keys x rows): a lane holds keys of one row of q, so maximum and sum are a
+// lane's own but for one exchange of halves, and the maps go into the product with v as
+// they lie (nmspmm_attn.h).
 // The maps' values are rounded to 16 bits before that product (the matrix instructions
 // take no more): half an ulp of each value, the same size as the output's own rounding.
 // Sums, maxima and products are in 32 bits.
@@ -17,273 +17,333 @@
 namespace nmspmm {
 namespace {
 
-// WAVES 4: 128 rows, 32 a wave, share tiles of 64 keys.  WAVES 1: 32 rows, tiles of 32
-// keys, for few rows: the keys are split over workgroups, whose sums k_diff_join joins.
-template <class T, int D, int DV, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, D <= 64 ? 2 : 1) void k_diff_forward(AttnArgs a) {
-    constexpr int KT = WAVES == 4 ? kKeyTileWide : kKeyTileNarrow;
+// BLOCKS blocks of 32 rows share tiles of KT keys in a ring of two.  MAPS 2: a wave makes both
+// maps of its block, whose products share v's operands; MAPS 1: two waves a block make one each and
+// meet at the end.  Both maps' sums of 256 channels do not fit a wave's registers, and of 128 they do: (64, 128)
+// runs 4 x 4096 rows of 8 heads in 0.49 ms with MAPS 2 and 0.61 with MAPS 1 (more reads of LDS and scalar instructions),
+// (128, 256) 2 x 4096 rows in 0.44 ms with MAPS 1 and 0.75 with the scores made for 128 channels at a time.
+template <class T, int D, int DV, int BLOCKS, int MAPS, int KT>
+__global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS), BLOCKS > 1 ? 2 : 1) void k_diff_forward(AttnArgs a) {
+    constexpr int WAVES = BLOCKS * (3 - MAPS);
     using KTile = Tile<T, D / 8, KT, WAVES>;
     using VTile = Tile<T, DV / 8, KT, WAVES>;
+    using KFeed = Feed<T, D / 8, KT, WAVES, 2>;
+    using VFeed = Feed<T, DV / 8, KT, WAVES, 1>;
     constexpr int STAGE = 2 * KTile::BYTES + VTile::BYTES;
+    static_assert(MAPS == 2 || BLOCKS * 64 * DV * 2 <= 2 * STAGE, "room for the second maps' products");
     __shared__ __attribute__((aligned(1024))) char shared[2 * STAGE];
     const uint32_t lds = lds_start(shared);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int block = MAPS == 2 ? wave : wave >> 1, map = MAPS == 2 ? 0 : wave & 1;   // the wave's first map
 
-    // workgroup -> (sequence, key head, row tile, split); long rows of a causal mask first
     int id = near_block(blockIdx.x, gridDim.x);
     const int split = id % a.splits;
     id /= a.splits;
-    const int chunk = id % a.chunks;
-    id /= a.chunks;
-    const int tile = a.row_tiles - 1 - id % a.row_tiles;
-    id /= a.row_tiles;
-    const int hk = id % a.Hk, b = id / a.Hk;
-    const int v0 = chunk * DV, width = a.dv - v0 < DV ? a.dv - v0 : DV;   // its channels of v
-    const Sequence s = sequence(a, b);
-    const int64_t wide_rows = (int64_t)s.nq * a.group;
-    const int64_t start = (int64_t)tile * (32 * WAVES);
-    if (start >= wide_rows) return;
-    const int rows = (int)(wide_rows - start < 32 * WAVES ? wide_rows - start : 32 * WAVES);
-
-    // this lane's row; lanes behind the last row repeat it and store nothing
-    const int mine = wave * 32 + (lane & 31);
-    const bool valid = mine < rows;
-    const int64_t number = start + (valid ? mine : rows - 1);
-    const int t = (int)(number / a.group), g = (int)(number - (int64_t)t * a.group), head = hk * a.group + g;
-    const int first = first_seen(a, s, t), last = last_seen(a, s, t);
-    // what the wave's and the workgroup's rows see: rows rise with t, and so do both ends
-    const int wave_low = __builtin_amdgcn_readlane(first, 0), wave_full = __builtin_amdgcn_readlane(first, 31);
-    const int wave_end = __builtin_amdgcn_readlane(last, 0);
-    const int wave_high = wave * 32 < rows ? __builtin_amdgcn_readlane(last, 31) : -1;
-    const int low = first_seen(a, s, (int)(start / a.group));
-    const int high = last_seen(a, s, (int)((start + rows - 1) / a.group));
-    int tile0 = low / KT, tiles = high >= low ? high / KT + 1 - tile0 : 0;
-    {   // this split's part of them
+    const RowTile r = row_tile<32 * BLOCKS>(a, id, lane, block);
+    if (r.rows <= 0) return;
+    const Sequence &s = r.s;
+    int tile0 = r.low / KT, tiles = r.high >= r.low ? r.high / KT + 1 - tile0 : 0;
+    if (a.splits > 1) {   // this split's part of them
         const int from = (int)((int64_t)tiles * split / a.splits), to = (int)((int64_t)tiles * (split + 1) / a.splits);
         tile0 += from;
         tiles = to - from;
     }
 
-    const T *kp = head_of<T>(a.k, s.batch, s.k0, 2 * hk), *vp = head_of<T>(a.v, s.batch, s.k0, hk) + v0;
-    auto stage = [&](int n) {
-        const int64_t j = (int64_t)(tile0 + n) * KT;
-        const uint32_t to = lds + (n & 1) * STAGE;
-        const int left = (int)(s.nk - j);
-        KTile::load(kp + j * a.k.token, a.k.token, left, a.d, a.vec, to, wave, lane);
-        KTile::load(kp + a.k.head + j * a.k.token, a.k.token, left, a.d, a.vec, to + KTile::BYTES, wave, lane);
-        VTile::load(vp + j * a.v.token, a.v.token, left, width, a.vec, to + 2 * KTile::BYTES, wave, lane);
+    const int64_t key0 = s.k0 + (int64_t)tile0 * KT;
+    const int left = s.nk - tile0 * KT;
+    KFeed keys(head_of<T>(a.k, s.batch, key0, 2 * r.hk), a.k.token, a.k.head, left, a.d, a.vec, wave, lane);
+    VFeed values(head_of<T>(a.v, s.batch, key0, r.hk), a.v.token, 0, left, a.dv, a.vec, wave, lane);
+    auto stage = [&](int n) {      // the next tile
+        keys.load(lds + (n & 1) * STAGE, wave, lane);
+        values.load(lds + (n & 1) * STAGE + 2 * KTile::BYTES, wave, lane);
     };
     if (tiles > 0) stage(0);
 
-    v8s q[2][D / 16];
+    v8s q[MAPS][D / 16];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < MAPS; ++i)
 #pragma unroll
         for (int c = 0; c < D / 16; ++c)
-            q[i][c] = row_operand(head_of<T>(a.q, s.batch, s.q0 + t, 2 * head + i), valid, c, a.d, a.vec, lane);
+            q[i][c] = row_operand(head_of<T>(a.q, s.batch, s.q0 + r.t, 2 * r.head + map + i), r.valid, c, a.d, a.vec, lane);
+    const float lam = a.splits > 1 ? 0.f : row_weight(a, r, lane);
 
-    v16f o[2][DV / 32];
-    float top[2], sum[2];
+    v16f o[MAPS][DV / 32];
+    float top[MAPS], sum[MAPS];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < MAPS; ++i) {
         top[i] = -__builtin_inff();
         sum[i] = 0.f;
 #pragma unroll
         for (int x = 0; x < DV / 32; ++x) o[i][x] = v16f{};
     }
 
+    const uint32_t k_at = lds + map * KTile::BYTES + KTile::rows_lane(lane);
+    const uint32_t v_at = lds + 2 * KTile::BYTES + VTile::turned_lane(lane);
     for (int n = 0; n < tiles; ++n) {
         arrive();
         if (n + 1 < tiles) stage(n + 1);
-        const uint32_t kt = lds + (n & 1) * STAGE, vt = kt + 2 * KTile::BYTES;
-#pragma unroll 1
+        const uint32_t kt = k_at + (n & 1) * STAGE, vt = v_at + (n & 1) * STAGE;
+#pragma unroll
         for (int kb = 0; kb < KT; kb += 32) {
             const int j0 = (tile0 + n) * KT + kb;
-            if (j0 > wave_high || j0 + 31 < wave_low) continue;
-            v16f z[2];
+            if (j0 > r.block_high || j0 + 31 < r.block_low) continue;
+            // Operands are read from LDS a few matrix instructions before their own; the compiler would
+            // put each read right before its use.
+            constexpr int AHEAD = 3, QK = MAPS * (D / 16), N = DV / 32;
+            v16f z[MAPS];
+            v8s f[QK + AHEAD];
+            auto key_operand = [&](int m) { return KTile::rows(kt + m % MAPS * KTile::BYTES, kb, m / MAPS); };
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                z[i] = v16f{};
+            for (int m = 0; m < AHEAD && m < QK; ++m) f[m] = key_operand(m);
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-                for (int c = 0; c < D / 16; ++c)
-                    z[i] = Mfma<T>::mul(KTile::rows(kt + i * KTile::BYTES, kb, c, lane), q[i][c], z[i]);
+            for (int m = 0; m < QK; ++m) {
+                if (m + AHEAD < QK) f[m + AHEAD] = key_operand(m + AHEAD);
+                __builtin_amdgcn_sched_barrier(0);
+                z[m % MAPS] = Mfma<T>::mul(f[m], q[m % MAPS][m / MAPS], m < MAPS ? v16f{} : z[m % MAPS]);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            if (j0 + 31 > wave_end || j0 < wave_full) {
-                const int at = j0 + 4 * (lane >> 5);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int j = at + 8 * (e / 4) + e % 4;
-                    const bool seen = j >= first && j <= last;
-                    z[0][e] = seen ? z[0][e] : -__builtin_inff();
-                    z[1][e] = seen ? z[1][e] : -__builtin_inff();
-                }
-            }
+            __builtin_amdgcn_s_setprio(0);
+            if (j0 + 31 > r.block_end || j0 < r.block_full) hide(r, j0, lane, z);
             // The maximum that the exponents are taken from follows the true one only when that has
             // grown by more than 2^8: a value is then at most 2^8, which 16 bits and the sums hold.  Each
             // row by itself: its bits do not depend on the rows beside it.
-            float now[2];
+            float now[MAPS], from[MAPS];
+            bool grown[MAPS], any = false;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int i = 0; i < MAPS; ++i) {
                 float m = z[i][0];
 #pragma unroll
                 for (int e = 1; e < 16; ++e) m = fmaxf(m, z[i][e]);
                 now[i] = half_max(m) * a.scale2;
+                grown[i] = now[i] > top[i] + 8.f;
+                any = any || grown[i];
             }
-            if (__any(now[0] > top[0] + 8.f || now[1] > top[1] + 8.f)) {
+            if (__any(any)) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const bool grown = now[i] > top[i] + 8.f;
-                    const float f = grown ? __builtin_amdgcn_exp2f(top[i] - now[i]) : 1.f;
-                    top[i] = grown ? now[i] : top[i];
-                    sum[i] *= f;
+                for (int i = 0; i < MAPS; ++i) {
+                    const float by = grown[i] ? __builtin_amdgcn_exp2f(top[i] - now[i]) : 1.f;
+                    top[i] = grown[i] ? now[i] : top[i];
+                    sum[i] *= by;
 #pragma unroll
-                    for (int x = 0; x < DV / 32; ++x) o[i][x] *= f;
+                    for (int x = 0; x < N; ++x) o[i][x] *= by;
                 }
             }
-            v8s p[2][2];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float from = top[i] == -__builtin_inff() ? 0.f : top[i];
-                float f[16], part = 0.f;
+            for (int i = 0; i < MAPS; ++i) from[i] = top[i] == -__builtin_inff() ? 0.f : top[i];
+            // values 8 c .. 8 c + 7 of the maps, two of them at a time (part k of PARTS)
+            constexpr int PARTS = MAPS * 4;
+            typedef T v2 __attribute__((ext_vector_type(2)));
+            v4i p[2][MAPS];
+            auto some = [&](int c, int k) {
+                const int i = k / 4, e = 8 * c + k % 4 * 2;
+                const float f0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i][e], a.scale2, -from[i]));
+                const float f1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i][e + 1], a.scale2, -from[i]));
+                sum[i] += f0 + f1;
+                p[c][i][k % 4] = __builtin_bit_cast(int, v2{(T)f0, (T)f1});
+            };
+            // the product of the first half with v beside the second half's exponentials
+            v8s w[2 * N + 2];
+            w[0] = VTile::turned(vt, kb, 0);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    f[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i][e], a.scale2, -from));
-                    part += f[e];
+            for (int k = 0; k < PARTS; ++k) some(0, k);
+            w[1] = VTile::turned(vt, kb, 1 % N);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int m = 0; m < 2 * N; ++m) {
+                if (m + 2 < 2 * N) w[m + 2] = VTile::turned(vt, kb + (m + 2) / N * 16, (m + 2) % N);
+#pragma unroll
+                for (int i = 0; i < MAPS; ++i) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    o[i][m % N] = Mfma<T>::mul(w[m], __builtin_bit_cast(v8s, p[m / N][i]), o[i][m % N]);
+                    if (m < N)
+#pragma unroll
+                        for (int k = (MAPS * m + i) * PARTS / (MAPS * N); k < (MAPS * m + i + 1) * PARTS / (MAPS * N); ++k)
+                            some(1, k);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                sum[i] += part;
-                p[i][0] = pack<T>(f, 0);
-                p[i][1] = pack<T>(f, 1);
             }
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int x = 0; x < DV / 32; ++x) {
-                    const v8s w = VTile::turned(vt, kb + 16 * c, x, lane);
-                    o[0][x] = Mfma<T>::mul(w, p[0][c], o[0][x]);
-                    o[1][x] = Mfma<T>::mul(w, p[1][c], o[1][x]);
-                }
+            __builtin_amdgcn_s_setprio(0);
         }
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) sum[i] = half_sum(sum[i]);
+    for (int i = 0; i < MAPS; ++i) sum[i] = half_sum(sum[i]);
 
     if (a.splits > 1) {
-        if (!valid) return;
+        if (!r.valid) return;
         // rows of a part: [sequence][key head][split][number]
-        const int64_t part = (((int64_t)b * a.Hk + hk) * a.splits + split) * ((int64_t)a.tq * a.group) + number;
-        float *ml = a.parts + (int64_t)a.batch * a.Hk * a.splits * a.tq * a.group * 2 * a.dv + part * 4;
-        if (lane < 32 && chunk == 0) *(v4f *)ml = v4f{top[0], sum[0], top[1], sum[1]};
+        const int64_t part =
+            (((int64_t)r.b * a.Hk + r.hk) * a.splits + split) * ((int64_t)a.tq * a.group) + r.t * a.group + r.g;
+        float *ml = a.parts + (int64_t)a.batch * a.Hk * a.splits * a.tq * a.group * 2 * a.dv + part * 4 + 2 * map;
         const bool vec = a.dv % 4 == 0;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < MAPS; ++i) {
+            if (lane < 32) {
+                ml[2 * i] = top[i];
+                ml[2 * i + 1] = sum[i];
+            }
 #pragma unroll
             for (int x = 0; x < DV / 32; ++x)
 #pragma unroll
                 for (int e = 0; e < 16; e += 4)
-                    store4(a.parts + (part * 2 + i) * a.dv + v0, 32 * x + 2 * e + 4 * (lane >> 5), width, vec, o[i][x][e],
+                    store4(a.parts + (part * 2 + map + i) * a.dv, 32 * x + 2 * e + 4 * (lane >> 5), a.dv, vec, o[i][x][e],
                            o[i][x][e + 1], o[i][x][e + 2], o[i][x][e + 3]);
+        }
         return;
     }
-    float lam = 0.f;
-    for (int k = 0; k < a.group; ++k) {   // the whole wave makes each head's weight
-        const float w = weight_of(a.weight, hk * a.group + k, lane).lam;
-        lam = k == g ? w : lam;
+#pragma unroll
+    for (int i = 0; i < MAPS; ++i) {
+        const float over = sum[i] == 0.f ? 0.f : 1.f / sum[i];
+#pragma unroll
+        for (int x = 0; x < DV / 32; ++x) o[i][x] *= over;
     }
-    if (!valid) return;
-    const float f1 = sum[0] == 0.f ? 0.f : 1.f / sum[0], f2 = sum[1] == 0.f ? 0.f : 1.f / sum[1];
-    T *op = head_of<T>(a.o, s.batch, s.q0 + t, head) + v0;
+    const uint32_t hand = lds + block * 64 * DV * 2 + lane * 16;
+    if constexpr (MAPS == 1) {   // the second map's wave hands its product to the first one's
+        arrive();
+        if (map) {
 #pragma unroll
-    for (int x = 0; x < DV / 32; ++x) {
-        o[0][x] *= f1;
-        o[1][x] *= f2;
+            for (int x = 0; x < DV / 32; ++x)
 #pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-            const int c = 32 * x + 2 * e + 4 * (lane >> 5);
-            float y[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) y[j] = o[0][x][e + j] - lam * o[1][x][e + j];
-            store4(op, c, width, a.vec_out, y[0], y[1], y[2], y[3]);
+                for (int e = 0; e < 16; e += 4)
+                    *(__attribute__((address_space(3))) v4f *)(uintptr_t)(hand + (x * 4 + e / 4) * 1024) =
+                        v4f{o[0][x][e], o[0][x][e + 1], o[0][x][e + 2], o[0][x][e + 3]};
         }
+        arrive();
     }
-    if (!a.kept) return;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        float most = 0.f;
-#pragma unroll
-        for (int x = 0; x < DV / 32; ++x)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) most = larger(most, magnitude(o[i][x][e]));
-        most = larger(most, __shfl_xor(most, 32));
-        const KeptScale k = kept_scale(most);
-        int16_t *to = a.kept + (((s.row0 + t) * a.H + head) * 2 + i) * a.dv + v0;
-        const bool vec = a.dv % 4 == 0;
+    if (!r.valid) return;
+    if (map == 0) {
+        T *op = head_of<T>(a.o, s.batch, s.q0 + r.t, r.head);
 #pragma unroll
         for (int x = 0; x < DV / 32; ++x)
 #pragma unroll
             for (int e = 0; e < 16; e += 4) {
-                const int c = 32 * x + 2 * e + 4 * (lane >> 5);
-                const v4s q4 = {kept_code(o[i][x][e], k.inv), kept_code(o[i][x][e + 1], k.inv),
-                                kept_code(o[i][x][e + 2], k.inv), kept_code(o[i][x][e + 3], k.inv)};
-                if (vec) {
-                    if (c < width) *(v4s *)(to + c) = q4;
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (c + j < width) to[c + j] = q4[j];
-                }
+                v4f y;
+                if constexpr (MAPS == 1)
+                    y = lds_load<v4f>(hand + (x * 4 + e / 4) * 1024);
+                else
+                    y = v4f{o[MAPS - 1][x][e], o[MAPS - 1][x][e + 1], o[MAPS - 1][x][e + 2], o[MAPS - 1][x][e + 3]};
+                store4(op, 32 * x + 2 * e + 4 * (lane >> 5), a.dv, a.vec_out, o[0][x][e] - lam * y[0],
+                       o[0][x][e + 1] - lam * y[1], o[0][x][e + 2] - lam * y[2], o[0][x][e + 3] - lam * y[3]);
             }
-        if (lane < 32) {
-            float *at = a.stats + (2 * (int64_t)head + i) * a.stat_rows * a.rows + s.row0 + t;
-            if (chunk == 0) at[0] = sum[i] == 0.f ? __builtin_inff() : top[i] + __builtin_amdgcn_logf(sum[i]);
-            at[(1 + chunk) * a.rows] = k.scale;
+    }
+    if (!a.kept) return;
+#pragma unroll
+    for (int i = 0; i < MAPS; ++i) {
+        float *at = a.stats + (2 * (int64_t)r.head + map + i) * a.stat_rows * a.rows + s.row0 + r.t;
+        if (lane < 32) at[0] = sum[i] == 0.f ? __builtin_inff() : top[i] + __builtin_amdgcn_logf(sum[i]);
+        int16_t *kept = a.kept + (((s.row0 + r.t) * a.H + r.head) * 2 + map + i) * a.dv;
+        const bool vec = a.dv % 4 == 0;
+#pragma unroll
+        for (int w = 0; w < (DV + kScaleWidth - 1) / kScaleWidth; ++w) {
+            if (w * kScaleWidth >= a.dv) break;
+            float most = 0.f;
+#pragma unroll
+            for (int x = w * 4; x < w * 4 + 4 && x < DV / 32; ++x)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) most = larger(most, magnitude(o[i][x][e]));
+            most = larger(most, __shfl_xor(most, 32));
+            const KeptScale k = kept_scale(most);
+            if (lane < 32) at[(1 + w) * a.rows] = k.scale;
+#pragma unroll
+            for (int x = w * 4; x < w * 4 + 4 && x < DV / 32; ++x)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const int c = 32 * x + 2 * e + 4 * (lane >> 5);
+                    const v4s q4 = {kept_code(o[i][x][e], k.inv), kept_code(o[i][x][e + 1], k.inv),
+                                    kept_code(o[i][x][e + 2], k.inv), kept_code(o[i][x][e + 3], k.inv)};
+                    if (vec) {
+                        if (c < a.dv) *(v4s *)(kept + c) = q4;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (c + j < a.dv) kept[c + j] = q4[j];
+                    }
+                }
         }
     }
 }
 
-// The splits' sums of one row and head, a wave each:  M = max of m_s,
+// The splits' sums of one row and head, a workgroup each:  M = max of m_s,
 // o_i = sum of 2^(m_s - M) O_s / sum of 2^(m_s - M) l_s.
+// A thread makes the factors of one split (of up to 256), then 4 channels of both maps over every
+// `turns`-th split; the turns meet in LDS.  The order of the sums is fixed.
 template <class T>
 __global__ __launch_bounds__(256) void k_diff_join(AttnArgs a) {
-    const int lane = threadIdx.x & 63;
+    __shared__ float factor[2][kMaxSplits], low[4][4];
+    __shared__ v4f sums[2][256];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t wide = (int64_t)a.tq * a.group, all = (int64_t)a.batch * a.Hk * wide;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= all) return;
-    const int64_t number = row % wide, outer = row / wide;
+    const int64_t row = blockIdx.x, number = row % wide, outer = row / wide;
     const int hk = (int)(outer % a.Hk), b = (int)(outer / a.Hk);
-    const int t = (int)(number / a.group), head = hk * a.group + (int)(number - (int64_t)t * a.group);
+    const int t = token_of(a, (int)number), head = hk * a.group + (int)number - t * a.group;
     const Sequence s = sequence(a, b);
     if (t >= s.nq) return;
-    const float *ml = a.parts + all * a.splits * 2 * a.dv;
     const int64_t part = outer * a.splits * wide + number;
-    float top[2] = {-__builtin_inff(), -__builtin_inff()}, sum[2] = {0.f, 0.f};
-    for (int n = 0; n < a.splits; ++n) {
-        const v4f m = *(const v4f *)(ml + (part + n * wide) * 4);
-        top[0] = fmaxf(top[0], m[0]);
-        top[1] = fmaxf(top[1], m[2]);
-    }
+    const float *ml = a.parts + all * a.splits * 2 * a.dv + part * 4;
+    const int n = threadIdx.x;
+    v4f mine = {-__builtin_inff(), 0.f, -__builtin_inff(), 0.f};
+    if (n < a.splits) mine = *(const v4f *)(ml + n * wide * 4);
     const float lam = weight_of(a.weight, head, lane).lam;
-    T *op = head_of<T>(a.o, s.batch, s.q0 + t, head);
-    float y[2][kMaxValueWidth / 64];
+    float top[2], sum[2];
 #pragma unroll
-    for (int n = 0; n < kMaxValueWidth / 64; ++n) y[0][n] = y[1][n] = 0.f;
-    for (int n = 0; n < a.splits; ++n) {
-        const v4f m = *(const v4f *)(ml + (part + n * wide) * 4);
-        const float *p = a.parts + (part + n * wide) * 2 * a.dv;
+    for (int i = 0; i < 2; ++i) {
+        float m = mine[2 * i];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if (m[2 * i + 1] == 0.f) continue;     // a split that saw no key
-            const float f = __builtin_amdgcn_exp2f(m[2 * i] - top[i]);
-            sum[i] += f * m[2 * i + 1];
+        for (int step = 1; step < 64; step <<= 1) m = fmaxf(m, __shfl_xor(m, step));
+        if (lane == 0) low[i][wave] = m;
+    }
+    __syncthreads();
 #pragma unroll
-            for (int x = 0; x < kMaxValueWidth / 64; ++x)
-                if (lane + 64 * x < a.dv) y[i][x] += f * p[i * a.dv + lane + 64 * x];
+    for (int i = 0; i < 2; ++i) {
+        top[i] = fmaxf(fmaxf(low[i][0], low[i][1]), fmaxf(low[i][2], low[i][3]));
+        // (a split that saw no key has no products)
+        const float f = mine[2 * i + 1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(mine[2 * i] - top[i]);
+        if (n < a.splits) factor[i][n] = f;
+        const float part_sum = wave_sum(f * mine[2 * i + 1]);
+        if (lane == 0) low[2 + i][wave] = part_sum;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) sum[i] = (low[2 + i][0] + low[2 + i][1]) + (low[2 + i][2] + low[2 + i][3]);
+    // channels: pieces of 4, `turns` threads each
+    const int pieces = (a.dv + 3) / 4, turns = 256 / pieces < a.splits ? 256 / pieces : a.splits;
+    const int c = n % pieces * 4, turn = n / pieces;
+    v4f y[2] = {v4f{0.f, 0.f, 0.f, 0.f}, v4f{0.f, 0.f, 0.f, 0.f}};
+    if (turn < turns) {
+        const bool vec = a.dv % 4 == 0;
+        for (int k = turn; k < a.splits; k += turns) {
+            const float *p = a.parts + (part + k * wide) * 2 * a.dv + c;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float f = factor[i][k];
+                if (f == 0.f) continue;
+                if (vec)
+                    y[i] += f * *(const v4f *)(p + i * a.dv);
+                else
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (c + j < a.dv) y[i][j] += f * p[i * a.dv + j];
+            }
         }
     }
+    sums[0][n] = y[0];
+    sums[1][n] = y[1];
+    __syncthreads();
+    if (wave) return;                 // pieces: at most 64
+    const bool live = lane < pieces;
+    if (live)
+        for (int k = 1; k < turns; ++k) {
+            y[0] += sums[0][k * pieces + lane];
+            y[1] += sums[1][k * pieces + lane];
+        }
+    else
+        y[0] = y[1] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int x = 0; x < kMaxValueWidth / 64; ++x) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) y[i][x] = sum[i] == 0.f ? 0.f : y[i][x] / sum[i];
-        if (lane + 64 * x < a.dv) op[lane + 64 * x] = (T)(y[0][x] - lam * y[1][x]);
+    for (int i = 0; i < 2; ++i) y[i] *= sum[i] == 0.f ? 0.f : 1.f / sum[i];
+    if (live) {
+        const v4f out = y[0] - lam * y[1];
+        store4(head_of<T>(a.o, s.batch, s.q0 + t, head), lane * 4, a.dv, a.vec_out, out[0], out[1], out[2], out[3]);
     }
     if (!a.kept) return;
 #pragma unroll
@@ -291,27 +351,30 @@ __global__ __launch_bounds__(256) void k_diff_join(AttnArgs a) {
         float *at = a.stats + (2 * (int64_t)head + i) * a.stat_rows * a.rows + s.row0 + t;
         if (lane == 0) at[0] = sum[i] == 0.f ? __builtin_inff() : top[i] + __builtin_amdgcn_logf(sum[i]);
         int16_t *to = a.kept + (((s.row0 + t) * a.H + head) * 2 + i) * a.dv;
+        const float most = larger(larger(magnitude(y[i][0]), magnitude(y[i][1])), larger(magnitude(y[i][2]), magnitude(y[i][3])));
 #pragma unroll
-        for (int c = 0; c < kMaxValueWidth / kScaleWidth; ++c) {
-            if (c * kScaleWidth >= a.dv) break;
-            const KeptScale k = kept_scale(wave_largest(larger(magnitude(y[i][2 * c]), magnitude(y[i][2 * c + 1]))));
-            if (lane == 0) at[(1 + c) * a.rows] = k.scale;
+        for (int w = 0; w < kMaxValueWidth / kScaleWidth; ++w) {
+            if (w * kScaleWidth >= a.dv) break;
+            const bool in = lane * 4 / kScaleWidth == w;
+            const KeptScale k = kept_scale(wave_largest(in ? most : 0.f));
+            if (lane == 0) at[(1 + w) * a.rows] = k.scale;
+            if (in)
 #pragma unroll
-            for (int x = 2 * c; x < 2 * c + 2; ++x)
-                if (lane + 64 * x < a.dv) to[lane + 64 * x] = kept_code(y[i][x], k.inv);
+                for (int j = 0; j < 4; ++j)
+                    if (lane * 4 + j < a.dv) to[lane * 4 + j] = kept_code(y[i][j], k.inv);
         }
     }
 }
 
-template <class T, int WAVES>
+template <class T, bool WIDE>
 int forward(int cls, const AttnArgs &a, hipStream_t s) {
-    const dim3 grid((unsigned)((int64_t)a.batch * a.Hk * a.row_tiles * a.chunks * a.splits)), block(64 * WAVES);
+    const dim3 grid((unsigned)((int64_t)a.batch * a.Hk * a.row_tiles * a.splits));
     if (cls == 0)
-        hipLaunchKernelGGL((k_diff_forward<T, 32, 64, WAVES>), grid, block, 0, s, a);
+        hipLaunchKernelGGL((k_diff_forward<T, 32, 64, WIDE ? 4 : 1, 2, WIDE ? 64 : 32>), grid, dim3(WIDE ? 256 : 64), 0, s, a);
     else if (cls == 1)
-        hipLaunchKernelGGL((k_diff_forward<T, 64, 128, WAVES>), grid, block, 0, s, a);
+        hipLaunchKernelGGL((k_diff_forward<T, 64, 128, WIDE ? 4 : 1, 2, WIDE ? 64 : 32>), grid, dim3(WIDE ? 256 : 64), 0, s, a);
     else
-        hipLaunchKernelGGL((k_diff_forward<T, 128, 128, WAVES>), grid, block, 0, s, a);
+        hipLaunchKernelGGL((k_diff_forward<T, 128, 256, WIDE ? 2 : 1, 1, 32>), grid, dim3(WIDE ? 256 : 128), 0, s, a);
     return (int)hipGetLastError();
 }
 
@@ -319,13 +382,12 @@ int forward(int cls, const AttnArgs &a, hipStream_t s) {
 
 int launch_diff_forward(int type, int cls, bool wide, const AttnArgs &a, void *stream) {
     const hipStream_t s = (hipStream_t)stream;
-    if (type == NM_TYPE_F16) return wide ? forward<half_t, 4>(cls, a, s) : forward<half_t, 1>(cls, a, s);
-    return wide ? forward<bf16_t, 4>(cls, a, s) : forward<bf16_t, 1>(cls, a, s);
+    if (type == NM_TYPE_F16) return wide ? forward<half_t, true>(cls, a, s) : forward<half_t, false>(cls, a, s);
+    return wide ? forward<bf16_t, true>(cls, a, s) : forward<bf16_t, false>(cls, a, s);
 }
 
 int launch_diff_join(int type, const AttnArgs &a, void *stream) {
-    const int64_t rows = (int64_t)a.batch * a.Hk * a.tq * a.group;
-    const dim3 grid((unsigned)((rows + 3) / 4));
+    const dim3 grid((unsigned)((int64_t)a.batch * a.Hk * a.tq * a.group));
     if (type == NM_TYPE_F16)
         hipLaunchKernelGGL(k_diff_join<half_t>, grid, dim3(256), 0, (hipStream_t)stream, a);
     else

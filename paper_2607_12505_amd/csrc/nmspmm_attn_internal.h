@@ -53,7 +53,6 @@ struct AttnArgs {
     int vec;                  // q, k, v (and do) are whole 16-byte pieces
     int vec_out;              // o (backward: dq, dk, dv) is whole 8-byte pieces
     int row_tiles, splits;
-    int chunks;               // of v's channels, a workgroup each
     float *parts;             // [batch * Hk * splits * tq * group] x 2 dv values, then the same x 4: m1, l1, m2, l2
     // backward
     Heads grad, dq, dk, dv_;  // do and the gradients
@@ -64,14 +63,15 @@ struct AttnArgs {
     int key_tiles;
 };
 
-// Width classes that the kernels are built for: (32, 64), (64, 128), (128, 256); the last
-// one's sums of v do not fit the registers beside both maps: the forward pass makes 128 channels
-// of them a workgroup (and the scores for each).
+// Width classes that the kernels are built for: (32, 64), (64, 128), (128, 256).
 inline int width_class(int d, int dv) { return d <= 32 && dv <= 64 ? 0 : d <= 64 && dv <= 128 ? 1 : 2; }
-inline int value_chunks(int cls, int dv) { return cls == 2 ? (dv + 127) / 128 : 1; }
 constexpr int kScaleWidth = 128;              // channels of a scale of `kept`
 inline int stat_rows_of(int dv) { return 1 + (dv + kScaleWidth - 1) / kScaleWidth; }
-constexpr int kRowTileWide = 128, kRowTileNarrow = 32, kKeyTileWide = 64, kKeyTileNarrow = 32, kGradKeys = 128;
+// Rows of a workgroup of the forward pass: many, and few whose keys may be split.
+inline int wide_rows(int cls) { return cls == 2 ? 64 : 128; }
+constexpr int kFewRows = 32, kFewRowsKeys = 32, kMaxSplits = 256;
+// Of the backward pass: rows and keys of a workgroup, keys of a tile.
+constexpr int kGradRows = 128, kGradKeys = 128, kGradKeyTile = 64;
 
 int launch_diff_forward(int type, int cls, bool wide, const AttnArgs &a, void *stream);
 int launch_diff_join(int type, const AttnArgs &a, void *stream);

@@ -221,13 +221,29 @@ static nm_status check_backward(const nm_diff_grad_args *args) {
 static int64_t grad_row_tiles(const nm_diff_grad_args &g) {
     return ((int64_t)g.tokens.tq * (g.H / g.Hk) + kGradRows - 1) / kGradRows;
 }
+// Parts of the rows for the gradients of the keys: as many as fill the device's workgroups (two a compute
+// unit) where the tiles of keys do not, of at least four steps of 32 rows on average.
+static int key_splits(const nm_diff_grad_args &g) {
+    const int64_t tiles = ((int64_t)g.tokens.tk + kGradKeys - 1) / kGradKeys;
+    const int64_t groups = (int64_t)g.tokens.batch * g.Hk * tiles * (width_class(g.d, g.dv_width) == 2 ? 2 : 1);
+    const int64_t steps = ((int64_t)g.tokens.tq + 31) / 32 * (g.H / g.Hk);
+    if (groups == 0) return 1;
+    int64_t splits = 2 * device_cu_count() / groups;
+    if (splits > steps / 4) splits = steps / 4;
+    return splits < 2 ? 1 : splits > 64 ? 64 : (int)splits;
+}
+static size_t key_parts_bytes(const nm_diff_grad_args &g) {
+    const int splits = key_splits(g);
+    return splits > 1 ? round256((size_t)g.tokens.batch * g.Hk * splits * g.tokens.tk * (2 * g.d + g.dv_width) * 4) : 0;
+}
 static size_t delta_bytes(const nm_diff_grad_args &g) { return round256((size_t)2 * g.H * rows_of(g.tokens) * 4); }
 
 extern "C" nm_status nm_diff_attention_backward_workspace(const nm_diff_grad_args *args, size_t *bytes) {
     if (!bytes) return NM_ERR_ARG;
     const nm_status st = check_backward(args);
     if (st != NM_OK) return st;
-    *bytes = delta_bytes(*args) + (size_t)args->H * args->tokens.batch * grad_row_tiles(*args) * 16;
+    *bytes = delta_bytes(*args) + key_parts_bytes(*args) +
+             (size_t)args->H * args->tokens.batch * grad_row_tiles(*args) * 16;
     return NM_OK;
 }
 
@@ -255,7 +271,8 @@ extern "C" nm_status nm_diff_attention_backward(const nm_diff_grad_args *args, v
     AttnArgs a;
     fill(a, g.tokens, g.weight, g.H, g.Hk, g.d, g.dv_width, g.scale);
     const int64_t row_tiles = grad_row_tiles(g), key_tiles = (g.tokens.tk + kGradKeys - 1) / kGradKeys;
-    if (!grid_fits((int64_t)a.batch * a.Hk * row_tiles * 4) || !grid_fits((int64_t)a.tq * a.group) || !grid_fits((int64_t)a.batch * a.Hk * key_tiles + 1))
+    if (!grid_fits((int64_t)a.batch * a.Hk * row_tiles * 4) || !grid_fits((int64_t)a.tq * a.group) || !grid_fits((int64_t)a.batch * a.Hk * key_tiles * 2 * 64 + 1) ||
+        !grid_fits((int64_t)a.batch * a.Hk * a.tk))
         return NM_ERR_SHAPE;
     a.q = heads_of(g.q);
     a.k = heads_of(g.k);
@@ -271,7 +288,9 @@ extern "C" nm_status nm_diff_attention_backward(const nm_diff_grad_args *args, v
     a.row_tiles = (int)row_tiles;
     a.key_tiles = (int)key_tiles;
     a.delta = (float *)ws;
-    a.dlam_parts = (float *)((char *)ws + delta_bytes(g));
+    a.key_splits = key_splits(g);
+    a.key_parts = (float *)((char *)ws + delta_bytes(g));
+    a.dlam_parts = (float *)((char *)ws + delta_bytes(g) + key_parts_bytes(g));
     a.dlam_count = (int)((int64_t)a.batch * row_tiles * 4);
     a.dlam = g.dlam;
     a.dq1 = g.dq1;
@@ -280,5 +299,6 @@ extern "C" nm_status nm_diff_attention_backward(const nm_diff_grad_args *args, v
     a.dk2 = g.dk2;
     const int cls = width_class(g.d, g.dv_width);
     if (a.batch > 0 && row_tiles > 0 && launch_diff_grad_q(g.type, cls, a, stream) != 0) return NM_ERR_HIP;
-    return launch_diff_grad_k(g.type, cls, a, stream) == 0 ? NM_OK : NM_ERR_HIP;
+    if (launch_diff_grad_k(g.type, cls, a, stream) != 0) return NM_ERR_HIP;
+    return a.key_splits == 1 || launch_diff_join_keys(g.type, a, stream) == 0 ? NM_OK : NM_ERR_HIP;
 }

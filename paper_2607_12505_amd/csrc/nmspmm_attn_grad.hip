@@ -13,6 +13,7 @@
 // rows of q (which also makes D1, D2 and the parts of dlam), one over rows for the
 // keys.  The second makes scores and dp again: 512 of 1792 operations a pair at width
 // 64 + 128, against sums of dq in memory by atomics, whose order would change results.
+// Where the keys make too few workgroups, the rows are split too, and a third kernel joins their sums.
 #include "nmspmm_attn.h"
 
 namespace nmspmm {
@@ -101,34 +102,69 @@ __global__ __launch_bounds__(256, DV <= 128 ? 2 : 1) void k_diff_grad_q(AttnArgs
         for (int kb = 0; kb < KT; kb += 32) {
             const int j0 = (tile0 + n) * KT + kb;
             if (j0 > r.block_high || j0 + 31 < r.block_low) continue;
-            v16f z[2] = {v16f{}, v16f{}}, dp = v16f{};
+            // scores of both maps and dp, operands read a few instructions ahead
+            constexpr int AHEAD = 3, QK = 2 * (D / 16), ALL = QK + DV / 16, N = D / 32;
+            v16f z[2], dp;
+            v8s f[ALL + AHEAD];
+            auto operand = [&](int m) {
+                return m < QK ? KTile::rows(k_at + slot + m % 2 * KTile::BYTES, kb, m / 2) : VTile::rows(v_at + slot, kb, m - QK);
+            };
 #pragma unroll
-            for (int c = 0; c < D / 16; ++c)
+            for (int m = 0; m < AHEAD; ++m) f[m] = operand(m);
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    z[i] = Mfma<T>::mul(KTile::rows(k_at + slot + i * KTile::BYTES, kb, c), q[i][c], z[i]);
-#pragma unroll
-            for (int c = 0; c < DV / 16; ++c) dp = Mfma<T>::mul(VTile::rows(v_at + slot, kb, c), grad[c], dp);
-            if (j0 + 31 > r.block_end || j0 < r.block_full) hide(r, j0, lane, z);
-            float part = 0.f;
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                float ds1[8], ds2[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[0][8 * c + e], a.scale2, -lse[0]));
-                    const float p2 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[1][8 * c + e], a.scale2, -lse[1]));
-                    part = __builtin_fmaf(p2, dp[8 * c + e], part);
-                    ds1[e] = p1 * (dp[8 * c + e] - d[0]);
-                    ds2[e] = p2 * (dp[8 * c + e] - d[1]);
-                }
-                const v8s b1 = pack<T>(ds1), b2 = pack<T>(ds2);
-#pragma unroll
-                for (int x = 0; x < D / 32; ++x) {
-                    dq[0][x] = Mfma<T>::mul(KTile::turned(k_turned + slot, kb + 16 * c, x), b1, dq[0][x]);
-                    dq[1][x] = Mfma<T>::mul(KTile::turned(k_turned + slot + KTile::BYTES, kb + 16 * c, x), b2, dq[1][x]);
-                }
+            for (int m = 0; m < ALL; ++m) {
+                if (m + AHEAD < ALL) f[m + AHEAD] = operand(m + AHEAD);
+                __builtin_amdgcn_sched_barrier(0);
+                if (m < QK)
+                    z[m % 2] = Mfma<T>::mul(f[m], q[m % 2][m / 2], m < 2 ? v16f{} : z[m % 2]);
+                else
+                    dp = Mfma<T>::mul(f[m], grad[m - QK], m == QK ? v16f{} : dp);
+                __builtin_amdgcn_sched_barrier(0);
             }
+            __builtin_amdgcn_s_setprio(0);
+            if (j0 + 31 > r.block_end || j0 < r.block_full) hide(r, j0, lane, z);
+            // ds of values 8 c .. 8 c + 7, two of them at a time (part k of 4)
+            typedef T v2 __attribute__((ext_vector_type(2)));
+            v4i ds[2][2];
+            float part = 0.f;
+            auto some = [&](int c, int k) {
+                float d1[2], d2[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int at = 8 * c + 2 * k + e;
+                    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[0][at], a.scale2, -lse[0]));
+                    const float p2 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[1][at], a.scale2, -lse[1]));
+                    part = __builtin_fmaf(p2, dp[at], part);
+                    d1[e] = p1 * (dp[at] - d[0]);
+                    d2[e] = p2 * (dp[at] - d[1]);
+                }
+                ds[c][0][k] = __builtin_bit_cast(int, v2{(T)d1[0], (T)d1[1]});
+                ds[c][1][k] = __builtin_bit_cast(int, v2{(T)d2[0], (T)d2[1]});
+            };
+            // the first half's products with k beside the second half's values
+            v8s w[4 * N + 2];
+            auto turned = [&](int m) {
+                return KTile::turned(k_turned + slot + m % 2 * KTile::BYTES, kb + m / (2 * N) * 16, m / 2 % N);
+            };
+            w[0] = turned(0);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) some(0, k);
+            w[1] = turned(1);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int m = 0; m < 4 * N; ++m) {
+                if (m + 2 < 4 * N) w[m + 2] = turned(m + 2);
+                __builtin_amdgcn_sched_barrier(0);
+                v16f &to = dq[m % 2][m / 2 % N];
+                to = Mfma<T>::mul(w[m], __builtin_bit_cast(v8s, ds[m / (2 * N)][m % 2]), to);
+                if (m < 2 * N)
+#pragma unroll
+                    for (int k = m * 4 / (2 * N); k < (m + 1) * 4 / (2 * N); ++k) some(1, k);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            __builtin_amdgcn_s_setprio(0);
             second += part;
         }
     }
@@ -152,10 +188,10 @@ __global__ __launch_bounds__(256, DV <= 128 ? 2 : 1) void k_diff_grad_q(AttnArgs
 }
 
 // dlam and the learned vectors' gradients from the parts, by one workgroup.
-__device__ __forceinline__ void weight_grads(const AttnArgs &a, int lane, int wave) {
-    __shared__ float totals[4];
+__device__ __forceinline__ void weight_grads(const AttnArgs &a, int lane, int wave, int waves) {
+    __shared__ float totals[8];
     float total = 0.f;
-    for (int h = wave; h < a.H; h += 4) {
+    for (int h = wave; h < a.H; h += waves) {
         float sum = 0.f;
         for (int64_t i = lane; i < a.dlam_count; i += 64) sum += a.dlam_parts[(int64_t)h * a.dlam_count + i];
         sum = -wave_sum(sum);
@@ -175,9 +211,10 @@ __device__ __forceinline__ void weight_grads(const AttnArgs &a, int lane, int wa
     if (a.weight.value || a.weight.per_head) return;
     if (lane == 0) totals[wave] = total;
     __syncthreads();
-    total = (totals[0] + totals[1]) + (totals[2] + totals[3]);
+    total = 0.f;
+    for (int n = 0; n < waves; ++n) total += totals[n];
     const Weight w = weight_of(a.weight, 0, lane);
-    for (int i = threadIdx.x; i < a.weight.n; i += 256) {
+    for (int i = threadIdx.x; i < a.weight.n; i += 64 * waves) {
         a.dq1[i] = total * w.e1 * a.weight.k1[i];
         a.dk1[i] = total * w.e1 * a.weight.q1[i];
         a.dq2[i] = -total * w.e2 * a.weight.k2[i];
@@ -185,38 +222,51 @@ __device__ __forceinline__ void weight_grads(const AttnArgs &a, int lane, int wa
     }
 }
 
-// dk and dv: 128 keys a workgroup, 32 a wave, over the rows of all heads that share them.
-// Scores as rows x keys, so a lane's rows are of one key and the maps are the operands of dv
-// and dk as they lie.  DK, DV_: which of the two a workgroup makes.
+// dk and dv: 128 keys a workgroup, over the rows of all heads that share them.  Scores as rows x keys, so a
+// lane's rows are of one key and the maps are the operands of dv and dk as they lie.
+// PAIR 2: two waves for each 32 keys take every other block of 32 rows, and their sums meet at the end;
+// k and v are read from LDS as q and do are, which leaves the registers to the sums (256 of them hold both
+// maps' operands too, but not without spilling, and a wait for a spilled register waits for the next
+// tile's loads as well: 4 x 4096 rows of 8 heads, width 64 + 128, 760 us and 672).
+// PAIR 1, for the widest class, whose k and v fill LDS: a wave each, k in registers.
 template <class T, int D, int DV>
 struct KeySteps {
-    static constexpr int QT = 32;
-    using QTile = Tile<T, D / 8, QT, 4>;
-    using GTile = Tile<T, DV / 8, QT, 4>;
-    using VTile = Tile<T, DV / 8, kGradKeys, 4>;
-    using QFeed = Feed<T, D / 8, QT, 4, 2>;
-    using GFeed = Feed<T, DV / 8, QT, 4, 1>;
-    using VFeed = Feed<T, DV / 8, kGradKeys, 4, 1>;
+    static constexpr int PAIR = DV <= 128 ? 2 : 1, WAVES = 4 * PAIR, QT = 32 * PAIR;
+    using QTile = Tile<T, D / 8, QT, WAVES>;
+    using GTile = Tile<T, DV / 8, QT, WAVES>;
+    using KTile = Tile<T, D / 8, kGradKeys, WAVES>;
+    using VTile = Tile<T, DV / 8, kGradKeys, WAVES>;
+    using QFeed = Feed<T, D / 8, QT, WAVES, 2>;
+    using GFeed = Feed<T, DV / 8, QT, WAVES, 1>;
+    using KFeed = Feed<T, D / 8, kGradKeys, WAVES, 2>;
+    using VFeed = Feed<T, DV / 8, kGradKeys, WAVES, 1>;
     static constexpr int TILES = 2 * QTile::BYTES + GTile::BYTES, STAGE = TILES + 1024;
-    static constexpr int BYTES = VTile::BYTES + 2 * STAGE;
+    static constexpr int KEYS = PAIR == 2 ? 2 * KTile::BYTES : 0, FIXED = KEYS + VTile::BYTES;
+    static constexpr int HAND = PAIR == 2 ? 4 * 64 * (2 * D + DV) * 2 : 0;      // the second waves' sums
+    static constexpr int BYTES = FIXED + 2 * STAGE > HAND ? FIXED + 2 * STAGE : HAND;
 };
+// DK, DV_: which of the two a workgroup makes.
 template <class T, int D, int DV, bool DK, bool DV_>
 __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int id, int lane, int wave) {
     using S = KeySteps<T, D, DV>;
     using QTile = typename S::QTile;
     using GTile = typename S::GTile;
+    using KTile = typename S::KTile;
     using VTile = typename S::VTile;
-    constexpr int QT = S::QT, TILES = S::TILES, STAGE = S::STAGE;
+    constexpr int PAIR = S::PAIR, QT = S::QT, TILES = S::TILES, STAGE = S::STAGE;
+    const int block = wave / PAIR, sub = wave % PAIR;             // the wave's 32 keys, and which blocks of rows
+    const int split = id % a.key_splits;
+    id /= a.key_splits;
     const int tile = id % a.key_tiles;
     id /= a.key_tiles;
     const int hk = id % a.Hk, b = id / a.Hk;
     const Sequence s = sequence(a, b);
     const int begin = tile * kGradKeys;
     if (begin >= s.nk) return;
-    const int key0 = begin + wave * 32, key = key0 + (lane & 31);
+    const int key0 = begin + block * 32, key = key0 + (lane & 31);
     const bool valid = key < s.nk;
     const int off = s.nk - s.nq;
-    // rows that see any of the workgroup's keys; any of the wave's, and all of them
+    // rows that see any of the workgroup's keys, and all of the wave's
     const int end = s.nk - 1 < begin + kGradKeys - 1 ? s.nk - 1 : begin + kGradKeys - 1;
     const int low = begin - off - a.right, high = end - off + a.left;
     auto clip = [&](int t) { return t < 0 ? 0 : t < s.nq ? t : s.nq - 1; };
@@ -224,44 +274,57 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
     const int tiles = s.nq > 0 && high >= 0 && low < s.nq ? (clip(high) - t0) / QT + 1 : 0;
     const int from = key - off - a.right;                       // rows that see this lane's key
     const uint32_t span = (uint32_t)a.right + (uint32_t)a.left;
-    const int wave_low = key0 - off - a.right, wave_high = key0 < s.nk ? key0 + 31 - off + a.left : -1;
-    const int full_low = wave_low + 31, full_high = key0 - off + a.left;
+    const int full_low = key0 + 31 - off - a.right, full_high = key0 - off + a.left;
 
-    const uint32_t steps_at = lds + VTile::BYTES;
-    auto queries_of = [&](int head) {
-        return typename S::QFeed(head_of<T>(a.q, s.batch, s.q0 + t0, 2 * head), a.q.token, a.q.head, s.nq - t0, a.d, a.vec, wave,
+    // steps: the tiles of rows of one head after the other; this split's part of them
+    const int all = tiles * a.group, step0 = a.key_splits > 1 ? (int)((int64_t)all * split / a.key_splits) : 0;
+    const int steps = (a.key_splits > 1 ? (int)((int64_t)all * (split + 1) / a.key_splits) : all) - step0;
+    int head = hk * a.group, at = 0;       // this step's head and tile of rows
+    if (step0 > 0) {
+        head += step0 / tiles;
+        at = step0 % tiles;
+    }
+    const uint32_t steps_at = lds + S::FIXED;
+    auto queries_of = [&](int head, int t) {
+        return typename S::QFeed(head_of<T>(a.q, s.batch, s.q0 + t, 2 * head), a.q.token, a.q.head, s.nq - t, a.d, a.vec, wave,
                                  lane);
     };
-    auto grads_of = [&](int head) {
-        return typename S::GFeed(head_of<T>(a.grad, s.batch, s.q0 + t0, head), a.grad.token, 0, s.nq - t0, a.dv, a.vec, wave,
+    auto grads_of = [&](int head, int t) {
+        return typename S::GFeed(head_of<T>(a.grad, s.batch, s.q0 + t, head), a.grad.token, 0, s.nq - t, a.dv, a.vec, wave,
                                  lane);
     };
-    auto queries = queries_of(hk * a.group);
-    auto grads = grads_of(hk * a.group);
+    auto queries = queries_of(head, t0 + at * QT);
+    auto grads = grads_of(head, t0 + at * QT);
     auto stage = [&](int n, int head, int t) {
         const uint32_t to = steps_at + (n & 1) * STAGE;
         queries.load(to, wave, lane);
         grads.load(to + 2 * QTile::BYTES, wave, lane);
-        // a wave each: logarithms of both maps' sums, D1 and D2 (a load is of 64 lanes: zeros behind the 32 rows)
-        const int left = s.nq - t;
-        const int64_t map = 2 * (int64_t)head + (wave & 1);
-        const float *stat = (wave < 2 ? a.stats + map * a.stat_rows * a.rows : a.delta + map * a.rows) + s.row0 + t;
-        dma4(buffer_of(stat, (left < QT ? left : QT) * 4), lane * 4, to + TILES + wave * 256);
+        // a wave each: logarithms of both maps' sums, D1 and D2 (a load is of 64 lanes: zeros behind the last row)
+        if (wave < 4) {
+            const int left = s.nq - t;
+            const int64_t map = 2 * (int64_t)head + (wave & 1);
+            const float *stat = (wave < 2 ? a.stats + map * a.stat_rows * a.rows : a.delta + map * a.rows) + s.row0 + t;
+            dma4(buffer_of(stat, (left < QT ? left : QT) * 4), lane * 4, to + TILES + wave * 256);
+        }
     };
-    const int steps = tiles * a.group;
     if (steps > 0) {
+        if (PAIR == 2)
+            typename S::KFeed(head_of<T>(a.k, s.batch, s.k0 + begin, 2 * hk), a.k.token, a.k.head, s.nk - begin, a.d, a.vec, wave,
+                              lane)
+                .load(lds, wave, lane);
         if (DK)
             typename S::VFeed(head_of<T>(a.v, s.batch, s.k0 + begin, hk), a.v.token, 0, s.nk - begin, a.dv, a.vec, wave, lane)
-                .load(lds, wave, lane);
-        stage(0, hk * a.group, t0);
+                .load(lds + S::KEYS, wave, lane);
+        stage(0, head, t0 + at * QT);
     }
 
     v8s k[2][D / 16];
+    if constexpr (PAIR == 1)
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c)
-            k[i][c] = row_operand(head_of<T>(a.k, s.batch, s.k0 + key, 2 * hk + i), valid, c, a.d, a.vec, lane);
+            for (int c = 0; c < D / 16; ++c)
+                k[i][c] = row_operand(head_of<T>(a.k, s.batch, s.k0 + key, 2 * hk + i), valid, c, a.d, a.vec, lane);
     v16f dk[2][D / 32], dv[DV / 32];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -270,38 +333,53 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
 #pragma unroll
     for (int x = 0; x < DV / 32; ++x) dv[x] = v16f{};
 
-    const uint32_t q_at = steps_at + QTile::rows_lane(lane), q_turned = steps_at + QTile::turned_lane(lane);
-    const uint32_t g_at = steps_at + 2 * QTile::BYTES + GTile::rows_lane(lane);
-    const uint32_t g_turned = steps_at + 2 * QTile::BYTES + GTile::turned_lane(lane);
-    const uint32_t v_at = lds + VTile::rows_lane(lane) + VTile::place_of(wave * 32);
-    const uint32_t stat_at = steps_at + TILES + (lane >> 5) * 16;
+    const uint32_t rows_at = steps_at + QTile::place_of(sub * 32), g_rows_at = steps_at + 2 * QTile::BYTES + GTile::place_of(sub * 32);
+    const uint32_t q_at = rows_at + QTile::rows_lane(lane), q_turned = rows_at + QTile::turned_lane(lane);
+    const uint32_t g_at = g_rows_at + GTile::rows_lane(lane), g_turned = g_rows_at + GTile::turned_lane(lane);
+    const uint32_t k_at = lds + KTile::rows_lane(lane) + KTile::place_of(block * 32);
+    const uint32_t v_at = lds + S::KEYS + VTile::rows_lane(lane) + VTile::place_of(block * 32);
+    const uint32_t stat_at = steps_at + TILES + sub * 128 + (lane >> 5) * 16;
     float lam = 0.f;
-    int head = hk * a.group, at = 0;       // this step's head and tile of rows
     for (int n = 0; n < steps; ++n) {
-        if (at == 0) lam = weight_of(a.weight, head, lane).lam;
+        if (n == 0 || at == 0) lam = weight_of(a.weight, head, lane).lam;
         arrive();
-        const int r0 = t0 + at * QT;
+        const int r0 = t0 + at * QT + sub * 32;
         const bool next = at + 1 == tiles;
         at = next ? 0 : at + 1;
         if (next && ++head < (hk + 1) * a.group) {
-            queries = queries_of(head);
-            grads = grads_of(head);
+            queries = queries_of(head, t0);
+            grads = grads_of(head, t0);
         }
         if (n + 1 < steps) stage(n + 1, head, t0 + at * QT);
-        if (r0 > wave_high || r0 + 31 < wave_low) continue;
+        // (Rows behind the last are zero in q and do and add nothing, and neither do rows that see none of the wave's
+        // keys.  They are few, and a branch around the step would cost copies of all sums.)
         const uint32_t slot = (n & 1) * STAGE;
-        v16f z[2] = {v16f{}, v16f{}}, dp = v16f{};
+        constexpr int AHEAD = 2, QK = 2 * (D / 16), ALL = QK + (DK ? DV / 16 : 0);
+        v16f z[2], dp = v16f{};
+        v8s f[ALL + AHEAD], g[ALL + AHEAD];        // operands, read a few instructions ahead
+        auto operands = [&](int m) {
+            if (m < QK) {
+                f[m] = QTile::rows(q_at + slot + m % 2 * QTile::BYTES, 0, m / 2);
+                if constexpr (PAIR == 2) g[m] = KTile::rows(k_at + m % 2 * KTile::BYTES, 0, m / 2);
+            } else {
+                f[m] = GTile::rows(g_at + slot, 0, m - QK);
+                g[m] = VTile::rows(v_at, 0, m - QK);
+            }
+        };
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c)
+        for (int m = 0; m < AHEAD; ++m) operands(m);
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                z[i] = Mfma<T>::mul(QTile::rows(q_at + slot + i * QTile::BYTES, 0, c), k[i][c], z[i]);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int c = 0; c < DV / 16; ++c)
-            if (DK) dp = Mfma<T>::mul(GTile::rows(g_at + slot, 0, c), VTile::rows(v_at, 0, c), dp);
-        __builtin_amdgcn_sched_barrier(0);
-        // (rows behind the last are zero in q and do: they add nothing)
+        for (int m = 0; m < ALL; ++m) {
+            if (m + AHEAD < ALL) operands(m + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
+            if (m < QK)
+                z[m % 2] = Mfma<T>::mul(f[m], PAIR == 2 ? g[m] : k[m % 2][m / 2], m < 2 ? v16f{} : z[m % 2]);
+            else
+                dp = Mfma<T>::mul(f[m], g[m], dp);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
         if (r0 < full_low || r0 + 31 > full_high) {
             const int first = r0 + 4 * (lane >> 5) - from;
 #pragma unroll
@@ -311,38 +389,108 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
                 z[1][e] = seen ? z[1][e] : -__builtin_inff();
             }
         }
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            float both[8], ds1[8], ds2[8];
-#pragma unroll
-            for (int e4 = 0; e4 < 2; ++e4) {
-                const uint32_t stat = stat_at + slot + 64 * c + 32 * e4;
-                const v4f l1 = lds_load<v4f>(stat), l2 = lds_load<v4f>(stat + 256);
-                const v4f d1 = lds_load<v4f>(stat + 512), d2 = lds_load<v4f>(stat + 768);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int e = 4 * e4 + j, from = 8 * c + e;
-                    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[0][from], a.scale2, -l1[j]));
-                    const float p2 = lam * __builtin_amdgcn_exp2f(__builtin_fmaf(z[1][from], a.scale2, -l2[j]));
-                    both[e] = p1 - p2;
-                    ds1[e] = p1 * (dp[from] - d1[j]);
-                    ds2[e] = p2 * (d2[j] - dp[from]);
-                }
+        // p1 - lam p2 and ds of values 8 c .. 8 c + 7, four of them at a time (part h of 2)
+        typedef T v4 __attribute__((ext_vector_type(4)));
+        typedef int v2i __attribute__((ext_vector_type(2)));
+        v4i made[2][3];
+        auto some = [&](int c, int h) {
+            const uint32_t stat = stat_at + slot + 64 * c + 32 * h;
+            const v4f l1 = lds_load<v4f>(stat), l2 = lds_load<v4f>(stat + 256);
+            v4f d1 = {}, d2 = {};
+            if (DK) {
+                d1 = lds_load<v4f>(stat + 512);
+                d2 = lds_load<v4f>(stat + 768);
             }
-            const v8s b0 = pack<T>(both), b1 = pack<T>(ds1), b2 = pack<T>(ds2);
-            __builtin_amdgcn_sched_barrier(0);      // (the second half's statistics would not fit the registers)
+            v4 r0, r1, r2;
 #pragma unroll
-            for (int x = 0; x < DV / 32; ++x)
-                if (DV_) dv[x] = Mfma<T>::mul(GTile::turned(g_turned + slot, 16 * c, x), b0, dv[x]);
-#pragma unroll
-            for (int x = 0; x < D / 32; ++x) {
-                if (!DK) break;
-                dk[0][x] = Mfma<T>::mul(QTile::turned(q_turned + slot, 16 * c, x), b1, dk[0][x]);
-                dk[1][x] = Mfma<T>::mul(QTile::turned(q_turned + slot + QTile::BYTES, 16 * c, x), b2, dk[1][x]);
+            for (int e = 0; e < 4; ++e) {
+                const int v = 8 * c + 4 * h + e;
+                const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[0][v], a.scale2, -l1[e]));
+                const float p2 = lam * __builtin_amdgcn_exp2f(__builtin_fmaf(z[1][v], a.scale2, -l2[e]));
+                r0[e] = (T)(p1 - p2);
+                r1[e] = (T)(p1 * (dp[v] - d1[e]));
+                r2[e] = (T)(p2 * (d2[e] - dp[v]));
             }
+            const v2i i0 = __builtin_bit_cast(v2i, r0), i1 = __builtin_bit_cast(v2i, r1), i2 = __builtin_bit_cast(v2i, r2);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                made[c][0][2 * h + e] = i0[e];
+                made[c][1][2 * h + e] = i1[e];
+                made[c][2][2 * h + e] = i2[e];
+            }
+        };
+        // the first half's products beside the second half's values
+        constexpr int NV = DV_ ? DV / 32 : 0, NK = DK ? 2 * (D / 32) : 0, NALL = NV + NK;
+        v8s w[2 * NALL + 2];
+        auto turned = [&](int m) {
+            const int c = m / NALL, x = m % NALL;
+            return x < NV ? GTile::turned(g_turned + slot, 16 * c, x)
+                          : QTile::turned(q_turned + slot + (x - NV) % 2 * QTile::BYTES, 16 * c, (x - NV) / 2);
+        };
+        some(0, 0);
+        some(0, 1);
+        w[0] = turned(0);
+        w[1] = turned(1);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int m = 0; m < 2 * NALL; ++m) {
+            if (m + 2 < 2 * NALL) w[m + 2] = turned(m + 2);
+            __builtin_amdgcn_sched_barrier(0);
+            const int c = m / NALL, x = m % NALL;
+            v16f &to = x < NV ? dv[x] : dk[(x - NV) % 2][(x - NV) / 2];
+            to = Mfma<T>::mul(w[m], __builtin_bit_cast(v8s, made[c][x < NV ? 0 : 1 + (x - NV) % 2]), to);
+            if (m < NALL && m % (NALL / 2) == 0) some(1, m / (NALL / 2));
+            __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_s_setprio(0);
+    }
+    if constexpr (PAIR == 2) {             // the second waves hand their sums to the first
+        constexpr int N = 2 * (D / 32) + DV / 32;
+        const uint32_t hand = lds + block * 64 * (2 * D + DV) * 2 + lane * 16;
+        auto sums = [&](int n) -> v16f & { return n < DV / 32 ? dv[n] : dk[(n - DV / 32) % 2][(n - DV / 32) / 2]; };
+        arrive();
+        if (sub) {
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4)
+                    *(__attribute__((address_space(3))) v4f *)(uintptr_t)(hand + (4 * n + e / 4) * 1024) =
+                        v4f{sums(n)[e], sums(n)[e + 1], sums(n)[e + 2], sums(n)[e + 3]};
+        }
+        arrive();
+        if (sub) return;
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const v4f y = lds_load<v4f>(hand + (4 * n + e / 4) * 1024);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sums(n)[e + j] += y[j];
+            }
     }
     if (!valid) return;
+    if (a.key_splits > 1) {                // sums in 32 bits, dk's before its scale: 2 d and dv of a key
+        float *part = a.key_parts + ((((int64_t)b * a.Hk + hk) * a.key_splits + split) * a.tk + key) * (2 * a.d + a.dv);
+        const bool vec = a.d % 4 == 0 && a.dv % 4 == 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4)
+                    if (DK)
+                        store4(part + i * a.d, 32 * x + 2 * e + 4 * (lane >> 5), a.d, vec, dk[i][x][e], dk[i][x][e + 1],
+                               dk[i][x][e + 2], dk[i][x][e + 3]);
+#pragma unroll
+        for (int x = 0; x < DV / 32; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                if (DV_)
+                    store4(part + 2 * a.d, 32 * x + 2 * e + 4 * (lane >> 5), a.dv, vec, dv[x][e], dv[x][e + 1], dv[x][e + 2],
+                           dv[x][e + 3]);
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         if (!DK) break;
@@ -367,12 +515,12 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
 // The widest class's sums of both do not fit the registers: a workgroup for dk and one for dv, each
 // with the scores.  The last workgroup of the launch makes the learned weights' gradients.
 template <class T, int D, int DV>
-__global__ __launch_bounds__(256, DV <= 128 ? 2 : 1) void k_diff_grad_k(AttnArgs a) {
+__global__ __launch_bounds__((KeySteps<T, D, DV>::WAVES * 64), (DV <= 128 ? 2 : 1)) void k_diff_grad_k(AttnArgs a) {
     __shared__ __attribute__((aligned(1024))) char shared[KeySteps<T, D, DV>::BYTES];
     const uint32_t lds = lds_start(shared);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     if (blockIdx.x == gridDim.x - 1) {
-        weight_grads(a, lane, wave);
+        weight_grads(a, lane, wave, KeySteps<T, D, DV>::WAVES);
         return;
     }
     const int id = near_block(blockIdx.x, gridDim.x - 1);
@@ -382,6 +530,32 @@ __global__ __launch_bounds__(256, DV <= 128 ? 2 : 1) void k_diff_grad_k(AttnArgs
         key_grads<T, D, DV, false, true>(a, lds, id >> 1, lane, wave);
     else
         key_grads<T, D, DV, true, false>(a, lds, id >> 1, lane, wave);
+}
+
+// The splits' sums of a key: a wave each, in the splits' order.
+template <class T>
+__global__ __launch_bounds__(256) void k_diff_join_keys(AttnArgs a) {
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= (int64_t)a.batch * a.Hk * a.tk) return;
+    const int key = (int)(row % a.tk);
+    const int64_t outer = row / a.tk;
+    const int hk = (int)(outer % a.Hk), b = (int)(outer / a.Hk), width = 2 * a.d + a.dv;
+    const Sequence s = sequence(a, b);
+    if (key >= s.nk) return;
+    const float *p = a.key_parts + (outer * a.key_splits * a.tk + key) * width;
+    const int64_t next = (int64_t)a.tk * width;
+    T *dk = head_of<T>(a.dk, s.batch, s.k0 + key, 2 * hk), *dv = head_of<T>(a.dv_, s.batch, s.k0 + key, hk);
+    for (int c = lane; c < width; c += 64) {
+        float sum = 0.f;
+        for (int n = 0; n < a.key_splits; ++n) sum += p[n * next + c];
+        if (c < a.d)
+            dk[c] = (T)(sum * a.scale);
+        else if (c < 2 * a.d)
+            dk[a.dk.head + c - a.d] = (T)(sum * a.scale);
+        else
+            dv[c - 2 * a.d] = (T)sum;
+    }
 }
 
 template <class T>
@@ -395,15 +569,20 @@ int grad_q(int cls, const AttnArgs &a, hipStream_t s) {
         hipLaunchKernelGGL((k_diff_grad_q<T, 128, 256>), grid, block, 0, s, a);
     return (int)hipGetLastError();
 }
+template <class T, int D, int DV>
+int grad_k(const AttnArgs &a, hipStream_t s) {
+    const int64_t groups = (int64_t)a.batch * a.Hk * a.key_tiles * a.key_splits * (DV <= 128 ? 1 : 2) + 1;
+    hipLaunchKernelGGL((k_diff_grad_k<T, D, DV>), dim3((unsigned)groups), dim3(KeySteps<T, D, DV>::WAVES * 64), 0, s, a);
+    return (int)hipGetLastError();
+}
 template <class T>
 int grad_k(int cls, const AttnArgs &a, hipStream_t s) {
-    const dim3 grid((unsigned)((int64_t)a.batch * a.Hk * a.key_tiles * (cls == 2 ? 2 : 1) + 1)), block(256);
-    if (cls == 0)
-        hipLaunchKernelGGL((k_diff_grad_k<T, 32, 64>), grid, block, 0, s, a);
-    else if (cls == 1)
-        hipLaunchKernelGGL((k_diff_grad_k<T, 64, 128>), grid, block, 0, s, a);
-    else
-        hipLaunchKernelGGL((k_diff_grad_k<T, 128, 256>), grid, block, 0, s, a);
+    return cls == 0 ? grad_k<T, 32, 64>(a, s) : cls == 1 ? grad_k<T, 64, 128>(a, s) : grad_k<T, 128, 256>(a, s);
+}
+template <class T>
+int join_keys(const AttnArgs &a, hipStream_t s) {
+    const int64_t rows = (int64_t)a.batch * a.Hk * a.tk;
+    hipLaunchKernelGGL(k_diff_join_keys<T>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
     return (int)hipGetLastError();
 }
 
@@ -414,6 +593,9 @@ int launch_diff_grad_q(int type, int cls, const AttnArgs &a, void *stream) {
 }
 int launch_diff_grad_k(int type, int cls, const AttnArgs &a, void *stream) {
     return type == NM_TYPE_F16 ? grad_k<half_t>(cls, a, (hipStream_t)stream) : grad_k<bf16_t>(cls, a, (hipStream_t)stream);
+}
+int launch_diff_join_keys(int type, const AttnArgs &a, void *stream) {
+    return type == NM_TYPE_F16 ? join_keys<half_t>(a, (hipStream_t)stream) : join_keys<bf16_t>(a, (hipStream_t)stream);
 }
 
 }  // namespace nmspmm

@@ -60,7 +60,8 @@ struct AttnArgs {
     float *dlam_parts;        // [H][batch * row_tiles * 4]
     int dlam_count;           // batch * row_tiles * 4
     float *dlam, *dq1, *dk1, *dq2, *dk2;
-    int key_tiles;
+    int key_tiles, key_splits;
+    float *key_parts;         // [batch * Hk * key_splits * tk][2 d + dv] (key_splits > 1)
 };
 
 // Width classes that the kernels are built for: (32, 64), (64, 128), (128, 256).
@@ -77,5 +78,6 @@ int launch_diff_forward(int type, int cls, bool wide, const AttnArgs &a, void *s
 int launch_diff_join(int type, const AttnArgs &a, void *stream);
 int launch_diff_grad_q(int type, int cls, const AttnArgs &a, void *stream);
 int launch_diff_grad_k(int type, int cls, const AttnArgs &a, void *stream);
+int launch_diff_join_keys(int type, const AttnArgs &a, void *stream);
 
 }  // namespace nmspmm

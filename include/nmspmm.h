@@ -671,7 +671,7 @@ nm_status nm_rotary(const nm_rotary_args *args, void *stream);
  * rows = batch * tq, or total_q.
  * type: NM_TYPE_F16 or NM_TYPE_BF16.  d <= 128, dv <= 256; scale > 0.  q, k, v apart from the outputs.
  * ws: nm_diff_attention_workspace bytes of device memory, any content, 16-byte
- * aligned (NULL where that is 0; it depends on sizes alone).  Without rows it is a no-op.
+ * aligned (NULL where that is 0; sizes decide it, and whether k_lens or offsets are given).  Without rows it is a no-op.
  * Errors: NM_ERR_ARG (NULL or misaligned pointer, another type, scale not positive or not finite), NM_ERR_SHAPE (a size or
  * stride out of range: sequences of 2^28 rows, token strides of 2^22 values), NM_ERR_WORKSPACE, NM_ERR_HIP. */
 typedef struct nm_heads {

@@ -84,8 +84,14 @@ void fill(AttnArgs &a, const nm_tokens &t, const nm_diff_weight &w, int H, int H
     a.weight = w;
 }
 
-// How the forward pass is cut: workgroups of many rows that share their tiles of keys, or of few rows, with the
-// keys in `splits` parts that a second kernel joins.
+// How the forward pass is cut: workgroups of many rows that share their tiles of keys, or of few rows, whose
+// keys go to the runs of a workgroup and in `splits` parts to several, which a second kernel joins.
+//   Few rows: up to 64, and more over long keys (tk > 1024) where workgroups of many would leave compute units
+//   without any (1 x 40 rows of 8 heads over 4096 keys 20 us).
+//   Splits: a workgroup a compute unit, of four tiles a wave at least (1 row of 8 heads over 577 keys
+//   in one 14.6 us, in three and a second kernel 13.3; over 8192 in eight 20.0).  Sequences of unequal length: twice as
+//   many where those are few and long (16 x 1 rows over up to 16384 keys, 4 key heads, 69 to 61 us; 8 over 32768, 8
+//   key heads, 162 to 129; 4 over 16384 would go 31 to 34 us, 64 over 4096 67 to 71).
 struct Cut {
     bool wide;
     int row_tiles, splits;
@@ -101,8 +107,10 @@ Cut cut_of(const nm_tokens &t, int H, int Hk, int cls) {
     c.splits = 1;
     if (!c.wide) {
         const int64_t groups = heads * c.row_tiles, key_tiles = (t.tk + kFewRowsKeys - 1) / kFewRowsKeys;
-        int64_t splits = groups ? 4 * cus / groups : 1;
-        if (splits > key_tiles) splits = key_tiles;
+        int64_t splits = groups ? (cls == 2 ? 2 : 1) * cus / groups : 1;
+        if ((t.k_lens || t.k_offsets) && 4 * groups <= cus && key_tiles >= 128 * splits) splits *= 2;
+        const int64_t most = key_tiles / (4 * key_runs(cls));
+        if (splits > most) splits = most;
         if (splits > kMaxSplits) splits = kMaxSplits;
         c.splits = splits > 1 ? (int)splits : 1;
     }

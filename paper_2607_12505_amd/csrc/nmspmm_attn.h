@@ -101,13 +101,10 @@ __device__ __forceinline__ void arrive() {
     asm volatile("" ::: "memory");
 }
 
-// The same with this wave's newest N loads still under way.
-template <int N>
-__device__ __forceinline__ void arrive_but() {
-    static_assert(N >= 0 && N < 64, "vmcnt range");
+// This wave's loads have arrived, in LDS that no other wave reads.
+__device__ __forceinline__ void arrive_alone() {
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4));
-    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_s_waitcnt(0);
     asm volatile("" ::: "memory");
 }
 

@@ -17,26 +17,137 @@
 namespace nmspmm {
 namespace {
 
+// What the runs of keys of one block of rows have made, joined:  M = max of m_s,
+// o_i = sum of 2^(m_s - M) O_s / sum of 2^(m_s - M) l_s, each wave for some of the channels.
+template <class T, int DV, int RUNS, int REGION>
+__device__ __forceinline__ void join_runs(const AttnArgs &a, const RowTile &r, uint32_t lds, int split, float lam,
+                                          float (&top)[2], float (&sum)[2], v16f (&o)[2][DV / 32], int lane, int run) {
+    constexpr int N = DV / 32;
+    static_assert(N <= RUNS, "a wave for each 32 channels");
+    __shared__ v4f ends[RUNS][32];
+    __shared__ float largest[N][2][32];
+    const int row = lane & 31;
+    const bool joins = run < N;                     // this wave makes the channels from 32 run
+    const uint32_t mine = lds + run * REGION + lane * 16;
+    if (lane < 32) ends[run][row] = v4f{top[0], sum[0], top[1], sum[1]};
+    v16f y[2] = {v16f{}, v16f{}};
+    float most[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        arrive();                                   // the tiles, or the other map's products, have been read
+#pragma unroll
+        for (int x = 0; x < N; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                *(__attribute__((address_space(3))) v4f *)(uintptr_t)(mine + (x * 4 + e / 4) * 1024) =
+                    v4f{o[i][x][e], o[i][x][e + 1], o[i][x][e + 2], o[i][x][e + 3]};
+        arrive();
+        float m = -__builtin_inff(), l = 0.f, f[RUNS];
+#pragma unroll
+        for (int n = 0; n < RUNS; ++n) m = fmaxf(m, ends[n][row][2 * i]);
+#pragma unroll
+        for (int n = 0; n < RUNS; ++n) {            // (a run that saw no key has no products)
+            f[n] = ends[n][row][2 * i + 1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ends[n][row][2 * i] - m);
+            l += f[n] * ends[n][row][2 * i + 1];
+        }
+        top[i] = m;
+        sum[i] = l;
+        if (!joins) continue;
+        const float over = a.splits > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int n = 0; n < RUNS; ++n)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const v4f p = lds_load<v4f>(lds + n * REGION + lane * 16 + (run * 4 + e / 4) * 1024);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[i][e + j] += f[n] * over * p[j];
+            }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) most[i] = larger(most[i], magnitude(y[i][e]));
+    }
+    if (a.splits > 1) {
+        if (!r.valid) return;
+        const int64_t part =
+            (((int64_t)r.b * a.Hk + r.hk) * a.splits + split) * ((int64_t)a.tq * a.group) + r.t * a.group + r.g;
+        float *ml = a.parts + (int64_t)a.batch * a.Hk * a.splits * a.tq * a.group * 2 * a.dv + part * 4;
+        if (run == 0 && lane < 32) *(v4f *)ml = v4f{top[0], sum[0], top[1], sum[1]};
+        const bool vec = a.dv % 4 == 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                if (joins)
+                    store4(a.parts + (part * 2 + i) * a.dv, 32 * run + 2 * e + 4 * (lane >> 5), a.dv, vec, y[i][e],
+                           y[i][e + 1], y[i][e + 2], y[i][e + 3]);
+        return;
+    }
+    if (r.valid && joins) {
+        T *op = head_of<T>(a.o, r.s.batch, r.s.q0 + r.t, r.head);
+#pragma unroll
+        for (int e = 0; e < 16; e += 4)
+            store4(op, 32 * run + 2 * e + 4 * (lane >> 5), a.dv, a.vec_out, y[0][e] - lam * y[1][e],
+                   y[0][e + 1] - lam * y[1][e + 1], y[0][e + 2] - lam * y[1][e + 2], y[0][e + 3] - lam * y[1][e + 3]);
+    }
+    if (!a.kept) return;
+    static_assert(DV <= kScaleWidth, "one scale a row and map");
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        most[i] = larger(most[i], __shfl_xor(most[i], 32));
+        if (joins && lane < 32) largest[run][i][row] = most[i];
+    }
+    arrive();
+    if (!r.valid || !joins) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        float m = largest[0][i][row];
+#pragma unroll
+        for (int n = 1; n < N; ++n) m = larger(m, largest[n][i][row]);
+        const KeptScale k = kept_scale(m);
+        if (run == 0 && lane < 32) {
+            float *at = a.stats + (2 * (int64_t)r.head + i) * a.stat_rows * a.rows + r.s.row0 + r.t;
+            at[0] = sum[i] == 0.f ? __builtin_inff() : top[i] + __builtin_amdgcn_logf(sum[i]);
+            at[a.rows] = k.scale;
+        }
+        int16_t *kept = a.kept + (((r.s.row0 + r.t) * a.H + r.head) * 2 + i) * a.dv;
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            const int c = 32 * run + 2 * e + 4 * (lane >> 5);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (c + j < a.dv) kept[c + j] = kept_code(y[i][e + j], k.inv);
+        }
+    }
+}
+
 // BLOCKS blocks of 32 rows share tiles of KT keys in a ring of two.  MAPS 2: a wave makes both
 // maps of its block, whose products share v's operands; MAPS 1: two waves a block make one each and
 // meet at the end.  Both maps' sums of 256 channels do not fit a wave's registers, and of 128 they do: (64, 128)
 // runs 4 x 4096 rows of 8 heads in 0.49 ms with MAPS 2 and 0.61 with MAPS 1 (more reads of LDS and scalar instructions),
 // (128, 256) 2 x 4096 rows in 0.44 ms with MAPS 1 and 0.75 with the scores made for 128 channels at a time.
-template <class T, int D, int DV, int BLOCKS, int MAPS, int KT>
-__global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS), BLOCKS > 1 ? 2 : 1) void k_diff_forward(AttnArgs a) {
-    constexpr int WAVES = BLOCKS * (3 - MAPS);
+// RUNS: runs of keys of one block of rows, a wave and a ring each, that meet at the end (few rows): the smallest calls
+// need no second kernel.  Bound by memory where the cache is long: 16 x 1 rows over 16384 keys (4 key heads of
+// 64 + 128, 537 MB) 112 us; where it is short, by a wave's 1.4 us for 32 keys: 1 row over 577, 14.6 us.  (Eight waves
+// with a tile each, one at its loads beside another that computes: 117 and 14.0 us.)
+template <class T, int D, int DV, int BLOCKS, int MAPS, int KT, int RUNS>
+__global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS) * RUNS, BLOCKS > 1 ? 2 : 1) void k_diff_forward(AttnArgs a) {
+    static_assert(RUNS == 1 || (BLOCKS == 1 && MAPS == 2), "runs of one block");
+    constexpr int WAVES = BLOCKS * (3 - MAPS);     // that share a ring
     using KTile = Tile<T, D / 8, KT, WAVES>;
     using VTile = Tile<T, DV / 8, KT, WAVES>;
     using KFeed = Feed<T, D / 8, KT, WAVES, 2>;
     using VFeed = Feed<T, DV / 8, KT, WAVES, 1>;
     constexpr int STAGE = 2 * KTile::BYTES + VTile::BYTES;
-    static_assert(MAPS == 2 || BLOCKS * 64 * DV * 2 <= 2 * STAGE, "room for the second maps' products");
-    __shared__ __attribute__((aligned(1024))) char shared[2 * STAGE];
-    const uint32_t lds = lds_start(shared);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    constexpr int SLOTS = 2;
+    static_assert(MAPS == 2 || BLOCKS * 64 * DV * 2 <= SLOTS * STAGE, "room for the second maps' products");
+    static_assert(RUNS == 1 || 64 * DV * 2 <= SLOTS * STAGE, "room for one map's products of a run");
+    __shared__ __attribute__((aligned(1024))) char shared[RUNS * SLOTS * STAGE];
+    const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int run = RUNS > 1 ? all : 0, wave = RUNS > 1 ? 0 : all;
+    const uint32_t lds = lds_start(shared) + run * SLOTS * STAGE;
     const int block = MAPS == 2 ? wave : wave >> 1, map = MAPS == 2 ? 0 : wave & 1;   // the wave's first map
 
-    int id = near_block(blockIdx.x, gridDim.x);
+    // (the parts of a cache share nothing: those of a long one go to all XCDs)
+    int id = RUNS > 1 ? (int)blockIdx.x : near_block(blockIdx.x, gridDim.x);
     const int split = id % a.splits;
     id /= a.splits;
     const RowTile r = row_tile<32 * BLOCKS>(a, id, lane, block);
@@ -48,14 +159,19 @@ __global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS), BLOCKS > 1 ? 2 : 1) void 
         tile0 += from;
         tiles = to - from;
     }
+    if (RUNS > 1) {
+        const int from = tiles * run / RUNS, to = tiles * (run + 1) / RUNS;
+        tile0 += from;
+        tiles = to - from;
+    }
 
     const int64_t key0 = s.k0 + (int64_t)tile0 * KT;
     const int left = s.nk - tile0 * KT;
     KFeed keys(head_of<T>(a.k, s.batch, key0, 2 * r.hk), a.k.token, a.k.head, left, a.d, a.vec, wave, lane);
     VFeed values(head_of<T>(a.v, s.batch, key0, r.hk), a.v.token, 0, left, a.dv, a.vec, wave, lane);
     auto stage = [&](int n) {      // the next tile
-        keys.load(lds + (n & 1) * STAGE, wave, lane);
-        values.load(lds + (n & 1) * STAGE + 2 * KTile::BYTES, wave, lane);
+        keys.load(lds + n % SLOTS * STAGE, wave, lane);
+        values.load(lds + n % SLOTS * STAGE + 2 * KTile::BYTES, wave, lane);
     };
     if (tiles > 0) stage(0);
 
@@ -80,9 +196,12 @@ __global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS), BLOCKS > 1 ? 2 : 1) void 
     const uint32_t k_at = lds + map * KTile::BYTES + KTile::rows_lane(lane);
     const uint32_t v_at = lds + 2 * KTile::BYTES + VTile::turned_lane(lane);
     for (int n = 0; n < tiles; ++n) {
-        arrive();
+        if (RUNS > 1)
+            arrive_alone();
+        else
+            arrive();
         if (n + 1 < tiles) stage(n + 1);
-        const uint32_t kt = k_at + (n & 1) * STAGE, vt = v_at + (n & 1) * STAGE;
+        const uint32_t kt = k_at + n % SLOTS * STAGE, vt = v_at + n % SLOTS * STAGE;
 #pragma unroll
         for (int kb = 0; kb < KT; kb += 32) {
             const int j0 = (tile0 + n) * KT + kb;
@@ -170,6 +289,10 @@ __global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS), BLOCKS > 1 ? 2 : 1) void 
 #pragma unroll
     for (int i = 0; i < MAPS; ++i) sum[i] = half_sum(sum[i]);
 
+    if constexpr (RUNS > 1) {
+        join_runs<T, DV, RUNS, SLOTS * STAGE>(a, r, lds_start(shared), split, lam, top, sum, o, lane, run);
+        return;
+    }
     if (a.splits > 1) {
         if (!r.valid) return;
         // rows of a part: [sequence][key head][split][number]
@@ -370,11 +493,11 @@ template <class T, bool WIDE>
 int forward(int cls, const AttnArgs &a, hipStream_t s) {
     const dim3 grid((unsigned)((int64_t)a.batch * a.Hk * a.row_tiles * a.splits));
     if (cls == 0)
-        hipLaunchKernelGGL((k_diff_forward<T, 32, 64, WIDE ? 4 : 1, 2, WIDE ? 64 : 32>), grid, dim3(WIDE ? 256 : 64), 0, s, a);
+        hipLaunchKernelGGL((k_diff_forward<T, 32, 64, WIDE ? 4 : 1, 2, WIDE ? 64 : 32, WIDE ? 1 : 4>), grid, dim3(256), 0, s, a);
     else if (cls == 1)
-        hipLaunchKernelGGL((k_diff_forward<T, 64, 128, WIDE ? 4 : 1, 2, WIDE ? 64 : 32>), grid, dim3(WIDE ? 256 : 64), 0, s, a);
+        hipLaunchKernelGGL((k_diff_forward<T, 64, 128, WIDE ? 4 : 1, 2, WIDE ? 64 : 32, WIDE ? 1 : 4>), grid, dim3(256), 0, s, a);
     else
-        hipLaunchKernelGGL((k_diff_forward<T, 128, 256, WIDE ? 2 : 1, 1, 32>), grid, dim3(WIDE ? 256 : 128), 0, s, a);
+        hipLaunchKernelGGL((k_diff_forward<T, 128, 256, WIDE ? 2 : 1, 1, 32, 1>), grid, dim3(WIDE ? 256 : 128), 0, s, a);
     return (int)hipGetLastError();
 }
 

@@ -71,6 +71,7 @@ inline int stat_rows_of(int dv) { return 1 + (dv + kScaleWidth - 1) / kScaleWidt
 // Rows of a workgroup of the forward pass: many, and few whose keys may be split.
 inline int wide_rows(int cls) { return cls == 2 ? 64 : 128; }
 constexpr int kFewRows = 32, kFewRowsKeys = 32, kMaxSplits = 256;
+inline int key_runs(int cls) { return cls == 2 ? 1 : 4; }    // of a workgroup of few rows
 // Of the backward pass: rows and keys of a workgroup, keys of a tile.
 constexpr int kGradRows = 128, kGradKeys = 128, kGradKeyTile = 64;
 

@@ -15,10 +15,67 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 from typing import NamedTuple, Optional
 
+from . import nmblock
 from .nmblock import NM_TYPE_F32, _empty, _handle, _index, _on, _ptr, _runtime, _type_of, _written
-from .nmspmm import _check, lib
+from .nmspmm import NM_OK, NmError, _check, lib
+
+
+def _packer(structure) -> struct.Struct:
+    """A C structure's values, one after the other, as its bytes: a call passes some forty, which ctypes would set one by
+    one at twice the host time of a small call's kernels."""
+    codes = {ctypes.c_void_p: "Q", ctypes.c_int64: "q", ctypes.c_int32: "i", ctypes.c_float: "f"}
+    parts, end = ["="], 0
+
+    def add(kind, at):
+        nonlocal end
+        if kind in codes:
+            parts.append(f"{at - end}x{codes[kind]}")
+            end = at + ctypes.sizeof(kind)
+        elif issubclass(kind, ctypes.Array):
+            for i in range(kind._length_):
+                add(kind._type_, at + i * ctypes.sizeof(kind._type_))
+        else:
+            for name, field in kind._fields_:
+                add(field, at + getattr(kind, name).offset)
+
+    add(structure, 0)
+    parts.append(f"{ctypes.sizeof(structure) - end}x")
+    return struct.Struct("".join(parts))
+
+
+class _Calls:
+    """What every call looks up, looked up once."""
+
+    def __init__(self):
+        L = lib()
+        self.rotary, self.forward, self.forward_size = L.nm_rotary, L.nm_diff_attention, L.nm_diff_attention_workspace
+        self.backward, self.backward_size = L.nm_diff_attention_backward, L.nm_diff_attention_backward_workspace
+        self.sizes = {}       # workspace bytes by shapes: sizes, not buffers
+
+
+_calls: Optional[_Calls] = None
+
+
+def _library() -> _Calls:
+    global _calls
+    if _calls is None:
+        _calls = _Calls()
+    return _calls
+
+
+def _size(query, key, args) -> int:
+    sizes = _calls.sizes
+    need = sizes.get(key)
+    if need is None:
+        size = ctypes.c_size_t()
+        _check(query(args, ctypes.byref(size)), "workspace")
+        if len(sizes) > 512:
+            sizes.clear()
+        need = sizes[key] = size.value
+    return need
 
 
 def _heads(t, name: str, rt, dims=(3,)):
@@ -64,7 +121,8 @@ class RotaryAxes:
         self.pairs, self.axes, self.style = len(freqs), max(axis) + 1, style
         self.freqs = torch.tensor(freqs, dtype=torch.float64, device=device)
         self.axis = torch.tensor(axis, dtype=torch.int32, device=device)
-        self._dev = self.freqs.get_device()
+        self._dev, self._interleaved = self.freqs.get_device(), style == "pairs"
+        self._freqs_at, self._axis_at = self.freqs.data_ptr(), self.axis.data_ptr()
 
     @classmethod
     def of_sections(cls, sections, theta: float = 10000.0, own_ladders: bool = False, style: str = "halves",
@@ -89,21 +147,28 @@ def _tokens_of(t, name: str):
     return b * n, t.stride(1) if n > 1 else t.stride(0)
 
 
+_ROTARY = _packer(NmRotaryArgs)
+_NO_PART = (0, 0, 0, 0, 0, 0, 0)
+
+
 def _rotary(parts, positions, axes: RotaryAxes, back: bool, stream):
     """parts: (x, out or None, name) of one or two tensors; the outputs."""
-    rt = _runtime()
+    rt = nmblock._rt or _runtime()
+    C = _calls or _library()
     torch = rt.torch
     x = parts[0][0]
     dev = _index(x, parts[0][2], rt)
     code = _type_of(x, parts[0][2], rt)
     if axes._dev != dev:
         raise ValueError(f"axes: on cuda:{axes._dev}, expected cuda:{dev}")
-    d, a, outs, tokens = x.shape[-1] if x.dim() else 0, NmRotaryArgs(), [], None
-    for i, (t, out, name) in enumerate(parts):
+    d = x.shape[-1] if x.dim() else 0
+    values, outs, tokens, heads = [], [], None, 0
+    for t, out, name in parts:
         _heads(t, name, rt, (3, 4))
-        _on(t, name, dev)
-        if t.dtype != x.dtype or t.shape[-1] != d:
-            raise ValueError(f"{name}: {t.dtype} of {t.shape[-1]} channels, expected {x.dtype} of {d}")
+        if t is not x:
+            _on(t, name, dev)
+            if t.dtype != x.dtype or t.shape[-1] != d:
+                raise ValueError(f"{name}: {t.dtype} of {t.shape[-1]} channels, expected {x.dtype} of {d}")
         n, stride = _tokens_of(t, name)
         if tokens not in (None, n):
             raise ValueError(f"{name}: {n} tokens, expected {tokens}")
@@ -116,12 +181,14 @@ def _rotary(parts, positions, axes: RotaryAxes, back: bool, stream):
             _heads(out, f"out of {name}", rt, (3, 4))
             _on(out, f"out of {name}", dev)
             _written(out, rt)
-        to = _tokens_of(out, f"out of {name}")[1]
-        a.part[i] = NmRotaryPart(t.data_ptr(), out.data_ptr(), stride, t.stride(-2), to, out.stride(-2), t.shape[-2])
+        heads += t.shape[-2]
+        values += (t.data_ptr(), out.data_ptr(), stride, t.stride(-2), _tokens_of(out, f"out of {name}")[1],
+                   out.stride(-2), t.shape[-2])
         outs.append(out)
     if d < 2 * axes.pairs:
         raise ValueError(f"{parts[0][2]}: {d} channels, fewer than those of {axes.pairs} pairs")
-    if positions.dtype not in (torch.int32, torch.float32):
+    real = positions.dtype == torch.float32
+    if not real and positions.dtype != torch.int32:
         raise ValueError(f"positions: {positions.dtype}, expected int32 or float32")
     if positions.dim() == 1 and axes.axes == 1:
         positions = positions.unsqueeze(0)
@@ -130,13 +197,15 @@ def _rotary(parts, positions, axes: RotaryAxes, back: bool, stream):
     if tokens > 1 and positions.stride(1) != 1:
         raise ValueError("positions: tokens must be consecutive")
     _on(positions, "positions", dev)
-    if tokens == 0 or all(t.shape[-2] == 0 for t, _, _ in parts):
+    if tokens == 0 or heads == 0:
         return outs
-    a.pos, a.ld_pos = positions.data_ptr(), positions.stride(0)
-    a.freq, a.axis, a.tokens, a.type = axes.freqs.data_ptr(), axes.axis.data_ptr(), tokens, code
-    a.pos_float, a.pairs, a.d, a.axes = positions.dtype == torch.float32, axes.pairs, d, axes.axes
-    a.interleaved, a.back = axes.style == "pairs", back
-    _check(lib().nm_rotary(ctypes.byref(a), _handle(stream, dev, rt)), "nm_rotary")
+    if len(parts) == 1:
+        values += _NO_PART
+    args = _ROTARY.pack(*values, positions.data_ptr(), positions.stride(0), axes._freqs_at, axes._axis_at, tokens, code, real,
+                        axes.pairs, d, axes.axes, axes._interleaved, back)
+    st = C.rotary(args, _handle(stream, dev, rt))
+    if st != NM_OK:
+        raise NmError(st, "nm_rotary")
     return outs
 
 
@@ -201,7 +270,7 @@ class DiffWeight:
             raise ValueError("value: must be a contiguous float32 vector on the device, one for each head")
         self.value, self.vectors, self.init = value.detach(), None, 0.0
         self._heads, self._dev = value.shape[0], value.get_device()
-        self._args = NmDiffWeight(_ptr(self.value))
+        self._args = (_ptr(self.value), 0, 0, 0, 0, 0.0, 0, 0)
 
     @classmethod
     def of_vectors(cls, q1, k1, q2, k2, init: float):
@@ -217,31 +286,31 @@ class DiffWeight:
         self = cls.__new__(cls)
         self.value, self.vectors, self.init = None, tuple(t.detach() for t in vectors), float(init)
         self._heads, self._dev = (q1.shape[0] if q1.dim() == 2 else None), q1.get_device()
-        self._args = NmDiffWeight(None, *(_ptr(t) for t in self.vectors), self.init, q1.shape[-1], int(q1.dim() == 2))
+        self._args = (0, *(_ptr(t) for t in self.vectors), self.init, q1.shape[-1], int(q1.dim() == 2))
         return self
 
-    def _for(self, heads: int, dev: int) -> NmDiffWeight:
-        if self._heads not in (None, heads) or self._dev != dev:
+    def _for(self, heads: int, dev: int) -> tuple:
+        if (self._heads is not None and self._heads != heads) or self._dev != dev:
             raise ValueError(f"weight: of {self._heads} heads on cuda:{self._dev}, expected {heads} on cuda:{dev}")
         return self._args
 
 
 class _Shape(NamedTuple):
-    """What a call's tensors say: heads, widths, the rows of q, and the C structure of its tokens."""
+    """What a call's tensors say: heads, widths, the rows of q, and the values of the C structure of its tokens."""
     H: int
     Hk: int
     d: int
     dv: int
     rows: int
     packed: bool
-    tokens: NmTokens
+    tokens: tuple
     code: int
     dev: int
 
 
 def _lens(t, name: str, n: int, rt, dev: int):
     if t is None:
-        return None
+        return 0
     if t.dtype != rt.torch.int32 or t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, expected contiguous torch.int32 ({n},)")
     _on(t, name, dev)
@@ -274,7 +343,9 @@ def _shape(q, k, v, causal, window, q_lens, k_lens, q_offsets, k_offsets, max_q,
         raise ValueError(f"k and v: {tuple(k.shape)} and {tuple(v.shape)}, expected {d} channels of k and the same tokens")
     if causal and window is not None:
         raise ValueError("causal and window: one of them")
-    left, right = (-1, 0) if causal else (-1, -1) if window is None else window
+    left, right = (-1, 0) if causal else (-1, -1) if window is None else (min(int(w), 1 << 30) for w in window)
+    if left < 0 or right < 0:
+        left, right = max(left, -1), max(right, -1)
     if packed:
         if q_lens is not None or k_lens is not None:
             raise ValueError("q_lens and k_lens: of padded sequences, not of packed ones")
@@ -289,8 +360,8 @@ def _shape(q, k, v, causal, window, q_lens, k_lens, q_offsets, k_offsets, max_q,
             raise ValueError("max_k: needed with k_offsets")
         qo, ko = _lens(q_offsets, "q_offsets", batch + 1, rt, dev), _lens(k_offsets, "k_offsets", batch + 1, rt, dev)
         rows = q.shape[0]
-        tokens = NmTokens(batch, min(int(max_q), rows), min(int(max_k), k.shape[0]), left, right, qo, ko, None, None,
-                          rows, k.shape[0])
+        tokens = (batch, min(int(max_q), rows), min(int(max_k), k.shape[0]), left, right, qo, ko, 0, 0, rows,
+                  k.shape[0])
     else:
         if k_offsets is not None or max_q is not None or max_k is not None:
             raise ValueError("k_offsets, max_q and max_k: of packed sequences, with q_offsets")
@@ -298,17 +369,21 @@ def _shape(q, k, v, causal, window, q_lens, k_lens, q_offsets, k_offsets, max_q,
         if k.shape[0] != batch:
             raise ValueError(f"k: {k.shape[0]} sequences, expected {batch}")
         rows = batch * tq
-        tokens = NmTokens(batch, tq, k.shape[1], left, right, None, None, _lens(q_lens, "q_lens", batch, rt, dev),
-                          _lens(k_lens, "k_lens", batch, rt, dev), 0, 0)
+        tokens = (batch, tq, k.shape[1], left, right, 0, 0, _lens(q_lens, "q_lens", batch, rt, dev),
+                  _lens(k_lens, "k_lens", batch, rt, dev), 0, 0)
     return _Shape(H, Hk, d, dv, rows, packed, tokens, code, dev)
 
 
-def _strided(t, packed: bool) -> NmHeads:
+def _strided(t, packed: bool) -> tuple:
+    """The values of NmHeads."""
     if packed:
         s0, s1, _ = t.stride()
-        return NmHeads(t.data_ptr(), 0, s0, s1)
+        return t.data_ptr(), 0, s0, s1
     s0, s1, s2, _ = t.stride()
-    return NmHeads(t.data_ptr(), s0, s1, s2)
+    return t.data_ptr(), s0, s1, s2
+
+
+_FORWARD, _BACKWARD = _packer(NmDiffArgs), _packer(NmDiffGradArgs)
 
 
 def _into(t, name: str, shape, like, stream, rt):
@@ -330,15 +405,10 @@ def _scale(scale, d: int) -> float:
     return scale
 
 
-def _workspace(query, a, like, stream, rt, name: str):
-    need = ctypes.c_size_t()
-    _check(query(ctypes.byref(a), ctypes.byref(need)), name)
-    return (_empty((need.value,), rt.u8, like, stream, rt) if need.value else None), need.value
-
-
 def _forward(q, k, v, weight, scale, causal, window, q_lens, k_lens, q_offsets, k_offsets, max_q, max_k, out, train,
              stream):
-    rt = _runtime()
+    rt = nmblock._rt or _runtime()
+    C = _calls or _library()
     s = _shape(q, k, v, causal, window, q_lens, k_lens, q_offsets, k_offsets, max_q, max_k, rt)
     out = _into(out, "out", (*q.shape[:-2], s.H, s.dv), q, stream, rt)
     kept = stats = None
@@ -346,11 +416,14 @@ def _forward(q, k, v, weight, scale, causal, window, q_lens, k_lens, q_offsets, 
         kept = _empty((s.rows, s.H, 2, s.dv), rt.torch.int16, q, stream, rt)
         stats = _empty((2 * s.H, _stat_rows(s.dv), s.rows), rt.f32, q, stream, rt)
     p = s.packed
-    a = NmDiffArgs(_strided(q, p), _strided(k, p), _strided(v, p), _strided(out, p), _ptr(kept), _ptr(stats), s.tokens,
-                   weight._for(s.H, s.dev), s.code, s.H, s.Hk, s.d, s.dv, _scale(scale, s.d))
-    L = lib()
-    ws, need = _workspace(L.nm_diff_attention_workspace, a, q, stream, rt, "nm_diff_attention_workspace")
-    _check(L.nm_diff_attention(ctypes.byref(a), _ptr(ws), need, _handle(stream, s.dev, rt)), "nm_diff_attention")
+    args = _FORWARD.pack(*_strided(q, p), *_strided(k, p), *_strided(v, p), *_strided(out, p),
+                         0 if kept is None else kept.data_ptr(), 0 if stats is None else stats.data_ptr(), *s.tokens,
+                         *weight._for(s.H, s.dev), s.code, s.H, s.Hk, s.d, s.dv, _scale(scale, s.d))
+    need = _size(C.forward_size, (*s.tokens[:3], s.H, s.Hk, s.d, s.dv, s.dev, s.tokens[6] != 0 or s.tokens[8] != 0), args)
+    ws = _empty((need,), rt.u8, q, stream, rt) if need else None
+    st = C.forward(args, _ptr(ws), need, _handle(stream, s.dev, rt))
+    if st != NM_OK:
+        raise NmError(st, "nm_diff_attention")
     return out, kept, stats
 
 
@@ -406,7 +479,8 @@ def diff_attention_backward(grad_o, forward: DiffForward, q, k, v, weight: DiffW
                             max_q=None, max_k=None, dq=None, dk=None, dv=None, stream=None) -> DiffGrads:
     """nm_diff_attention_backward: from grad_o (of o's shape), at what diff_attention_train returned for the same
     arguments.  Rows behind a sequence's end are left as they were in given dq, dk and dv."""
-    rt = _runtime()
+    rt = nmblock._rt or _runtime()
+    C = _calls or _library()
     s = _shape(q, k, v, causal, window, q_lens, k_lens, q_offsets, k_offsets, max_q, max_k, rt)
     _, kept, stats = forward
     shape = (*q.shape[:-2], s.H, s.dv)
@@ -426,12 +500,13 @@ def diff_attention_backward(grad_o, forward: DiffForward, q, k, v, weight: DiffW
         each = _empty((4, *weight.vectors[0].shape), rt.f32, q, stream, rt)
         vectors = list(each.unbind(0))
     p = s.packed
-    a = NmDiffGradArgs(*(_strided(t, p) for t in (q, k, v, grad_o, dq, dk, dv)), kept.data_ptr(), stats.data_ptr(),
-                       dlam.data_ptr(), *(_ptr(t) for t in vectors), s.tokens, w, s.code, s.H, s.Hk, s.d, s.dv,
-                       _scale(scale, s.d))
-    L = lib()
-    ws, need = _workspace(L.nm_diff_attention_backward_workspace, a, q, stream, rt,
-                          "nm_diff_attention_backward_workspace")
-    _check(L.nm_diff_attention_backward(ctypes.byref(a), _ptr(ws), need, _handle(stream, s.dev, rt)),
-           "nm_diff_attention_backward")
+    args = _BACKWARD.pack(*(x for t in (q, k, v, grad_o, dq, dk, dv) for x in _strided(t, p)), kept.data_ptr(),
+                          stats.data_ptr(), dlam.data_ptr(), *(_ptr(t) or 0 for t in vectors), *s.tokens, *w, s.code, s.H,
+                          s.Hk, s.d, s.dv, _scale(scale, s.d))
+    key = ("backward", *s.tokens[:3], s.rows, s.H, s.Hk, s.d, s.dv, s.dev)
+    need = _size(C.backward_size, key, args)
+    ws = _empty((need,), rt.u8, q, stream, rt) if need else None
+    st = C.backward(args, _ptr(ws), need, _handle(stream, s.dev, rt))
+    if st != NM_OK:
+        raise NmError(st, "nm_diff_attention_backward")
     return DiffGrads(dq, dk, dv, dlam, *vectors)

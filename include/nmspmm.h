@@ -654,7 +654,7 @@ nm_status nm_rotary(const nm_rotary_args *args, void *stream);
  * and [batch x tk], of which the first q_lens[b] rows and k_lens[b] keys count (device
  * int32 [batch]; NULL: all); or packed behind each other: q_offsets and k_offsets, device
  * int32 [batch + 1], with tq and tk at least the longest lengths and total_q, total_k
- * rows in all (the batch strides are not read).  Lengths and offsets outside the tensors are
+ * rows in all (the batch strides are not read).  Offsets must not fall.  Lengths and offsets outside the tensors are
  * taken as the nearest inside.  Rows of o behind a sequence's end stay as they were; what q, k
  * and v hold there does not matter.  Within a sequence a key that a row does not see has
  * no weight for it, but where v there is infinite or NaN, the row may be NaN.
@@ -673,7 +673,7 @@ nm_status nm_rotary(const nm_rotary_args *args, void *stream);
  * ws: nm_diff_attention_workspace bytes of device memory, any content, 16-byte
  * aligned (NULL where that is 0; sizes decide it, and whether k_lens or offsets are given).  Without rows it is a no-op.
  * Errors: NM_ERR_ARG (NULL or misaligned pointer, another type, scale not positive or not finite), NM_ERR_SHAPE (a size or
- * stride out of range: sequences of 2^28 rows, token strides of 2^22 values), NM_ERR_WORKSPACE, NM_ERR_HIP. */
+ * stride out of range: sequences of 2^28 rows, token strides of 2^22 values, 2^24 workgroups), NM_ERR_WORKSPACE, NM_ERR_HIP. */
 typedef struct nm_heads {
     void *p;
     int64_t batch, token, head;   /* strides in values */

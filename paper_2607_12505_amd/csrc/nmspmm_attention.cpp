@@ -11,10 +11,20 @@ namespace {
 bool aligned(const void *p, int to) { return ((uintptr_t)p & (uintptr_t)(to - 1)) == 0; }
 size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Whether heads of `width` 16-bit values are whole pieces of `values` values at their boundaries.
+// Whether heads of `width` 16-bit values are whole pieces of `values` values at their boundaries, and rows apart (loads
+// of whole tiles tell rows behind the last by where they lie).
 bool pieces(const nm_heads &t, int width, int values) {
     return aligned(t.p, 2 * values) && t.token % values == 0 && t.head % values == 0 && t.batch % values == 0 &&
-           width % values == 0;
+           width % values == 0 && t.token >= width;
+}
+
+// A tensor with strides that do not matter, along dimensions of one, put out of the way.
+nm_heads extent(nm_heads t, const nm_tokens &tokens, bool keys, int heads, int width) {
+    const int64_t n = keys ? (tokens.k_offsets ? tokens.total_k : tokens.tk) : tokens.q_offsets ? tokens.total_q : tokens.tq;
+    if (tokens.batch <= 1 || tokens.q_offsets) t.batch = 0;
+    if (n <= 1) t.token = (width + 7) & ~7;
+    if (heads <= 1) t.head = 0;
+    return t;
 }
 
 nm_status check_tokens(const nm_tokens &t) {
@@ -119,7 +129,7 @@ Cut cut_of(const nm_tokens &t, int H, int Hk, int cls) {
 size_t parts_bytes(const nm_tokens &t, int H, int dv, int splits) {
     return splits > 1 ? (size_t)t.batch * H * t.tq * splits * (2 * dv + 4) * 4 : 0;
 }
-bool grid_fits(int64_t n) { return n < (1ll << 31); }
+bool grid_fits(int64_t n) { return n < (1ll << 24); }   // a launch's threads are counted in 32 bits
 
 }  // namespace
 
@@ -181,7 +191,8 @@ extern "C" nm_status nm_diff_attention_workspace(const nm_diff_args *args, size_
     if (!bytes) return NM_ERR_ARG;
     const nm_status st = check_forward(args);
     if (st != NM_OK) return st;
-    *bytes = parts_bytes(args->tokens, args->H, args->dv, cut_of(args->tokens, args->H, args->Hk, width_class(args->d, args->dv)).splits);
+    const Cut c = cut_of(args->tokens, args->H, args->Hk, width_class(args->d, args->dv));
+    *bytes = parts_bytes(args->tokens, args->H, args->dv, c.splits);
     return NM_OK;
 }
 
@@ -191,8 +202,10 @@ extern "C" nm_status nm_diff_attention(const nm_diff_args *args, void *ws, size_
     if (st != NM_OK) return st;
     const nm_diff_args &g = *args;
     const int64_t rows = rows_of(g.tokens), keys = keys_of(g.tokens);
-    for (const nm_heads *t : {&g.q, &g.k, &g.v, &g.o})
-        if ((st = check_tensor(*t, (t == &g.k || t == &g.v ? keys : rows) > 0)) != NM_OK) return st;
+    const nm_heads q = extent(g.q, g.tokens, false, 2 * g.H, g.d), k = extent(g.k, g.tokens, true, 2 * g.Hk, g.d),
+                   v = extent(g.v, g.tokens, true, g.Hk, g.dv), o = extent(g.o, g.tokens, false, g.H, g.dv);
+    for (const nm_heads *t : {&q, &k, &v, &o})
+        if ((st = check_tensor(*t, (t == &k || t == &v ? keys : rows) > 0)) != NM_OK) return st;
     if (!aligned(g.kept, 16) || !aligned(g.stats, 4) || !g.kept != !g.stats) return NM_ERR_ARG;
     if (rows == 0 || g.tokens.batch == 0 || g.tokens.tq == 0) return NM_OK;
     const Cut c = cut_of(g.tokens, g.H, g.Hk, width_class(g.d, g.dv));
@@ -200,17 +213,17 @@ extern "C" nm_status nm_diff_attention(const nm_diff_args *args, void *ws, size_
     if (need && (!ws || ws_bytes < need || !aligned(ws, 16))) return NM_ERR_WORKSPACE;
     AttnArgs a;
     fill(a, g.tokens, g.weight, g.H, g.Hk, g.d, g.dv, g.scale);
-    if (!grid_fits((int64_t)a.batch * a.Hk * c.row_tiles * c.splits) ||
-        !grid_fits((int64_t)a.batch * a.H * a.tq) || !grid_fits((int64_t)a.tq * a.group))
+    if (!grid_fits((int64_t)a.batch * a.Hk * c.row_tiles * c.splits) || (int64_t)a.tq * a.group >= (1ll << 31) ||
+        (c.splits > 1 && !grid_fits((int64_t)a.batch * a.H * a.tq)))
         return NM_ERR_SHAPE;
-    a.q = heads_of(g.q);
-    a.k = heads_of(g.k);
-    a.v = heads_of(g.v);
-    a.o = heads_of(g.o);
+    a.q = heads_of(q);
+    a.k = heads_of(k);
+    a.v = heads_of(v);
+    a.o = heads_of(o);
     a.kept = g.kept;
     a.stats = g.stats;
-    a.vec = pieces(g.q, g.d, 8) && pieces(g.k, g.d, 8) && pieces(g.v, g.dv, 8);
-    a.vec_out = pieces(g.o, g.dv, 4);
+    a.vec = pieces(q, g.d, 8) && pieces(k, g.d, 8) && pieces(v, g.dv, 8);
+    a.vec_out = pieces(o, g.dv, 4);
     a.row_tiles = c.row_tiles;
     a.splits = c.splits;
     a.parts = (float *)ws;
@@ -262,9 +275,13 @@ extern "C" nm_status nm_diff_attention_backward(const nm_diff_grad_args *args, v
     if (st != NM_OK) return st;
     const nm_diff_grad_args &g = *args;
     const int64_t rows = rows_of(g.tokens), keys = keys_of(g.tokens);
-    for (const nm_heads *t : {&g.q, &g.grad_o, &g.dq})
+    const nm_heads q = extent(g.q, g.tokens, false, 2 * g.H, g.d), dq = extent(g.dq, g.tokens, false, 2 * g.H, g.d),
+                   grad_o = extent(g.grad_o, g.tokens, false, g.H, g.dv_width),
+                   k = extent(g.k, g.tokens, true, 2 * g.Hk, g.d), dk = extent(g.dk, g.tokens, true, 2 * g.Hk, g.d),
+                   v = extent(g.v, g.tokens, true, g.Hk, g.dv_width), dv = extent(g.dv, g.tokens, true, g.Hk, g.dv_width);
+    for (const nm_heads *t : {&q, &grad_o, &dq})
         if ((st = check_tensor(*t, rows > 0)) != NM_OK) return st;
-    for (const nm_heads *t : {&g.k, &g.v, &g.dk, &g.dv})
+    for (const nm_heads *t : {&k, &v, &dk, &dv})
         if ((st = check_tensor(*t, keys > 0)) != NM_OK) return st;
     if (!g.dlam || !aligned(g.dlam, 4) || !aligned(g.kept, 16) || !aligned(g.stats, 4) ||
         (rows > 0 && (!g.kept || !g.stats)))
@@ -279,24 +296,26 @@ extern "C" nm_status nm_diff_attention_backward(const nm_diff_grad_args *args, v
     AttnArgs a;
     fill(a, g.tokens, g.weight, g.H, g.Hk, g.d, g.dv_width, g.scale);
     const int64_t row_tiles = grad_row_tiles(g), key_tiles = (g.tokens.tk + kGradKeys - 1) / kGradKeys;
-    if (!grid_fits((int64_t)a.batch * a.Hk * row_tiles * 4) || !grid_fits((int64_t)a.tq * a.group) || !grid_fits((int64_t)a.batch * a.Hk * key_tiles * 2 * 64 + 1) ||
-        !grid_fits((int64_t)a.batch * a.Hk * a.tk))
+    const int splits = key_splits(g);
+    if (!grid_fits((int64_t)a.batch * a.Hk * row_tiles) || (int64_t)a.tq * a.group >= (1ll << 31) ||
+        !grid_fits((int64_t)a.batch * a.Hk * key_tiles * splits * 2 + 1) ||
+        (int64_t)a.batch * row_tiles * 4 >= (1ll << 31))
         return NM_ERR_SHAPE;
-    a.q = heads_of(g.q);
-    a.k = heads_of(g.k);
-    a.v = heads_of(g.v);
-    a.grad = heads_of(g.grad_o);
-    a.dq = heads_of(g.dq);
-    a.dk = heads_of(g.dk);
-    a.dv_ = heads_of(g.dv);
+    a.q = heads_of(q);
+    a.k = heads_of(k);
+    a.v = heads_of(v);
+    a.grad = heads_of(grad_o);
+    a.dq = heads_of(dq);
+    a.dk = heads_of(dk);
+    a.dv_ = heads_of(dv);
     a.kept = (int16_t *)g.kept;
     a.stats = (float *)g.stats;
-    a.vec = pieces(g.q, g.d, 8) && pieces(g.k, g.d, 8) && pieces(g.v, g.dv_width, 8) && pieces(g.grad_o, g.dv_width, 8);
-    a.vec_out = pieces(g.dq, g.d, 4) && pieces(g.dk, g.d, 4) && pieces(g.dv, g.dv_width, 4);
+    a.vec = pieces(q, g.d, 8) && pieces(k, g.d, 8) && pieces(v, g.dv_width, 8) && pieces(grad_o, g.dv_width, 8);
+    a.vec_out = pieces(dq, g.d, 4) && pieces(dk, g.d, 4) && pieces(dv, g.dv_width, 4);
     a.row_tiles = (int)row_tiles;
     a.key_tiles = (int)key_tiles;
     a.delta = (float *)ws;
-    a.key_splits = key_splits(g);
+    a.key_splits = splits;
     a.key_parts = (float *)((char *)ws + delta_bytes(g));
     a.dlam_parts = (float *)((char *)ws + delta_bytes(g) + key_parts_bytes(g));
     a.dlam_count = (int)((int64_t)a.batch * row_tiles * 4);

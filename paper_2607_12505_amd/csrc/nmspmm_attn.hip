@@ -69,7 +69,7 @@ __device__ __forceinline__ void join_runs(const AttnArgs &a, const RowTile &r, u
         if (!r.valid) return;
         const int64_t part =
             (((int64_t)r.b * a.Hk + r.hk) * a.splits + split) * ((int64_t)a.tq * a.group) + r.t * a.group + r.g;
-        float *ml = a.parts + (int64_t)a.batch * a.Hk * a.splits * a.tq * a.group * 2 * a.dv + part * 4;
+        float *ml = a.parts + part * 4, *sums = a.parts + (int64_t)a.batch * a.Hk * a.splits * a.tq * a.group * 4;
         if (run == 0 && lane < 32) *(v4f *)ml = v4f{top[0], sum[0], top[1], sum[1]};
         const bool vec = a.dv % 4 == 0;
 #pragma unroll
@@ -77,7 +77,7 @@ __device__ __forceinline__ void join_runs(const AttnArgs &a, const RowTile &r, u
 #pragma unroll
             for (int e = 0; e < 16; e += 4)
                 if (joins)
-                    store4(a.parts + (part * 2 + i) * a.dv, 32 * run + 2 * e + 4 * (lane >> 5), a.dv, vec, y[i][e],
+                    store4(sums + (part * 2 + i) * a.dv, 32 * run + 2 * e + 4 * (lane >> 5), a.dv, vec, y[i][e],
                            y[i][e + 1], y[i][e + 2], y[i][e + 3]);
         return;
     }
@@ -298,7 +298,7 @@ __global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS) * RUNS, BLOCKS > 1 ? 2 : 1
         // rows of a part: [sequence][key head][split][number]
         const int64_t part =
             (((int64_t)r.b * a.Hk + r.hk) * a.splits + split) * ((int64_t)a.tq * a.group) + r.t * a.group + r.g;
-        float *ml = a.parts + (int64_t)a.batch * a.Hk * a.splits * a.tq * a.group * 2 * a.dv + part * 4 + 2 * map;
+        float *ml = a.parts + part * 4 + 2 * map, *sums = a.parts + (int64_t)a.batch * a.Hk * a.splits * a.tq * a.group * 4;
         const bool vec = a.dv % 4 == 0;
 #pragma unroll
         for (int i = 0; i < MAPS; ++i) {
@@ -310,7 +310,7 @@ __global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS) * RUNS, BLOCKS > 1 ? 2 : 1
             for (int x = 0; x < DV / 32; ++x)
 #pragma unroll
                 for (int e = 0; e < 16; e += 4)
-                    store4(a.parts + (part * 2 + map + i) * a.dv, 32 * x + 2 * e + 4 * (lane >> 5), a.dv, vec, o[i][x][e],
+                    store4(sums + (part * 2 + map + i) * a.dv, 32 * x + 2 * e + 4 * (lane >> 5), a.dv, vec, o[i][x][e],
                            o[i][x][e + 1], o[i][x][e + 2], o[i][x][e + 3]);
         }
         return;
@@ -403,7 +403,7 @@ __global__ __launch_bounds__(256) void k_diff_join(AttnArgs a) {
     const Sequence s = sequence(a, b);
     if (t >= s.nq) return;
     const int64_t part = outer * a.splits * wide + number;
-    const float *ml = a.parts + all * a.splits * 2 * a.dv + part * 4;
+    const float *ml = a.parts + part * 4, *products = a.parts + all * a.splits * 4;
     const int n = threadIdx.x;
     v4f mine = {-__builtin_inff(), 0.f, -__builtin_inff(), 0.f};
     if (n < a.splits) mine = *(const v4f *)(ml + n * wide * 4);
@@ -436,7 +436,7 @@ __global__ __launch_bounds__(256) void k_diff_join(AttnArgs a) {
     if (turn < turns) {
         const bool vec = a.dv % 4 == 0;
         for (int k = turn; k < a.splits; k += turns) {
-            const float *p = a.parts + (part + k * wide) * 2 * a.dv + c;
+            const float *p = products + (part + k * wide) * 2 * a.dv + c;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const float f = factor[i][k];

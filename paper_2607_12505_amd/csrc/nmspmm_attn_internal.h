@@ -53,7 +53,7 @@ struct AttnArgs {
     int vec;                  // q, k, v (and do) are whole 16-byte pieces
     int vec_out;              // o (backward: dq, dk, dv) is whole 8-byte pieces
     int row_tiles, splits;
-    float *parts;             // [batch * Hk * splits * tq * group] x 2 dv values, then the same x 4: m1, l1, m2, l2
+    float *parts;             // [batch * Hk * splits * tq * group] x 4: m1, l1, m2, l2, then the same x 2 dv values
     // backward
     Heads grad, dq, dk, dv_;  // do and the gradients
     float *delta;             // [2 H][rows]: do . o1, do . o2

@@ -102,6 +102,7 @@ int launch(bool vec, const RotaryArgs &a, hipStream_t stream) {
     const int64_t room = 16384 / (8 * a.pairs);
     per = per < 1 ? 1 : per > room ? room : per;
     const int64_t grid = (a.tokens + per - 1) / per;
+    if (grid >= (1ll << 24)) return (int)hipErrorInvalidConfiguration;   // a launch's threads are counted in 32 bits
     const size_t lds = (size_t)per * a.pairs * 8;
     if (vec)
         k_rotary<T, true><<<dim3((unsigned)grid), kRotaryThreads, lds, stream>>>(a, (int)per);

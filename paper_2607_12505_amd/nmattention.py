@@ -86,6 +86,12 @@ def _heads(t, name: str, rt, dims=(3,)):
         raise ValueError(f"{name}: channels must be consecutive")
 
 
+def _apart(t, name: str):
+    """Refuses an output of which several places are one."""
+    if 0 in t.stride() and any(s == 0 and n > 1 for s, n in zip(t.stride(), t.shape)):
+        raise ValueError(f"{name}: an expanded tensor cannot be written")
+
+
 # ---------------------------------------------------------------- rotary positions
 
 class NmRotaryPart(ctypes.Structure):
@@ -179,6 +185,7 @@ def _rotary(parts, positions, axes: RotaryAxes, back: bool, stream):
             if out.dtype != t.dtype or out.shape != t.shape:
                 raise ValueError(f"out of {name}: {out.dtype} {tuple(out.shape)}, expected {t.dtype} {tuple(t.shape)}")
             _heads(out, f"out of {name}", rt, (3, 4))
+            _apart(out, f"out of {name}")
             _on(out, f"out of {name}", dev)
             _written(out, rt)
         heads += t.shape[-2]
@@ -393,6 +400,7 @@ def _into(t, name: str, shape, like, stream, rt):
     if t.dtype != like.dtype or tuple(t.shape) != tuple(shape) or (t.shape[-1] > 1 and t.stride(-1) != 1):
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, expected {like.dtype} {tuple(shape)} with consecutive "
                          "channels")
+    _apart(t, name)
     _on(t, name, like.get_device())
     return _written(t, rt)
 

@@ -121,6 +121,7 @@ def test_attention_refuses():
         assert f(ctypes.byref(diff(**bad)), FAKE, 1 << 40, NUL) == ARG, bad
     for bad in BAD_SHAPE + [dict(dv=257), dict(dv=0)]:
         assert f(ctypes.byref(diff(**bad)), FAKE, 1 << 40, NUL) == SHAPE, bad
+    assert f(ctypes.byref(diff(tokens__batch=1 << 23, tokens__tq=1, tokens__tk=1)), NUL, 0, NUL) == SHAPE   # a launch's size
     for nothing in (dict(tokens__batch=0), dict(tokens__tq=0, q__p=None, o__p=None)):
         assert f(ctypes.byref(diff(**nothing)), NUL, 0, NUL) == OK
     # few rows over long keys need a workspace for their parts

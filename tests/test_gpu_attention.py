@@ -252,6 +252,56 @@ def test_inside_the_rows_of_one_product(T, pad):
         assert torch.equal(a, b)
 
 
+# parts of few and of many rows over long keys, their number and widths odd, alone and by several row tiles
+@pytest.mark.parametrize("T", TYPES)
+@pytest.mark.parametrize("B,Tq,Tk,H,Hk,d,dv", [(1, 1, 3000, 1, 1, 64, 33), (1, 100, 3001, 2, 1, 64, 128), (1, 3, 2050, 3, 1, 31, 63),
+                                               (1, 70, 1500, 1, 1, 128, 256), (1, 1, 2000, 3, 3, 127, 255)])
+def test_parts_of_the_keys(T, B, Tq, Tk, H, Hk, d, dv):
+    g = gen(Tk)
+    q, k, v, lam, spans = dense(g, T, B, Tq, Tk, H, Hk, d, dv)
+    check(q, k, v, na.DiffWeight(lam), lam, spans, (-1, 0), grad=randn(g, T, B, Tq, H, dv))
+
+
+@pytest.mark.parametrize("T", TYPES)
+@pytest.mark.parametrize("n", [1, 75, 130])
+def test_expanded_inputs(T, n):
+    # rows that are all one place in memory: those behind the last are not
+    g, B, H, Hk, d, dv = gen(16), 2, 4, 2, 64, 128
+    q, k, v, lam, _ = dense(g, T, B, n, n, H, Hk, d, dv)
+    do, weight = randn(g, T, B, n, H, dv), na.DiffWeight(lam)
+    for places in ((B, 1), (1, n), (1, 1)):
+        cut = [t[:places[0], :places[1]].expand_as(t) for t in (q, k, v, do)]
+        for which in range(4):
+            some = [c if i == which else t for i, (c, t) in enumerate(zip(cut, (q, k, v, do)))]
+            near = [t.contiguous() for t in some]
+            f = na.diff_attention_train(*some[:3], weight, causal=True)
+            want = na.diff_attention_train(*near[:3], weight, causal=True)
+            for a, b in zip(f, want):
+                assert torch.equal(a, b)
+            for a, b in zip(na.diff_attention_backward(some[3], f, *some[:3], weight, causal=True)[:4],
+                            na.diff_attention_backward(near[3], want, *near[:3], weight, causal=True)[:4]):
+                assert torch.equal(a, b)
+    for out in (torch.empty(B, 1, H, dv, dtype=T, device="cuda").expand(B, 9, H, dv),
+                torch.empty(1, 9, H, dv, dtype=T, device="cuda").expand(B, 9, H, dv)):
+        with pytest.raises(ValueError):
+            na.diff_attention(q[:, :1].expand(B, 9, 2 * H, d), k, v, weight, out=out)
+
+
+def test_strides_of_dimensions_of_one():
+    T, g = torch.float16, gen(17)
+    q, k, v, lam, _ = dense(g, T, 1, 1, 40, 1, 1, 64, 128)
+    do, weight = randn(g, T, 1, 1, 1, 128), na.DiffWeight(lam)
+    far = 1 << 40
+    some = [q.as_strided(q.shape, (far + 1, far + 3, 64, 1)), k.as_strided(k.shape, (3, 128, 64, 1)),
+            v.as_strided(v.shape, (5, 128, far + 7, 1)), do.as_strided(do.shape, (far, far, far, 1))]
+    f, want = na.diff_attention_train(*some[:3], weight), na.diff_attention_train(q, k, v, weight)
+    for a, b in zip(f, want):
+        assert torch.equal(a, b)
+    for a, b in zip(na.diff_attention_backward(some[3], f, *some[:3], weight)[:4],
+                    na.diff_attention_backward(do, want, q, k, v, weight)[:4]):
+        assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("T", TYPES)
 def test_rows_that_see_nothing(T):
     # more rows than keys under the causal mask: the first rows see none

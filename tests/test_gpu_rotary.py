@@ -137,6 +137,16 @@ def test_refusals():
         na.RotaryAxes([1.0], [0], style="thirds")
 
 
+def test_expanded_inputs():
+    axes, T = na.RotaryAxes.of_sections((4, 4)), torch.bfloat16
+    x = torch.randn(1, 3, 16, generator=torch.Generator().manual_seed(8)).to(T).cuda()
+    pos = torch.arange(14, dtype=torch.int32).view(2, 7).cuda()
+    for some in (x.expand(7, 3, 16), x[:, :1].expand(7, 5, 16)):
+        assert torch.equal(na.rotary(some, pos, axes), na.rotary(some.contiguous(), pos, axes))
+        with pytest.raises(ValueError):
+            na.rotary(some, pos, axes, out=some)
+
+
 def test_given_stream_and_captured_graph():
     g = gen(8)
     axes = na.RotaryAxes.of_sections((16, 16))

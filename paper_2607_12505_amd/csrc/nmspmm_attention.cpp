@@ -11,11 +11,10 @@ namespace {
 bool aligned(const void *p, int to) { return ((uintptr_t)p & (uintptr_t)(to - 1)) == 0; }
 size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Whether heads of `width` 16-bit values are whole pieces of `values` values at their boundaries, and rows apart (loads
+// Whether heads of `width` 16-bit values are whole 16-byte pieces at their boundaries, and rows apart (loads
 // of whole tiles tell rows behind the last by where they lie).
-bool pieces(const nm_heads &t, int width, int values) {
-    return aligned(t.p, 2 * values) && t.token % values == 0 && t.head % values == 0 && t.batch % values == 0 &&
-           width % values == 0 && t.token >= width;
+bool pieces(const nm_heads &t, int width) {
+    return aligned(t.p, 16) && t.token % 8 == 0 && t.head % 8 == 0 && t.batch % 8 == 0 && width % 8 == 0 && t.token >= width;
 }
 
 // A tensor with strides that do not matter, along dimensions of one, put out of the way.
@@ -144,14 +143,11 @@ extern "C" nm_status nm_rotary(const nm_rotary_args *args, void *stream) {
         return NM_ERR_SHAPE;
     const int eb = g.type == NM_TYPE_F32 ? 4 : 2;
     int64_t heads = 0;
-    bool vec = g.d % 8 == 0 && (g.interleaved ? g.pairs % 4 == 0 : g.pairs % 8 == 0);
     for (const nm_rotary_part &p : g.part) {
         if (p.heads < 0 || p.x_token < 0 || p.x_head < 0 || p.out_token < 0 || p.out_head < 0) return NM_ERR_SHAPE;
         heads += p.heads;
         if (p.heads == 0 || g.tokens == 0) continue;
         if (!p.x || !p.out || !aligned(p.x, eb) || !aligned(p.out, eb)) return NM_ERR_ARG;
-        vec = vec && aligned(p.x, 16) && aligned(p.out, 16) && p.x_token % 8 == 0 && p.x_head % 8 == 0 &&
-              p.out_token % 8 == 0 && p.out_head % 8 == 0;
     }
     if (heads >= (1 << 16)) return NM_ERR_SHAPE;
     if (heads == 0) return NM_ERR_ARG;
@@ -174,7 +170,7 @@ extern "C" nm_status nm_rotary(const nm_rotary_args *args, void *stream) {
     a.interleaved = g.interleaved != 0;
     a.axes = g.axes;
     a.sign = g.back ? -1.f : 1.f;
-    return launch_rotary(g.type, vec, a, stream) == 0 ? NM_OK : NM_ERR_HIP;
+    return launch_rotary(g.type, a, stream) == 0 ? NM_OK : NM_ERR_HIP;
 }
 
 // ---------------------------------------------------------------- differential attention
@@ -222,8 +218,7 @@ extern "C" nm_status nm_diff_attention(const nm_diff_args *args, void *ws, size_
     a.o = heads_of(o);
     a.kept = g.kept;
     a.stats = g.stats;
-    a.vec = pieces(q, g.d, 8) && pieces(k, g.d, 8) && pieces(v, g.dv, 8);
-    a.vec_out = pieces(o, g.dv, 4);
+    a.pieces = pieces(q, g.d) && pieces(k, g.d) && pieces(v, g.dv);
     a.row_tiles = c.row_tiles;
     a.splits = c.splits;
     a.parts = (float *)ws;
@@ -310,8 +305,7 @@ extern "C" nm_status nm_diff_attention_backward(const nm_diff_grad_args *args, v
     a.dv_ = heads_of(dv);
     a.kept = (int16_t *)g.kept;
     a.stats = (float *)g.stats;
-    a.vec = pieces(q, g.d, 8) && pieces(k, g.d, 8) && pieces(v, g.dv_width, 8) && pieces(grad_o, g.dv_width, 8);
-    a.vec_out = pieces(dq, g.d, 4) && pieces(dk, g.d, 4) && pieces(dv, g.dv_width, 4);
+    a.pieces = pieces(q, g.d) && pieces(k, g.d) && pieces(v, g.dv_width) && pieces(grad_o, g.dv_width);
     a.row_tiles = (int)row_tiles;
     a.key_tiles = (int)key_tiles;
     a.delta = (float *)ws;

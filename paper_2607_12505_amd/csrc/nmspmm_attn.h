@@ -177,11 +177,34 @@ struct Tile {
     }
 };
 
+// Values c .. c + 7 of a row of `width`, c < width, zero from there on, at any alignment of its type (the hardware's
+// loads take it).  A row's last values are the end of its last 8, which moved() brings to their places: `over` of them
+// lie before the piece.
+__device__ __forceinline__ int piece_over(int c, int width) { return width >= 8 && c + 8 > width ? c + 8 - width : 0; }
+template <class T>
+__device__ __forceinline__ v8s row_piece(const T *row, int c, int width, int over) {
+    typedef short v8any __attribute__((ext_vector_type(8), aligned(2)));
+    const short *p = (const short *)row;
+    if (width >= 8) return *(const v8any *)(p + c - over);
+    v8s v = {};
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+        if (c + e < width) v[e] = p[c + e];
+    return v;
+}
+__device__ __forceinline__ v8s moved(v8s v, int over) {        // 0 < over < 8
+    typedef uint64_t v2l __attribute__((ext_vector_type(2)));
+    const v2l x = __builtin_bit_cast(v2l, v);
+    const int bits = 16 * over;
+    const v2l y = bits >= 64 ? v2l{x[1] >> (bits - 64), 0} : v2l{x[0] >> bits | x[1] << (64 - bits), x[1] >> bits};
+    return __builtin_bit_cast(v8s, y);
+}
+
 // Loads of tile after tile of rows, of one tensor or of two `second` values apart (their tiles one behind the
-// other): rows behind the last and columns from `width` on are zero, whatever memory holds there.  In whole
+// other): rows behind the last and columns from `width` on are zero, whatever memory holds there.  PIECES: in whole
 // pieces at 16-byte boundaries the loads go straight to LDS and arrive later (LOADS of them by every
-// wave); otherwise a value at a time, at once.  What a load needs but its tile's base is made once.
-template <class T, int CPR, int ROWS, int WAVES, int TENSORS>
+// wave); otherwise through registers, at once, by kernels of their own (beside the others' they cost spilled registers).  What a load needs but its tile's base is made once.
+template <class T, int CPR, int ROWS, int WAVES, int TENSORS, bool PIECES>
 struct Feed {
     using Place = Tile<T, CPR, ROWS, WAVES>;
     static constexpr int GROUPS = Place::GROUPS, LOADS = TENSORS * GROUPS / WAVES;
@@ -192,11 +215,10 @@ struct Feed {
     int64_t stride, second, bytes;      // bytes: from p to the end of the last row
     int left, width, first;             // rows left; this wave's first group
     uint32_t offset[EACH];              // of a lane; past any buffer where its piece is not of the columns
-    bool vec;
-    __device__ __forceinline__ Feed(const T *from, int64_t row_stride, int64_t tensor_stride, int rows, int columns, bool whole,
-                                    int wave, int lane)
+    __device__ __forceinline__ Feed(const T *from, int64_t row_stride, int64_t tensor_stride, int rows, int columns, int wave,
+                                    int lane)
         : p(from), stride(row_stride), second(tensor_stride), bytes(((int64_t)(rows - 1) * row_stride + columns) * 2),
-          left(rows), width(columns), vec(whole) {
+          left(rows), width(columns) {
         first = SPREAD ? wave % GROUPS : wave;
         if (SPREAD) p += wave / GROUPS * second;
         const int c = lane % CPR;
@@ -208,7 +230,7 @@ struct Feed {
     }
     __device__ __forceinline__ void load(uint32_t lds, int wave, int lane) {
         if (SPREAD) lds += wave / GROUPS * Place::BYTES;
-        if (vec) {
+        if constexpr (PIECES) {
             const int records = left <= 0 ? 0 : bytes < 0x7FFFFFFF ? (int)bytes : 0x7FFFFFFF;
 #pragma unroll
             for (int t = 0; t < (SPREAD ? 1 : TENSORS); ++t) {
@@ -218,21 +240,27 @@ struct Feed {
                     dma16(buffer, offset[i], lds + t * Place::BYTES + Place::group_at(i * WAVES + first));
             }
         } else {
-            typedef T v8 __attribute__((ext_vector_type(8)));
-            const int c = lane % CPR * 8;
+            constexpr int BATCH = LOADS < 8 ? LOADS : 8;        // loads under way together
+            const int c = lane % CPR * 8, over = piece_over(c, width);
 #pragma unroll 1
-            for (int n = 0; n < LOADS; ++n) {
-                const int t = n / EACH, group = n % EACH * WAVES + first;
-                const int row = Place::row_of_group(group) + Place::row_of_place(lane / CPR);
-                const T *from = p + t * second + row * stride;
-                v8 v;
+            for (int n = 0; n < LOADS; n += BATCH) {
+                v8s v[BATCH];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    v[e] = (T)0.f;
-                    if (row < left && c + e < width) v[e] = from[c + e];
+                for (int i = 0; i < BATCH; ++i) {
+                    const int t = (n + i) / EACH, group = (n + i) % EACH * WAVES + first;
+                    const int row = Place::row_of_group(group) + Place::row_of_place(lane / CPR);
+                    v[i] = v8s{};
+                    if (row < left && c < width) v[i] = row_piece(p + t * second + row * stride, c, width, over);
                 }
-                *(__attribute__((address_space(3))) v8 *)(uintptr_t)(lds + t * Place::BYTES + Place::group_at(group) +
-                                                                    lane * 16) = v;
+                if (over > 0)
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i) v[i] = moved(v[i], over);
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) {
+                    const int t = (n + i) / EACH, group = (n + i) % EACH * WAVES + first;
+                    *(__attribute__((address_space(3))) v8s *)(uintptr_t)(lds + t * Place::BYTES + Place::group_at(group) +
+                                                                         lane * 16) = v[i];
+                }
             }
         }
         p += ROWS * stride;
@@ -241,33 +269,28 @@ struct Feed {
     }
 };
 
-// The B operand of a row in memory, k = 16 c .. 16 c + 15, zero from `width` on.
-template <class T>
-__device__ __forceinline__ v8s row_operand(const T *p, bool valid, int c, int width, bool vec, int lane) {
+// The B operand of a row in memory, k = 16 c .. 16 c + 15, zero from `width` on; PIECES as above.
+template <bool PIECES, class T>
+__device__ __forceinline__ v8s row_operand(const T *p, bool valid, int c, int width, int lane) {
     const int at = 16 * c + 8 * (lane >> 5);
-    v8s r = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (!valid || at >= width) return r;
-    if (vec) return *(const v8s *)(p + at);
-    typedef T v8 __attribute__((ext_vector_type(8)));
-    v8 v = __builtin_bit_cast(v8, r);
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (at + e < width) v[e] = p[at + e];
-    return __builtin_bit_cast(v8s, v);
+    if (!valid || at >= width) return v8s{};
+    if constexpr (PIECES) return *(const v8s *)(p + at);
+    const int over = piece_over(at, width);
+    const v8s v = row_piece(p, at, width, over);
+    return over > 0 ? moved(v, over) : v;
 }
 
-// 4 values of a row at column c of `width`.
-template <class T>
-__device__ __forceinline__ void store4(T *p, int c, int width, bool vec, float a, float b, float d, float e) {
-    typedef T v4 __attribute__((ext_vector_type(4)));
-    if (vec) {
-        if (c < width) *(v4 *)(p + c) = v4{(T)a, (T)b, (T)d, (T)e};
+// 4 values of a row at column c of `width`, at any alignment of their type.
+template <class T, class X>
+__device__ __forceinline__ void store4(T *p, int c, int width, X a, X b, X d, X e) {
+    typedef T v4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    if (c + 4 <= width) {
+        *(v4 *)(p + c) = v4{(T)a, (T)b, (T)d, (T)e};
         return;
     }
     if (c < width) p[c] = (T)a;
     if (c + 1 < width) p[c + 1] = (T)b;
     if (c + 2 < width) p[c + 2] = (T)d;
-    if (c + 3 < width) p[c + 3] = (T)e;
 }
 
 // Codes in 16 bits of values of which `top` is the largest magnitude: what the backward pass

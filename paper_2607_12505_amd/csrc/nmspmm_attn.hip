@@ -71,22 +71,21 @@ __device__ __forceinline__ void join_runs(const AttnArgs &a, const RowTile &r, u
             (((int64_t)r.b * a.Hk + r.hk) * a.splits + split) * ((int64_t)a.tq * a.group) + r.t * a.group + r.g;
         float *ml = a.parts + part * 4, *sums = a.parts + (int64_t)a.batch * a.Hk * a.splits * a.tq * a.group * 4;
         if (run == 0 && lane < 32) *(v4f *)ml = v4f{top[0], sum[0], top[1], sum[1]};
-        const bool vec = a.dv % 4 == 0;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int e = 0; e < 16; e += 4)
                 if (joins)
-                    store4(sums + (part * 2 + i) * a.dv, 32 * run + 2 * e + 4 * (lane >> 5), a.dv, vec, y[i][e],
-                           y[i][e + 1], y[i][e + 2], y[i][e + 3]);
+                    store4(sums + (part * 2 + i) * a.dv, 32 * run + 2 * e + 4 * (lane >> 5), a.dv, y[i][e], y[i][e + 1],
+                           y[i][e + 2], y[i][e + 3]);
         return;
     }
     if (r.valid && joins) {
         T *op = head_of<T>(a.o, r.s.batch, r.s.q0 + r.t, r.head);
 #pragma unroll
         for (int e = 0; e < 16; e += 4)
-            store4(op, 32 * run + 2 * e + 4 * (lane >> 5), a.dv, a.vec_out, y[0][e] - lam * y[1][e],
-                   y[0][e + 1] - lam * y[1][e + 1], y[0][e + 2] - lam * y[1][e + 2], y[0][e + 3] - lam * y[1][e + 3]);
+            store4(op, 32 * run + 2 * e + 4 * (lane >> 5), a.dv, y[0][e] - lam * y[1][e], y[0][e + 1] - lam * y[1][e + 1],
+                   y[0][e + 2] - lam * y[1][e + 2], y[0][e + 3] - lam * y[1][e + 3]);
     }
     if (!a.kept) return;
     static_assert(DV <= kScaleWidth, "one scale a row and map");
@@ -111,10 +110,8 @@ __device__ __forceinline__ void join_runs(const AttnArgs &a, const RowTile &r, u
         int16_t *kept = a.kept + (((r.s.row0 + r.t) * a.H + r.head) * 2 + i) * a.dv;
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
-            const int c = 32 * run + 2 * e + 4 * (lane >> 5);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (c + j < a.dv) kept[c + j] = kept_code(y[i][e + j], k.inv);
+            store4(kept, 32 * run + 2 * e + 4 * (lane >> 5), a.dv, kept_code(y[i][e], k.inv), kept_code(y[i][e + 1], k.inv),
+                   kept_code(y[i][e + 2], k.inv), kept_code(y[i][e + 3], k.inv));
         }
     }
 }
@@ -128,14 +125,14 @@ __device__ __forceinline__ void join_runs(const AttnArgs &a, const RowTile &r, u
 // need no second kernel.  Bound by memory where the cache is long: 16 x 1 rows over 16384 keys (4 key heads of
 // 64 + 128, 537 MB) 112 us; where it is short, by a wave's 1.4 us for 32 keys: 1 row over 577, 14.6 us.  (Eight waves
 // with a tile each, one at its loads beside another that computes: 117 and 14.0 us.)
-template <class T, int D, int DV, int BLOCKS, int MAPS, int KT, int RUNS>
+template <class T, int D, int DV, int BLOCKS, int MAPS, int KT, int RUNS, bool PIECES>
 __global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS) * RUNS, BLOCKS > 1 ? 2 : 1) void k_diff_forward(AttnArgs a) {
     static_assert(RUNS == 1 || (BLOCKS == 1 && MAPS == 2), "runs of one block");
     constexpr int WAVES = BLOCKS * (3 - MAPS);     // that share a ring
     using KTile = Tile<T, D / 8, KT, WAVES>;
     using VTile = Tile<T, DV / 8, KT, WAVES>;
-    using KFeed = Feed<T, D / 8, KT, WAVES, 2>;
-    using VFeed = Feed<T, DV / 8, KT, WAVES, 1>;
+    using KFeed = Feed<T, D / 8, KT, WAVES, 2, PIECES>;
+    using VFeed = Feed<T, DV / 8, KT, WAVES, 1, PIECES>;
     constexpr int STAGE = 2 * KTile::BYTES + VTile::BYTES;
     constexpr int SLOTS = 2;
     static_assert(MAPS == 2 || BLOCKS * 64 * DV * 2 <= SLOTS * STAGE, "room for the second maps' products");
@@ -167,8 +164,8 @@ __global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS) * RUNS, BLOCKS > 1 ? 2 : 1
 
     const int64_t key0 = s.k0 + (int64_t)tile0 * KT;
     const int left = s.nk - tile0 * KT;
-    KFeed keys(head_of<T>(a.k, s.batch, key0, 2 * r.hk), a.k.token, a.k.head, left, a.d, a.vec, wave, lane);
-    VFeed values(head_of<T>(a.v, s.batch, key0, r.hk), a.v.token, 0, left, a.dv, a.vec, wave, lane);
+    KFeed keys(head_of<T>(a.k, s.batch, key0, 2 * r.hk), a.k.token, a.k.head, left, a.d, wave, lane);
+    VFeed values(head_of<T>(a.v, s.batch, key0, r.hk), a.v.token, 0, left, a.dv, wave, lane);
     auto stage = [&](int n) {      // the next tile
         keys.load(lds + n % SLOTS * STAGE, wave, lane);
         values.load(lds + n % SLOTS * STAGE + 2 * KTile::BYTES, wave, lane);
@@ -180,7 +177,7 @@ __global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS) * RUNS, BLOCKS > 1 ? 2 : 1
     for (int i = 0; i < MAPS; ++i)
 #pragma unroll
         for (int c = 0; c < D / 16; ++c)
-            q[i][c] = row_operand(head_of<T>(a.q, s.batch, s.q0 + r.t, 2 * r.head + map + i), r.valid, c, a.d, a.vec, lane);
+            q[i][c] = row_operand<PIECES>(head_of<T>(a.q, s.batch, s.q0 + r.t, 2 * r.head + map + i), r.valid, c, a.d, lane);
     const float lam = a.splits > 1 ? 0.f : row_weight(a, r, lane);
 
     v16f o[MAPS][DV / 32];
@@ -299,7 +296,6 @@ __global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS) * RUNS, BLOCKS > 1 ? 2 : 1
         const int64_t part =
             (((int64_t)r.b * a.Hk + r.hk) * a.splits + split) * ((int64_t)a.tq * a.group) + r.t * a.group + r.g;
         float *ml = a.parts + part * 4 + 2 * map, *sums = a.parts + (int64_t)a.batch * a.Hk * a.splits * a.tq * a.group * 4;
-        const bool vec = a.dv % 4 == 0;
 #pragma unroll
         for (int i = 0; i < MAPS; ++i) {
             if (lane < 32) {
@@ -310,7 +306,7 @@ __global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS) * RUNS, BLOCKS > 1 ? 2 : 1
             for (int x = 0; x < DV / 32; ++x)
 #pragma unroll
                 for (int e = 0; e < 16; e += 4)
-                    store4(sums + (part * 2 + map + i) * a.dv, 32 * x + 2 * e + 4 * (lane >> 5), a.dv, vec, o[i][x][e],
+                    store4(sums + (part * 2 + map + i) * a.dv, 32 * x + 2 * e + 4 * (lane >> 5), a.dv, o[i][x][e],
                            o[i][x][e + 1], o[i][x][e + 2], o[i][x][e + 3]);
         }
         return;
@@ -346,8 +342,8 @@ __global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS) * RUNS, BLOCKS > 1 ? 2 : 1
                     y = lds_load<v4f>(hand + (x * 4 + e / 4) * 1024);
                 else
                     y = v4f{o[MAPS - 1][x][e], o[MAPS - 1][x][e + 1], o[MAPS - 1][x][e + 2], o[MAPS - 1][x][e + 3]};
-                store4(op, 32 * x + 2 * e + 4 * (lane >> 5), a.dv, a.vec_out, o[0][x][e] - lam * y[0],
-                       o[0][x][e + 1] - lam * y[1], o[0][x][e + 2] - lam * y[2], o[0][x][e + 3] - lam * y[3]);
+                store4(op, 32 * x + 2 * e + 4 * (lane >> 5), a.dv, o[0][x][e] - lam * y[0], o[0][x][e + 1] - lam * y[1],
+                       o[0][x][e + 2] - lam * y[2], o[0][x][e + 3] - lam * y[3]);
             }
     }
     if (!a.kept) return;
@@ -356,7 +352,6 @@ __global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS) * RUNS, BLOCKS > 1 ? 2 : 1
         float *at = a.stats + (2 * (int64_t)r.head + map + i) * a.stat_rows * a.rows + s.row0 + r.t;
         if (lane < 32) at[0] = sum[i] == 0.f ? __builtin_inff() : top[i] + __builtin_amdgcn_logf(sum[i]);
         int16_t *kept = a.kept + (((s.row0 + r.t) * a.H + r.head) * 2 + map + i) * a.dv;
-        const bool vec = a.dv % 4 == 0;
 #pragma unroll
         for (int w = 0; w < (DV + kScaleWidth - 1) / kScaleWidth; ++w) {
             if (w * kScaleWidth >= a.dv) break;
@@ -373,15 +368,8 @@ __global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS) * RUNS, BLOCKS > 1 ? 2 : 1
 #pragma unroll
                 for (int e = 0; e < 16; e += 4) {
                     const int c = 32 * x + 2 * e + 4 * (lane >> 5);
-                    const v4s q4 = {kept_code(o[i][x][e], k.inv), kept_code(o[i][x][e + 1], k.inv),
-                                    kept_code(o[i][x][e + 2], k.inv), kept_code(o[i][x][e + 3], k.inv)};
-                    if (vec) {
-                        if (c < a.dv) *(v4s *)(kept + c) = q4;
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (c + j < a.dv) kept[c + j] = q4[j];
-                    }
+                    store4(kept, c, a.dv, kept_code(o[i][x][e], k.inv), kept_code(o[i][x][e + 1], k.inv),
+                           kept_code(o[i][x][e + 2], k.inv), kept_code(o[i][x][e + 3], k.inv));
                 }
         }
     }
@@ -434,15 +422,15 @@ __global__ __launch_bounds__(256) void k_diff_join(AttnArgs a) {
     const int c = n % pieces * 4, turn = n / pieces;
     v4f y[2] = {v4f{0.f, 0.f, 0.f, 0.f}, v4f{0.f, 0.f, 0.f, 0.f}};
     if (turn < turns) {
-        const bool vec = a.dv % 4 == 0;
+        typedef float v4any __attribute__((ext_vector_type(4), aligned(4)));
         for (int k = turn; k < a.splits; k += turns) {
             const float *p = products + (part + k * wide) * 2 * a.dv + c;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const float f = factor[i][k];
                 if (f == 0.f) continue;
-                if (vec)
-                    y[i] += f * *(const v4f *)(p + i * a.dv);
+                if (c + 4 <= a.dv)
+                    y[i] += f * *(const v4any *)(p + i * a.dv);
                 else
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
@@ -466,7 +454,7 @@ __global__ __launch_bounds__(256) void k_diff_join(AttnArgs a) {
     for (int i = 0; i < 2; ++i) y[i] *= sum[i] == 0.f ? 0.f : 1.f / sum[i];
     if (live) {
         const v4f out = y[0] - lam * y[1];
-        store4(head_of<T>(a.o, s.batch, s.q0 + t, head), lane * 4, a.dv, a.vec_out, out[0], out[1], out[2], out[3]);
+        store4(head_of<T>(a.o, s.batch, s.q0 + t, head), lane * 4, a.dv, out[0], out[1], out[2], out[3]);
     }
     if (!a.kept) return;
 #pragma unroll
@@ -482,31 +470,35 @@ __global__ __launch_bounds__(256) void k_diff_join(AttnArgs a) {
             const KeptScale k = kept_scale(wave_largest(in ? most : 0.f));
             if (lane == 0) at[(1 + w) * a.rows] = k.scale;
             if (in)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (lane * 4 + j < a.dv) to[lane * 4 + j] = kept_code(y[i][j], k.inv);
+                store4(to, lane * 4, a.dv, kept_code(y[i][0], k.inv), kept_code(y[i][1], k.inv), kept_code(y[i][2], k.inv),
+                       kept_code(y[i][3], k.inv));
         }
     }
 }
 
-template <class T, bool WIDE>
+template <class T, bool WIDE, bool PIECES>
 int forward(int cls, const AttnArgs &a, hipStream_t s) {
-    const dim3 grid((unsigned)((int64_t)a.batch * a.Hk * a.row_tiles * a.splits));
+    const dim3 grid((unsigned)((int64_t)a.batch * a.Hk * a.row_tiles * a.splits)), block(cls < 2 || WIDE ? 256 : 128);
+    constexpr int BLOCKS = WIDE ? 4 : 1, KT = WIDE ? 64 : 32, RUNS = WIDE ? 1 : 4;
     if (cls == 0)
-        hipLaunchKernelGGL((k_diff_forward<T, 32, 64, WIDE ? 4 : 1, 2, WIDE ? 64 : 32, WIDE ? 1 : 4>), grid, dim3(256), 0, s, a);
+        hipLaunchKernelGGL((k_diff_forward<T, 32, 64, BLOCKS, 2, KT, RUNS, PIECES>), grid, block, 0, s, a);
     else if (cls == 1)
-        hipLaunchKernelGGL((k_diff_forward<T, 64, 128, WIDE ? 4 : 1, 2, WIDE ? 64 : 32, WIDE ? 1 : 4>), grid, dim3(256), 0, s, a);
+        hipLaunchKernelGGL((k_diff_forward<T, 64, 128, BLOCKS, 2, KT, RUNS, PIECES>), grid, block, 0, s, a);
     else
-        hipLaunchKernelGGL((k_diff_forward<T, 128, 256, WIDE ? 2 : 1, 1, 32, 1>), grid, dim3(WIDE ? 256 : 128), 0, s, a);
+        hipLaunchKernelGGL((k_diff_forward<T, 128, 256, WIDE ? 2 : 1, 1, 32, 1, PIECES>), grid, block, 0, s, a);
     return (int)hipGetLastError();
+}
+template <class T>
+int forward(int cls, bool wide, const AttnArgs &a, hipStream_t s) {
+    if (a.pieces) return wide ? forward<T, true, true>(cls, a, s) : forward<T, false, true>(cls, a, s);
+    return wide ? forward<T, true, false>(cls, a, s) : forward<T, false, false>(cls, a, s);
 }
 
 }  // namespace
 
 int launch_diff_forward(int type, int cls, bool wide, const AttnArgs &a, void *stream) {
     const hipStream_t s = (hipStream_t)stream;
-    if (type == NM_TYPE_F16) return wide ? forward<half_t, true>(cls, a, s) : forward<half_t, false>(cls, a, s);
-    return wide ? forward<bf16_t, true>(cls, a, s) : forward<bf16_t, false>(cls, a, s);
+    return type == NM_TYPE_F16 ? forward<half_t>(cls, wide, a, s) : forward<bf16_t>(cls, wide, a, s);
 }
 
 int launch_diff_join(int type, const AttnArgs &a, void *stream) {

@@ -21,13 +21,13 @@ namespace {
 
 // dq, D1, D2 and the parts of dlam: rows as in the forward pass, scores transposed, so a
 // lane's keys are of one row and ds is the operand of dq as it lies.
-template <class T, int D, int DV>
+template <class T, int D, int DV, bool PIECES>
 __global__ __launch_bounds__(256, DV <= 128 ? 2 : 1) void k_diff_grad_q(AttnArgs a) {
     constexpr int KT = kGradKeyTile;
     using KTile = Tile<T, D / 8, KT, 4>;
     using VTile = Tile<T, DV / 8, KT, 4>;
-    using KFeed = Feed<T, D / 8, KT, 4, 2>;
-    using VFeed = Feed<T, DV / 8, KT, 4, 1>;
+    using KFeed = Feed<T, D / 8, KT, 4, 2, PIECES>;
+    using VFeed = Feed<T, DV / 8, KT, 4, 1, PIECES>;
     constexpr int STAGE = 2 * KTile::BYTES + VTile::BYTES;
     __shared__ __attribute__((aligned(1024))) char shared[2 * STAGE];
     const uint32_t lds = lds_start(shared);
@@ -42,8 +42,8 @@ __global__ __launch_bounds__(256, DV <= 128 ? 2 : 1) void k_diff_grad_q(AttnArgs
     const int tile0 = r.low / KT, tiles = r.high >= r.low ? r.high / KT + 1 - tile0 : 0;
     const int64_t key0 = s.k0 + (int64_t)tile0 * KT;
     const int left = s.nk - tile0 * KT;
-    KFeed keys(head_of<T>(a.k, s.batch, key0, 2 * r.hk), a.k.token, a.k.head, left, a.d, a.vec, wave, lane);
-    VFeed values(head_of<T>(a.v, s.batch, key0, r.hk), a.v.token, 0, left, a.dv, a.vec, wave, lane);
+    KFeed keys(head_of<T>(a.k, s.batch, key0, 2 * r.hk), a.k.token, a.k.head, left, a.d, wave, lane);
+    VFeed values(head_of<T>(a.v, s.batch, key0, r.hk), a.v.token, 0, left, a.dv, wave, lane);
     auto stage = [&](int n) {      // the next tile
         keys.load(lds + (n & 1) * STAGE, wave, lane);
         values.load(lds + (n & 1) * STAGE + 2 * KTile::BYTES, wave, lane);
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(256, DV <= 128 ? 2 : 1) void k_diff_grad_q(AttnArgs
     for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int c = 0; c < D / 16; ++c)
-            q[i][c] = row_operand(head_of<T>(a.q, s.batch, s.q0 + r.t, 2 * r.head + i), r.valid, c, a.d, a.vec, lane);
+            q[i][c] = row_operand<PIECES>(head_of<T>(a.q, s.batch, s.q0 + r.t, 2 * r.head + i), r.valid, c, a.d, lane);
     const float lam = row_weight(a, r, lane);
     float d[2], lse[2];
     {
@@ -65,11 +65,11 @@ __global__ __launch_bounds__(256, DV <= 128 ? 2 : 1) void k_diff_grad_q(AttnArgs
         float sums[2][(DV + kScaleWidth - 1) / kScaleWidth] = {};
 #pragma unroll
         for (int c = 0; c < DV / 16; ++c) {
-            grad[c] = row_operand(gp, r.valid, c, a.dv, a.vec, lane);
+            grad[c] = row_operand<PIECES>(gp, r.valid, c, a.dv, lane);
             const v8 x = __builtin_bit_cast(v8, grad[c]);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const v8s y = row_operand(kept + i * a.dv, r.valid, c, a.dv, a.dv % 8 == 0, lane);
+                const v8s y = row_operand<PIECES>(kept + i * a.dv, r.valid, c, a.dv, lane);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sums[i][c * 16 / kScaleWidth] += (float)x[e] * (float)y[e];
             }
@@ -182,8 +182,8 @@ __global__ __launch_bounds__(256, DV <= 128 ? 2 : 1) void k_diff_grad_q(AttnArgs
         for (int x = 0; x < D / 32; ++x)
 #pragma unroll
             for (int e = 0; e < 16; e += 4)
-                store4(out, 32 * x + 2 * e + 4 * (lane >> 5), a.d, a.vec_out, dq[i][x][e] * f, dq[i][x][e + 1] * f,
-                       dq[i][x][e + 2] * f, dq[i][x][e + 3] * f);
+                store4(out, 32 * x + 2 * e + 4 * (lane >> 5), a.d, dq[i][x][e] * f, dq[i][x][e + 1] * f, dq[i][x][e + 2] * f,
+                       dq[i][x][e + 3] * f);
     }
 }
 
@@ -229,26 +229,26 @@ __device__ __forceinline__ void weight_grads(const AttnArgs &a, int lane, int wa
 // maps' operands too, but not without spilling, and a wait for a spilled register waits for the next
 // tile's loads as well: 4 x 4096 rows of 8 heads, width 64 + 128, 760 us and 672).
 // PAIR 1, for the widest class, whose k and v fill LDS: a wave each, k in registers.
-template <class T, int D, int DV>
+template <class T, int D, int DV, bool PIECES>
 struct KeySteps {
     static constexpr int PAIR = DV <= 128 ? 2 : 1, WAVES = 4 * PAIR, QT = 32 * PAIR;
     using QTile = Tile<T, D / 8, QT, WAVES>;
     using GTile = Tile<T, DV / 8, QT, WAVES>;
     using KTile = Tile<T, D / 8, kGradKeys, WAVES>;
     using VTile = Tile<T, DV / 8, kGradKeys, WAVES>;
-    using QFeed = Feed<T, D / 8, QT, WAVES, 2>;
-    using GFeed = Feed<T, DV / 8, QT, WAVES, 1>;
-    using KFeed = Feed<T, D / 8, kGradKeys, WAVES, 2>;
-    using VFeed = Feed<T, DV / 8, kGradKeys, WAVES, 1>;
+    using QFeed = Feed<T, D / 8, QT, WAVES, 2, PIECES>;
+    using GFeed = Feed<T, DV / 8, QT, WAVES, 1, PIECES>;
+    using KFeed = Feed<T, D / 8, kGradKeys, WAVES, 2, PIECES>;
+    using VFeed = Feed<T, DV / 8, kGradKeys, WAVES, 1, PIECES>;
     static constexpr int TILES = 2 * QTile::BYTES + GTile::BYTES, STAGE = TILES + 1024;
     static constexpr int KEYS = PAIR == 2 ? 2 * KTile::BYTES : 0, FIXED = KEYS + VTile::BYTES;
     static constexpr int HAND = PAIR == 2 ? 4 * 64 * (2 * D + DV) * 2 : 0;      // the second waves' sums
     static constexpr int BYTES = FIXED + 2 * STAGE > HAND ? FIXED + 2 * STAGE : HAND;
 };
 // DK, DV_: which of the two a workgroup makes.
-template <class T, int D, int DV, bool DK, bool DV_>
+template <class T, int D, int DV, bool PIECES, bool DK, bool DV_>
 __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int id, int lane, int wave) {
-    using S = KeySteps<T, D, DV>;
+    using S = KeySteps<T, D, DV, PIECES>;
     using QTile = typename S::QTile;
     using GTile = typename S::GTile;
     using KTile = typename S::KTile;
@@ -286,12 +286,10 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
     }
     const uint32_t steps_at = lds + S::FIXED;
     auto queries_of = [&](int head, int t) {
-        return typename S::QFeed(head_of<T>(a.q, s.batch, s.q0 + t, 2 * head), a.q.token, a.q.head, s.nq - t, a.d, a.vec, wave,
-                                 lane);
+        return typename S::QFeed(head_of<T>(a.q, s.batch, s.q0 + t, 2 * head), a.q.token, a.q.head, s.nq - t, a.d, wave, lane);
     };
     auto grads_of = [&](int head, int t) {
-        return typename S::GFeed(head_of<T>(a.grad, s.batch, s.q0 + t, head), a.grad.token, 0, s.nq - t, a.dv, a.vec, wave,
-                                 lane);
+        return typename S::GFeed(head_of<T>(a.grad, s.batch, s.q0 + t, head), a.grad.token, 0, s.nq - t, a.dv, wave, lane);
     };
     auto queries = queries_of(head, t0 + at * QT);
     auto grads = grads_of(head, t0 + at * QT);
@@ -309,11 +307,10 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
     };
     if (steps > 0) {
         if (PAIR == 2)
-            typename S::KFeed(head_of<T>(a.k, s.batch, s.k0 + begin, 2 * hk), a.k.token, a.k.head, s.nk - begin, a.d, a.vec, wave,
-                              lane)
+            typename S::KFeed(head_of<T>(a.k, s.batch, s.k0 + begin, 2 * hk), a.k.token, a.k.head, s.nk - begin, a.d, wave, lane)
                 .load(lds, wave, lane);
         if (DK)
-            typename S::VFeed(head_of<T>(a.v, s.batch, s.k0 + begin, hk), a.v.token, 0, s.nk - begin, a.dv, a.vec, wave, lane)
+            typename S::VFeed(head_of<T>(a.v, s.batch, s.k0 + begin, hk), a.v.token, 0, s.nk - begin, a.dv, wave, lane)
                 .load(lds + S::KEYS, wave, lane);
         stage(0, head, t0 + at * QT);
     }
@@ -324,7 +321,7 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int c = 0; c < D / 16; ++c)
-                k[i][c] = row_operand(head_of<T>(a.k, s.batch, s.k0 + key, 2 * hk + i), valid, c, a.d, a.vec, lane);
+                k[i][c] = row_operand<PIECES>(head_of<T>(a.k, s.batch, s.k0 + key, 2 * hk + i), valid, c, a.d, lane);
     v16f dk[2][D / 32], dv[DV / 32];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -472,7 +469,6 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
     if (!valid) return;
     if (a.key_splits > 1) {                // sums in 32 bits, dk's before its scale: 2 d and dv of a key
         float *part = a.key_parts + ((((int64_t)b * a.Hk + hk) * a.key_splits + split) * a.tk + key) * (2 * a.d + a.dv);
-        const bool vec = a.d % 4 == 0 && a.dv % 4 == 0;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -480,14 +476,14 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
 #pragma unroll
                 for (int e = 0; e < 16; e += 4)
                     if (DK)
-                        store4(part + i * a.d, 32 * x + 2 * e + 4 * (lane >> 5), a.d, vec, dk[i][x][e], dk[i][x][e + 1],
+                        store4(part + i * a.d, 32 * x + 2 * e + 4 * (lane >> 5), a.d, dk[i][x][e], dk[i][x][e + 1],
                                dk[i][x][e + 2], dk[i][x][e + 3]);
 #pragma unroll
         for (int x = 0; x < DV / 32; ++x)
 #pragma unroll
             for (int e = 0; e < 16; e += 4)
                 if (DV_)
-                    store4(part + 2 * a.d, 32 * x + 2 * e + 4 * (lane >> 5), a.dv, vec, dv[x][e], dv[x][e + 1], dv[x][e + 2],
+                    store4(part + 2 * a.d, 32 * x + 2 * e + 4 * (lane >> 5), a.dv, dv[x][e], dv[x][e + 1], dv[x][e + 2],
                            dv[x][e + 3]);
         return;
     }
@@ -499,8 +495,8 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
         for (int x = 0; x < D / 32; ++x)
 #pragma unroll
             for (int e = 0; e < 16; e += 4)
-                store4(out, 32 * x + 2 * e + 4 * (lane >> 5), a.d, a.vec_out, dk[i][x][e] * a.scale,
-                       dk[i][x][e + 1] * a.scale, dk[i][x][e + 2] * a.scale, dk[i][x][e + 3] * a.scale);
+                store4(out, 32 * x + 2 * e + 4 * (lane >> 5), a.d, dk[i][x][e] * a.scale, dk[i][x][e + 1] * a.scale,
+                       dk[i][x][e + 2] * a.scale, dk[i][x][e + 3] * a.scale);
     }
     if (!DV_) return;
     T *out = head_of<T>(a.dv_, s.batch, s.k0 + key, hk);
@@ -508,28 +504,27 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
     for (int x = 0; x < DV / 32; ++x)
 #pragma unroll
         for (int e = 0; e < 16; e += 4)
-            store4(out, 32 * x + 2 * e + 4 * (lane >> 5), a.dv, a.vec_out, dv[x][e], dv[x][e + 1], dv[x][e + 2],
-                   dv[x][e + 3]);
+            store4(out, 32 * x + 2 * e + 4 * (lane >> 5), a.dv, dv[x][e], dv[x][e + 1], dv[x][e + 2], dv[x][e + 3]);
 }
 
 // The widest class's sums of both do not fit the registers: a workgroup for dk and one for dv, each
 // with the scores.  The last workgroup of the launch makes the learned weights' gradients.
-template <class T, int D, int DV>
-__global__ __launch_bounds__((KeySteps<T, D, DV>::WAVES * 64), (DV <= 128 ? 2 : 1)) void k_diff_grad_k(AttnArgs a) {
-    __shared__ __attribute__((aligned(1024))) char shared[KeySteps<T, D, DV>::BYTES];
+template <class T, int D, int DV, bool PIECES>
+__global__ __launch_bounds__((KeySteps<T, D, DV, PIECES>::WAVES * 64), (DV <= 128 ? 2 : 1)) void k_diff_grad_k(AttnArgs a) {
+    __shared__ __attribute__((aligned(1024))) char shared[KeySteps<T, D, DV, PIECES>::BYTES];
     const uint32_t lds = lds_start(shared);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     if (blockIdx.x == gridDim.x - 1) {
-        weight_grads(a, lane, wave, KeySteps<T, D, DV>::WAVES);
+        weight_grads(a, lane, wave, KeySteps<T, D, DV, PIECES>::WAVES);
         return;
     }
     const int id = near_block(blockIdx.x, gridDim.x - 1);
     if constexpr (DV <= 128)
-        key_grads<T, D, DV, true, true>(a, lds, id, lane, wave);
+        key_grads<T, D, DV, PIECES, true, true>(a, lds, id, lane, wave);
     else if (id & 1)
-        key_grads<T, D, DV, false, true>(a, lds, id >> 1, lane, wave);
+        key_grads<T, D, DV, PIECES, false, true>(a, lds, id >> 1, lane, wave);
     else
-        key_grads<T, D, DV, true, false>(a, lds, id >> 1, lane, wave);
+        key_grads<T, D, DV, PIECES, true, false>(a, lds, id >> 1, lane, wave);
 }
 
 // The splits' sums of a key: a wave each, in the splits' order.
@@ -558,26 +553,29 @@ __global__ __launch_bounds__(256) void k_diff_join_keys(AttnArgs a) {
     }
 }
 
-template <class T>
+template <class T, bool PIECES>
 int grad_q(int cls, const AttnArgs &a, hipStream_t s) {
     const dim3 grid((unsigned)((int64_t)a.batch * a.Hk * a.row_tiles)), block(256);
     if (cls == 0)
-        hipLaunchKernelGGL((k_diff_grad_q<T, 32, 64>), grid, block, 0, s, a);
+        hipLaunchKernelGGL((k_diff_grad_q<T, 32, 64, PIECES>), grid, block, 0, s, a);
     else if (cls == 1)
-        hipLaunchKernelGGL((k_diff_grad_q<T, 64, 128>), grid, block, 0, s, a);
+        hipLaunchKernelGGL((k_diff_grad_q<T, 64, 128, PIECES>), grid, block, 0, s, a);
     else
-        hipLaunchKernelGGL((k_diff_grad_q<T, 128, 256>), grid, block, 0, s, a);
+        hipLaunchKernelGGL((k_diff_grad_q<T, 128, 256, PIECES>), grid, block, 0, s, a);
     return (int)hipGetLastError();
 }
-template <class T, int D, int DV>
+template <class T, int D, int DV, bool PIECES>
 int grad_k(const AttnArgs &a, hipStream_t s) {
     const int64_t groups = (int64_t)a.batch * a.Hk * a.key_tiles * a.key_splits * (DV <= 128 ? 1 : 2) + 1;
-    hipLaunchKernelGGL((k_diff_grad_k<T, D, DV>), dim3((unsigned)groups), dim3(KeySteps<T, D, DV>::WAVES * 64), 0, s, a);
+    hipLaunchKernelGGL((k_diff_grad_k<T, D, DV, PIECES>), dim3((unsigned)groups), dim3(KeySteps<T, D, DV, PIECES>::WAVES * 64), 0,
+                       s, a);
     return (int)hipGetLastError();
 }
-template <class T>
+template <class T, bool PIECES>
 int grad_k(int cls, const AttnArgs &a, hipStream_t s) {
-    return cls == 0 ? grad_k<T, 32, 64>(a, s) : cls == 1 ? grad_k<T, 64, 128>(a, s) : grad_k<T, 128, 256>(a, s);
+    return cls == 0   ? grad_k<T, 32, 64, PIECES>(a, s)
+           : cls == 1 ? grad_k<T, 64, 128, PIECES>(a, s)
+                      : grad_k<T, 128, 256, PIECES>(a, s);
 }
 template <class T>
 int join_keys(const AttnArgs &a, hipStream_t s) {
@@ -589,10 +587,14 @@ int join_keys(const AttnArgs &a, hipStream_t s) {
 }  // namespace
 
 int launch_diff_grad_q(int type, int cls, const AttnArgs &a, void *stream) {
-    return type == NM_TYPE_F16 ? grad_q<half_t>(cls, a, (hipStream_t)stream) : grad_q<bf16_t>(cls, a, (hipStream_t)stream);
+    const hipStream_t s = (hipStream_t)stream;
+    if (type == NM_TYPE_F16) return a.pieces ? grad_q<half_t, true>(cls, a, s) : grad_q<half_t, false>(cls, a, s);
+    return a.pieces ? grad_q<bf16_t, true>(cls, a, s) : grad_q<bf16_t, false>(cls, a, s);
 }
 int launch_diff_grad_k(int type, int cls, const AttnArgs &a, void *stream) {
-    return type == NM_TYPE_F16 ? grad_k<half_t>(cls, a, (hipStream_t)stream) : grad_k<bf16_t>(cls, a, (hipStream_t)stream);
+    const hipStream_t s = (hipStream_t)stream;
+    if (type == NM_TYPE_F16) return a.pieces ? grad_k<half_t, true>(cls, a, s) : grad_k<half_t, false>(cls, a, s);
+    return a.pieces ? grad_k<bf16_t, true>(cls, a, s) : grad_k<bf16_t, false>(cls, a, s);
 }
 int launch_diff_join_keys(int type, const AttnArgs &a, void *stream) {
     return type == NM_TYPE_F16 ? join_keys<half_t>(a, (hipStream_t)stream) : join_keys<bf16_t>(a, (hipStream_t)stream);

@@ -25,7 +25,7 @@ struct RotaryArgs {
     float sign;               // of the angle
 };
 constexpr int kMaxRotaryWidth = 1024;
-int launch_rotary(int type, bool vec, const RotaryArgs &a, void *stream);
+int launch_rotary(int type, const RotaryArgs &a, void *stream);
 
 // ---------------------------------------------------------------- differential attention
 
@@ -50,8 +50,7 @@ struct AttnArgs {
     int batch, tq, tk, H, Hk, group, d, dv, left, right;
     float scale, scale2;      // and in base 2
     nm_diff_weight weight;
-    int vec;                  // q, k, v (and do) are whole 16-byte pieces
-    int vec_out;              // o (backward: dq, dk, dv) is whole 8-byte pieces
+    int pieces;               // q, k, v (and do) are whole 16-byte pieces, rows apart
     int row_tiles, splits;
     float *parts;             // [batch * Hk * splits * tq * group] x 4: m1, l1, m2, l2, then the same x 2 dv values
     // backward

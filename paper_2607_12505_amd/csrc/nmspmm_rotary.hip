@@ -16,12 +16,71 @@ namespace {
 
 constexpr int kRotaryThreads = 256;
 
-// Tokens of a workgroup: `per` of them, whose angles lie in LDS.
-// VEC: items of 8 channels at 16-byte boundaries (halves: 8 pairs as two pieces; pairs: 4
-// pairs in one), else of one pair; the channels past the pairs are copied by the same piece.
-template <class T, bool VEC>
+// Up to 8 values at any alignment of their type (the hardware's loads and stores take it), in pieces of 8, 4, 2 and 1.
+template <class T>
+struct Some {
+    typedef T vec __attribute__((ext_vector_type(8)));
+    template <int N>
+    using any = T __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+    template <int N, int AT = 0>
+    static __device__ __forceinline__ void get(const T *p, vec &v) {
+        constexpr int W = N >= 8 ? 8 : N >= 4 ? 4 : N >= 2 ? 2 : 1;
+        const any<W> x = *(const any<W> *)(p + AT);
+#pragma unroll
+        for (int j = 0; j < W; ++j) v[AT + j] = x[j];
+        if constexpr (N > W) get<N - W, AT + W>(p, v);
+    }
+    template <int N, int AT = 0>
+    static __device__ __forceinline__ void put(T *p, const vec &v) {
+        constexpr int W = N >= 8 ? 8 : N >= 4 ? 4 : N >= 2 ? 2 : 1;
+        any<W> x;
+#pragma unroll
+        for (int j = 0; j < W; ++j) x[j] = v[AT + j];
+        *(any<W> *)(p + AT) = x;
+        if constexpr (N > W) put<N - W, AT + W>(p, v);
+    }
+    static __device__ __forceinline__ vec load(const T *p, int n) {
+        vec v = {};
+        if (n >= 8) {
+            get<8>(p, v);
+            return v;
+        }
+        switch (n) {
+            case 1: get<1>(p, v); break;
+            case 2: get<2>(p, v); break;
+            case 3: get<3>(p, v); break;
+            case 4: get<4>(p, v); break;
+            case 5: get<5>(p, v); break;
+            case 6: get<6>(p, v); break;
+            case 7: get<7>(p, v); break;
+            default: break;
+        }
+        return v;
+    }
+    static __device__ __forceinline__ void store(T *p, int n, const vec &v) {
+        if (n >= 8) return put<8>(p, v);
+        switch (n) {
+            case 1: put<1>(p, v); break;
+            case 2: put<2>(p, v); break;
+            case 3: put<3>(p, v); break;
+            case 4: put<4>(p, v); break;
+            case 5: put<5>(p, v); break;
+            case 6: put<6>(p, v); break;
+            case 7: put<7>(p, v); break;
+            default: break;
+        }
+    }
+};
+
+__host__ __device__ constexpr int angles_of(int pairs) { return (pairs + 7) & ~7; }
+
+// Tokens of a workgroup: `per` of them, whose angles lie in LDS.  An item is two pieces of 8
+// channels: 8 pairs, or channels past the pairs, which are copied.
+template <class T>
 __global__ __launch_bounds__(kRotaryThreads) void k_rotary(RotaryArgs a, int per) {
-    extern __shared__ float2 turn[];
+    using vec = typename Some<T>::vec;
+    extern __shared__ __attribute__((aligned(16))) float2 turn[];       // angles of a token: whole items of pairs
+    const int row = angles_of(a.pairs);
     const int64_t t0 = (int64_t)blockIdx.x * per;
     const int n = (int)(a.tokens - t0 < per ? a.tokens - t0 : per);
     for (int e = threadIdx.x; e < n * a.pairs; e += kRotaryThreads) {
@@ -32,14 +91,13 @@ __global__ __launch_bounds__(kRotaryThreads) void k_rotary(RotaryArgs a, int per
         const double turns = pos * a.freq[i] * 0.15915494309189533577;
         float s, c;
         sincospif((float)(2.0 * (turns - __builtin_rint(turns))), &s, &c);
-        turn[e] = make_float2(c, s * a.sign);
+        turn[t * row + i] = make_float2(c, s * a.sign);
     }
     __syncthreads();
     const int heads = a.part[0].heads + a.part[1].heads;
     // items of a head: the pairs' and those of the channels behind them
-    const int turned = !VEC ? a.pairs : a.interleaved ? a.pairs / 4 : a.pairs / 8;
-    const int rest = VEC ? (a.d - 2 * a.pairs) / 8 : a.d - 2 * a.pairs;
-    const int items = turned + rest, token_items = heads * items;
+    const int rest = a.d - 2 * a.pairs, turned = (a.pairs + 7) / 8, copied = (rest + 15) / 16;
+    const int items = turned + copied, token_items = heads * items;
     for (int e = threadIdx.x; e < n * token_items; e += kRotaryThreads) {
         const int t = e / token_items, r = e - t * token_items;
         int h = r / items;
@@ -49,74 +107,58 @@ __global__ __launch_bounds__(kRotaryThreads) void k_rotary(RotaryArgs a, int per
         if (second) h -= a.part[0].heads;
         const T *x = (const T *)p.x + (t0 + t) * p.x_token + h * p.x_head;
         T *out = (T *)p.out + (t0 + t) * p.out_token + h * p.out_head;
-        const float2 *at = turn + t * a.pairs;
-        if constexpr (!VEC) {
-            if (i >= turned) {
-                const int c = 2 * a.pairs + i - turned;
-                out[c] = x[c];
-                continue;
+        const float2 *at = turn + t * row;
+        // the item's pieces, neighbours' side by side
+        const bool turns = i < turned;
+        const int first = turns ? 8 * i : 2 * a.pairs + 8 * (i - turned), end = turns ? 2 * a.pairs : a.d;
+        const bool halves = turns && !a.interleaved;
+        const int c0 = first, c1 = first + (halves ? a.pairs : 8 * (turns ? turned : copied));
+        const int n0 = (halves ? a.pairs : end) - c0, n1 = end - c1;
+        vec v0 = Some<T>::load(x + c0, n0), v1 = Some<T>::load(x + c1, n1);
+        if (halves) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float2 z = at[8 * i + j];
+                const float u = (float)v0[j], w = (float)v1[j];
+                v0[j] = (T)(u * z.x - w * z.y);
+                v1[j] = (T)(u * z.y + w * z.x);
             }
-            const int cu = a.interleaved ? 2 * i : i, cw = a.interleaved ? 2 * i + 1 : i + a.pairs;
-            const float u = (float)x[cu], w = (float)x[cw];
-            const float2 z = at[i];
-            out[cu] = (T)(u * z.x - w * z.y);
-            out[cw] = (T)(u * z.y + w * z.x);
-        } else {
-            if (i >= turned) {
-                const int c = 2 * a.pairs + (i - turned) * 8;
-                *(typename Raw8<T>::vec *)(out + c) = load8(x + c).v;
-            } else if (a.interleaved) {
-                const auto v = load8(x + 8 * i).v;
-                float f[8];
+        } else if (turns) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float2 z = at[4 * i + j];
-                    const float u = (float)v[2 * j], w = (float)v[2 * j + 1];
-                    f[2 * j] = u * z.x - w * z.y;
-                    f[2 * j + 1] = u * z.y + w * z.x;
-                }
-                store8(out + 8 * i, f);
-            } else {
-                const auto vu = load8(x + 8 * i).v, vw = load8(x + a.pairs + 8 * i).v;
-                float fu[8], fw[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float2 z = at[8 * i + j];
-                    const float u = (float)vu[j], w = (float)vw[j];
-                    fu[j] = u * z.x - w * z.y;
-                    fw[j] = u * z.y + w * z.x;
-                }
-                store8(out + 8 * i, fu);
-                store8(out + a.pairs + 8 * i, fw);
+            for (int j = 0; j < 4; ++j) {
+                const float2 z0 = at[4 * i + j], z1 = at[4 * (i + turned) + j];
+                const float u0 = (float)v0[2 * j], w0 = (float)v0[2 * j + 1], u1 = (float)v1[2 * j], w1 = (float)v1[2 * j + 1];
+                v0[2 * j] = (T)(u0 * z0.x - w0 * z0.y);
+                v0[2 * j + 1] = (T)(u0 * z0.y + w0 * z0.x);
+                v1[2 * j] = (T)(u1 * z1.x - w1 * z1.y);
+                v1[2 * j + 1] = (T)(u1 * z1.y + w1 * z1.x);
             }
         }
+        Some<T>::store(out + c0, n0, v0);
+        Some<T>::store(out + c1, n1, v1);
     }
 }
 
 template <class T>
-int launch(bool vec, const RotaryArgs &a, hipStream_t stream) {
+int launch(const RotaryArgs &a, hipStream_t stream) {
     const int heads = a.part[0].heads + a.part[1].heads;
     // as many tokens as give every thread two items, within the angles' room
-    const int64_t items = (int64_t)heads * (vec ? (a.d + 15) / 16 : (a.d + 1) / 2);
+    const int64_t items = (int64_t)heads * ((a.d + 15) / 16);
     int64_t per = (2 * kRotaryThreads + items - 1) / items;
-    const int64_t room = 16384 / (8 * a.pairs);
+    const int64_t room = 16384 / (8 * angles_of(a.pairs));
     per = per < 1 ? 1 : per > room ? room : per;
     const int64_t grid = (a.tokens + per - 1) / per;
     if (grid >= (1ll << 24)) return (int)hipErrorInvalidConfiguration;   // a launch's threads are counted in 32 bits
-    const size_t lds = (size_t)per * a.pairs * 8;
-    if (vec)
-        k_rotary<T, true><<<dim3((unsigned)grid), kRotaryThreads, lds, stream>>>(a, (int)per);
-    else
-        k_rotary<T, false><<<dim3((unsigned)grid), kRotaryThreads, lds, stream>>>(a, (int)per);
+    const size_t lds = (size_t)per * angles_of(a.pairs) * 8;
+    k_rotary<T><<<dim3((unsigned)grid), kRotaryThreads, lds, stream>>>(a, (int)per);
     return (int)hipGetLastError();
 }
 
 }  // namespace
 
-int launch_rotary(int type, bool vec, const RotaryArgs &a, void *stream) {
+int launch_rotary(int type, const RotaryArgs &a, void *stream) {
     const hipStream_t s = (hipStream_t)stream;
-    return type == NM_TYPE_F16 ? launch<half_t>(vec, a, s)
-                               : type == NM_TYPE_BF16 ? launch<bf16_t>(vec, a, s) : launch<float>(vec, a, s);
+    return type == NM_TYPE_F16 ? launch<half_t>(a, s) : type == NM_TYPE_BF16 ? launch<bf16_t>(a, s) : launch<float>(a, s);
 }
 
 }  // namespace nmspmm

@@ -91,6 +91,10 @@ __global__ __launch_bounds__(256, DV <= 128 ? 2 : 1) void k_diff_grad_q(AttnArgs
 #pragma unroll
         for (int x = 0; x < D / 32; ++x) dq[i][x] = v16f{};
     float second = 0.f;   // sum of p2 dp over this lane's keys
+    // A row that sees one key has ds = 0: the codes would leave 2^-16 of dp.  Its D1 and D2 are dp itself, which the
+    // kernel of the keys makes by the same instructions.
+    const bool one = r.first == r.last, any_one = __any(one);
+    float only = 0.f;
 
     const uint32_t k_at = lds + KTile::rows_lane(lane), k_turned = lds + KTile::turned_lane(lane);
     const uint32_t v_at = lds + 2 * KTile::BYTES + VTile::rows_lane(lane);
@@ -123,7 +127,14 @@ __global__ __launch_bounds__(256, DV <= 128 ? 2 : 1) void k_diff_grad_q(AttnArgs
                 __builtin_amdgcn_sched_barrier(0);
             }
             __builtin_amdgcn_s_setprio(0);
-            if (j0 + 31 > r.block_end || j0 < r.block_full) hide(r, j0, lane, z);
+            if (j0 + 31 > r.block_end || j0 < r.block_full) {
+                hide(r, j0, lane, z);
+                if (any_one) {
+                    const int at = r.first - j0 - 4 * (lane >> 5);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) only = at == 8 * (e / 4) + e % 4 ? dp[e] : only;
+                }
+            }
             // ds of values 8 c .. 8 c + 7, two of them at a time (part k of 4)
             typedef T v2 __attribute__((ext_vector_type(2)));
             v4i ds[2][2];
@@ -173,11 +184,13 @@ __global__ __launch_bounds__(256, DV <= 128 ? 2 : 1) void k_diff_grad_q(AttnArgs
         const float w = wave_sum(r.g == k ? second : 0.f);
         if (lane == 0) lam_part[(int64_t)k * a.dlam_count] = w;
     }
+    only = half_sum(only);
     if (!r.valid) return;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
+        if (one && lane < 32) a.delta[(2 * (int64_t)r.head + i) * a.rows + s.row0 + r.t] = only;
         T *out = head_of<T>(a.dq, s.batch, s.q0 + r.t, 2 * r.head + i);
-        const float f = i ? -lam * a.scale : a.scale;
+        const float f = one ? 0.f : i ? -lam * a.scale : a.scale;
 #pragma unroll
         for (int x = 0; x < D / 32; ++x)
 #pragma unroll

@@ -263,6 +263,23 @@ def test_parts_of_the_keys(T, B, Tq, Tk, H, Hk, d, dv):
 
 
 @pytest.mark.parametrize("T", TYPES)
+@pytest.mark.parametrize("d,dv", [(32, 64), (64, 128), (61, 107), (128, 256), (100, 200)])
+def test_rows_that_see_one_key_have_no_gradient_of_scores(T, d, dv):
+    # p is 1 whatever the score: q and k get zeros, not the roundings of dp - D
+    g, H, Hk = gen(18), 4, 2
+    for B, Tq, Tk, window in ((57, 1, 1, (-1, 0)), (2, 3, 1, (-1, -1)), (1, 200, 200, (0, 0)), (1, 9, 40, (0, 0)), (2, 40, 40, (-1, 0))):
+        q, k, v, lam, spans = dense(g, T, B, Tq, Tk, H, Hk, d, dv)
+        do, weight = randn(g, T, B, Tq, H, dv), na.DiffWeight(lam)
+        check(q, k, v, weight, lam, spans, window, grad=do)
+        got = na.diff_attention_backward(do, na.diff_attention_train(q, k, v, weight, window=window), q, k, v, weight,
+                                         window=window)
+        if window == (-1, 0) and Tk > 1:                  # the first row alone, whose key others see
+            assert (got.dq[:, 0] == 0).all() and not (got.dq[:, 1:] == 0).any(dim=-1).all()
+        else:
+            assert (got.dq == 0).all() and (got.dk == 0).all()
+
+
+@pytest.mark.parametrize("T", TYPES)
 @pytest.mark.parametrize("n", [1, 75, 130])
 def test_expanded_inputs(T, n):
     # rows that are all one place in memory: those behind the last are not

@@ -95,8 +95,11 @@ void fill(AttnArgs &a, const nm_tokens &t, const nm_diff_weight &w, int H, int H
 
 // How the forward pass is cut: workgroups of many rows that share their tiles of keys, or of few rows, whose
 // keys go to the runs of a workgroup and in `splits` parts to several, which a second kernel joins.
-//   Few rows: up to 64, and more over long keys (tk > 1024) where workgroups of many would leave compute units
-//   without any (1 x 40 rows of 8 heads over 4096 keys 20 us).
+//   Few rows: up to 64, and more where workgroups of many would leave too much of the device without work (468 shapes of 65 to
+//   1024 causal rows over 256 to 8192 keys; the rule is within 1 % of the better variant on average).  Many and few:
+//     32 + 64:   4 x 512 rows of 8 heads over 1024 keys (128 workgroups of many) 27.5 and 22.5 us, 4 x 1024 (256) 27 and 36
+//     64 + 128:  4 x 200 over 2048 (64) 62 and 44, 4 x 512 over 1024 (128) 34 and 44
+//     128 + 256: 4 x 256 over 512 (128) 23 and 41, over 8192 238 and 208, 4 x 512 over 8192 (256) 246 and 335
 //   Splits: a workgroup a compute unit, of four tiles a wave at least (1 row of 8 heads over 577 keys
 //   in one 14.6 us, in three and a second kernel 13.3; over 8192 in eight 20.0).  Sequences of unequal length: twice as
 //   many where those are few and long (16 x 1 rows over up to 16384 keys, 4 key heads, 69 to 61 us; 8 over 32768, 8
@@ -110,13 +113,15 @@ Cut cut_of(const nm_tokens &t, int H, int Hk, int cls) {
     const int cus = device_cu_count();
     const int64_t wide_groups = heads * ((rows + wide_rows(cls) - 1) / wide_rows(cls));
     Cut c;
-    c.wide = rows > 64 && (wide_groups >= cus || t.tk <= 1024);
+    c.wide = rows > 64 && (cls == 0   ? 4 * wide_groups >= 3 * cus
+                           : cls == 1 ? 8 * wide_groups >= 3 * cus
+                                      : wide_groups >= cus || 16 * wide_groups >= t.tk);
     const int tile = c.wide ? wide_rows(cls) : kFewRows;
     c.row_tiles = (int)((rows + tile - 1) / tile);
     c.splits = 1;
     if (!c.wide) {
         const int64_t groups = heads * c.row_tiles, key_tiles = (t.tk + kFewRowsKeys - 1) / kFewRowsKeys;
-        int64_t splits = groups ? (cls == 2 ? 2 : 1) * cus / groups : 1;
+        int64_t splits = groups ? (cls >= 2 ? 2 : 1) * cus / groups : 1;
         if ((t.k_lens || t.k_offsets) && 4 * groups <= cus && key_tiles >= 128 * splits) splits *= 2;
         const int64_t most = key_tiles / (4 * key_runs(cls));
         if (splits > most) splits = most;
@@ -241,7 +246,7 @@ static int64_t grad_row_tiles(const nm_diff_grad_args &g) {
 // unit) where the tiles of keys do not, of at least four steps of 32 rows on average.
 static int key_splits(const nm_diff_grad_args &g) {
     const int64_t tiles = ((int64_t)g.tokens.tk + kGradKeys - 1) / kGradKeys;
-    const int64_t groups = (int64_t)g.tokens.batch * g.Hk * tiles * (width_class(g.d, g.dv_width) == 2 ? 2 : 1);
+    const int64_t groups = (int64_t)g.tokens.batch * g.Hk * tiles * (width_class(g.d, g.dv_width) == 3 ? 2 : 1);
     const int64_t steps = ((int64_t)g.tokens.tq + 31) / 32 * (g.H / g.Hk);
     if (groups == 0) return 1;
     int64_t splits = 2 * device_cu_count() / groups;

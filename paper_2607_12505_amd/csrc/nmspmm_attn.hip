@@ -378,7 +378,8 @@ __global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS) * RUNS, BLOCKS > 1 ? 2 : 1
 // The splits' sums of one row and head, a workgroup each:  M = max of m_s,
 // o_i = sum of 2^(m_s - M) O_s / sum of 2^(m_s - M) l_s.
 // A thread makes the factors of one split (of up to 256), then 4 channels of both maps over every
-// `turns`-th split; the turns meet in LDS.  The order of the sums is fixed.
+// `turns`-th split; the turns meet in LDS.  The order of the sums is fixed.  Bound by the latency of its three dependent
+// steps: 16 x 1 rows of 16 heads with 8 splits 5.3 us (a wave for a row and head, one split after another: 26 us).
 template <class T>
 __global__ __launch_bounds__(256) void k_diff_join(AttnArgs a) {
     __shared__ float factor[2][kMaxSplits], low[4][4];
@@ -484,6 +485,8 @@ int forward(int cls, const AttnArgs &a, hipStream_t s) {
         hipLaunchKernelGGL((k_diff_forward<T, 32, 64, BLOCKS, 2, KT, RUNS, PIECES>), grid, block, 0, s, a);
     else if (cls == 1)
         hipLaunchKernelGGL((k_diff_forward<T, 64, 128, BLOCKS, 2, KT, RUNS, PIECES>), grid, block, 0, s, a);
+    else if (cls == 2)
+        hipLaunchKernelGGL((k_diff_forward<T, 128, 128, WIDE ? 2 : 1, 1, 32, 1, PIECES>), grid, block, 0, s, a);
     else
         hipLaunchKernelGGL((k_diff_forward<T, 128, 256, WIDE ? 2 : 1, 1, 32, 1, PIECES>), grid, block, 0, s, a);
     return (int)hipGetLastError();

@@ -20,9 +20,11 @@ namespace nmspmm {
 namespace {
 
 // dq, D1, D2 and the parts of dlam: rows as in the forward pass, scores transposed, so a
-// lane's keys are of one row and ds is the operand of dq as it lies.
+// lane's keys are of one row and ds is the operand of dq as it lies.  128 rows a workgroup share tiles of 64 keys in a ring
+// of two.  Bound by matrix instructions (8 d + 2 dv operations a pair) and the exponentials and products beside
+// them: 2 x 4096 causal rows of 8 heads, 4 key heads, 64 + 128, 163 us, 630 TFLOP/s.
 template <class T, int D, int DV, bool PIECES>
-__global__ __launch_bounds__(256, DV <= 128 ? 2 : 1) void k_diff_grad_q(AttnArgs a) {
+__global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void k_diff_grad_q(AttnArgs a) {
     constexpr int KT = kGradKeyTile;
     using KTile = Tile<T, D / 8, KT, 4>;
     using VTile = Tile<T, DV / 8, KT, 4>;
@@ -241,10 +243,11 @@ __device__ __forceinline__ void weight_grads(const AttnArgs &a, int lane, int wa
 // k and v are read from LDS as q and do are, which leaves the registers to the sums (256 of them hold both
 // maps' operands too, but not without spilling, and a wait for a spilled register waits for the next
 // tile's loads as well: 4 x 4096 rows of 8 heads, width 64 + 128, 760 us and 672).
-// PAIR 1, for the widest class, whose k and v fill LDS: a wave each, k in registers.
+// PAIR 1, for keys of 128 channels, which with v would fill LDS: a wave each, k in registers.
+// Bound as the kernel above (8 d + 4 dv operations a pair): 239 us there, 575 TFLOP/s.
 template <class T, int D, int DV, bool PIECES>
 struct KeySteps {
-    static constexpr int PAIR = DV <= 128 ? 2 : 1, WAVES = 4 * PAIR, QT = 32 * PAIR;
+    static constexpr int PAIR = D <= 64 ? 2 : 1, WAVES = 4 * PAIR, QT = 32 * PAIR;
     using QTile = Tile<T, D / 8, QT, WAVES>;
     using GTile = Tile<T, DV / 8, QT, WAVES>;
     using KTile = Tile<T, D / 8, kGradKeys, WAVES>;
@@ -523,7 +526,7 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
 // The widest class's sums of both do not fit the registers: a workgroup for dk and one for dv, each
 // with the scores.  The last workgroup of the launch makes the learned weights' gradients.
 template <class T, int D, int DV, bool PIECES>
-__global__ __launch_bounds__((KeySteps<T, D, DV, PIECES>::WAVES * 64), (DV <= 128 ? 2 : 1)) void k_diff_grad_k(AttnArgs a) {
+__global__ __launch_bounds__((KeySteps<T, D, DV, PIECES>::WAVES * 64), (D <= 64 ? 2 : 1)) void k_diff_grad_k(AttnArgs a) {
     __shared__ __attribute__((aligned(1024))) char shared[KeySteps<T, D, DV, PIECES>::BYTES];
     const uint32_t lds = lds_start(shared);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -540,7 +543,7 @@ __global__ __launch_bounds__((KeySteps<T, D, DV, PIECES>::WAVES * 64), (DV <= 12
         key_grads<T, D, DV, PIECES, true, false>(a, lds, id >> 1, lane, wave);
 }
 
-// The splits' sums of a key: a wave each, in the splits' order.
+// The splits' sums of a key: a wave each, in the splits' order.  Bound by memory: two splits there, 84 MB in 20 us.
 template <class T>
 __global__ __launch_bounds__(256) void k_diff_join_keys(AttnArgs a) {
     const int lane = threadIdx.x & 63;
@@ -573,6 +576,8 @@ int grad_q(int cls, const AttnArgs &a, hipStream_t s) {
         hipLaunchKernelGGL((k_diff_grad_q<T, 32, 64, PIECES>), grid, block, 0, s, a);
     else if (cls == 1)
         hipLaunchKernelGGL((k_diff_grad_q<T, 64, 128, PIECES>), grid, block, 0, s, a);
+    else if (cls == 2)
+        hipLaunchKernelGGL((k_diff_grad_q<T, 128, 128, PIECES>), grid, block, 0, s, a);
     else
         hipLaunchKernelGGL((k_diff_grad_q<T, 128, 256, PIECES>), grid, block, 0, s, a);
     return (int)hipGetLastError();
@@ -588,6 +593,7 @@ template <class T, bool PIECES>
 int grad_k(int cls, const AttnArgs &a, hipStream_t s) {
     return cls == 0   ? grad_k<T, 32, 64, PIECES>(a, s)
            : cls == 1 ? grad_k<T, 64, 128, PIECES>(a, s)
+           : cls == 2 ? grad_k<T, 128, 128, PIECES>(a, s)
                       : grad_k<T, 128, 256, PIECES>(a, s);
 }
 template <class T>

@@ -63,14 +63,14 @@ struct AttnArgs {
     float *key_parts;         // [batch * Hk * key_splits * tk][2 d + dv] (key_splits > 1)
 };
 
-// Width classes that the kernels are built for: (32, 64), (64, 128), (128, 256).
-inline int width_class(int d, int dv) { return d <= 32 && dv <= 64 ? 0 : d <= 64 && dv <= 128 ? 1 : 2; }
+// Width classes that the kernels are built for: (32, 64), (64, 128), (128, 128), (128, 256).
+inline int width_class(int d, int dv) { return d <= 32 && dv <= 64 ? 0 : d <= 64 && dv <= 128 ? 1 : dv <= 128 ? 2 : 3; }
 constexpr int kScaleWidth = 128;              // channels of a scale of `kept`
 inline int stat_rows_of(int dv) { return 1 + (dv + kScaleWidth - 1) / kScaleWidth; }
 // Rows of a workgroup of the forward pass: many, and few whose keys may be split.
-inline int wide_rows(int cls) { return cls == 2 ? 64 : 128; }
+inline int wide_rows(int cls) { return cls >= 2 ? 64 : 128; }
 constexpr int kFewRows = 32, kFewRowsKeys = 32, kMaxSplits = 256;
-inline int key_runs(int cls) { return cls == 2 ? 1 : 4; }    // of a workgroup of few rows
+inline int key_runs(int cls) { return cls >= 2 ? 1 : 4; }    // of a workgroup of few rows
 // Of the backward pass: rows and keys of a workgroup, keys of a tile.
 constexpr int kGradRows = 128, kGradKeys = 128, kGradKeyTile = 64;
 

@@ -263,7 +263,17 @@ def test_parts_of_the_keys(T, B, Tq, Tk, H, Hk, d, dv):
 
 
 @pytest.mark.parametrize("T", TYPES)
-@pytest.mark.parametrize("d,dv", [(32, 64), (64, 128), (61, 107), (128, 256), (100, 200)])
+@pytest.mark.parametrize("window", [(-1, 0), (40, 3)])
+@pytest.mark.parametrize("B,Tq,Tk,H,Hk,d,dv", [(1, 200, 300, 1, 1, 128, 128), (2, 70, 90, 4, 2, 100, 90), (1, 129, 128, 2, 1, 72, 16),
+                                               (1, 90, 1500, 2, 1, 128, 120), (1, 1, 3000, 1, 1, 97, 127), (1, 2, 7, 2, 2, 65, 1)])
+def test_keys_as_wide_as_values(T, window, B, Tq, Tk, H, Hk, d, dv):
+    g = gen(B + Tq * 3 + Tk * 5 + d)
+    q, k, v, lam, spans = dense(g, T, B, Tq, Tk, H, Hk, d, dv)
+    check(q, k, v, na.DiffWeight(lam), lam, spans, window, grad=randn(g, T, B, Tq, H, dv))
+
+
+@pytest.mark.parametrize("T", TYPES)
+@pytest.mark.parametrize("d,dv", [(32, 64), (64, 128), (61, 107), (128, 128), (128, 256), (100, 200)])
 def test_rows_that_see_one_key_have_no_gradient_of_scores(T, d, dv):
     # p is 1 whatever the score: q and k get zeros, not the roundings of dp - D
     g, H, Hk = gen(18), 4, 2

@@ -11,10 +11,9 @@ namespace {
 bool aligned(const void *p, int to) { return ((uintptr_t)p & (uintptr_t)(to - 1)) == 0; }
 size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Whether heads of `width` 16-bit values are whole 16-byte pieces at their boundaries, and rows apart (loads
-// of whole tiles tell rows behind the last by where they lie).
+// Whether heads of `width` 16-bit values are whole 16-byte pieces at their boundaries.
 bool pieces(const nm_heads &t, int width) {
-    return aligned(t.p, 16) && t.token % 8 == 0 && t.head % 8 == 0 && t.batch % 8 == 0 && width % 8 == 0 && t.token >= width;
+    return aligned(t.p, 16) && t.token % 8 == 0 && t.head % 8 == 0 && t.batch % 8 == 0 && width % 8 == 0;
 }
 
 // A tensor with strides that do not matter, along dimensions of one, put out of the way.

@@ -74,25 +74,26 @@ __device__ __forceinline__ uint32_t lds_start(char *lds) {
     return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
 }
 
-// 16 bytes a lane straight to LDS, lane l's at lds + 16 l (lds wave-uniform); zeros
-// where the offset lies past the buffer.  M0 holds the LDS address; the wait states
-// cover its write and a vector instruction's write of the resource's registers.
-__device__ __forceinline__ void dma16(v4i buffer, uint32_t offset, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(buffer),
-                 "s"(lds)
-                 : "memory", "m0");
-}
-__device__ __forceinline__ void dma4(v4i buffer, uint32_t offset, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(offset), "s"(buffer),
-                 "s"(lds)
-                 : "memory", "m0");
-}
-__device__ __forceinline__ v4i buffer_of(const void *p, int64_t bytes) {
+// 16 or 4 bytes a lane straight to LDS, lane l's at lds + 16 l or 4 l (lds wave-uniform), from a uniform base
+// and a lane's offset, or from a lane's address.  M0 holds the LDS address; the wait states cover its write and a
+// vector instruction's write of the base's registers.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
+__device__ __forceinline__ const void *uniform(const void *p) {
     const uint64_t at = (uint64_t)p;
-    return v4i{__builtin_amdgcn_readfirstlane((int)(uint32_t)at),
-               __builtin_amdgcn_readfirstlane((int)((uint32_t)(at >> 32) & 0xFFFFu)),
-               __builtin_amdgcn_readfirstlane((int)(bytes < 0 ? 0 : bytes)), 0x00020000};
+    return (const void *)((uint64_t)uniform((uint32_t)(at >> 32)) << 32 | uniform((uint32_t)at));
 }
+__device__ __forceinline__ void dma16(const void *base, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(uniform(lds))
+                 : "memory", "m0");
+}
+__device__ __forceinline__ void dma16(const void *at, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(at), "s"(uniform(lds)) : "memory", "m0");
+}
+__device__ __forceinline__ void dma4(const void *at, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 4\n\tglobal_load_lds_dword %0, off" ::"v"(at), "s"(uniform(lds)) : "memory", "m0");
+}
+// What lanes load whose piece is behind a tensor's rows or columns.
+__device__ const int zeros[4] __attribute__((aligned(16))) = {0, 0, 0, 0};
 // All of this wave's loads have arrived, then the workgroup's barrier.
 __device__ __forceinline__ void arrive() {
     asm volatile("" ::: "memory");
@@ -212,32 +213,38 @@ struct Feed {
     static constexpr int EACH = SPREAD ? 1 : GROUPS / WAVES; // loads of one tensor
     static_assert(TENSORS * GROUPS % WAVES == 0 && (SPREAD || GROUPS % WAVES == 0), "as many loads by every wave");
     const T *p;
-    int64_t stride, second, bytes;      // bytes: from p to the end of the last row
+    int64_t stride, second;
     int left, width, first;             // rows left; this wave's first group
-    uint32_t offset[EACH];              // of a lane; past any buffer where its piece is not of the columns
+    uint32_t offset[EACH];              // of a lane, in bytes
     __device__ __forceinline__ Feed(const T *from, int64_t row_stride, int64_t tensor_stride, int rows, int columns, int wave,
                                     int lane)
-        : p(from), stride(row_stride), second(tensor_stride), bytes(((int64_t)(rows - 1) * row_stride + columns) * 2),
-          left(rows), width(columns) {
+        : p(from), stride(row_stride), second(tensor_stride), left(rows), width(columns) {
         first = SPREAD ? wave % GROUPS : wave;
         if (SPREAD) p += wave / GROUPS * second;
         const int c = lane % CPR;
 #pragma unroll
         for (int i = 0; i < EACH; ++i)
-            offset[i] = c * 8 < width ? (uint32_t)(Place::row_of_place(lane / CPR) + Place::row_of_group(i * WAVES + first)) *
-                                                (uint32_t)stride * 2 + c * 16
-                                      : 0x80000000u;
+            offset[i] = (uint32_t)(Place::row_of_place(lane / CPR) + Place::row_of_group(i * WAVES + first)) *
+                            (uint32_t)stride * 2 + c * 16;
     }
     __device__ __forceinline__ void load(uint32_t lds, int wave, int lane) {
         if (SPREAD) lds += wave / GROUPS * Place::BYTES;
         if constexpr (PIECES) {
-            const int records = left <= 0 ? 0 : bytes < 0x7FFFFFFF ? (int)bytes : 0x7FFFFFFF;
+            const bool whole = left >= ROWS && width == CPR * 8;
+            const bool column = lane % CPR * 8 < width;
 #pragma unroll
             for (int t = 0; t < (SPREAD ? 1 : TENSORS); ++t) {
-                const v4i buffer = buffer_of(p + t * second, records);
+                const char *from = (const char *)uniform(p + t * second);
 #pragma unroll
-                for (int i = 0; i < EACH; ++i)
-                    dma16(buffer, offset[i], lds + t * Place::BYTES + Place::group_at(i * WAVES + first));
+                for (int i = 0; i < EACH; ++i) {
+                    const uint32_t to = lds + t * Place::BYTES + Place::group_at(i * WAVES + first);
+                    if (whole) {
+                        dma16(from, offset[i], to);
+                    } else {
+                        const int row = Place::row_of_place(lane / CPR) + Place::row_of_group(i * WAVES + first);
+                        dma16(column && row < left ? from + offset[i] : (const char *)zeros, to);
+                    }
+                }
             }
         } else {
             constexpr int BATCH = LOADS < 8 ? LOADS : 8;        // loads under way together
@@ -264,7 +271,6 @@ struct Feed {
             }
         }
         p += ROWS * stride;
-        bytes -= ROWS * stride * 2;
         left -= ROWS;
     }
 };

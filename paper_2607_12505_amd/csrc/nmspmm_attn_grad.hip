@@ -318,16 +318,18 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
             const int left = s.nq - t;
             const int64_t map = 2 * (int64_t)head + (wave & 1);
             const float *stat = (wave < 2 ? a.stats + map * a.stat_rows * a.rows : a.delta + map * a.rows) + s.row0 + t;
-            dma4(buffer_of(stat, (left < QT ? left : QT) * 4), lane * 4, to + TILES + wave * 256);
+            dma4(lane < (left < QT ? left : QT) ? stat + lane : (const float *)zeros, to + TILES + wave * 256);
         }
     };
     if (steps > 0) {
-        if (PAIR == 2)
-            typename S::KFeed(head_of<T>(a.k, s.batch, s.k0 + begin, 2 * hk), a.k.token, a.k.head, s.nk - begin, a.d, wave, lane)
-                .load(lds, wave, lane);
-        if (DK)
-            typename S::VFeed(head_of<T>(a.v, s.batch, s.k0 + begin, hk), a.v.token, 0, s.nk - begin, a.dv, wave, lane)
-                .load(lds + S::KEYS, wave, lane);
+        if (PAIR == 2) {
+            typename S::KFeed keys(head_of<T>(a.k, s.batch, s.k0 + begin, 2 * hk), a.k.token, a.k.head, s.nk - begin, a.d, wave, lane);
+            keys.load(lds, wave, lane);
+        }
+        if (DK) {
+            typename S::VFeed values(head_of<T>(a.v, s.batch, s.k0 + begin, hk), a.v.token, 0, s.nk - begin, a.dv, wave, lane);
+            values.load(lds + S::KEYS, wave, lane);
+        }
         stage(0, head, t0 + at * QT);
     }
 

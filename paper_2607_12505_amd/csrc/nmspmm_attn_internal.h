@@ -50,7 +50,7 @@ struct AttnArgs {
     int batch, tq, tk, H, Hk, group, d, dv, left, right;
     float scale, scale2;      // and in base 2
     nm_diff_weight weight;
-    int pieces;               // q, k, v (and do) are whole 16-byte pieces, rows apart
+    int pieces;               // q, k, v (and do) are whole 16-byte pieces at their boundaries
     int row_tiles, splits;
     float *parts;             // [batch * Hk * splits * tq * group] x 4: m1, l1, m2, l2, then the same x 2 dv values
     // backward

@@ -230,20 +230,22 @@ struct Feed {
     __device__ __forceinline__ void load(uint32_t lds, int wave, int lane) {
         if (SPREAD) lds += wave / GROUPS * Place::BYTES;
         if constexpr (PIECES) {
-            const bool whole = left >= ROWS && width == CPR * 8;
-            const bool column = lane % CPR * 8 < width;
+            if (left >= ROWS && width == CPR * 8) {
 #pragma unroll
-            for (int t = 0; t < (SPREAD ? 1 : TENSORS); ++t) {
-                const char *from = (const char *)uniform(p + t * second);
+                for (int t = 0; t < (SPREAD ? 1 : TENSORS); ++t) {
+                    const void *from = uniform(p + t * second);
 #pragma unroll
-                for (int i = 0; i < EACH; ++i) {
-                    const uint32_t to = lds + t * Place::BYTES + Place::group_at(i * WAVES + first);
-                    if (whole) {
-                        dma16(from, offset[i], to);
-                    } else {
-                        const int row = Place::row_of_place(lane / CPR) + Place::row_of_group(i * WAVES + first);
-                        dma16(column && row < left ? from + offset[i] : (const char *)zeros, to);
-                    }
+                    for (int i = 0; i < EACH; ++i)
+                        dma16(from, offset[i], lds + t * Place::BYTES + Place::group_at(i * WAVES + first));
+                }
+            } else {
+                const bool column = lane % CPR * 8 < width;
+#pragma unroll
+                for (int n = 0; n < LOADS; ++n) {
+                    const int t = n / EACH, group = n % EACH * WAVES + first;
+                    const int row = Place::row_of_place(lane / CPR) + Place::row_of_group(group);
+                    const char *at = (const char *)(p + t * second) + offset[n % EACH];
+                    dma16(column && row < left ? at : (const char *)zeros, lds + t * Place::BYTES + Place::group_at(group));
                 }
             }
         } else {

@@ -100,7 +100,7 @@ void fill(AttnArgs &a, const nm_tokens &t, const nm_diff_weight &w, int H, int H
 //     64 + 128:  4 x 200 over 2048 (64) 62 and 44, 4 x 512 over 1024 (128) 34 and 44
 //     128 + 256: 4 x 256 over 512 (128) 23 and 41, over 8192 238 and 208, 4 x 512 over 8192 (256) 246 and 335
 //   Splits: a workgroup a compute unit, of four tiles a wave at least (1 row of 8 heads over 577 keys
-//   in one 14.6 us, in three and a second kernel 13.3; over 8192 in eight 20.0).  Sequences of unequal length: twice as
+//   in one 14.3 us, in three and a second kernel 13.3; over 8192 in eight 20.0).  Sequences of unequal length: twice as
 //   many where those are few and long (16 x 1 rows over up to 16384 keys, 4 key heads, 69 to 61 us; 8 over 32768, 8
 //   key heads, 162 to 129; 4 over 16384 would go 31 to 34 us, 64 over 4096 67 to 71).
 struct Cut {

@@ -123,8 +123,8 @@ __device__ __forceinline__ void join_runs(const AttnArgs &a, const RowTile &r, u
 // (128, 256) 2 x 4096 rows in 0.44 ms with MAPS 1 and 0.75 with the scores made for 128 channels at a time.
 // RUNS: runs of keys of one block of rows, a wave and a ring each, that meet at the end (few rows): the smallest calls
 // need no second kernel.  Bound by memory where the cache is long: 16 x 1 rows over 16384 keys (4 key heads of
-// 64 + 128, 537 MB) 112 us; where it is short, by a wave's 1.4 us for 32 keys: 1 row over 577, 14.6 us.  (Eight waves
-// with a tile each, one at its loads beside another that computes: 117 and 14.0 us.)
+// 64 + 128, 537 MB) 110 us; where it is short, by the latency of a wave's five tiles: 1 row over 577, 14.3 us.
+// (Eight waves with a tile each, one at its loads beside another that computes: 117 and 14.0 us.)
 template <class T, int D, int DV, int BLOCKS, int MAPS, int KT, int RUNS, bool PIECES>
 __global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS) * RUNS, BLOCKS > 1 ? 2 : 1) void k_diff_forward(AttnArgs a) {
     static_assert(RUNS == 1 || (BLOCKS == 1 && MAPS == 2), "runs of one block");

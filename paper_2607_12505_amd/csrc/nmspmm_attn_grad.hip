@@ -22,7 +22,7 @@ namespace {
 // dq, D1, D2 and the parts of dlam: rows as in the forward pass, scores transposed, so a
 // lane's keys are of one row and ds is the operand of dq as it lies.  128 rows a workgroup share tiles of 64 keys in a ring
 // of two.  Bound by matrix instructions (8 d + 2 dv operations a pair) and the exponentials and products beside
-// them: 2 x 4096 causal rows of 8 heads, 4 key heads, 64 + 128, 163 us, 630 TFLOP/s.
+// them: 2 x 4096 causal rows of 8 heads, 4 key heads, 64 + 128, 158 us, 650 TFLOP/s.
 template <class T, int D, int DV, bool PIECES>
 __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void k_diff_grad_q(AttnArgs a) {
     constexpr int KT = kGradKeyTile;
@@ -244,7 +244,7 @@ __device__ __forceinline__ void weight_grads(const AttnArgs &a, int lane, int wa
 // maps' operands too, but not without spilling, and a wait for a spilled register waits for the next
 // tile's loads as well: 4 x 4096 rows of 8 heads, width 64 + 128, 760 us and 672).
 // PAIR 1, for keys of 128 channels, which with v would fill LDS: a wave each, k in registers.
-// Bound as the kernel above (8 d + 4 dv operations a pair): 239 us there, 575 TFLOP/s.
+// Bound as the kernel above (8 d + 4 dv operations a pair): 236 us there, 580 TFLOP/s.
 template <class T, int D, int DV, bool PIECES>
 struct KeySteps {
     static constexpr int PAIR = D <= 64 ? 2 : 1, WAVES = 4 * PAIR, QT = 32 * PAIR;

@@ -204,7 +204,8 @@ __device__ __forceinline__ v8s moved(v8s v, int over) {        // 0 < over < 8
 // Loads of tile after tile of rows, of one tensor or of two `second` values apart (their tiles one behind the
 // other): rows behind the last and columns from `width` on are zero, whatever memory holds there.  PIECES: in whole
 // pieces at 16-byte boundaries the loads go straight to LDS and arrive later (LOADS of them by every
-// wave); otherwise through registers, at once, by kernels of their own (beside the others' they cost spilled registers).  What a load needs but its tile's base is made once.
+// wave); otherwise through registers, at once, by kernels of their own (beside the others' they cost spilled
+// registers).  What a load needs but its tile's base is made once.
 template <class T, int CPR, int ROWS, int WAVES, int TENSORS, bool PIECES>
 struct Feed {
     using Place = Tile<T, CPR, ROWS, WAVES>;

@@ -323,7 +323,8 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
     };
     if (steps > 0) {
         if (PAIR == 2) {
-            typename S::KFeed keys(head_of<T>(a.k, s.batch, s.k0 + begin, 2 * hk), a.k.token, a.k.head, s.nk - begin, a.d, wave, lane);
+            typename S::KFeed keys(head_of<T>(a.k, s.batch, s.k0 + begin, 2 * hk), a.k.token, a.k.head, s.nk - begin, a.d,
+                                   wave, lane);
             keys.load(lds, wave, lane);
         }
         if (DK) {
@@ -348,7 +349,8 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
 #pragma unroll
     for (int x = 0; x < DV / 32; ++x) dv[x] = v16f{};
 
-    const uint32_t rows_at = steps_at + QTile::place_of(sub * 32), g_rows_at = steps_at + 2 * QTile::BYTES + GTile::place_of(sub * 32);
+    const uint32_t rows_at = steps_at + QTile::place_of(sub * 32);
+    const uint32_t g_rows_at = steps_at + 2 * QTile::BYTES + GTile::place_of(sub * 32);
     const uint32_t q_at = rows_at + QTile::rows_lane(lane), q_turned = rows_at + QTile::turned_lane(lane);
     const uint32_t g_at = g_rows_at + GTile::rows_lane(lane), g_turned = g_rows_at + GTile::turned_lane(lane);
     const uint32_t k_at = lds + KTile::rows_lane(lane) + KTile::place_of(block * 32);

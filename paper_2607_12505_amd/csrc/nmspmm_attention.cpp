@@ -257,13 +257,17 @@ static size_t key_parts_bytes(const nm_diff_grad_args &g) {
     return splits > 1 ? round256((size_t)g.tokens.batch * g.Hk * splits * g.tokens.tk * (2 * g.d + g.dv_width) * 4) : 0;
 }
 static size_t delta_bytes(const nm_diff_grad_args &g) { return round256((size_t)2 * g.H * rows_of(g.tokens) * 4); }
+static size_t dlam_bytes(const nm_diff_grad_args &g) { return (size_t)g.H * g.tokens.batch * grad_row_tiles(g) * 16; }
+static int64_t grad_key_tiles(const nm_diff_grad_args &g) { return ((int64_t)g.tokens.tk + kGradKeys - 1) / kGradKeys; }
+static size_t norms_bytes(const nm_diff_grad_args &g) { return (size_t)g.Hk * g.tokens.batch * grad_key_tiles(g) * 4; }
+static size_t tops_bytes(const nm_diff_grad_args &g) { return (size_t)g.Hk * g.tokens.batch * grad_row_tiles(g) * 16; }
 
 extern "C" nm_status nm_diff_attention_backward_workspace(const nm_diff_grad_args *args, size_t *bytes) {
     if (!bytes) return NM_ERR_ARG;
     const nm_status st = check_backward(args);
     if (st != NM_OK) return st;
-    *bytes = delta_bytes(*args) + key_parts_bytes(*args) +
-             (size_t)args->H * args->tokens.batch * grad_row_tiles(*args) * 16;
+    *bytes = delta_bytes(*args) + key_parts_bytes(*args) + dlam_bytes(*args) + tops_bytes(*args) +
+             norms_bytes(*args);
     return NM_OK;
 }
 
@@ -294,7 +298,7 @@ extern "C" nm_status nm_diff_attention_backward(const nm_diff_grad_args *args, v
     if (need && (!ws || ws_bytes < need || !aligned(ws, 16))) return NM_ERR_WORKSPACE;
     AttnArgs a;
     fill(a, g.tokens, g.weight, g.H, g.Hk, g.d, g.dv_width, g.scale);
-    const int64_t row_tiles = grad_row_tiles(g), key_tiles = (g.tokens.tk + kGradKeys - 1) / kGradKeys;
+    const int64_t row_tiles = grad_row_tiles(g), key_tiles = grad_key_tiles(g);
     const int splits = key_splits(g);
     if (!grid_fits((int64_t)a.batch * a.Hk * row_tiles) || (int64_t)a.tq * a.group >= (1ll << 31) ||
         !grid_fits((int64_t)a.batch * a.Hk * key_tiles * splits * 2 + 1) ||
@@ -317,12 +321,16 @@ extern "C" nm_status nm_diff_attention_backward(const nm_diff_grad_args *args, v
     a.key_parts = (float *)((char *)ws + delta_bytes(g));
     a.dlam_parts = (float *)((char *)ws + delta_bytes(g) + key_parts_bytes(g));
     a.dlam_count = (int)((int64_t)a.batch * row_tiles * 4);
+    a.tops = (float *)((char *)a.dlam_parts + dlam_bytes(g));
+    a.norms = (float *)((char *)a.tops + tops_bytes(g));
     a.dlam = g.dlam;
     a.dq1 = g.dq1;
     a.dk1 = g.dk1;
     a.dq2 = g.dq2;
     a.dk2 = g.dk2;
     const int cls = width_class(g.d, g.dv_width);
+    if (g.type == NM_TYPE_F16 && a.batch > 0 && row_tiles > 0 && key_tiles > 0 && launch_diff_norms(a, stream) != 0)
+        return NM_ERR_HIP;
     if (a.batch > 0 && row_tiles > 0 && launch_diff_grad_q(g.type, cls, a, stream) != 0) return NM_ERR_HIP;
     if (launch_diff_grad_k(g.type, cls, a, stream) != 0) return NM_ERR_HIP;
     return a.key_splits == 1 || launch_diff_join_keys(g.type, a, stream) == 0 ? NM_OK : NM_ERR_HIP;

@@ -13,6 +13,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "nmspmm_attn_internal.h"
 #include "nmspmm_values.h"
 
@@ -316,6 +318,21 @@ __device__ __forceinline__ short kept_code(float x, float inv) {
     int r;
     asm("v_cvt_i32_f32 %0, %1" : "=v"(r) : "v"(__builtin_rintf(x * inv)));
     return (short)r;
+}
+
+// Powers of two that take small values up before a rounding to binary16, whose exponents end at 2^-14 and whose
+// steps at 2^-24: gradients of scores over thousands of keys lie below both.  bfloat16 has binary32's exponents.
+template <class T>
+constexpr bool kFewExponents = sizeof(T) == 2 && std::is_same<T, half_t>::value;
+__device__ __forceinline__ float power(int e) { return __builtin_bit_cast(float, (uint32_t)(127 + e) << 23); }
+// x >= 0 is below 2^exponent(x), the exponent held within lo .. hi (infinities and NaN: hi)
+__device__ __forceinline__ int exponent(float x, int lo, int hi) {
+    const int e = (int)(__builtin_bit_cast(uint32_t, x) >> 23) - 126;
+    return e < lo ? lo : e > hi ? hi : e;
+}
+__device__ __forceinline__ int half_up(int e) { return (e + 1) >> 1; }        // of a square's exponent: x^2 < 2^e, x < 2^this
+__device__ __forceinline__ float inverse(float power) {
+    return __builtin_bit_cast(float, (254u << 23) - __builtin_bit_cast(uint32_t, power));
 }
 
 // ---------------------------------------------------------------- sequences

@@ -7,7 +7,12 @@
 // scale for each row, 2^-16 of its largest value.  (Products rounded to the type, and the output among
 // them, put dq and dk at up to 2.5 times the error of a form in 32 bits.)  dlam takes the sums of p2 dp
 // themselves, in 32 bits.
-// ds and p1 - lam p2 are rounded to 16 bits once, for the matrix instructions.
+// ds and p1 - lam p2 are rounded to 16 bits once, for the matrix instructions.  In binary16 ds is scaled
+// by powers of two before that and its sums are scaled back, by |dp - D| <= 2 |do| |v|, the largest norm of
+// the keys' v in tiles of 128 made by a kernel of its own: for dq a row by itself, for dk all rows that a workgroup's
+// keys see.  (Unscaled, do of 1e-4 over 4096 keys lost 14 % of ds, and do of 1e3 had infinities.  With a running
+// maximum of |dp| in place of the norms the kernel of dq spilled at 128 channels: 2 x 2048 rows of 4 heads, 128 + 256, 297 us
+// against 245.)
 //
 // Two kernels, each with its sums in registers in a fixed order: one over keys for the
 // rows of q (which also makes D1, D2 and the parts of dlam), one over rows for the
@@ -18,6 +23,48 @@
 
 namespace nmspmm {
 namespace {
+
+// The largest |v|^2 of 128 keys (of those that are finite: a row that sees another is not finite whatever its scale), a
+// workgroup a tile, 16 lanes a key.  Bound by memory and its launch: 2 x 2048 keys of 4 heads, 256 channels (8 MB), 5 us.
+__global__ __launch_bounds__(256) void k_diff_norms(AttnArgs a) {
+    __shared__ float largest[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int tile = blockIdx.x % a.key_tiles, outer = blockIdx.x / a.key_tiles, hk = outer % a.Hk, b = outer / a.Hk;
+    const Sequence s = sequence(a, b);
+    typedef half_t v8 __attribute__((ext_vector_type(8)));
+    constexpr int KEYS = kGradKeys / 16;         // of a thread: its loads are under way together
+    const int key0 = tile * kGradKeys + threadIdx.x / 16;
+    float sum[KEYS] = {}, most = 0.f;
+    for (int c = lane % 16 * 8; c < a.dv; c += 128) {
+        const int over = piece_over(c, a.dv);
+        v8s y[KEYS];
+#pragma unroll
+        for (int n = 0; n < KEYS; ++n) {
+            y[n] = v8s{};
+            if (key0 + 16 * n < s.nk) y[n] = row_piece(head_of<half_t>(a.v, s.batch, s.k0 + key0 + 16 * n, hk), c, a.dv, over);
+        }
+#pragma unroll
+        for (int n = 0; n < KEYS; ++n) {
+            const v8 x = __builtin_bit_cast(v8, over > 0 ? moved(y[n], over) : y[n]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[n] += (float)x[e] * (float)x[e];
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < KEYS; ++n) {             // over the 16 lanes of a key
+        float x = sum[n];
+        x += dpp<0xB1>(0.f, x);
+        x += dpp<0x4E>(0.f, x);
+        x += dpp<0x141>(0.f, x);
+        x += dpp<0x140>(0.f, x);
+        most = fmaxf(most, x < __builtin_inff() ? x : 0.f);
+    }
+    most = wave_largest(most);
+    if (lane == 0) largest[wave] = most;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        a.norms[blockIdx.x] = fmaxf(fmaxf(largest[0], largest[1]), fmaxf(largest[2], largest[3]));
+}
 
 // dq, D1, D2 and the parts of dlam: rows as in the forward pass, scores transposed, so a
 // lane's keys are of one row and ds is the operand of dq as it lies.  128 rows a workgroup share tiles of 64 keys in a ring
@@ -37,8 +84,10 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void k_diff_grad_q(AttnArgs a
     const RowTile r = row_tile<kGradRows>(a, near_block(blockIdx.x, gridDim.x), lane, wave);
     const Sequence &s = r.s;
     float *lam_part = a.dlam_parts + (int64_t)r.hk * a.group * a.dlam_count + ((int64_t)r.b * a.row_tiles + r.tile) * 4 + wave;
+    float *top_part = a.tops + (((int64_t)r.b * a.Hk + r.hk) * a.row_tiles + r.tile) * 4 + wave;
     if (r.rows <= 0) {
         for (int k = lane; k < a.group; k += 64) lam_part[(int64_t)k * a.dlam_count] = 0.f;
+        if (lane == 0) *top_part = 0.f;
         return;
     }
     const int tile0 = r.low / KT, tiles = r.high >= r.low ? r.high / KT + 1 - tile0 : 0;
@@ -60,6 +109,8 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void k_diff_grad_q(AttnArgs a
             q[i][c] = row_operand<PIECES>(head_of<T>(a.q, s.batch, s.q0 + r.t, 2 * r.head + i), r.valid, c, a.d, lane);
     const float lam = row_weight(a, r, lane);
     float d[2], lse[2];
+    constexpr bool kScaled = kFewExponents<T>;
+    float square = 0.f;   // of this lane's part of do
     {
         typedef T v8 __attribute__((ext_vector_type(8)));
         const T *gp = head_of<T>(a.grad, s.batch, s.q0 + r.t, r.head);
@@ -69,6 +120,9 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void k_diff_grad_q(AttnArgs a
         for (int c = 0; c < DV / 16; ++c) {
             grad[c] = row_operand<PIECES>(gp, r.valid, c, a.dv, lane);
             const v8 x = __builtin_bit_cast(v8, grad[c]);
+            if (kScaled)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) square += (float)x[e] * (float)x[e];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const v8s y = row_operand<PIECES>(kept + i * a.dv, r.valid, c, a.dv, lane);
@@ -93,6 +147,19 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void k_diff_grad_q(AttnArgs a
 #pragma unroll
         for (int x = 0; x < D / 32; ++x) dq[i][x] = v16f{};
     float second = 0.f;   // sum of p2 dp over this lane's keys
+    // binary16: the power of two of this row's ds (and of d from here on).  2^13 <= up |do| |v| < 2^14, so |ds| is
+    // at most 2^15.  (|do|^2 |v|^2 is below 2^80; at kMostSquare it is not finite.)
+    constexpr int kLeastSquare = -100, kMostSquare = 90;
+    float up = 1.f;
+    if (kScaled) {
+        const float *norms = a.norms + ((int64_t)r.b * a.Hk + r.hk) * a.key_tiles;
+        float most = 0.f;
+        if (r.high >= r.low)
+            for (int i = r.low / kGradKeys + lane; i <= r.high / kGradKeys; i += 64) most = fmaxf(most, norms[i]);
+        up = power(14 - half_up(exponent(half_sum(square) * wave_largest(most), kLeastSquare, kMostSquare)));
+        d[0] *= up;
+        d[1] *= up;
+    }
     // A row that sees one key has ds = 0: the codes would leave 2^-16 of dp.  Its D1 and D2 are dp itself, which the
     // kernel of the keys makes by the same instructions.
     const bool one = r.first == r.last, any_one = __any(one);
@@ -149,8 +216,8 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void k_diff_grad_q(AttnArgs a
                     const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[0][at], a.scale2, -lse[0]));
                     const float p2 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[1][at], a.scale2, -lse[1]));
                     part = __builtin_fmaf(p2, dp[at], part);
-                    d1[e] = p1 * (dp[at] - d[0]);
-                    d2[e] = p2 * (dp[at] - d[1]);
+                    d1[e] = p1 * (kScaled ? __builtin_fmaf(dp[at], up, -d[0]) : dp[at] - d[0]);
+                    d2[e] = p2 * (kScaled ? __builtin_fmaf(dp[at], up, -d[1]) : dp[at] - d[1]);
                 }
                 ds[c][0][k] = __builtin_bit_cast(int, v2{(T)d1[0], (T)d1[1]});
                 ds[c][1][k] = __builtin_bit_cast(int, v2{(T)d2[0], (T)d2[1]});
@@ -187,12 +254,18 @@ __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void k_diff_grad_q(AttnArgs a
         if (lane == 0) lam_part[(int64_t)k * a.dlam_count] = w;
     }
     only = half_sum(only);
+    if (kScaled) {        // (rows that are not finite leave no bound: what they add is not finite at any scale)
+        const float bound = inverse(up) * 0x1p14f * fmaxf(1.f, __builtin_fabsf(lam));
+        const bool counts = r.valid && !one && up > power(14 - half_up(kMostSquare)) && bound < __builtin_inff();
+        const float most = wave_largest(counts ? bound : 0.f);
+        if (lane == 0) *top_part = most;
+    }
     if (!r.valid) return;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         if (one && lane < 32) a.delta[(2 * (int64_t)r.head + i) * a.rows + s.row0 + r.t] = only;
         T *out = head_of<T>(a.dq, s.batch, s.q0 + r.t, 2 * r.head + i);
-        const float f = one ? 0.f : i ? -lam * a.scale : a.scale;
+        const float f = one ? 0.f : (i ? -lam * a.scale : a.scale) * (kScaled ? inverse(up) : 1.f);
 #pragma unroll
         for (int x = 0; x < D / 32; ++x)
 #pragma unroll
@@ -356,6 +429,16 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
     const uint32_t k_at = lds + KTile::rows_lane(lane) + KTile::place_of(block * 32);
     const uint32_t v_at = lds + S::KEYS + VTile::rows_lane(lane) + VTile::place_of(block * 32);
     const uint32_t stat_at = steps_at + TILES + sub * 128 + (lane >> 5) * 16;
+    // binary16: the power of two of ds, at most 2^15 by the bounds of the rows from t0 on (rows number t * group + g, 32 a bound)
+    constexpr bool kScaled = DK && kFewExponents<T>;
+    float up = 1.f;
+    if (kScaled && steps > 0) {
+        const float *tops = a.tops + ((int64_t)b * a.Hk + hk) * a.row_tiles * 4;
+        const int to = ((clip(high) + 1) * a.group - 1) / 32;
+        float most = 0.f;
+        for (int i = t0 * a.group / 32 + lane; i <= to; i += 64) most = fmaxf(most, tops[i]);
+        up = power(14 - exponent(wave_largest(most), -60, 100));
+    }
     float lam = 0.f;
     for (int n = 0; n < steps; ++n) {
         if (n == 0 || at == 0) lam = weight_of(a.weight, head, lane).lam;
@@ -425,8 +508,14 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
                 const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[0][v], a.scale2, -l1[e]));
                 const float p2 = lam * __builtin_amdgcn_exp2f(__builtin_fmaf(z[1][v], a.scale2, -l2[e]));
                 r0[e] = (T)(p1 - p2);
-                r1[e] = (T)(p1 * (dp[v] - d1[e]));
-                r2[e] = (T)(p2 * (d2[e] - dp[v]));
+                if (kScaled) {
+                    const float x = dp[v] * up;
+                    r1[e] = (T)(p1 * __builtin_fmaf(-d1[e], up, x));
+                    r2[e] = (T)(p2 * __builtin_fmaf(d2[e], up, -x));
+                } else {
+                    r1[e] = (T)(p1 * (dp[v] - d1[e]));
+                    r2[e] = (T)(p2 * (d2[e] - dp[v]));
+                }
             }
             const v2i i0 = __builtin_bit_cast(v2i, r0), i1 = __builtin_bit_cast(v2i, r1), i2 = __builtin_bit_cast(v2i, r2);
 #pragma unroll
@@ -487,6 +576,7 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
             }
     }
     if (!valid) return;
+    const float down = inverse(up);
     if (a.key_splits > 1) {                // sums in 32 bits, dk's before its scale: 2 d and dv of a key
         float *part = a.key_parts + ((((int64_t)b * a.Hk + hk) * a.key_splits + split) * a.tk + key) * (2 * a.d + a.dv);
 #pragma unroll
@@ -496,8 +586,8 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
 #pragma unroll
                 for (int e = 0; e < 16; e += 4)
                     if (DK)
-                        store4(part + i * a.d, 32 * x + 2 * e + 4 * (lane >> 5), a.d, dk[i][x][e], dk[i][x][e + 1],
-                               dk[i][x][e + 2], dk[i][x][e + 3]);
+                        store4(part + i * a.d, 32 * x + 2 * e + 4 * (lane >> 5), a.d, dk[i][x][e] * down, dk[i][x][e + 1] * down,
+                               dk[i][x][e + 2] * down, dk[i][x][e + 3] * down);
 #pragma unroll
         for (int x = 0; x < DV / 32; ++x)
 #pragma unroll
@@ -510,13 +600,14 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         if (!DK) break;
+        const float f = a.scale * down;
         T *out = head_of<T>(a.dk, s.batch, s.k0 + key, 2 * hk + i);
 #pragma unroll
         for (int x = 0; x < D / 32; ++x)
 #pragma unroll
             for (int e = 0; e < 16; e += 4)
-                store4(out, 32 * x + 2 * e + 4 * (lane >> 5), a.d, dk[i][x][e] * a.scale, dk[i][x][e + 1] * a.scale,
-                       dk[i][x][e + 2] * a.scale, dk[i][x][e + 3] * a.scale);
+                store4(out, 32 * x + 2 * e + 4 * (lane >> 5), a.d, dk[i][x][e] * f, dk[i][x][e + 1] * f, dk[i][x][e + 2] * f,
+                       dk[i][x][e + 3] * f);
     }
     if (!DV_) return;
     T *out = head_of<T>(a.dv_, s.batch, s.k0 + key, hk);
@@ -609,6 +700,11 @@ int join_keys(const AttnArgs &a, hipStream_t s) {
 
 }  // namespace
 
+int launch_diff_norms(const AttnArgs &a, void *stream) {
+    const dim3 grid((unsigned)((int64_t)a.batch * a.Hk * a.key_tiles));
+    hipLaunchKernelGGL(k_diff_norms, grid, dim3(256), 0, (hipStream_t)stream, a);
+    return (int)hipGetLastError();
+}
 int launch_diff_grad_q(int type, int cls, const AttnArgs &a, void *stream) {
     const hipStream_t s = (hipStream_t)stream;
     if (type == NM_TYPE_F16) return a.pieces ? grad_q<half_t, true>(cls, a, s) : grad_q<half_t, false>(cls, a, s);

@@ -58,6 +58,8 @@ struct AttnArgs {
     float *delta;             // [2 H][rows]: do . o1, do . o2
     float *dlam_parts;        // [H][batch * row_tiles * 4]
     int dlam_count;           // batch * row_tiles * 4
+    float *tops;              // [batch * Hk][row_tiles * 4]: of 32 rows, at least their largest |do| |v| max(1, |lam|)
+    float *norms;             // [batch * Hk][key_tiles]: the largest |v|^2 of a tile's keys
     float *dlam, *dq1, *dk1, *dq2, *dk2;
     int key_tiles, key_splits;
     float *key_parts;         // [batch * Hk * key_splits * tk][2 d + dv] (key_splits > 1)
@@ -76,6 +78,7 @@ constexpr int kGradRows = 128, kGradKeys = 128, kGradKeyTile = 64;
 
 int launch_diff_forward(int type, int cls, bool wide, const AttnArgs &a, void *stream);
 int launch_diff_join(int type, const AttnArgs &a, void *stream);
+int launch_diff_norms(const AttnArgs &a, void *stream);
 int launch_diff_grad_q(int type, int cls, const AttnArgs &a, void *stream);
 int launch_diff_grad_k(int type, int cls, const AttnArgs &a, void *stream);
 int launch_diff_join_keys(int type, const AttnArgs &a, void *stream);

@@ -708,8 +708,8 @@ nm_status nm_diff_attention(const nm_diff_args *args, void *ws, size_t ws_bytes,
  *   dq_i = scale ds_i k_i;  dk_i = scale ds_i^T q_i;  dlam = -sum over rows of D_1
  * dk and dv are summed over the heads that share them; dq1, dk1, dq2, dk2 (with value NULL) are the learned
  * vectors' gradients, of their shapes, dlam float32 [H]; all have to be given.  p_0 - lam p_1 and ds_i are
- * rounded to the type once before their products; in binary16 ds is scaled by powers of two around that, by the sizes of
- * grad_o and v, so that small gradients keep their bits and large ones stay finite.  Rows and keys
+ * rounded to the type once before their products; in binary16 they are scaled by powers of two around that, by the sizes of lam,
+ * grad_o and v, so that small maps and gradients keep their bits and large ones stay finite.  Rows and keys
  * behind a sequence's end stay as they were.  With batch == 0 the weights' gradients are set to zero.
  * No output may overlap an input or another output (dq, dk and dv may lie inside the rows of one
  * buffer).  ws: nm_diff_attention_backward_workspace bytes, as above. */

@@ -7,10 +7,12 @@
 // scale for each row, 2^-16 of its largest value.  (Products rounded to the type, and the output among
 // them, put dq and dk at up to 2.5 times the error of a form in 32 bits.)  dlam takes the sums of p2 dp
 // themselves, in 32 bits.
-// ds and p1 - lam p2 are rounded to 16 bits once, for the matrix instructions.  In binary16 ds is scaled
-// by powers of two before that and its sums are scaled back, by |dp - D| <= 2 |do| |v|, the largest norm of
+// ds and p1 - lam p2 are rounded to 16 bits once, for the matrix instructions.  In binary16 both are scaled
+// by powers of two before that and their sums are scaled back: the maps by |p1 - lam p2| <= 1 + |lam|, ds
+// by |dp - D| <= 2 |do| |v|, the largest norm of
 // the keys' v in tiles of 128 made by a kernel of its own: for dq a row by itself, for dk all rows that a workgroup's
-// keys see.  (Unscaled, do of 1e-4 over 4096 keys lost 14 % of ds, and do of 1e3 had infinities.  With a running
+// keys see.  (Unscaled, do of 1e-4 over 4096 keys lost 14 % of ds, do of 1e3 had infinities, and dv over 9000 keys was up
+// to 7 times its bound off.  With a running
 // maximum of |dp| in place of the norms the kernel of dq spilled at 128 channels: 2 x 2048 rows of 4 heads, 128 + 256, 297 us
 // against 245.)
 //
@@ -429,19 +431,29 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
     const uint32_t k_at = lds + KTile::rows_lane(lane) + KTile::place_of(block * 32);
     const uint32_t v_at = lds + S::KEYS + VTile::rows_lane(lane) + VTile::place_of(block * 32);
     const uint32_t stat_at = steps_at + TILES + sub * 128 + (lane >> 5) * 16;
-    // binary16: the power of two of ds, at most 2^15 by the bounds of the rows from t0 on (rows number t * group + g, 32 a bound)
-    constexpr bool kScaled = DK && kFewExponents<T>;
-    float up = 1.f;
-    if (kScaled && steps > 0) {
+    // binary16: powers of two of the maps for dv (`maps_up` max(|p1 - lam p2|) <= 2^15 of all heads that share it) and of ds for
+    // dk (at most 2^15 by the bounds of the rows from t0 on, which have numbers t * group + g, 32 a bound)
+    constexpr bool kScaled = kFewExponents<T>;
+    float maps_up = 1.f, up = 1.f;
+    if (kScaled && DV_) {
+        float most = 0.f;
+        for (int g = 0; g < a.group; ++g) {
+            const float w = __builtin_fabsf(weight_of(a.weight, hk * a.group + g, lane).lam);
+            most = fmaxf(most, w < __builtin_inff() ? w : 0.f);
+        }
+        maps_up = power(15 - exponent(1.f + most, 1, 30));
+    }
+    if (kScaled && DK && steps > 0) {
         const float *tops = a.tops + ((int64_t)b * a.Hk + hk) * a.row_tiles * 4;
         const int to = ((clip(high) + 1) * a.group - 1) / 32;
         float most = 0.f;
         for (int i = t0 * a.group / 32 + lane; i <= to; i += 64) most = fmaxf(most, tops[i]);
-        up = power(14 - exponent(wave_largest(most), -60, 100));
+        up = power(14 - exponent(wave_largest(most), -40, 100));
     }
+    const float beside = up * inverse(maps_up);          // of dp - D, beside the maps' own
     float lam = 0.f;
     for (int n = 0; n < steps; ++n) {
-        if (n == 0 || at == 0) lam = weight_of(a.weight, head, lane).lam;
+        if (n == 0 || at == 0) lam = weight_of(a.weight, head, lane).lam * maps_up;       // (as p2 is used)
         arrive();
         const int r0 = t0 + at * QT + sub * 32;
         const bool next = at + 1 == tiles;
@@ -505,13 +517,14 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int v = 8 * c + 4 * h + e;
-                const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[0][v], a.scale2, -l1[e]));
+                float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[0][v], a.scale2, -l1[e]));
+                if (kScaled && DV_) p1 *= maps_up;
                 const float p2 = lam * __builtin_amdgcn_exp2f(__builtin_fmaf(z[1][v], a.scale2, -l2[e]));
                 r0[e] = (T)(p1 - p2);
-                if (kScaled) {
-                    const float x = dp[v] * up;
-                    r1[e] = (T)(p1 * __builtin_fmaf(-d1[e], up, x));
-                    r2[e] = (T)(p2 * __builtin_fmaf(d2[e], up, -x));
+                if (kScaled && DK) {
+                    const float x = dp[v] * beside;
+                    r1[e] = (T)(p1 * __builtin_fmaf(-d1[e], beside, x));
+                    r2[e] = (T)(p2 * __builtin_fmaf(d2[e], beside, -x));
                 } else {
                     r1[e] = (T)(p1 * (dp[v] - d1[e]));
                     r2[e] = (T)(p2 * (d2[e] - dp[v]));
@@ -576,7 +589,7 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
             }
     }
     if (!valid) return;
-    const float down = inverse(up);
+    const float down = inverse(up), maps_down = inverse(maps_up);
     if (a.key_splits > 1) {                // sums in 32 bits, dk's before its scale: 2 d and dv of a key
         float *part = a.key_parts + ((((int64_t)b * a.Hk + hk) * a.key_splits + split) * a.tk + key) * (2 * a.d + a.dv);
 #pragma unroll
@@ -593,8 +606,8 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
 #pragma unroll
             for (int e = 0; e < 16; e += 4)
                 if (DV_)
-                    store4(part + 2 * a.d, 32 * x + 2 * e + 4 * (lane >> 5), a.dv, dv[x][e], dv[x][e + 1], dv[x][e + 2],
-                           dv[x][e + 3]);
+                    store4(part + 2 * a.d, 32 * x + 2 * e + 4 * (lane >> 5), a.dv, dv[x][e] * maps_down,
+                           dv[x][e + 1] * maps_down, dv[x][e + 2] * maps_down, dv[x][e + 3] * maps_down);
         return;
     }
 #pragma unroll
@@ -615,7 +628,8 @@ __device__ __forceinline__ void key_grads(const AttnArgs &a, uint32_t lds, int i
     for (int x = 0; x < DV / 32; ++x)
 #pragma unroll
         for (int e = 0; e < 16; e += 4)
-            store4(out, 32 * x + 2 * e + 4 * (lane >> 5), a.dv, dv[x][e], dv[x][e + 1], dv[x][e + 2], dv[x][e + 3]);
+            store4(out, 32 * x + 2 * e + 4 * (lane >> 5), a.dv, dv[x][e] * maps_down, dv[x][e + 1] * maps_down,
+                   dv[x][e + 2] * maps_down, dv[x][e + 3] * maps_down);
 }
 
 // The widest class's sums of both do not fit the registers: a workgroup for dk and one for dv, each

@@ -5,6 +5,7 @@ Bounds, with u = 2^-11, E = 2^-24 and the names of attention_util (a 16-bit roun
 its scaled place).  dp = do v^T; top = |do| of a row (for dk: of the rows, times max(1, |lam|)) times the largest |v|:
   ds for dq is scaled so that top is 2^13 or more:      2^-25 / 2^13 top = 2^-38 top
   ds for dk is scaled so that top is 2^12 or more:      2^-37 top (the rows' tops are known to a factor of 2)
+  p0 - lam p1 for dv is scaled so that 1 + |lam| (the largest of the heads that share it) is 2^14 or more: 2^-39 (1 + |lam|)
 A row's own bits: every operation but the last rounding scales by powers of two, so gradients of 2^-s do are those of do
 times 2^-s, to one rounding of each (2 steps of 2^-24 where they leave the normal range, else none).  (The sum over
 heads of dk's bounds has their roundings of the output once each: more than there are.)"""
@@ -174,3 +175,28 @@ def test_large_gradients_and_weights_stay_finite():
             for name, t, (w, room) in (("dq", got.dq[0, :, i], want[2 * i]), ("dk", got.dk[0, :, i], want[2 * i + 1])):
                 if float(w.abs().max()) < 60000:
                     au.within(t, w, room, (name, i, lam))
+
+
+# one row, so that no sum hides what a key loses; maps of 2^-16 and far below
+@pytest.mark.parametrize("d,dv", WIDTHS)
+@pytest.mark.parametrize("Tq,Tk,lams", [(1, 70000, (0.6,)), (1, 70000, (0.3, 40.0)), (2, 50001, (0.8,)), (3, 9000, (0.0,)),
+                                        (1, 5, (2e5,)), (40, 300, (1e4, 0.5))])
+def test_gradients_of_values_keep_their_bits(d, dv, Tq, Tk, lams):
+    g, H = gen(Tk + d), len(lams)
+    q, k, v = randn(g, 1, Tq, 2 * H, d), randn(g, 1, Tk, 2, d), 0.01 * randn(g, 1, Tk, 1, dv)
+    q, k, v = (t.to(T).cuda() for t in (q, k, v))
+    # outputs of about 1: off the last steps of their own type
+    do = (min(Tk, 4096) / (1 + max(lams)) * randn(g, 1, Tq, H, dv)).to(T).cuda()
+    weight = na.DiffWeight(torch.tensor(lams, device="cuda"))
+    f = na.diff_attention_train(q, k, v, weight)
+    got = na.diff_attention_backward(do, f, q, k, v, weight).dv[0, :, 0]
+    scale = float(torch.tensor(d ** -0.5, dtype=torch.float32))
+    want = room = 0.0
+    for h, lam in enumerate(weight.value.tolist()):
+        at = slice(2 * h, 2 * h + 2)
+        p, S = maps(q[0, :, at].double().cpu(), k[0].double().cpu(), scale, au.seen(Tq, Tk, -1, -1))
+        kap = (2 * (d + 8) * S + 16) * E + (Tq * H / 16 + 32) * E
+        x, y = p[0] - lam * p[1], do[0, :, h].double().cpu()
+        want = want + x.t() @ y
+        room = room + (U + kap) * ((p[0] + lam * p[1]).t() @ y.abs()) + 2.0 ** -39 * (1 + max(lams)) * y.abs().sum(0)
+    au.within(got, want, room + U * want.abs() + 2.0 ** -25, "dv")

@@ -324,6 +324,9 @@ __device__ __forceinline__ short kept_code(float x, float inv) {
 // steps at 2^-24: gradients of scores over thousands of keys lie below both.  bfloat16 has binary32's exponents.
 template <class T>
 constexpr bool kFewExponents = sizeof(T) == 2 && std::is_same<T, half_t>::value;
+// The forward pass's maps and their sums are 2^this of themselves.
+template <class T>
+constexpr float kMapsUp = kFewExponents<T> ? 7.f : 0.f;
 __device__ __forceinline__ float power(int e) { return __builtin_bit_cast(float, (uint32_t)(127 + e) << 23); }
 // x >= 0 is below 2^exponent(x), the exponent held within lo .. hi (infinities and NaN: hi)
 __device__ __forceinline__ int exponent(float x, int lo, int hi) {

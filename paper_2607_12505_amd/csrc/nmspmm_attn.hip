@@ -7,7 +7,9 @@
 // lane's own but for one exchange of halves, and the maps go into the product with v as
 // they lie (nmspmm_attn.h).
 // The maps' values are rounded to 16 bits before that product (the matrix instructions
-// take no more): half an ulp of each value, the same size as the output's own rounding.
+// take no more): half an ulp of each value, the same size as the output's own rounding.  Binary16 holds them times
+// 2^7: its ulps end at 2^-24, which keys of little weight reach (as they are, a row lost keys of 2^-25 of the
+// largest altogether); now at 2^-31 of the largest, the maximum's lag (below) included.
 // Sums, maxima and products are in 32 bits.
 //
 // The rows of a workgroup are those of all heads that share a key head: row (token
@@ -104,7 +106,7 @@ __device__ __forceinline__ void join_runs(const AttnArgs &a, const RowTile &r, u
         const KeptScale k = kept_scale(m);
         if (run == 0 && lane < 32) {
             float *at = a.stats + (2 * (int64_t)r.head + i) * a.stat_rows * a.rows + r.s.row0 + r.t;
-            at[0] = sum[i] == 0.f ? __builtin_inff() : top[i] + __builtin_amdgcn_logf(sum[i]);
+            at[0] = sum[i] == 0.f ? __builtin_inff() : top[i] - kMapsUp<T> + __builtin_amdgcn_logf(sum[i]);
             at[a.rows] = k.scale;
         }
         int16_t *kept = a.kept + (((r.s.row0 + r.t) * a.H + r.head) * 2 + i) * a.dv;
@@ -222,7 +224,7 @@ __global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS) * RUNS, BLOCKS > 1 ? 2 : 1
             __builtin_amdgcn_s_setprio(0);
             if (j0 + 31 > r.block_end || j0 < r.block_full) hide(r, j0, lane, z);
             // The maximum that the exponents are taken from follows the true one only when that has
-            // grown by more than 2^8: a value is then at most 2^8, which 16 bits and the sums hold.  Each
+            // grown by more than 2^8: a value is then at most 2^8 (2^15 in binary16), which 16 bits and the sums hold.  Each
             // row by itself: its bits do not depend on the rows beside it.
             float now[MAPS], from[MAPS];
             bool grown[MAPS], any = false;
@@ -246,7 +248,7 @@ __global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS) * RUNS, BLOCKS > 1 ? 2 : 1
                 }
             }
 #pragma unroll
-            for (int i = 0; i < MAPS; ++i) from[i] = top[i] == -__builtin_inff() ? 0.f : top[i];
+            for (int i = 0; i < MAPS; ++i) from[i] = top[i] == -__builtin_inff() ? 0.f : top[i] - kMapsUp<T>;
             // values 8 c .. 8 c + 7 of the maps, two of them at a time (part k of PARTS)
             constexpr int PARTS = MAPS * 4;
             typedef T v2 __attribute__((ext_vector_type(2)));
@@ -350,7 +352,7 @@ __global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS) * RUNS, BLOCKS > 1 ? 2 : 1
 #pragma unroll
     for (int i = 0; i < MAPS; ++i) {
         float *at = a.stats + (2 * (int64_t)r.head + map + i) * a.stat_rows * a.rows + s.row0 + r.t;
-        if (lane < 32) at[0] = sum[i] == 0.f ? __builtin_inff() : top[i] + __builtin_amdgcn_logf(sum[i]);
+        if (lane < 32) at[0] = sum[i] == 0.f ? __builtin_inff() : top[i] - kMapsUp<T> + __builtin_amdgcn_logf(sum[i]);
         int16_t *kept = a.kept + (((s.row0 + r.t) * a.H + r.head) * 2 + map + i) * a.dv;
 #pragma unroll
         for (int w = 0; w < (DV + kScaleWidth - 1) / kScaleWidth; ++w) {
@@ -461,7 +463,7 @@ __global__ __launch_bounds__(256) void k_diff_join(AttnArgs a) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         float *at = a.stats + (2 * (int64_t)head + i) * a.stat_rows * a.rows + s.row0 + t;
-        if (lane == 0) at[0] = sum[i] == 0.f ? __builtin_inff() : top[i] + __builtin_amdgcn_logf(sum[i]);
+        if (lane == 0) at[0] = sum[i] == 0.f ? __builtin_inff() : top[i] - kMapsUp<T> + __builtin_amdgcn_logf(sum[i]);
         int16_t *to = a.kept + (((s.row0 + t) * a.H + head) * 2 + i) * a.dv;
         const float most = larger(larger(magnitude(y[i][0]), magnitude(y[i][1])), larger(magnitude(y[i][2]), magnitude(y[i][3])));
 #pragma unroll

@@ -5,6 +5,7 @@ Bounds, with u = 2^-11, E = 2^-24 and the names of attention_util (a 16-bit roun
 its scaled place).  dp = do v^T; top = |do| of a row (for dk: of the rows, times max(1, |lam|)) times the largest |v|:
   ds for dq is scaled so that top is 2^13 or more:      2^-25 / 2^13 top = 2^-38 top
   ds for dk is scaled so that top is 2^12 or more:      2^-37 top (the rows' tops are known to a factor of 2)
+  maps in the forward pass are 2^7 or more where their scores are largest: 2^-32 for each |v|
   p0 - lam p1 for dv is scaled so that 1 + |lam| (the largest of the heads that share it) is 2^14 or more: 2^-39 (1 + |lam|)
 A row's own bits: every operation but the last rounding scales by powers of two, so gradients of 2^-s do are those of do
 times 2^-s, to one rounding of each (2 steps of 2^-24 where they leave the normal range, else none).  (The sum over
@@ -200,3 +201,32 @@ def test_gradients_of_values_keep_their_bits(d, dv, Tq, Tk, lams):
         want = want + x.t() @ y
         room = room + (U + kap) * ((p[0] + lam * p[1]).t() @ y.abs()) + 2.0 ** -39 * (1 + max(lams)) * y.abs().sum(0)
     au.within(got, want, room + U * want.abs() + 2.0 ** -25, "dv")
+
+
+# a key that takes nearly all of a row and has no value itself: the row is what the others add, 2^-25.5 of it each (values
+# of hundreds; few rows, and many rows in tiles that are shared)
+@pytest.mark.parametrize("d,dv", WIDTHS)
+@pytest.mark.parametrize("B,Tq,Tk,sink", [(1, 1, 4000, 0), (1, 1, 300, 299), (2, 3, 9001, 4500), (100, 130, 70, 3), (1, 40, 2100, 7)])
+def test_keys_of_little_weight_count(d, dv, B, Tq, Tk, sink):
+    g = gen(Tk + d)
+    q, k, v = randn(g, 1, Tq, 2, d) * 0.05, randn(g, 1, Tk, 2, d) * 0.05, 200 + 100 * randn(g, 1, Tk, 1, dv)
+    q[..., 0] = 1.0
+    k[..., 0], v[0, sink] = 0.0, 0.0
+    scale = float(torch.tensor(d ** -0.5, dtype=torch.float32))
+    k[0, sink, 0, 0] = 25.5 * math.log(2) / scale                       # of the first map alone
+    q, k, v = (t.to(T).expand(B, *t.shape[1:]).contiguous().cuda() for t in (q, k, v))
+    for lam in (0.0, 2.0 ** -20):
+        weight = na.DiffWeight(torch.tensor([lam], device="cuda"))
+        f = na.diff_attention_train(q, k, v, weight)
+        assert torch.equal(na.diff_attention(q, k, v, weight), f.o)
+        v64 = v[0, :, 0].double().cpu()
+        p, S = maps(q[0].double().cpu(), k[0].double().cpu(), scale, au.seen(Tq, Tk, -1, -1))
+        kappa = (2 * (d + 8) * S + 16) * E + (Tk / 16 + 32) * E
+        o = p @ v64
+        room = (U + kappa) * (p @ v64.abs()) + 2.0 ** -32 * v64.abs().sum(0)
+        for b in (0, B - 1):
+            au.within(f.o[b, :, 0], o[0] - lam * o[1], room[0] + lam * room[1] + U * (o[0] - lam * o[1]).abs() + 2.0 ** -25)
+            for i in (0, 1):
+                scales = f.stats[i, 1:, b * Tq:(b + 1) * Tq].repeat_interleave(128, 0)[:dv].t()
+                kept = f.kept[b * Tq:(b + 1) * Tq, 0, i].double() * scales.double()
+                au.within(kept, o[i], room[i] + o[i].abs().amax(1, keepdim=True) * (2.0 ** -16 * 1.01 + 4 * E), ("kept", i))

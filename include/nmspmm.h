@@ -664,7 +664,8 @@ nm_status nm_rotary(const nm_rotary_args *args, void *stream);
  * float32 [n] for all heads, or [H x n] with per_head.
  *
  * Scores, sums and products are in binary32; the maps are rounded to the type once before the
- * product with v (the matrix instructions' operand).  kept and stats (both or neither NULL) are what
+ * product with v (the matrix instructions' operand; in binary16 times a power of two, so that a key counts down to 2^-32 of
+ * a row's largest weight).  kept and stats (both or neither NULL) are what
  * the backward pass reads: kept, device int16 [rows x H x 2 x dv], codes of p_i v; stats, device float32
  * [2 H x (1 + ceil(dv / 128)) x rows]: the base-2 logarithm of a map's sum (plus infinity where a row sees none), then
  * the scale of the codes of each 128 channels, their largest magnitude / 32767 (NaN where one is not finite).
@@ -710,7 +711,9 @@ nm_status nm_diff_attention(const nm_diff_args *args, void *ws, size_t ws_bytes,
  * vectors' gradients, of their shapes, dlam float32 [H]; all have to be given.  p_0 - lam p_1 and ds_i are
  * rounded to the type once before their products; in binary16 they are scaled by powers of two around that, by the sizes of lam,
  * grad_o and v, so that small maps and gradients keep their bits and large ones stay finite.  Rows and keys
- * behind a sequence's end stay as they were.  With batch == 0 the weights' gradients are set to zero.
+ * behind a sequence's end stay as they were, and what the inputs hold there does not matter; within a sequence an infinity or
+ * NaN in q, k, v or grad_o may make any gradient of the heads that share its key head NaN, also where the mask hides it.
+ * With batch == 0 the weights' gradients are set to zero.
  * No output may overlap an input or another output (dq, dk and dv may lie inside the rows of one
  * buffer).  ws: nm_diff_attention_backward_workspace bytes, as above. */
 typedef struct nm_diff_grad_args {

@@ -241,8 +241,14 @@ static nm_status check_backward(const nm_diff_grad_args *args) {
 static int64_t grad_row_tiles(const nm_diff_grad_args &g) {
     return ((int64_t)g.tokens.tq * (g.H / g.Hk) + kGradRows - 1) / kGradRows;
 }
-// Parts of the rows for the gradients of the keys: as many as fill the device's workgroups (two a compute
-// unit) where the tiles of keys do not, of at least four steps of 32 rows on average.
+// Parts of the rows for the gradients of the keys: up to two workgroups for each compute unit where the tiles of keys make
+// fewer, of at least four steps of 32 rows on average.  A compute unit holds one at a time in every class (LDS of 135 KB at
+// 64 + 128, 86 at 128 + 128, 136 at 128 + 256; at 32 + 64 the registers of eight waves), so beyond one for each the parts
+// only even out unequal tiles, against sums in memory and their join.  Backward passes in one, two and four parts,
+// * the rule's:
+//   2 x 4096 rows of 8 heads, 4 key heads, 64 + 128, causal 419, 374*, 375 us; without a mask 513, 541*, 568
+//   2 x 2048 rows of 4 heads, 64 + 128, causal 139, 122, 128*; without a mask 140, 128, 142*
+//   the same, 128 + 256, causal 240, 230*, 238; without a mask 243, 271*, 296
 static int key_splits(const nm_diff_grad_args &g) {
     const int64_t tiles = ((int64_t)g.tokens.tk + kGradKeys - 1) / kGradKeys;
     const int64_t groups = (int64_t)g.tokens.batch * g.Hk * tiles * (width_class(g.d, g.dv_width) == 3 ? 2 : 1);

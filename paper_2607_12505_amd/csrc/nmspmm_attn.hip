@@ -121,11 +121,12 @@ __device__ __forceinline__ void join_runs(const AttnArgs &a, const RowTile &r, u
 // BLOCKS blocks of 32 rows share tiles of KT keys in a ring of two.  MAPS 2: a wave makes both
 // maps of its block, whose products share v's operands; MAPS 1: two waves a block make one each and
 // meet at the end.  Both maps' sums of 256 channels do not fit a wave's registers, and of 128 they do: (64, 128)
-// runs 4 x 4096 rows of 8 heads in 0.49 ms with MAPS 2 and 0.61 with MAPS 1 (more reads of LDS and scalar instructions),
+// runs 4 x 4096 rows of 8 heads in 0.47 ms with MAPS 2 and 0.61 with MAPS 1 (more reads of LDS and scalar instructions),
 // (128, 256) 2 x 4096 rows in 0.44 ms with MAPS 1 and 0.75 with the scores made for 128 channels at a time.
 // RUNS: runs of keys of one block of rows, a wave and a ring each, that meet at the end (few rows): the smallest calls
 // need no second kernel.  Bound by memory where the cache is long: 16 x 1 rows over 16384 keys (4 key heads of
-// 64 + 128, 537 MB) 110 us; where it is short, by the latency of a wave's five tiles: 1 row over 577, 14.3 us.
+// 64 + 128, 537 MB) 110 us; where it is short, by a fixed 6 us (the launch, q, the weight, joining the runs: 1 row of 8 heads
+// over 32 to 128 keys 7.7 us) and 1.5 us for each tile that a wave has after its first: over 577 keys, five tiles, 14 us.
 // (Eight waves with a tile each, one at its loads beside another that computes: 117 and 14.0 us.)
 template <class T, int D, int DV, int BLOCKS, int MAPS, int KT, int RUNS, bool PIECES>
 __global__ __launch_bounds__(64 * BLOCKS * (3 - MAPS) * RUNS, BLOCKS > 1 ? 2 : 1) void k_diff_forward(AttnArgs a) {

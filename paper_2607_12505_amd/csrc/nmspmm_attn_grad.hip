@@ -27,7 +27,8 @@ namespace nmspmm {
 namespace {
 
 // The largest |v|^2 of 128 keys (of those that are finite: a row that sees another is not finite whatever its scale), a
-// workgroup a tile, 16 lanes a key.  Bound by memory and its launch: 2 x 2048 keys of 4 heads, 256 channels (8 MB), 5 us.
+// workgroup a tile, 16 lanes a key.  Bound by the latency of its launch, loads and sums: 8 MB, 2 x 2048 keys of 4 heads with
+// 256 channels or 32 x 197 of 6 with 128, 5 us.
 __global__ __launch_bounds__(256) void k_diff_norms(AttnArgs a) {
     __shared__ float largest[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -71,7 +72,7 @@ __global__ __launch_bounds__(256) void k_diff_norms(AttnArgs a) {
 // dq, D1, D2 and the parts of dlam: rows as in the forward pass, scores transposed, so a
 // lane's keys are of one row and ds is the operand of dq as it lies.  128 rows a workgroup share tiles of 64 keys in a ring
 // of two.  Bound by matrix instructions (8 d + 2 dv operations a pair) and the exponentials and products beside
-// them: 2 x 4096 causal rows of 8 heads, 4 key heads, 64 + 128, 158 us, 650 TFLOP/s.
+// them: 2 x 4096 causal rows of 8 heads, 4 key heads, 64 + 128, 154 us, 670 TFLOP/s (binary16 158).
 template <class T, int D, int DV, bool PIECES>
 __global__ __launch_bounds__(256, D <= 64 ? 2 : 1) void k_diff_grad_q(AttnArgs a) {
     constexpr int KT = kGradKeyTile;
@@ -319,7 +320,8 @@ __device__ __forceinline__ void weight_grads(const AttnArgs &a, int lane, int wa
 // maps' operands too, but not without spilling, and a wait for a spilled register waits for the next
 // tile's loads as well: 4 x 4096 rows of 8 heads, width 64 + 128, 760 us and 672).
 // PAIR 1, for keys of 128 channels, which with v would fill LDS: a wave each, k in registers.
-// Bound as the kernel above (8 d + 4 dv operations a pair): 236 us there, 580 TFLOP/s.
+// Bound as the kernel above (8 d + 4 dv operations a pair): 227 us there, 600 TFLOP/s; binary16, with two products more for
+// each value, 247.
 template <class T, int D, int DV, bool PIECES>
 struct KeySteps {
     static constexpr int PAIR = D <= 64 ? 2 : 1, WAVES = 4 * PAIR, QT = 32 * PAIR;

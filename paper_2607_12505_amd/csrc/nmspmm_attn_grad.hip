@@ -12,7 +12,7 @@
 // by |dp - D| <= 2 |do| |v|, the largest norm of
 // the keys' v in tiles of 128 made by a kernel of its own: for dq a row by itself, for dk all rows that a workgroup's
 // keys see.  (Unscaled, do of 1e-4 over 4096 keys lost 14 % of ds, do of 1e3 had infinities, and dv over 9000 keys was up
-// to 7 times its bound off.  With a running
+// to 9 times its bound off.  With a running
 // maximum of |dp| in place of the norms the kernel of dq spilled at 128 channels: 2 x 2048 rows of 4 heads, 128 + 256, 297 us
 // against 245.)
 //
